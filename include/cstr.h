@@ -47,6 +47,7 @@ extern "C" {
 
 #define CSTR_F32 0              /* logits are IEEE fp32                               */
 #define CSTR_BF16 1             /* logits are bfloat16                                */
+#define CSTR_F16 2              /* IEEE half (keys, values and queries only)          */
 
 #define CSTR_MAX_TABLES 16      /* tables one cstr_step call can mix                  */
 
@@ -57,6 +58,7 @@ typedef struct cstr_workspace cstr_workspace_t; /* per-stream scratch of cstr_st
 typedef struct cstr_pda cstr_pda_t;             /* device copy of a byte-level PDA            */
 typedef struct cstr_pda_table cstr_pda_table_t; /* token-level PDA: masks per (state, top)    */
 typedef struct cstr_pda_workspace cstr_pda_workspace_t; /* per-stream scratch of cstr_pda_step */
+typedef struct cstr_cache cstr_cache_t;         /* key / value cache of a batch with one prompt */
 
 /* ------------------------------------------------------------------ DFA */
 
@@ -502,6 +504,138 @@ int cstr_step_static(const cstr_table_t *const *tables, int32_t n_tables,
                      const int32_t *row_table, const void *logits, int32_t dtype, int64_t ld,
                      const float *noise, int32_t *states, int32_t *tokens_out, void *masked_out,
                      uint8_t *accept_out, int32_t batch, void *cuda_stream);
+
+/* ------------------------------------------- keys, values and attention */
+
+/*
+ * A constrained batch usually answers one prompt: the API's description, the
+ * schema, the examples (Section 2.4: many constraints and requests per
+ * deployment, one model).  Its rows then share the prompt's keys and values,
+ * held once, and each row has a cache of its own later tokens.  The calls below
+ * are the model's attention over both, and the row caches' upkeep; the logits
+ * that follow go to cstr_step.  (The paper has no counterpart: it leaves the
+ * model outside.)
+ *
+ * Record the arrays of one attention layer:
+ *   dtype        CSTR_BF16 or CSTR_F16: of keys, values, queries and outputs
+ *   batch        rows, >= 1;  n_heads query heads, a multiple of n_kv_heads: query
+ *                head h reads key / value head h / (n_heads / n_kv_heads)
+ *   head_dim     a multiple of 8, 8 .. 128
+ *   max_tokens   most tokens a row gets in one call, >= 1 (1 + drafted tokens)
+ *   prefix_k, prefix_v   DEVICE [prefix_len][n_kv_heads][head_dim], the prompt's; may be
+ *                NULL when prefix_len is 0
+ *   prefix_strides  HOST int64 [4]: token and head stride of prefix_k, then of prefix_v
+ *                (may be NULL when prefix_len is 0)
+ *   cache_k, cache_v     DEVICE [batch][cap][n_kv_heads][head_dim]: the rows' slots
+ *   cache_strides   HOST int64 [6]: row, slot and head stride of cache_k, then of cache_v
+ *   weight       DEVICE float [batch][n_kv_heads][cap]: attention weight each slot has
+ *                received so far, or NULL (then nothing can be accumulated or evicted)
+ *   age          DEVICE int32 [batch][n_kv_heads][cap]: position of each slot's token in
+ *                its row, or NULL (then no causal mask among new tokens, no eviction)
+ *   lens         DEVICE int32 [batch]: filled slots; slots 0 .. lens-1 hold the row's
+ *                tokens, in any order
+ * Strides count elements and are multiples of 8, and arrays of keys and values
+ * start on 16 bytes (else CSTR_ERR_SHAPE); the head_dim elements are adjacent.
+ * The caller keeps the arrays; slots at and past lens[b] are never read.  A handle
+ * serves one stream at a time.  Allocates device memory.
+ */
+int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, int32_t n_kv_heads,
+                      int32_t head_dim, int32_t max_tokens, const void *prefix_k,
+                      const void *prefix_v, int64_t prefix_len, const int64_t *prefix_strides,
+                      void *cache_k, void *cache_v, int32_t cap, const int64_t *cache_strides,
+                      float *weight, int32_t *age, int32_t *lens, cstr_cache_t **out);
+void cstr_free_cache(cstr_cache_t *cache);
+
+/*
+ * Put new tokens into the rows' caches; where a row would exceed its budget,
+ * evict the entries that have received the least attention.  For every row and
+ * key / value head, with n = n_new[b] tokens and len = lens[b]:
+ *   evicted   the max(0, len + n - budget) first entries in the order
+ *             (protected, weight, slot), protected = age >= pos[b] + n - recent:
+ *             the row's last `recent` tokens, the new ones among them; a NaN
+ *             weight comes before every other
+ *   new length  min(len + n, budget)
+ *   moves     old entries that stay but lie past the new length, then the new
+ *             tokens, take the free slots below it (evicted ones, or at and past
+ *             len) in ascending order; every other entry keeps its slot
+ *   new token i: weight 0, age pos[b] + i
+ *   k_new, v_new  DEVICE [batch][n_tokens][n_kv_heads][head_dim] of the cache's dtype
+ *   new_strides   HOST int64 [6]: row, token and head stride of k_new, then of v_new
+ *                 (multiples of 8; 16-byte aligned arrays)
+ *   n_tokens      0 .. min(max_tokens, budget); n_new  DEVICE int32 [batch] (clamped
+ *                 to [0, n_tokens]) or NULL: all rows get n_tokens
+ *   pos           DEVICE int32 [batch]: position of each row's first new token
+ *   budget        1 .. cap;  recent  0 .. budget
+ * n_tokens = 0 (k_new, v_new may be NULL) only shrinks rows to the budget.
+ * Needs weight and age (else CSTR_ERR_NULL).  Enqueues one kernel on cuda_stream;
+ * no allocation, no host synchronisation.
+ */
+int cstr_cache_insert(cstr_cache_t *cache, const void *k_new, const void *v_new,
+                      const int64_t *new_strides, int32_t n_tokens, const int32_t *n_new,
+                      const int32_t *pos, int32_t budget, int32_t recent, void *cuda_stream);
+
+/*
+ * Attention of every row's newest tokens over the shared prompt and the row's
+ * cache (which holds them already).  For row b, token t, head h, with the keys
+ * k_x of the prompt and of the slots j < lens[b] that t may see
+ * (pos NULL: all; else age[b][.][j] <= pos[b] + t, so that drafted tokens do not
+ * see later ones):
+ *   lse = log sum_x exp(scale q.k_x),   out = sum_x exp(scale q.k_x - lse) v_x
+ * accumulated in 32 bits, rounded once.  A token that sees nothing, and every
+ * token t >= n_query[b], gets out = 0 and lse = -infinity; what lies in keys and
+ * values that a token does not see (NaN, infinity) does not reach it.
+ *   q, out        DEVICE [batch][n_tokens][n_heads][head_dim]; strides HOST int64 [3]: row,
+ *                 token, head (multiples of 8; 16-byte aligned); must not overlap
+ *   n_tokens      1 .. max_tokens; n_query  DEVICE int32 [batch] or NULL: all n_tokens
+ *   pos           DEVICE int32 [batch]: position of token 0, or NULL
+ *   accumulate    non-zero: weight[b][h / group][j] += exp(scale q.k_j - lse), summed over
+ *                 the row's tokens and the heads of the group in a fixed order
+ *   lse_out       DEVICE float [batch][n_tokens][n_heads] or NULL
+ * Only enqueues work on cuda_stream; no allocation, no host synchronisation.
+ */
+int cstr_cache_attention(cstr_cache_t *cache, const void *q, const int64_t *q_strides,
+                         int32_t n_tokens, const int32_t *pos, const int32_t *n_query, float scale,
+                         int32_t accumulate, void *out, const int64_t *out_strides,
+                         float *lse_out, void *cuda_stream);
+
+/* ------------------------------------------------- loss under constraints */
+
+/*
+ * Clipped policy loss with a KL term over the constrained distribution, and its
+ * gradient, for `rows` sampled tokens.  A policy that answers under a constraint
+ * samples from the softmax over the allowed tokens (Algorithm 2: disallowed
+ * logits are -infinity), so the ratio of new and old policy has to be taken there
+ * too.  With A = the tokens that the row's automaton state allows (as in
+ * cstr_step; all tokens when n_tables is 0), z = logits / temperature:
+ *   logp = z[a] - log sum_{v in A} exp z[v],    r = exp(logp - old_logp)
+ *   loss = w ( -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv)
+ *              + kl_coef (exp(ref_logp - logp) - (ref_logp - logp) - 1) )
+ *   dlogits[v] = d loss / d logits[v]: 0 outside A; where the clip is strictly
+ *              the smaller term, the first summand gives none
+ * Statistics are held in 32 bits; dlogits is rounded once to its type.
+ *   tables, n_tables, row_table   as in cstr_step; n_tables 0 .. CSTR_MAX_TABLES
+ *   states      DEVICE int32 [rows]: state before the token (NULL exactly when n_tables is 0)
+ *   logits      DEVICE [rows][ld] of dtype CSTR_F32 or CSTR_BF16;  ld >= vocab_size
+ *   vocab_size  equal to the tables' V
+ *   actions     DEVICE int32 [rows]: the sampled token a
+ *   old_logp, advantages   DEVICE float [rows]
+ *   ref_logp    DEVICE float [rows] or NULL (no KL term; kl_coef is ignored)
+ *   weight      DEVICE float [rows] or NULL (1): w, e.g. 1 / tokens, 0 for padding
+ *   loss_out, logp_out   DEVICE float [rows]
+ *   dlogits     DEVICE [rows][ld] of dtype or NULL (no gradient); may be the same buffer
+ *               as logits; columns >= vocab_size are not written
+ * A row whose state is -1 or out of range, whose table index or action is out of
+ * range, or whose action is not allowed or has a logit of -infinity, gets loss 0, logp -infinity, gradient 0; a row of weight 0 gets loss 0 and gradient 0
+ * whatever its logits hold.  Other rows propagate NaN.
+ * Only enqueues one kernel on cuda_stream; no allocation, no host synchronisation.
+ */
+int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                     const int32_t *states, const void *logits, int32_t dtype, int64_t ld,
+                     int32_t vocab_size, float temperature, const int32_t *actions,
+                     const float *old_logp, const float *ref_logp, const float *advantages,
+                     const float *weight, float clip_low, float clip_high, float kl_coef,
+                     float *loss_out, float *logp_out, void *dlogits, int32_t rows,
+                     void *cuda_stream);
 
 /* Message for the calling thread's most recent error ("" if none). */
 const char *cstr_last_error(void);

@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libcstr.so")
 # the test-only setters of include/cstr_debug.h.  Tests run their small cases against it.
 CHECK_LIB_PATH = os.path.join(PKG_DIR, "libcstr_check.so")
 CHECK_FLAGS = ["-DCSTR_BOUNDS_CHECK", "-DCSTR_TESTING"]
-SOURCES = ["cstr_host.cu", "cstr_build.cu", "cstr_step.cu", "cstr_pda.cu"]
+SOURCES = ["cstr_host.cu", "cstr_build.cu", "cstr_step.cu", "cstr_pda.cu", "cstr_cache.cu",
+           "cstr_cache_attn.cu", "cstr_loss.cu"]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,49 @@
+// Internal definitions of the key / value cache and its attention (not part of the ABI).
+#pragma once
+
+#include "cstr_internal.cuh"
+
+// What cstr_cache_create recorded: caller-owned arrays and their strides (in
+// elements), and the scratch that the handle's calls share.
+struct cstr_cache {
+    int device;
+    int32_t sm_count;
+    int32_t dtype, batch, n_heads, n_kv_heads, head_dim, max_tokens, cap;
+    int64_t prefix_len;
+    const void *prefix_k, *prefix_v;
+    int64_t pk_st, pk_sh, pv_st, pv_sh;                   // token, head
+    void *cache_k, *cache_v;
+    int64_t ck_sb, ck_ss, ck_sh, cv_sb, cv_ss, cv_sh;     // row, slot, head
+    float *weight;       // DEVICE [batch][n_kv_heads][cap] or null
+    int32_t *age;        // DEVICE [batch][n_kv_heads][cap] or null
+    int32_t *lens;       // DEVICE [batch]
+    unsigned int *ticket;   // DEVICE [batch]: arrivals of a row's insert CTAs, left zero by each call
+    int32_t *list;       // DEVICE [batch][n_kv_heads][2][cap], only for caps beyond the insert
+                         // kernel's shared memory
+};
+
+// Attention of the rows' own keys (and of prefix keys not taken by another kernel).
+struct cstr_row_args {
+    const void *q;
+    int64_t q_sb, q_st, q_sh;
+    void *out;
+    int64_t o_sb, o_st, o_sh;
+    float *lse_out;      // [batch][tokens][heads] or null
+    int32_t tokens;
+    const int32_t *pos, *n_query;
+    float scale_log2;    // softmax scale x log2(e)
+    int32_t accumulate;
+};
+int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, cudaStream_t stream);
+
+struct cstr_insert_args {
+    const void *k_new, *v_new;
+    int64_t k_sb, k_st, k_sh, v_sb, v_st, v_sh;
+    int32_t tokens;
+    const int32_t *n_new, *pos;
+    int32_t budget, recent;
+};
+int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStream_t stream);
+
+// Largest cap whose eviction keys and move list fit the insert kernel's shared memory.
+#define CSTR_INSERT_SMEM_SLOTS 24576

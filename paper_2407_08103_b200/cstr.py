@@ -17,6 +17,7 @@ from .build import CHECK_LIB_PATH, LIB_PATH
 
 CSTR_F32 = 0
 CSTR_BF16 = 1
+CSTR_F16 = 2
 CSTR_MAX_TABLES = 16
 CSTR_STATIC_MAX_BATCH = 4096
 
@@ -32,6 +33,8 @@ EXPORTS = [
     "cstr_pda_workspace_create",
     "cstr_free_pda_workspace", "cstr_pda_step", "cstr_pda_step_history",
     "cstr_pda_accept_draft", "cstr_pda_step_status",
+    "cstr_cache_create", "cstr_free_cache", "cstr_cache_insert", "cstr_cache_attention",
+    "cstr_policy_loss",
 ]
 
 # entry points of the checking build only (include/cstr_debug.h)
@@ -63,6 +66,13 @@ def _load(path, debug):
         for name in ("cstr_free_dfa", "cstr_free_vocab", "cstr_free_table", "cstr_free_workspace",
                      "cstr_free_pda", "cstr_free_pda_table", "cstr_free_pda_workspace"):
             getattr(L, name).restype = None
+        L.cstr_free_cache.restype = None
+        # called once per layer and decoding step: declared, so that plain ints can be passed
+        ptr, i32, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
+        L.cstr_cache_insert.argtypes = [ptr, ptr, ptr, ptr, i32, ptr, ptr, i32, i32, ptr]
+        L.cstr_cache_attention.argtypes = [ptr, ptr, ptr, i32, ptr, ptr, f32, i32, ptr, ptr, ptr, ptr]
+        L.cstr_policy_loss.argtypes = [ptr, i32, ptr, ptr, ptr, i32, ctypes.c_int64, i32, f32, ptr, ptr,
+                                       ptr, ptr, ptr, f32, f32, f32, ptr, ptr, ptr, i32, ptr]
         L.is_check_build = debug
         _libs[path] = L
     return _libs[path]
@@ -172,6 +182,11 @@ class PdaTable(_Handle):
 
 class PdaWorkspace(_Handle):
     _free = "cstr_free_pda_workspace"
+
+
+class Cache(_Handle):
+    _free = "cstr_free_cache"
+    arrays = ()   # keep the tensors behind the handle alive
 
 
 def cstr_load_dfa(trans, accept, start_state=0) -> Dfa:
@@ -601,6 +616,184 @@ def cstr_pda_step_status(ws: PdaWorkspace, stream=None):
     vals = [ctypes.c_int64() for _ in range(3)]
     _check(lib().cstr_pda_step_status(ws.ptr, _stream_ptr(stream), *[ctypes.byref(v) for v in vals]))
     return tuple(int(v.value) for v in vals)
+
+
+def _rows_arg(name, t, batch, device, dtype):
+    """Checked per-row vector -> address (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() < batch or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be a contiguous %s tensor with one entry per row on %s"
+                         % (name, dtype, device))
+    return t.data_ptr()
+
+
+def cstr_cache_create(cache_k, cache_v, lens, n_heads: int, prefix_k=None, prefix_v=None,
+                      weight=None, age=None, max_tokens: int = 1) -> Cache:
+    """Record the arrays of one attention layer.  CUDA tensors: ``cache_k`` / ``cache_v``
+    ``[B][cap][n_kv_heads][D]`` bfloat16 or float16, any strides that are multiples of 8 with
+    adjacent ``D``; ``prefix_k`` / ``prefix_v`` ``[P][n_kv_heads][D]`` or None; ``lens`` int32
+    ``[B]``; ``weight`` float32 and ``age`` int32 ``[B][n_kv_heads][cap]`` contiguous or None."""
+    import torch
+    codes = {torch.bfloat16: CSTR_BF16, torch.float16: CSTR_F16}
+    if cache_k.dtype not in codes:
+        raise TypeError("keys and values must be bfloat16 or float16")
+    if cache_k.dim() != 4:
+        raise ValueError("cache_k must be [B][cap][n_kv_heads][D]")
+    batch, cap, heads, dim = cache_k.shape
+    if (prefix_k is None) != (prefix_v is None):
+        raise ValueError("prefix_k and prefix_v go together")
+    length = 0 if prefix_k is None else prefix_k.shape[0]
+    for name, t, shape in (("cache_k", cache_k, (batch, cap, heads, dim)),
+                           ("cache_v", cache_v, (batch, cap, heads, dim)),
+                           ("prefix_k", prefix_k, (length, heads, dim)),
+                           ("prefix_v", prefix_v, (length, heads, dim))):
+        if t is None:
+            continue
+        if t.dtype != cache_k.dtype:
+            raise TypeError("%s must have the dtype of cache_k" % name)
+        if tuple(t.shape) != shape or (t.numel() and t.stride(-1) != 1):
+            raise ValueError("%s must be %s with unit inner stride" % (name, list(shape)))
+    for name, t, dt, n in (("lens", lens, torch.int32, (batch,)),
+                           ("weight", weight, torch.float32, (batch, heads, cap)),
+                           ("age", age, torch.int32, (batch, heads, cap))):
+        if t is not None and (t.dtype != dt or tuple(t.shape) != n or not t.is_contiguous()):
+            raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dt, list(n)))
+    for name, t in (("cache_k", cache_k), ("cache_v", cache_v), ("prefix_k", prefix_k),
+                    ("prefix_v", prefix_v), ("lens", lens), ("weight", weight), ("age", age)):
+        if t is not None and (not t.is_cuda or t.device != cache_k.device):
+            raise ValueError("%s must be a CUDA tensor on the device of cache_k" % name)
+    ps = None if length == 0 else (ctypes.c_int64 * 4)(
+        prefix_k.stride(0), prefix_k.stride(1), prefix_v.stride(0), prefix_v.stride(1))
+    cs = (ctypes.c_int64 * 6)(*cache_k.stride()[:3], *cache_v.stride()[:3])
+    out = ctypes.c_void_p()
+    _check(lib().cstr_cache_create(
+        ctypes.c_int32(codes[cache_k.dtype]), ctypes.c_int32(batch), ctypes.c_int32(n_heads),
+        ctypes.c_int32(heads), ctypes.c_int32(dim), ctypes.c_int32(max_tokens),
+        _dev_ptr(prefix_k) if length else None, _dev_ptr(prefix_v) if length else None,
+        ctypes.c_int64(length), ps, _dev_ptr(cache_k), _dev_ptr(cache_v), ctypes.c_int32(cap), cs,
+        _dev_ptr(weight), _dev_ptr(age), _dev_ptr(lens), ctypes.byref(out)))
+    c = Cache(out)
+    c.arrays = (cache_k, cache_v, prefix_k, prefix_v, lens, weight, age)
+    c.batch, c.n_heads, c.n_kv_heads, c.head_dim = batch, n_heads, heads, dim
+    c.dtype, c.device = cache_k.dtype, cache_k.device
+    return c
+
+
+def _tokens_arg(name, t, cache, tokens, heads):
+    """Checked ``[B][tokens][heads][D]`` tensor -> (address, its first three strides)."""
+    if t.dtype != cache.dtype:
+        raise TypeError("%s must have the dtype of the cache" % name)
+    shape = t.shape
+    if len(shape) != 4 or shape[0] != cache.batch or shape[1] != tokens or shape[2] != heads \
+            or shape[3] != cache.head_dim or t.device != cache.device:
+        raise ValueError("%s must be [%d][%d][%d][%d] on %s"
+                         % (name, cache.batch, tokens, heads, cache.head_dim, cache.device))
+    st = t.stride()
+    if st[3] != 1:
+        raise ValueError("%s must have unit inner stride" % name)
+    return t.data_ptr(), st
+
+
+def cstr_cache_insert(cache: Cache, k_new, v_new, pos, budget: int, recent: int = 0, n_new=None,
+                      stream=None) -> None:
+    """Put ``k_new`` / ``v_new`` ``[B][T][n_kv_heads][D]`` (None: only shrink) into the rows' caches;
+    rows that would exceed ``budget`` entries lose those with the least accumulated weight, the
+    last ``recent`` tokens excepted.  ``pos`` int32 ``[B]``: position of each row's first new
+    token; ``n_new`` int32 ``[B]`` or None."""
+    import torch
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new go together")
+    kp = vp = strides = None
+    tokens = 0
+    if k_new is not None:
+        tokens = k_new.shape[1] if k_new.dim() == 4 else -1
+        kp, ks = _tokens_arg("k_new", k_new, cache, tokens, cache.n_kv_heads)
+        vp, vs = _tokens_arg("v_new", v_new, cache, tokens, cache.n_kv_heads)
+        strides = (ctypes.c_int64 * 6)(ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
+    if pos is None:
+        raise ValueError("pos is required")
+    rc = lib().cstr_cache_insert(cache.ptr, kp, vp, strides, tokens,
+                                 _rows_arg("n_new", n_new, cache.batch, cache.device, torch.int32),
+                                 _rows_arg("pos", pos, cache.batch, cache.device, torch.int32),
+                                 budget, recent, _stream_ptr(stream))
+    if rc:
+        _check(rc)
+
+
+def cstr_cache_attention(cache: Cache, q, out, scale: float | None = None, pos=None, n_query=None,
+                         accumulate: bool = False, lse_out=None, stream=None) -> None:
+    """Attention of ``q`` ``[B][T][n_heads][D]`` over the shared prompt and the rows' caches into
+    ``out`` (same shape).  ``scale`` defaults to ``D ** -0.5``; ``pos`` int32 ``[B]`` (position of
+    token 0) makes it causal; ``n_query`` int32 ``[B]`` or None; ``accumulate`` adds to the cache's
+    weights; ``lse_out`` float32 ``[B][T][n_heads]`` contiguous or None."""
+    import torch
+    tokens = q.shape[1] if q.dim() == 4 else -1
+    qp, qs = _tokens_arg("q", q, cache, tokens, cache.n_heads)
+    op, os_ = _tokens_arg("out", out, cache, tokens, cache.n_heads)
+    lp = None
+    if lse_out is not None:
+        lp = _rows_arg("lse_out", lse_out, cache.batch * tokens * cache.n_heads, cache.device, torch.float32)
+    rc = lib().cstr_cache_attention(
+        cache.ptr, qp, (ctypes.c_int64 * 3)(qs[0], qs[1], qs[2]), tokens,
+        _rows_arg("pos", pos, cache.batch, cache.device, torch.int32),
+        _rows_arg("n_query", n_query, cache.batch, cache.device, torch.int32),
+        cache.head_dim ** -0.5 if scale is None else scale, 1 if accumulate else 0, op,
+        (ctypes.c_int64 * 3)(os_[0], os_[1], os_[2]), lp, _stream_ptr(stream))
+    if rc:
+        _check(rc)
+
+
+def cstr_policy_loss(tables, logits, states, actions, old_logp, advantages, loss_out, logp_out,
+                     ref_logp=None, weight=None, dlogits=None, clip_low: float = 0.2,
+                     clip_high: float = 0.2, kl_coef: float = 0.0, temperature: float = 1.0,
+                     row_table=None, stream=None) -> None:
+    """Clipped policy loss with a KL term over the constrained distribution; with ``dlogits`` also
+    the gradient.  CUDA tensors: ``logits`` / ``dlogits`` ``[N][ld]`` float32 or bfloat16 (may be the
+    same tensor), ``states`` / ``actions`` / ``row_table`` int32 ``[N]``, the others float32 ``[N]``.
+    ``tables`` None or empty (with ``states`` None): unconstrained."""
+    import torch
+    if isinstance(tables, Table):
+        tables = [tables]
+    tables = tables or []
+    if logits.dtype == torch.float32:
+        dtype = CSTR_F32
+    elif logits.dtype == torch.bfloat16:
+        dtype = CSTR_BF16
+    else:
+        raise TypeError("logits must be float32 or bfloat16")
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [N][V] with unit inner stride")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor")
+    n, vocab = logits.shape
+    ld, device = (logits.stride(0) if n > 1 else max(vocab, logits.stride(0))), logits.device
+    dp = None
+    if dlogits is not None:
+        if dlogits.dtype != logits.dtype:
+            raise TypeError("dlogits must have the dtype of logits")
+        if dlogits.shape != logits.shape or dlogits.stride() != logits.stride() or dlogits.device != device:
+            raise ValueError("dlogits must have the layout of logits")
+        dp = dlogits.data_ptr()
+    if bool(tables) != (states is not None):
+        raise ValueError("states go with tables")
+    for name, t in (("actions", actions), ("old_logp", old_logp), ("advantages", advantages),
+                    ("loss_out", loss_out), ("logp_out", logp_out)):
+        if t is None:
+            raise ValueError("%s is required" % name)
+    f32, i32 = torch.float32, torch.int32
+    rc = lib().cstr_policy_loss(
+        (ctypes.c_void_p * len(tables))(*[t.ptr.value for t in tables]) if tables else None,
+        len(tables), _rows_arg("row_table", row_table, n, device, i32),
+        _rows_arg("states", states, n, device, i32), logits.data_ptr(), dtype, ld, vocab, temperature,
+        _rows_arg("actions", actions, n, device, i32), _rows_arg("old_logp", old_logp, n, device, f32),
+        _rows_arg("ref_logp", ref_logp, n, device, f32),
+        _rows_arg("advantages", advantages, n, device, f32),
+        _rows_arg("weight", weight, n, device, f32), clip_low, clip_high, kl_coef,
+        _rows_arg("loss_out", loss_out, n, device, f32), _rows_arg("logp_out", logp_out, n, device, f32),
+        dp, n, _stream_ptr(stream))
+    if rc:
+        _check(rc)
 
 
 def cstr_last_error() -> str:
