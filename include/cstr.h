@@ -598,6 +598,13 @@ int cstr_cache_attention(cstr_cache_t *cache, const void *q, const int64_t *q_st
                          int32_t accumulate, void *out, const int64_t *out_strides,
                          float *lse_out, void *cuda_stream);
 
+/*
+ * Thread blocks of cstr_cache_attention calls since the last status call whose
+ * bounded waits gave up (the outputs are then not valid; never expected: 0).
+ * Synchronises cuda_stream, then resets the count.
+ */
+int cstr_cache_status(cstr_cache_t *cache, void *cuda_stream, int64_t *gave_up);
+
 /* ------------------------------------------------- loss under constraints */
 
 /*

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libcstr.so")
 CHECK_LIB_PATH = os.path.join(PKG_DIR, "libcstr_check.so")
 CHECK_FLAGS = ["-DCSTR_BOUNDS_CHECK", "-DCSTR_TESTING"]
 SOURCES = ["cstr_host.cu", "cstr_build.cu", "cstr_step.cu", "cstr_pda.cu", "cstr_cache.cu",
-           "cstr_cache_attn.cu", "cstr_loss.cu"]
+           "cstr_cache_attn.cu", "cstr_prefix.cu", "cstr_loss.cu"]
 
 
 def _nvcc() -> str:
@@ -42,7 +42,7 @@ def build_library(force: bool = False, verbose: bool = False, check: bool = Fals
     if not force and not _stale(path):
         return path
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3",
-           "-std=c++17", "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
+           "-std=c++17", "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
     if check:
         cmd += CHECK_FLAGS
     cmd += ["-o", path] + [os.path.join(CSRC, s) for s in SOURCES]

@@ -262,6 +262,9 @@ extern "C" void cstr_free_cache(cstr_cache_t *c)
         return;
     cudaFree(c->ticket);
     cudaFree(c->list);
+    cudaFree(c->part_o);
+    cudaFree(c->part_ml);
+    cudaFree(c->status);
     delete c;
 }
 
@@ -335,6 +338,10 @@ extern "C" int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, 
         e = cudaMalloc((void **)&c->ticket, (size_t)batch * 4);
     if (e == cudaSuccess)
         e = cudaMemset(c->ticket, 0, (size_t)batch * 4);
+    if (e == cudaSuccess)
+        e = cudaMalloc((void **)&c->status, 4);
+    if (e == cudaSuccess)
+        e = cudaMemset(c->status, 0, 4);
     if (e == cudaSuccess && cap > CSTR_INSERT_SMEM_SLOTS && weight && age)
         e = cudaMalloc((void **)&c->list, (size_t)batch * n_kv_heads * cap * 8);
     if (e != cudaSuccess) {
@@ -342,6 +349,13 @@ extern "C" int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, 
                        "cstr_cache_create: %s", cudaGetErrorString(e));
         cstr_free_cache(c);
         return rc;
+    }
+    if (prefix_len > 0) {
+        rc = cstr_prefix_init(c);
+        if (rc) {
+            cstr_free_cache(c);
+            return rc;
+        }
     }
     *out = c;
     return CSTR_OK;
@@ -423,5 +437,28 @@ extern "C" int cstr_cache_attention(cstr_cache_t *c, const void *q, const int64_
     a.n_query = n_query;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.accumulate = accumulate ? 1 : 0;
-    return cstr_launch_row_attention(*c, a, (cudaStream_t)cuda_stream);
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    const bool tensor = c->has_maps && c->prefix_len >= 128;
+    if (tensor) {
+        rc = cstr_launch_prefix(*c, a, stream);
+        if (rc)
+            return rc;
+    }
+    return cstr_launch_row_attention(*c, a, !tensor, stream);
+}
+
+extern "C" int cstr_cache_status(cstr_cache_t *c, void *cuda_stream, int64_t *gave_up)
+{
+    if (!c || !gave_up)
+        return cstr_fail(CSTR_ERR_NULL, "cstr_cache_status: null pointer");
+    const int rc = cstr_check_device(c->device, "cache");
+    if (rc)
+        return rc;
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    int n = 0;
+    CSTR_CUDA_TRY(cudaMemcpyAsync(&n, c->status, 4, cudaMemcpyDeviceToHost, stream));
+    CSTR_CUDA_TRY(cudaMemsetAsync(c->status, 0, 4, stream));
+    CSTR_CUDA_TRY(cudaStreamSynchronize(stream));
+    *gave_up = n;
+    return CSTR_OK;
 }

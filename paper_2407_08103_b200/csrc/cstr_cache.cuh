@@ -18,6 +18,12 @@ struct cstr_cache {
     int32_t *age;        // DEVICE [batch][n_kv_heads][cap] or null
     int32_t *lens;       // DEVICE [batch]
     unsigned int *ticket;   // DEVICE [batch]: arrivals of a row's insert CTAs, left zero by each call
+    // attention of the whole batch over the prompt on the tensor cores (cstr_prefix.cu)
+    int has_maps;        // the copy engine can read the prompt: maps and scratch below are there
+    alignas(64) unsigned char map_k[128], map_v[128];     // tensor maps of prefix_k, prefix_v
+    float *part_o;       // DEVICE parts' outputs, [block][head_dim (padded) / 4][128][4]
+    void *part_ml;       // DEVICE float2 [block][128]: parts' maximum and sum
+    int *status;         // DEVICE [1]: CTAs whose bounded waits gave up (never expected)
     int32_t *list;       // DEVICE [batch][n_kv_heads][2][cap], only for caps beyond the insert
                          // kernel's shared memory
 };
@@ -34,7 +40,20 @@ struct cstr_row_args {
     float scale_log2;    // softmax scale x log2(e)
     int32_t accumulate;
 };
-int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, cudaStream_t stream);
+// with_prefix: the prompt's keys belong to the row kernel's lists; else cstr_launch_prefix has
+// been launched before on the stream, and its parts are joined
+int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, bool with_prefix,
+                              cudaStream_t stream);
+
+// How the prefix kernel deals its work out: `pairs` groups of 256 query rows per key / value head,
+// `tiles` key tiles of 128; units (head, group, tile) in this order, CTA i of `grid` takes
+// [i units / grid, (i + 1) units / grid).
+struct cstr_prefix_plan {
+    int pairs, tiles, grid;
+};
+cstr_prefix_plan cstr_plan_prefix(const cstr_cache &c, int tokens);
+int cstr_prefix_init(cstr_cache *c);
+int cstr_launch_prefix(const cstr_cache &c, const cstr_row_args &a, cudaStream_t stream);
 
 struct cstr_insert_args {
     const void *k_new, *v_new;

@@ -47,8 +47,39 @@ struct RowParams {
     int accumulate;
     int split;           // CTAs of a cluster, sharing one key list
     int score_cap;       // slots per query row whose scores fit in shared memory (0: recompute)
+    // parts of the prefix kernel (null: none); see cstr_prefix_plan
+    const float4 *part_o;
+    const float2 *part_ml;
+    int pairs, tiles, grid;
     unsigned long long *oob;
 };
+
+// The prefix kernel's parts for one query row: blocks first, first + step, ... (n of them), at `row`.
+struct PartList {
+    long long first;
+    int n, step, row;
+};
+
+__device__ __forceinline__ PartList parts_of(const RowParams &p, int kh, int m)
+{
+    const int pair = m >> 8, local = m & 255;
+    const bool two_tiles = p.B * p.G * p.T - (pair << 8) > 128;
+    const long long item = (long long)kh * p.pairs + pair, units = (long long)p.Hk * p.pairs * p.tiles;
+    const long long c0 = ((item * p.tiles + 1) * p.grid - 1) / units;
+    const long long c1 = ((item + 1) * p.tiles * p.grid - 1) / units;
+    PartList l;
+    l.row = local & 127;
+    if (two_tiles) {
+        l.first = (c0 + item) * 2 + (local >> 7);
+        l.step = 2;
+        l.n = (int)(c1 - c0 + 1);
+    } else {
+        l.first = (c0 + item) * 2;
+        l.step = 1;
+        l.n = 2 * (int)(c1 - c0 + 1);
+    }
+    return l;
+}
 
 template <typename T> struct Half2;
 template <> struct Half2<__nv_bfloat16> {
@@ -523,6 +554,8 @@ row_attention_kernel(const __grid_constant__ RowParams p)
             cluster.sync();
         else
             __syncthreads();
+        if (p.part_ml)
+            asm volatile("griddepcontrol.wait;" ::: "memory");      // the prefix kernel has finished
 
         // ... and the cluster's, through distributed shared memory; each CTA finishes a share
         // of the outputs and the weights of its own slots
@@ -530,39 +563,61 @@ row_attention_kernel(const __grid_constant__ RowParams p)
             float top = -CUDART_INF_F;
             for (int c = 0; c < p.split; ++c)
                 top = fmaxf(top, p.split > 1 ? *cluster.map_shared_rank(s_cm + r, c) : s_cm[r]);
+            const int t = (r0 + r) / p.G, g = (r0 + r) - t * p.G;
+            const bool real = t < nq;
+            const PartList parts = p.part_ml && real ? parts_of(p, kh, b * R + r0 + r) : PartList{0, 0, 0, 0};
+            for (int i = 0; i < parts.n; ++i)
+                top = fmaxf(top, p.part_ml[(parts.first + (long long)i * parts.step) * 128 + parts.row].x);
             const float ref = top == -CUDART_INF_F ? 0.f : top;
             float sum = 0.f;
+            for (int i = 0; i < parts.n; ++i) {
+                const float2 ml = p.part_ml[(parts.first + (long long)i * parts.step) * 128 + parts.row];
+                sum += exp2_fast(ml.x - ref) * ml.y;
+            }
             for (int c = 0; c < p.split; ++c)
                 sum += p.split > 1 ? exp2_fast(*cluster.map_shared_rank(s_cm + r, c) - ref) * *cluster.map_shared_rank(s_cl + r, c)
                                    : exp2_fast(s_cm[r] - ref) * s_cl[r];
             // nothing seen: +infinity, so that 2^(x - lse) is 0 for every key
             const float lse = sum == 0.f ? CUDART_INF_F : ref + log2f(sum);
             s_lse[r] = lse;
-            if (part == 0 && p.lse_out) {
-                const int t = (r0 + r) / p.G, g = (r0 + r) - t * p.G;
+            if (part == 0 && p.lse_out)
                 p.lse_out[((long long)b * p.T + t) * p.Hq + kh * p.G + g] =
                     sum == 0.f ? -CUDART_INF_F : lse * kLn2;
-            }
         }
         __syncthreads();
-        const int pairs = nr * (p.D / 2);
-        for (int i = part * kWarps * 32 + tid; i < pairs; i += p.split * kWarps * 32) {
-            const int r = i / (p.D / 2), d = 2 * (i - r * (p.D / 2));
-            float2 v = make_float2(0.f, 0.f);
-            for (int c = 0; c < p.split; ++c) {
-                const float *so = p.split > 1 ? cluster.map_shared_rank(s_o, c) : s_o;
-                const float cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, c) : s_cm[r];
-                const float f = exp2_fast(cm - s_lse[r]);
-                const float2 u = *reinterpret_cast<const float2 *>(so + r * DP + d);
-                if (cm != -CUDART_INF_F) {
+        // rows run fastest: the parts keep neighbouring rows side by side
+        const int pieces = nr * (p.D / 4);
+        for (int i = part * kWarps * 32 + tid; i < pieces; i += p.split * kWarps * 32) {
+            const int d4 = i / nr, r = i - d4 * nr;
+            const int t = (r0 + r) / p.G, g = (r0 + r) - t * p.G;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            auto add = [&](float m, const float4 &u) {
+                const float f = exp2_fast(m - s_lse[r]);
+                if (m != -CUDART_INF_F) {
                     v.x += f * u.x;
                     v.y += f * u.y;
+                    v.z += f * u.z;
+                    v.w += f * u.w;
+                }
+            };
+            if (p.part_ml && t < nq) {
+                const PartList parts = parts_of(p, kh, b * R + r0 + r);
+                for (int k = 0; k < parts.n; ++k) {
+                    const long long block = parts.first + (long long)k * parts.step;
+                    const float m = p.part_ml[block * 128 + parts.row].x;
+                    // (a part without keys has no outputs)
+                    if (m != -CUDART_INF_F)
+                        add(m, p.part_o[(block * (DP / 4) + d4) * 128 + parts.row]);
                 }
             }
-            const int t = (r0 + r) / p.G, g = (r0 + r) - t * p.G;
+            for (int c = 0; c < p.split; ++c) {
+                const float *so = p.split > 1 ? cluster.map_shared_rank(s_o, c) : s_o;
+                const float m = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, c) : s_cm[r];
+                add(m, *reinterpret_cast<const float4 *>(so + r * DP + 4 * d4));
+            }
             char *dst = (char *)p.out + ((long long)b * p.o_sb + (long long)t * p.o_st +
-                                         (long long)(kh * p.G + g) * p.o_sh + d) * 2;
-            *reinterpret_cast<unsigned *>(dst) = Half2<T>::pack(v.x, v.y);
+                                         (long long)(kh * p.G + g) * p.o_sh + 4 * d4) * 2;
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(Half2<T>::pack(v.x, v.y), Half2<T>::pack(v.z, v.w));
         }
         // the next rows reuse the memory that peers read, and a CTA must not leave while they do.
         // (Every CTA of the cluster takes the same number of cluster barriers: what follows has none.)
@@ -661,13 +716,18 @@ int launch(const cstr_cache &c, RowParams p, cudaStream_t stream)
     cfg.blockDim = dim3(kWarps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = p.split;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    if (p.part_ml) {                     // may start beside the prefix kernel, and waits for its parts
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.numAttrs = 2;
+    }
     CSTR_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
     return CSTR_OK;
 }
@@ -684,7 +744,8 @@ int launch_typed(const cstr_cache &c, const RowParams &p, cudaStream_t stream)
 
 }  // namespace
 
-int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, cudaStream_t stream)
+int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, bool with_prefix,
+                              cudaStream_t stream)
 {
     RowParams p;
     memset(&p, 0, sizeof p);
@@ -710,7 +771,15 @@ int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, cudaS
     p.G = c.n_heads / c.n_kv_heads;
     p.D = c.head_dim;
     p.cap = c.cap;
-    p.P = (int)c.prefix_len;
+    p.P = with_prefix ? (int)c.prefix_len : 0;
+    if (!with_prefix) {
+        const cstr_prefix_plan s = cstr_plan_prefix(c, a.tokens);
+        p.part_o = (const float4 *)c.part_o;
+        p.part_ml = (const float2 *)c.part_ml;
+        p.pairs = s.pairs;
+        p.tiles = s.tiles;
+        p.grid = s.grid;
+    }
     p.scale_log2 = a.scale_log2;
     p.accumulate = a.accumulate;
     p.oob = CSTR_OOB_RECORD();

@@ -1,0 +1,618 @@
+// Attention of a whole batch over the prompt that its rows share, on the tensor
+// cores: for one key / value head all query rows of the batch form one matrix of
+// M = batch x tokens x group rows, so the prompt's keys and values are read once
+// per 256 of them instead of once per row.
+//
+// Mathematics: as in the row kernel, one pass over the keys with the running
+// maximum m and sum l of a base-2 softmax and o = sum 2^(x - m) v, over a part
+// of the prompt; parts (m, l, o) are joined by the row kernel.
+//
+// One CTA works on two "streams", each with its own 128-row scores S and output
+// O in tensor memory (4 x 128 columns = all 512):
+//   more than 128 query rows left: two tiles of query rows over the same keys;
+//   else: one tile, the streams taking alternate key tiles.
+// While the 128 threads of one stream turn its S into probabilities P, the
+// tensor cores work for the other stream.  One thread issues all products,
+// S = Q K^T (both operands from shared memory) and O += P V (P from tensor
+// memory, over its own S), one thread issues the copies into a ring of tiles.
+//
+// Split: the units (key tile x group of 256 query rows) are dealt out evenly and
+// contiguously to one CTA per SM, so a CTA starts or ends within a row group and
+// no SM idles in a last wave, whatever the sizes; each (CTA, row group) segment
+// leaves one part.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math_constants.h>
+#include <string.h>
+
+#include "cstr_cache.cuh"
+
+namespace {
+
+constexpr int kThreads = 384;        // warps 0-3: copies, products, tensor memory, -; 4-7, 8-11: streams
+constexpr int kTile = 128;           // query rows and keys of a tile
+// A maximum that grew by less than 2^8 keeps the old reference: P stays below 2^8, in range of
+// both 16-bit types, and the rescaling of O (a round trip through registers) is left out.
+constexpr float kLazy = 8.f;
+constexpr unsigned kWaitLimit = 1u << 22;
+
+template <int DP> struct Shape {
+    static constexpr int kTileBytes = kTile * DP * 2;
+    static constexpr int kSlots = DP == 128 ? 5 : 8;
+    static constexpr int kSmem = (2 + kSlots) * kTileBytes + 1024 /* alignment */ + 256;
+};
+
+struct PrefixParams {
+    const void *q;
+    long long q_sb, q_st, q_sh;
+    float *part_o;
+    float2 *part_ml;
+    int *status;
+    int M, T, G, R, D, P, Hk;        // R = T G query rows of one batch row
+    int tiles, pairs, grid;
+    float scale_log2;                // >= 0: a negative scale flips the queries' signs
+    int flip;
+};
+
+__device__ __forceinline__ unsigned smem_addr(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <typename T> __device__ __forceinline__ unsigned pack2(float lo, float hi);
+template <> __device__ __forceinline__ unsigned pack2<__nv_bfloat16>(float lo, float hi)
+{
+    unsigned u;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+    return u;
+}
+template <> __device__ __forceinline__ unsigned pack2<__half>(float lo, float hi)
+{
+    unsigned u;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+    return u;
+}
+
+// ---- barriers: every wait ends, after kWaitLimit tries with the CTA's abort flag set ----
+
+__device__ __forceinline__ void bar_init(unsigned bar, unsigned count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(unsigned bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __noinline__ bool bar_wait_slow(unsigned bar, unsigned parity, volatile int *abort)
+{
+    for (unsigned i = 0; i < kWaitLimit; ++i) {
+        if (bar_try(bar, parity))
+            return true;
+        if (*abort)
+            return false;
+    }
+    *abort = 1;
+    return false;
+}
+__device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile int *abort)
+{
+    return bar_try(bar, parity) || bar_wait_slow(bar, parity, abort);
+}
+
+// ---- tensor memory and products ---------------------------------------------
+
+__device__ __forceinline__ void tmem_ld32(float (&r)[32], unsigned addr)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+          "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+          "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+          "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(unsigned addr, const float (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        ::"f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]),
+          "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]),
+          "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]),
+          "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31]),
+          "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(unsigned addr, const unsigned (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void commit(unsigned bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Shared-memory operand with 128-byte rows in the 128-byte swizzle; `lead`: bytes between blocks of
+// 64 elements along the row dimension of a transposed operand.
+__device__ __forceinline__ unsigned long long operand(unsigned addr, unsigned lead)
+{
+    return (unsigned long long)((addr & 0x3ffffu) >> 4) | ((unsigned long long)(lead >> 4) << 16) |
+           ((unsigned long long)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+__device__ __forceinline__ void mma_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool add)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(unsigned d, unsigned a, unsigned long long b, unsigned idesc, bool add)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((unsigned)add) : "memory");
+}
+
+__device__ __forceinline__ void tma_tile(unsigned dst, const CUtensorMap *map, int x, int key, int head, unsigned bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"((unsigned long long)map), "r"(x), "r"(key), "r"(head), "r"(bar) : "memory");
+}
+
+// The part of one CTA's unit range that lies in one row group.
+struct Segment {
+    int item, tile0, tiles, rows;    // key tiles [tile0, tile0 + tiles); query rows of the group
+    bool pair_rows;                  // two row tiles (else: one, key tiles alternating)
+};
+
+struct Walk {
+    const PrefixParams &p;
+    long long at, end;
+    __device__ __forceinline__ explicit Walk(const PrefixParams &p_) : p(p_)
+    {
+        const long long units = (long long)p.Hk * p.pairs * p.tiles;
+        at = units * blockIdx.x / p.grid;
+        end = units * (blockIdx.x + 1) / p.grid;
+    }
+    __device__ __forceinline__ bool next(Segment &s)
+    {
+        if (at >= end)
+            return false;
+        s.item = (int)(at / p.tiles);
+        s.tile0 = (int)(at - (long long)s.item * p.tiles);
+        s.tiles = (int)min((long long)(p.tiles - s.tile0), end - at);
+        const int pair = s.item % p.pairs;
+        s.rows = min(p.M - pair * 2 * kTile, 2 * kTile);
+        s.pair_rows = s.rows > kTile;
+        at += s.tiles;
+        return true;
+    }
+};
+
+// Place of a tile in a segment's sequence of copies: the first `lead` key tiles, then value tile i
+// and key tile i + lead in turn - the order in which the products use them.
+__device__ __forceinline__ int place_k(int i, int lead) { return i < lead ? i : 2 * i - lead + 1; }
+__device__ __forceinline__ int place_v(int i, int lead, int n)
+{
+    return i <= n - lead ? lead + 2 * i : n + i;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                        const __grid_constant__ PrefixParams p)
+{
+    using S = Shape<DP>;
+    constexpr int kSlots = S::kSlots;
+    extern __shared__ char smem_raw[];
+    __shared__ __align__(8) unsigned long long s_bar[2 * kSlots + 9];
+    __shared__ unsigned s_tmem;
+    __shared__ int s_abort;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    const unsigned raw = smem_addr(smem_raw);
+    const unsigned q_tile = (raw + 1023u) & ~1023u;              // [2][kTile][DP], swizzled
+    char *q_ptr = smem_raw + (q_tile - raw);
+    const unsigned ring = q_tile + 2 * S::kTileBytes;
+    const unsigned bars = smem_addr(s_bar);
+    auto full = [&](int slot) { return bars + 8u * slot; };
+    auto empty = [&](int slot) { return bars + 8u * (kSlots + slot); };
+    const unsigned q_full = bars + 8u * (2 * kSlots), drain = q_full + 56, q_free = q_full + 64;
+    auto s_full = [&](int s) { return q_full + 8u * (1 + s); };
+    auto p_full = [&](int s) { return q_full + 8u * (3 + s); };
+    auto o_full = [&](int s) { return q_full + 8u * (5 + s); };
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int *abort = &s_abort;
+    if (tid == 0) {
+        s_abort = 0;
+        for (int i = 0; i < kSlots; ++i) {
+            bar_init(full(i), 1);
+            bar_init(empty(i), 1);
+        }
+        bar_init(q_full, 256);
+        for (int s = 0; s < 2; ++s) {
+            bar_init(s_full(s), 1);
+            bar_init(p_full(s), 4);
+            bar_init(o_full(s), 1);
+        }
+        bar_init(drain, 1);
+        bar_init(q_free, 8);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        fence_before();
+    }
+    __syncthreads();
+    fence_after();
+    const unsigned tmem = s_tmem;
+    const unsigned t_s = tmem, t_o = tmem + 2 * kTile;           // S (and P over it), O: + stream * 128
+
+    Walk walk(p);
+    Segment g;
+    if (warp == 0) {
+        if (lane == 0) {                                         // copies
+            unsigned count = 0;
+            bool alive = true;
+            auto put = [&](const CUtensorMap *map, int key_tile, int head) {
+                const int slot = count % kSlots;
+                alive = alive && bar_wait(empty(slot), ((count / kSlots) & 1u) ^ 1u, abort);
+                if (!alive)
+                    return;
+                bar_expect(full(slot), S::kTileBytes);
+#pragma unroll
+                for (int x = 0; x < DP / 64; ++x)
+                    tma_tile(ring + slot * S::kTileBytes + x * (kTile * 128), map, x * 64, key_tile * kTile, head, full(slot));
+                ++count;
+            };
+            while (alive && walk.next(g)) {
+                const int head = g.item / p.pairs;
+                const int lead = min(g.pair_rows ? 1 : 2, g.tiles);
+                for (int i = 0; i < lead; ++i)
+                    put(&map_k, g.tile0 + i, head);
+                for (int i = 0; i < g.tiles && alive; ++i) {
+                    put(&map_v, g.tile0 + i, head);
+                    if (i + lead < g.tiles)
+                        put(&map_k, g.tile0 + i + lead, head);
+                }
+            }
+            if (*abort)                                          // let the copies in flight land
+                for (unsigned i = count > kSlots ? count - kSlots : 0; i < count; ++i)
+                    for (unsigned k = 0; k < kWaitLimit && !bar_try(full(i % kSlots), (i / kSlots) & 1u); ++k) {}
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {                                         // products
+            constexpr unsigned type = sizeof(T) && __is_same(T, __nv_bfloat16) ? 1u : 0u;
+            constexpr unsigned idesc = (1u << 4) | (type << 7) | (type << 10) | ((kTile / 16) << 24);
+            constexpr unsigned idesc_s = idesc | ((kTile / 8) << 17);
+            constexpr unsigned idesc_o = idesc | (1u << 16) | ((DP / 8) << 17);
+            unsigned base = 0, seg = 0, p_count[2] = {0, 0};
+            bool alive = true;
+            while (alive && walk.next(g)) {
+                const int lead = min(g.pair_rows ? 1 : 2, g.tiles);
+                const int visits = g.pair_rows ? 2 * g.tiles : g.tiles;
+                const int shift = g.pair_rows ? 1 : 0;
+                alive = bar_wait(q_full, seg & 1u, abort);
+                ++seg;
+                auto scores = [&](int n) {
+                    const unsigned at = base + place_k(n >> shift, lead);
+                    const int slot = at % kSlots;
+                    alive = alive && bar_wait(full(slot), (at / kSlots) & 1u, abort);
+                    if (!alive)
+                        return;
+                    fence_after();
+                    const int s = n & 1;
+                    const unsigned qa = q_tile + (g.pair_rows ? s : 0) * S::kTileBytes, ka = ring + slot * S::kTileBytes;
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const unsigned off = (k / 4) * (kTile * 128) + (k % 4) * 32;
+                        mma_ss(t_s + s * kTile, operand(qa + off, 16), operand(ka + off, 16), idesc_s, k > 0);
+                    }
+                    commit(s_full(s));
+                    if (!g.pair_rows || s == 1)
+                        commit(empty(slot));
+                };
+                if (alive)
+                    scores(0);
+                if (alive && visits > 1)
+                    scores(1);
+                for (int n = 0; n < visits && alive; ++n) {
+                    const int s = n & 1;
+                    const unsigned at = base + place_v(n >> shift, lead, g.tiles);
+                    const int slot = at % kSlots;
+                    alive = bar_wait(full(slot), (at / kSlots) & 1u, abort) && bar_wait(p_full(s), p_count[s] & 1u, abort);
+                    if (!alive)
+                        break;
+                    ++p_count[s];
+                    fence_after();
+                    const unsigned va = ring + slot * S::kTileBytes;
+#pragma unroll
+                    for (int k = 0; k < kTile / 16; ++k)
+                        mma_ts(t_o + s * kTile, t_s + s * kTile + 8 * k, operand(va + k * 2048, kTile * 128), idesc_o,
+                               n >= 2 || k > 0);
+                    commit(o_full(s));
+                    if (!g.pair_rows || s == 1)
+                        commit(empty(slot));
+                    if (n + 2 < visits)
+                        scores(n + 2);
+                }
+                base += 2 * g.tiles;
+            }
+            if (*abort) {                                        // let the products in flight end
+                commit(drain);
+                for (unsigned k = 0; k < kWaitLimit && !bar_try(drain, 0); ++k) {}
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        const int s = (warp - 4) >> 2, row = ((warp & 3) << 5) + lane;    // stream; row of its tile = TMEM lane
+        const unsigned lane_base = (unsigned)((warp & 3) << 5) << 16;
+        const unsigned my_s = t_s + s * kTile + lane_base, my_o = t_o + s * kTile + lane_base;
+        unsigned seg = 0, done = 0;                              // segments; visits of this stream so far
+        bool alive = true;
+        while (alive && walk.next(g)) {
+            // both streams have seen their last scores: the query tiles may be replaced
+            __syncwarp();
+            if (lane == 0)
+                bar_arrive(q_free);
+            if (!(alive = __all_sync(0xffffffffu, bar_wait(q_free, seg & 1u, abort))))
+                break;
+            ++seg;
+            const int head = g.item / p.pairs, row0 = (g.item % p.pairs) * 2 * kTile;
+            const int q_rows = g.pair_rows ? 2 * kTile : kTile;
+            for (int i = tid - 128; i < q_rows * (DP / 8); i += 256) {
+                const int r = i / (DP / 8), ch = i % (DP / 8);
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (r < g.rows && ch * 8 < p.D) {
+                    const int m = row0 + r, b = m / p.R, in = m - b * p.R, t = in / p.G, gh = in - t * p.G;
+                    v = *reinterpret_cast<const uint4 *>((const char *)p.q + 2 * ((long long)b * p.q_sb + (long long)t * p.q_st +
+                                                         (long long)(head * p.G + gh) * p.q_sh + ch * 8));
+                    if (p.flip)
+                        v.x ^= 0x80008000u, v.y ^= 0x80008000u, v.z ^= 0x80008000u, v.w ^= 0x80008000u;
+                }
+                *reinterpret_cast<uint4 *>(q_ptr + (r / kTile) * S::kTileBytes + (ch / 8) * (kTile * 128) +
+                                           (r % kTile) * 128 + (((ch ^ r) & 7) << 4)) = v;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            bar_arrive(q_full);
+
+            const int my_row = g.pair_rows ? s * kTile + row : row;      // row of the group
+            const bool warp_on = my_row - lane < g.rows;
+            const int visits = g.pair_rows ? 2 * g.tiles : g.tiles;
+            float m = -CUDART_INF_F, l = 0.f;
+            int mine = 0;                                        // visits of this stream in this segment
+            for (int n = s; n < visits; n += 2, ++mine, ++done) {
+                if (!(alive = __all_sync(0xffffffffu, bar_wait(s_full(s), done & 1u, abort))))
+                    break;
+                fence_after();
+                if (warp_on) {
+                    float x[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        tmem_ld32(x[c], my_s + 32 * c);
+                    tmem_wait_ld();
+                    const int valid = p.P - (g.tile0 + (g.pair_rows ? n >> 1 : n)) * kTile;
+                    if (valid < kTile) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (c * 32 + i >= valid)
+                                    x[c][i] = -CUDART_INF_F;
+                    }
+                    float top[4] = {x[0][0], x[1][0], x[2][0], x[3][0]};
+#pragma unroll
+                    for (int i = 1; i < 32; ++i)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            top[c] = fmaxf(top[c], x[c][i]);
+                    const float seen = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+                    const bool grow = seen > m + kLazy || (m == -CUDART_INF_F && seen > m);
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float to = grow ? seen : m;
+                        const float f = m == to ? 1.f : exp2_fast(m - to);
+                        l *= f;
+                        m = to;
+                        if (mine > 0) {                          // O so far counts from the old maximum
+                            if (!(alive = __all_sync(0xffffffffu, bar_wait(o_full(s), (done - 1) & 1u, abort))))
+                                break;
+                            fence_after();
+#pragma unroll
+                            for (int c = 0; c < DP / 32; ++c) {
+                                float o[32];
+                                tmem_ld32(o, my_o + 32 * c);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    o[i] *= f;
+                                tmem_st32(my_o + 32 * c, o);
+                            }
+                        }
+                    }
+                    const float ref = m == -CUDART_INF_F ? 0.f : m;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        unsigned w[16];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const float a = exp2_fast(fmaf(x[c][i], p.scale_log2, -ref));
+                            const float b = exp2_fast(fmaf(x[c][i + 1], p.scale_log2, -ref));
+                            sum[i & 2] += a;
+                            sum[(i & 2) + 1] += b;
+                            // rounded to the values' type for the second product; the sum is not
+                            w[i / 2] = pack2<T>(a, b);
+                        }
+                        tmem_st16(my_s + 16 * c, w);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_wait_st();
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    bar_arrive(p_full(s));
+            }
+            if (!alive)
+                break;
+            // this segment's part: O as [DP / 4][128][4], so that a warp's rows are adjacent
+            const long long block = ((long long)blockIdx.x + g.item) * 2 + s;
+            if (mine > 0) {
+                if (!(alive = __all_sync(0xffffffffu, bar_wait(o_full(s), (done - 1) & 1u, abort))))
+                    break;
+                fence_after();
+            }
+            if (warp_on) {
+                if (mine > 0) {
+                    float4 *dst = reinterpret_cast<float4 *>(p.part_o) + block * (DP / 4) * kTile + row;
+#pragma unroll
+                    for (int c = 0; c < DP / 32; ++c) {
+                        float o[32];
+                        tmem_ld32(o, my_o + 32 * c);
+                        tmem_wait_ld();
+                        if (my_row < g.rows)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                dst[(c * 8 + i) * kTile] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    }
+                }
+                if (my_row < g.rows)
+                    p.part_ml[block * kTile + row] = make_float2(m, l);
+            }
+            fence_before();
+        }
+    }
+    __syncthreads();
+    if (tid == 0 && s_abort)
+        atomicAdd(p.status, 1);
+    if (warp == 2) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+template <typename T, int DP>
+int launch(const cstr_cache &c, const PrefixParams &p, cudaStream_t stream)
+{
+    auto kernel = prefix_attention_kernel<T, DP>;
+    CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kSmem));
+    CUtensorMap k, v;
+    memcpy(&k, c.map_k, sizeof k);
+    memcpy(&v, c.map_v, sizeof v);
+    kernel<<<p.grid, kThreads, Shape<DP>::kSmem, stream>>>(k, v, p);
+    CSTR_CUDA_TRY(cudaGetLastError());
+    return CSTR_OK;
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+}  // namespace
+
+cstr_prefix_plan cstr_plan_prefix(const cstr_cache &c, int tokens)
+{
+    cstr_prefix_plan s;
+    const long long rows = (long long)c.batch * tokens * (c.n_heads / c.n_kv_heads);
+    s.pairs = (int)((rows + 2 * kTile - 1) / (2 * kTile));
+    s.tiles = (int)((c.prefix_len + kTile - 1) / kTile);
+    const long long units = (long long)c.n_kv_heads * s.pairs * s.tiles;
+    s.grid = (int)(units < c.sm_count ? units : c.sm_count);
+    return s;
+}
+
+int cstr_prefix_init(cstr_cache *c)
+{
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    CSTR_CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
+    if (!fn || found != cudaDriverEntryPointSuccess)
+        return cstr_fail(CSTR_ERR_CUDA, "cstr_cache_create: the driver has no cuTensorMapEncodeTiled");
+    for (int i = 0; i < 2; ++i) {
+        CUtensorMap map;
+        const cuuint64_t dims[3] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->prefix_len, (cuuint64_t)c->n_kv_heads};
+        const int64_t st = i ? c->pv_st : c->pk_st, sh = i ? c->pv_sh : c->pk_sh;
+        // the stride of a dimension of extent 1 is never used, but has to be a valid one
+        const cuuint64_t strides[2] = {(cuuint64_t)(c->prefix_len > 1 ? st * 2 : 16),
+                                       (cuuint64_t)(c->n_kv_heads > 1 ? sh * 2 : 16)};
+        const cuuint32_t box[3] = {64, kTile, 1}, ones[3] = {1, 1, 1};
+        const CUresult r = ((EncodeTiled)fn)(
+            &map, c->dtype == CSTR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+            const_cast<void *>(i ? c->prefix_v : c->prefix_k), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS)
+            return CSTR_OK;              // strides that the copy engine cannot take: the row kernel reads the prompt
+        static_assert(sizeof map == sizeof c->map_k, "tensor map size");
+        memcpy(i ? c->map_v : c->map_k, &map, sizeof map);
+    }
+    // parts: every (CTA, row group) segment has one; CTA index + group index numbers them
+    const cstr_prefix_plan s = cstr_plan_prefix(*c, c->max_tokens);
+    const size_t blocks = ((size_t)c->sm_count + (size_t)c->n_kv_heads * s.pairs) * 2;
+    const size_t dp = c->head_dim > 64 ? 128 : 64;
+    CSTR_CUDA_TRY(cudaMalloc((void **)&c->part_o, blocks * kTile * dp * sizeof(float)));
+    CSTR_CUDA_TRY(cudaMalloc((void **)&c->part_ml, blocks * kTile * sizeof(float2)));
+    c->has_maps = 1;
+    return CSTR_OK;
+}
+
+int cstr_launch_prefix(const cstr_cache &c, const cstr_row_args &a, cudaStream_t stream)
+{
+    PrefixParams p;
+    memset(&p, 0, sizeof p);
+    const cstr_prefix_plan s = cstr_plan_prefix(c, a.tokens);
+    p.q = a.q;
+    p.q_sb = a.q_sb, p.q_st = a.q_st, p.q_sh = a.q_sh;
+    p.part_o = c.part_o;
+    p.part_ml = (float2 *)c.part_ml;
+    p.status = c.status;
+    p.T = a.tokens;
+    p.G = c.n_heads / c.n_kv_heads;
+    p.R = p.T * p.G;
+    p.M = c.batch * p.R;
+    p.D = c.head_dim;
+    p.P = (int)c.prefix_len;
+    p.Hk = c.n_kv_heads;
+    p.tiles = s.tiles;
+    p.pairs = s.pairs;
+    p.grid = s.grid;
+    p.flip = a.scale_log2 < 0.f;
+    p.scale_log2 = p.flip ? -a.scale_log2 : a.scale_log2;
+    const bool wide = c.head_dim > 64;
+    if (c.dtype == CSTR_BF16)
+        return wide ? launch<__nv_bfloat16, 128>(c, p, stream) : launch<__nv_bfloat16, 64>(c, p, stream);
+    return wide ? launch<__half, 128>(c, p, stream) : launch<__half, 64>(c, p, stream);
+}

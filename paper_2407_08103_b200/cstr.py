@@ -34,6 +34,7 @@ EXPORTS = [
     "cstr_free_pda_workspace", "cstr_pda_step", "cstr_pda_step_history",
     "cstr_pda_accept_draft", "cstr_pda_step_status",
     "cstr_cache_create", "cstr_free_cache", "cstr_cache_insert", "cstr_cache_attention",
+    "cstr_cache_status",
     "cstr_policy_loss",
 ]
 
@@ -742,6 +743,14 @@ def cstr_cache_attention(cache: Cache, q, out, scale: float | None = None, pos=N
         (ctypes.c_int64 * 3)(os_[0], os_[1], os_[2]), lp, _stream_ptr(stream))
     if rc:
         _check(rc)
+
+
+def cstr_cache_status(cache: Cache, stream=None) -> int:
+    """Thread blocks of attention calls whose bounded waits gave up since the last status call
+    (0 unless something is badly wrong).  Synchronises the stream."""
+    out = ctypes.c_int64()
+    _check(lib().cstr_cache_status(cache.ptr, _stream_ptr(stream), ctypes.byref(out)))
+    return int(out.value)
 
 
 def cstr_policy_loss(tables, logits, states, actions, old_logp, advantages, loss_out, logp_out,
