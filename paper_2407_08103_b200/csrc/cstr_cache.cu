@@ -12,17 +12,22 @@ namespace {
 // ---- insertion -------------------------------------------------------------
 //
 // One CTA per row and key / value head.  Entries are ordered by (protected,
-// weight, slot).  Their 32-bit keys (order-preserving bits of the weight;
-// all ones when protected; 0 for NaN) are read once into shared memory; the
-// e-th smallest key is found by four passes over 8-bit digits, counting into
-// 256 bins, and ties at that key are taken in slot order.  Evicted slots below
-// the new length and surviving slots past it are then enumerated in slot order
-// by ballots and prefix sums, and the i-th free place gets the i-th mover.  All
-// of it is counting, so the result does not depend on the order of atomics.
+// weight, slot); their 32-bit keys are order-preserving bits of the weight, all
+// ones when protected, 0 for NaN.
+//   One entry to evict (a decoding step with a full cache): the smallest (key,
+// slot) pair, found while the row is read.
+//   More: the keys are put into shared memory, the e-th smallest is found by
+// three passes over digits of 11, 11 and 10 bits (counts per digit, then a scan),
+// and ties at that key are taken in slot order.  Evicted slots below the new
+// length, and surviving ones past it, are listed in slot order: each warp counts
+// its own range, the counts are added up across warps, and the warp writes from
+// there.  The i-th free place gets the i-th mover.
+// All of it is counting, so no result depends on the order of atomics.
 //
 // Bound: 8 bytes per entry (weight, age) are read; only new tokens, and
 // survivors past the new length, are copied.
-constexpr int kInsertThreads = 256;
+constexpr int kMaxThreads = 256;
+constexpr int kBins = 2048;
 
 struct InsertParams {
     const char *k_new, *v_new;
@@ -35,6 +40,7 @@ struct InsertParams {
     unsigned int *ticket;
     int32_t *list;       // null: keys and places live in shared memory
     int B, Hk, D, cap, T, budget, recent;
+    int wide;            // weight and age rows can be read 16 bytes at a time
     unsigned long long *oob;
 };
 
@@ -48,33 +54,149 @@ __device__ __forceinline__ unsigned evict_key(float w, int age, int protect_from
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Exclusive prefix over the block of one flag per thread; total in *all.
-__device__ __forceinline__ int block_rank(bool flag, int *s_warp, int &all)
+// f(slot, key) for the slots [0, len) of a row, each by one thread of the CTA
+template <typename F>
+__device__ __forceinline__ void for_keys(const InsertParams &p, const float *weight, const int32_t *age, int len,
+                                         int protect_from, F f)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const unsigned hits = __ballot_sync(0xffffffffu, flag);
-    __syncthreads();                                              // s_warp free again
-    if (lane == 0)
-        s_warp[warp] = __popc(hits);
-    __syncthreads();
-    int before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < kInsertThreads / 32; ++w) {
-        before += w < warp ? s_warp[w] : 0;
-        all += s_warp[w];
+    if (p.wide) {
+#pragma unroll 4
+        for (int j = threadIdx.x * 4; j < len; j += blockDim.x * 4) {
+            const float4 w = *reinterpret_cast<const float4 *>(weight + j);
+            const int4 a = *reinterpret_cast<const int4 *>(age + j);
+            f(j, evict_key(w.x, a.x, protect_from));
+            if (j + 1 < len)
+                f(j + 1, evict_key(w.y, a.y, protect_from));
+            if (j + 2 < len)
+                f(j + 2, evict_key(w.z, a.z, protect_from));
+            if (j + 3 < len)
+                f(j + 3, evict_key(w.w, a.w, protect_from));
+        }
+    } else {
+#pragma unroll 4
+        for (int j = threadIdx.x; j < len; j += blockDim.x)
+            f(j, evict_key(weight[j], age[j], protect_from));
     }
-    return before + __popc(hits & ((1u << lane) - 1u));
 }
 
-__global__ void __launch_bounds__(kInsertThreads)
+// Lists the free places below new_len (ascending, from place[0]) and the surviving slots at or past
+// it (ascending, from place[cap - 1] downwards); returns the number of the latter.  `evict` >= 2.
+__device__ __forceinline__ int choose(const InsertParams &p, const unsigned *keys, int *place, int *s_bin, int *s_word,
+                                      int len, int new_len, int evict)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    unsigned prefix = 0, fixed = 0;                               // digits found so far, and their mask
+    int want = evict;                                             // rank among the keys with this prefix
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const unsigned digits = pass == 2 ? 1023u : 2047u;
+        for (int i = tid; i < kBins; i += blockDim.x)
+            s_bin[i] = 0;
+        __syncthreads();
+        for (int j = tid; j - lane < len; j += blockDim.x) {      // whole warps
+            const unsigned k = j < len ? keys[j] : 0u;
+            const bool in = j < len && (k & fixed) == prefix;
+            const unsigned d = in ? (k >> shift) & digits : 0xffffffffu;
+            int same;
+            __match_all_sync(0xffffffffu, d, &same);              // e.g. nothing weighed yet: all zero
+            if (same) {
+                if (in && lane == 0)
+                    atomicAdd(&s_bin[d], 32);
+            } else if (in)
+                atomicAdd(&s_bin[d], 1);
+        }
+        __syncthreads();
+        // first digit whose running count reaches `want`: a thread adds up its bins, the warps scan
+        const int per = kBins / (int)blockDim.x;
+        int sum = 0;
+        for (int i = 0; i < per; ++i)
+            sum += s_bin[tid * per + i];
+        int upto = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, upto, off);
+            upto += lane >= off ? o : 0;
+        }
+        if (lane == 31)
+            s_word[warp] = upto;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w)
+            upto += s_word[w];
+        if (upto >= want && upto - sum < want) {                  // one thread
+            int below = upto - sum, d = tid * per;
+            while (below + s_bin[d] < want)
+                below += s_bin[d++];
+            s_word[kMaxThreads / 32] = d;
+            s_word[kMaxThreads / 32 + 1] = below;
+        }
+        __syncthreads();
+        prefix |= (unsigned)s_word[kMaxThreads / 32] << shift;
+        fixed |= digits << shift;
+        want -= s_word[kMaxThreads / 32 + 1];
+        __syncthreads();
+    }
+    // evicted: key < prefix, and the first `want` slots with key == prefix
+    const int span = ((len + warps - 1) / warps + 31) & ~31;      // slots of a warp
+    const int lo = min(warp * span, len), hi = min(lo + span, len);
+    int ties = 0;
+    for (int j = lo + lane; j - lane < hi; j += 32)
+        ties += __popc(__ballot_sync(0xffffffffu, j < hi && keys[j] == prefix));
+    if (lane == 0)
+        s_word[warp] = ties;
+    __syncthreads();
+    int tie0 = 0;
+    for (int w = 0; w < warp; ++w)
+        tie0 += s_word[w];
+    __syncthreads();
+    int holes = 0, movers = 0;
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {                     // count, then write
+        int hole0 = 0, mover0 = 0, tie = tie0;
+        if (round == 1) {
+            if (lane == 0)
+                s_word[warp] = holes, s_word[kMaxThreads / 32 + warp] = movers;
+            __syncthreads();
+            for (int w = 0; w < warp; ++w)
+                hole0 += s_word[w], mover0 += s_word[kMaxThreads / 32 + w];
+        }
+        holes = movers = 0;
+        for (int j = lo + lane; j - lane < hi; j += 32) {
+            const unsigned k = j < hi ? keys[j] : 0xffffffffu, below = (1u << lane) - 1u;
+            const unsigned equal = __ballot_sync(0xffffffffu, j < hi && k == prefix);
+            const bool gone = j < hi && (k < prefix || (k == prefix && tie + __popc(equal & below) < want));
+            tie += __popc(equal);
+            const unsigned hole = __ballot_sync(0xffffffffu, gone && j < new_len);
+            const unsigned mover = __ballot_sync(0xffffffffu, j < hi && !gone && j >= new_len);
+            if (round == 1) {
+                if (gone && j < new_len)
+                    place[hole0 + holes + __popc(hole & below)] = j;
+                if (j < hi && !gone && j >= new_len)
+                    place[p.cap - 1 - (mover0 + movers + __popc(mover & below))] = j;
+            }
+            holes += __popc(hole);
+            movers += __popc(mover);
+        }
+        if (round == 1 && warp == warps - 1 && lane == 0) {       // totals
+            s_word[2 * (kMaxThreads / 32)] = hole0 + holes;
+            s_word[2 * (kMaxThreads / 32) + 1] = mover0 + movers;
+        }
+    }
+    __syncthreads();
+    const int all = s_word[2 * (kMaxThreads / 32)];
+    for (int j = len + tid; j < new_len; j += blockDim.x)         // free places past the old length
+        place[all + j - len] = j;
+    __syncthreads();
+    return s_word[2 * (kMaxThreads / 32) + 1];
+}
+
+__global__ void __launch_bounds__(kMaxThreads)
 cache_insert_kernel(const __grid_constant__ InsertParams p)
 {
     extern __shared__ int s_dyn[];
-    __shared__ int s_bin[256];
-    __shared__ int s_warp[kInsertThreads / 32];
-    __shared__ int s_digit, s_below;
-    const int tid = threadIdx.x;
+    __shared__ int s_word[2 * (kMaxThreads / 32) + 2];
+    __shared__ unsigned long long s_least[kMaxThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.x / p.Hk, kh = blockIdx.x - b * p.Hk;
     const int len = min(max(p.lens[b], 0), p.cap);
     const int n = p.n_new ? min(max(p.n_new[b], 0), p.T) : p.T;
@@ -84,110 +206,93 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
     const long long entry0 = ((long long)b * p.Hk + kh) * p.cap;
     float *weight = p.weight + entry0;
     int32_t *age = p.age + entry0;
-    unsigned *keys = reinterpret_cast<unsigned *>(p.list ? p.list + entry0 * 2 : s_dyn);
-    int *place = reinterpret_cast<int *>(keys + p.cap);           // free places, ascending
+    int *s_bin = s_dyn;
+    unsigned *keys = reinterpret_cast<unsigned *>(p.list ? p.list + entry0 * 2 : s_dyn + kBins);
+    int *place = reinterpret_cast<int *>(keys + p.cap);
     int n_old = 0;                                                // survivors past the new length
+    int only = len;                                               // the place, where there is one to fill
 
-    if (evict > 0) {
-        const int protect_from = pos + n - p.recent;
-        for (int j = tid; j < len; j += kInsertThreads)
-            keys[j] = evict_key(weight[j], age[j], protect_from);
-        unsigned prefix = 0;
-        int want = evict;                                         // rank within the current prefix
-#pragma unroll 1
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            s_bin[tid] = 0;
-            __syncthreads();
-            for (int j = tid; j < len; j += kInsertThreads) {
-                const unsigned k = keys[j];
-                if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8)))
-                    atomicAdd(&s_bin[(k >> shift) & 255u], 1);
-            }
-            __syncthreads();
-            if (tid < 32) {                                       // first digit whose count reaches want
-                int sum = 0;
+    if (evict == 1) {
+        unsigned long long least = ~0ull;
+        for_keys(p, weight, age, len, pos + n - p.recent, [&](int j, unsigned k) {
+            const unsigned long long at = ((unsigned long long)k << 32) | (unsigned)j;
+            least = at < least ? at : least;
+        });
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    sum += s_bin[tid * 8 + i];
-                int upto = sum;
-#pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const int o = __shfl_up_sync(0xffffffffu, upto, off);
-                    upto += tid >= off ? o : 0;
-                }
-                const unsigned reach = __ballot_sync(0xffffffffu, upto >= want);
-                if (tid == __ffs((int)reach) - 1) {
-                    int below = upto - sum, d = 0;
-                    while (d < 7 && below + s_bin[tid * 8 + d] < want)
-                        below += s_bin[tid * 8 + d++];
-                    s_digit = tid * 8 + d;
-                    s_below = below;
-                }
-            }
-            __syncthreads();
-            prefix |= (unsigned)s_digit << shift;
-            want -= s_below;
-            __syncthreads();
+        for (int off = 16; off > 0; off >>= 1) {
+            const unsigned long long o = __shfl_xor_sync(0xffffffffu, least, off);
+            least = o < least ? o : least;
         }
-        // evicted: key < prefix, and the first `want` slots with key == prefix.  Free places and
-        // movers in slot order; movers are listed from the end of `place`.
-        int ties = 0, holes = 0;
-        for (int j0 = 0; j0 < len; j0 += kInsertThreads) {
-            const int j = j0 + tid;
-            const unsigned k = j < len ? keys[j] : 0u;
-            int all;
-            const int tie = block_rank(j < len && k == prefix, s_warp, all) + ties;
-            const bool gone = j < len && (k < prefix || (k == prefix && tie < want));
-            ties += all;
-            const int hole = block_rank(gone && j < new_len, s_warp, all) + holes;
-            if (gone && j < new_len)
-                place[hole] = j;
-            holes += all;
-            if (j0 + kInsertThreads > new_len && len > new_len) {  // uniform
-                const int mover = block_rank(j < len && !gone && j >= new_len, s_warp, all) + n_old;
-                if (j < len && !gone && j >= new_len)
-                    place[p.cap - 1 - mover] = j;
-                n_old += all;
-            }
-        }
-        for (int j = len + tid; j < new_len; j += kInsertThreads)
-            place[holes + j - len] = j;
+        if (lane == 0)
+            s_least[warp] = least;
         __syncthreads();
+        for (int w = 0; w < (int)(blockDim.x >> 5); ++w)
+            least = s_least[w] < least ? s_least[w] : least;
+        only = (int)(unsigned)least;
     }
+    // One token into one place, or a row that only grows: no list.  (evict == 1: the free places are
+    // the evicted slot and [len, new_len); with n == 0 the last entry moves into the evicted slot
+    // unless it is that slot.)
+    const bool listed = evict > 1;
+    if (listed) {
+        for_keys(p, weight, age, len, pos + n - p.recent, [&](int j, unsigned k) { keys[j] = k; });
+        __syncthreads();
+        n_old = choose(p, keys, place, s_bin, s_word, len, new_len, evict);
+    } else if (evict == 1) {
+        // the last entry stays but lies past the new length: only when nothing is added
+        n_old = new_len < len && only < new_len ? 1 : 0;
+    }
+    const int moves = n_old + n;
+    auto place_of = [&](int mv) {
+        if (listed)
+            return place[mv];
+        return evict == 1 ? (mv == 0 ? only : len + mv - 1) : len + mv;
+    };
+    auto mover = [&](int mv) { return listed ? place[p.cap - 1 - mv] : len - 1; };
 
-    // copies: mover i -> free place i, 16 bytes a thread
-    const int moves = evict > 0 ? n_old + n : n;
-    const int per = p.D / 8;                                      // 16-byte pieces of a row
-    for (int i = tid; i < moves * per * 2; i += kInsertThreads) {
-        const int half = i >= moves * per;                        // keys first, then values
-        const int at = i - half * moves * per;
-        const int mv = at / per, piece = at - mv * per;
-        const int dst = evict > 0 ? place[mv] : len + mv;
-        if (!CSTR_INB(p.oob, dst, p.cap, CSTR_SITE_CACHE))
-            continue;
-        const long long sb = half ? p.cv_sb : p.ck_sb, ss = half ? p.cv_ss : p.ck_ss,
-                        sh = half ? p.cv_sh : p.ck_sh;
-        char *cache = (half ? p.cv : p.ck) + ((long long)b * sb + (long long)kh * sh) * 2;
-        const char *from;
-        if (mv < n_old) {
-            const int j = place[p.cap - 1 - mv];
-            if (!CSTR_INB(p.oob, j, p.cap, CSTR_SITE_CACHE))
-                continue;
-            from = cache + (long long)j * ss * 2;
-        } else {
-            const int t = mv - n_old;
-            from = half ? p.v_new + ((long long)b * p.nv_sb + (long long)t * p.nv_st + (long long)kh * p.nv_sh) * 2
-                        : p.k_new + ((long long)b * p.nk_sb + (long long)t * p.nk_st + (long long)kh * p.nk_sh) * 2;
+    // copies: 16 bytes a thread, keys and values of four places in flight
+    const int per = p.D / 8, at_once = (int)blockDim.x / per;     // pieces of a row; places side by side
+    const int piece = tid % per;
+    char *ck = p.ck + ((long long)b * p.ck_sb + (long long)kh * p.ck_sh) * 2 + piece * 16;
+    char *cv = p.cv + ((long long)b * p.cv_sb + (long long)kh * p.cv_sh) * 2 + piece * 16;
+    const char *nk = p.k_new + ((long long)b * p.nk_sb + (long long)kh * p.nk_sh) * 2 + piece * 16;
+    const char *nv = p.v_new + ((long long)b * p.nv_sb + (long long)kh * p.nv_sh) * 2 + piece * 16;
+    if (tid < at_once * per) {
+        for (int mv0 = tid / per; mv0 < moves; mv0 += 4 * at_once) {
+            uint4 k[4], v[4];
+            int dst[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int mv = mv0 + i * at_once;
+                dst[i] = -1;
+                if (mv >= moves)
+                    continue;
+                const bool old = mv < n_old;
+                const int from = old ? mover(mv) : mv - n_old;
+                dst[i] = place_of(mv);
+                if (!CSTR_INB(p.oob, dst[i], p.cap, CSTR_SITE_CACHE) ||
+                    !CSTR_INB(p.oob, from, old ? p.cap : p.T, CSTR_SITE_CACHE)) {
+                    dst[i] = -1;
+                    continue;
+                }
+                k[i] = *reinterpret_cast<const uint4 *>(old ? ck + from * p.ck_ss * 2 : nk + from * p.nk_st * 2);
+                v[i] = *reinterpret_cast<const uint4 *>(old ? cv + from * p.cv_ss * 2 : nv + from * p.nv_st * 2);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (dst[i] < 0)
+                    continue;
+                *reinterpret_cast<uint4 *>(ck + dst[i] * p.ck_ss * 2) = k[i];
+                *reinterpret_cast<uint4 *>(cv + dst[i] * p.cv_ss * 2) = v[i];
+            }
         }
-        *reinterpret_cast<uint4 *>(cache + (long long)dst * ss * 2 + piece * 16) =
-            *reinterpret_cast<const uint4 *>(from + piece * 16);
     }
-    for (int mv = tid; mv < moves; mv += kInsertThreads) {
-        const int dst = evict > 0 ? place[mv] : len + mv;
+    for (int mv = tid; mv < moves; mv += blockDim.x) {
+        const int dst = place_of(mv);
         if (!CSTR_INB(p.oob, dst, p.cap, CSTR_SITE_CACHE))
             continue;
         if (mv < n_old) {
-            const int j = place[p.cap - 1 - mv];
+            const int j = mover(mv);
             weight[dst] = weight[j];
             age[dst] = age[j];
         } else {
@@ -247,11 +352,19 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
     p.budget = a.budget;
     p.recent = a.recent;
     p.oob = CSTR_OOB_RECORD();
-    const int smem = c.list ? 0 : c.cap * 8;
+    // Single tokens evict at most one entry (unless the budget has just been lowered): small CTAs,
+    // so that all rows are in flight at once, and the list's memory in the handle's scratch.
+    const bool single = a.tokens <= 1;
+    const bool shared = !single && c.cap <= CSTR_INSERT_SMEM_SLOTS;
+    if (shared)
+        p.list = nullptr;
+    p.wide = c.cap % 4 == 0 && aligned16(c.weight) && aligned16(c.age);
+    const int threads = single && c.cap <= 2048 ? 64 : kMaxThreads;
+    const int smem = kBins * 4 + (shared ? c.cap * 8 : 0);
     if (smem > 48 * 1024)
         CSTR_CUDA_TRY(cudaFuncSetAttribute(cache_insert_kernel,
                                            cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    cache_insert_kernel<<<(unsigned)(c.batch * c.n_kv_heads), kInsertThreads, smem, stream>>>(p);
+    cache_insert_kernel<<<(unsigned)(c.batch * c.n_kv_heads), threads, smem, stream>>>(p);
     CSTR_CUDA_TRY(cudaGetLastError());
     return CSTR_OK;
 }
@@ -342,7 +455,7 @@ extern "C" int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, 
         e = cudaMalloc((void **)&c->status, 4);
     if (e == cudaSuccess)
         e = cudaMemset(c->status, 0, 4);
-    if (e == cudaSuccess && cap > CSTR_INSERT_SMEM_SLOTS && weight && age)
+    if (e == cudaSuccess && weight && age)
         e = cudaMalloc((void **)&c->list, (size_t)batch * n_kv_heads * cap * 8);
     if (e != cudaSuccess) {
         rc = cstr_fail(e == cudaErrorMemoryAllocation ? CSTR_ERR_NOMEM : CSTR_ERR_CUDA,
@@ -420,6 +533,9 @@ extern "C" int cstr_cache_attention(cstr_cache_t *c, const void *q, const int64_
         rc = strides_ok("cstr_cache_attention", out_strides, 3);
     if (rc)
         return rc;
+    for (int i = 0; i < 3; ++i)
+        if (q_strides[i] > (1ll << 33) || q_strides[i] < -(1ll << 33))
+            return cstr_fail(CSTR_ERR_SHAPE, "cstr_cache_attention: q stride %lld is too large", (long long)q_strides[i]);
     if (!aligned16(q) || !aligned16(out))
         return cstr_fail(CSTR_ERR_SHAPE, "cstr_cache_attention: q and out must start on 16 bytes");
     rc = cstr_check_device(c->device, "cache");

@@ -24,8 +24,26 @@ struct cstr_cache {
     float *part_o;       // DEVICE parts' outputs, [block][head_dim (padded) / 4][128][4]
     void *part_ml;       // DEVICE float2 [block][128]: parts' maximum and sum
     int *status;         // DEVICE [1]: CTAs whose bounded waits gave up (never expected)
-    int32_t *list;       // DEVICE [batch][n_kv_heads][2][cap], only for caps beyond the insert
-                         // kernel's shared memory
+    int32_t *list;       // DEVICE [batch][n_kv_heads][2][cap]: the insert kernel's keys and places, where
+                         // they are not in shared memory
+};
+
+// n / d for 0 <= n < 2^31 by a multiplication: mul = ceil(2^(31 + log) / d), log = ceil(log2 d),
+// n mul / 2^(31 + log) = (high word of 2 n x mul) / 2^log
+struct cstr_divisor {
+    unsigned mul;
+    int log;
+    __host__ void set(unsigned d)
+    {
+        log = 0;
+        while ((1ull << log) < d)
+            ++log;
+        mul = (unsigned)(((1ull << (31 + log)) + d - 1) / d);
+    }
+    __device__ __forceinline__ int operator()(int n) const
+    {
+        return (int)(__umulhi(2u * (unsigned)n, mul) >> log);
+    }
 };
 
 // Attention of the rows' own keys (and of prefix keys not taken by another kernel).
@@ -64,5 +82,6 @@ struct cstr_insert_args {
 };
 int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStream_t stream);
 
-// Largest cap whose eviction keys and move list fit the insert kernel's shared memory.
+// Largest cap whose keys and places fit the insert kernel's shared memory (8 bytes a slot beside
+// 8 KB of bins).
 #define CSTR_INSERT_SMEM_SLOTS 24576

@@ -11,8 +11,11 @@
 // so the kernel is bound by their bytes.  Hence every warp runs by itself over
 // its own chunks of 16 keys, with its own ring of asynchronous copies: no
 // barrier in the loop, and copies stay in flight while a chunk is worked on.
-// The products run on m16n8k16 matrix instructions: with at most 32 query rows
-// per pass they are far from being the limit.
+// The products run on m16n8k16 matrix instructions in transposed form, S' = K Q'
+// and O' = V' P': the keys and the head's elements fill the 16 rows of an
+// instruction, and its 8 columns are query rows, so that the usual 4 or 8 query
+// rows of a key / value head waste nothing (the other way round they would fill
+// a quarter or a half of 16).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -26,8 +29,9 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kStages = 3;
+constexpr int kSlots = 3;        // units (keys or values of a chunk) in a warp's ring
 constexpr int kChunk = 16;       // keys per step of a warp
+constexpr float kLazy = 8.f;
 constexpr float kLn2 = 0.693147180559945309f;
 
 struct RowParams {
@@ -50,34 +54,35 @@ struct RowParams {
     // parts of the prefix kernel (null: none); see cstr_prefix_plan
     const float4 *part_o;
     const float2 *part_ml;
-    int pairs, tiles, grid;
+    int pairs, tiles, grid, max_parts;
+    int narrow;          // units x grid fits in 32 bits
+    cstr_divisor by_g;
     unsigned long long *oob;
 };
 
-// The prefix kernel's parts for one query row: blocks first, first + step, ... (n of them), at `row`.
+// The prefix kernel's parts for one query row: blocks first, first + 2, ... (n of them), at `row`.
 struct PartList {
-    long long first;
-    int n, step, row;
+    int first, n, row;
 };
 
 __device__ __forceinline__ PartList parts_of(const RowParams &p, int kh, int m)
 {
     const int pair = m >> 8, local = m & 255;
-    const bool two_tiles = p.B * p.G * p.T - (pair << 8) > 128;
-    const long long item = (long long)kh * p.pairs + pair, units = (long long)p.Hk * p.pairs * p.tiles;
-    const long long c0 = ((item * p.tiles + 1) * p.grid - 1) / units;
-    const long long c1 = ((item + 1) * p.tiles * p.grid - 1) / units;
+    const int item = kh * p.pairs + pair;
+    int c0, c1;                          // first and last CTA with a segment of this row group
+    if (p.narrow) {
+        const unsigned units = (unsigned)(p.Hk * p.pairs * p.tiles), first = (unsigned)(item * p.tiles);
+        c0 = (int)(((first + 1) * p.grid - 1) / units);
+        c1 = (int)(((first + p.tiles) * p.grid - 1) / units);
+    } else {
+        const long long units = (long long)p.Hk * p.pairs * p.tiles, first = (long long)item * p.tiles;
+        c0 = (int)(((first + 1) * p.grid - 1) / units);
+        c1 = (int)(((first + p.tiles) * p.grid - 1) / units);
+    }
     PartList l;
     l.row = local & 127;
-    if (two_tiles) {
-        l.first = (c0 + item) * 2 + (local >> 7);
-        l.step = 2;
-        l.n = (int)(c1 - c0 + 1);
-    } else {
-        l.first = (c0 + item) * 2;
-        l.step = 1;
-        l.n = 2 * (int)(c1 - c0 + 1);
-    }
+    l.first = (c0 + item) * 2 + (local >> 7);
+    l.n = c1 - c0 + 1;
     return l;
 }
 
@@ -88,10 +93,7 @@ template <> struct Half2<__nv_bfloat16> {
         __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<unsigned *>(&v);
     }
-    static __device__ __forceinline__ float2 unpack(unsigned u)
-    {
-        return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162 *>(&u));
-    }
+    static __device__ __forceinline__ float value(unsigned short h) { return __uint_as_float((unsigned)h << 16); }
     static __device__ __forceinline__ bool finite(unsigned short h) { return (h & 0x7f80u) != 0x7f80u; }
 };
 template <> struct Half2<__half> {
@@ -100,10 +102,7 @@ template <> struct Half2<__half> {
         __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<unsigned *>(&v);
     }
-    static __device__ __forceinline__ float2 unpack(unsigned u)
-    {
-        return __half22float2(*reinterpret_cast<__half2 *>(&u));
-    }
+    static __device__ __forceinline__ float value(unsigned short h) { return __half2float(__ushort_as_half(h)); }
     static __device__ __forceinline__ bool finite(unsigned short h) { return (h & 0x7c00u) != 0x7c00u; }
 };
 
@@ -147,6 +146,14 @@ __device__ __forceinline__ void ldsm4_trans(unsigned (&r)[4], unsigned addr)
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
+// 8x8 matrix of 16-bit elements, transposed across the warp
+__device__ __forceinline__ unsigned transpose8(unsigned v)
+{
+    unsigned r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
 template <typename T>
 __device__ __forceinline__ void mma16816(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1);
 template <>
@@ -168,6 +175,13 @@ __device__ __forceinline__ void mma16816<__half>(float (&c)[4], const unsigned (
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// *p += v without waiting for the old value.  Every weight gets exactly one addition per pass,
+// always from the CTA that owns the slot, so the result does not depend on any order.
+__device__ __forceinline__ void add_once(float *p, float v)
+{
+    asm volatile("red.global.add.f32 [%0], %1;" ::"l"(p), "f"(v) : "memory");
+}
+
 // Byte offset of 16-byte chunk `ch` of row `r` in a tile of DP-element rows: the
 // chunk index is XORed with the row so that the eight rows of an 8x8 matrix hit
 // all 32 banks.
@@ -177,9 +191,9 @@ template <int DP> __device__ __forceinline__ unsigned tile_off(int r, int ch)
 }
 
 template <int DP> struct RowShape {
-    static constexpr int kTile = kChunk * DP * 2;                // bytes of one K (or V) chunk
-    static constexpr int kStage = 2 * kTile + kChunk * 4;        // K, V, ages
-    static constexpr int kRing = kWarps * kStages * kStage;
+    static constexpr int kUnit = kChunk * DP * 2 + kChunk * 4;   // keys (or values) of a chunk, ages
+    static constexpr int kRing = kWarps * kSlots * kUnit;
+    static constexpr int kPitch = DP + 4;                        // floats per row of the partial outputs
 };
 
 // Key list of one CTA: indices [x0, x1) of the row's list (prefix keys, then slots).
@@ -190,88 +204,119 @@ struct KeySource {
     const int32_t *ageb;
     int x0, x1;
 
-    __device__ __forceinline__ void fetch(unsigned stage, int base, int lane, bool want_v) const
+    // the keys (and ages) or the values of the chunk at `base` into a ring slot
+    __device__ __forceinline__ void fetch(unsigned to, bool values, int base, int lane) const
     {
-        constexpr int CH = DP / 8;                 // 16-byte chunks per key
+        constexpr int CH = DP / 8;                 // 16-byte pieces per key
         constexpr int KPI = 32 / CH;               // keys per warp instruction
-        const int ch = lane % CH;
-        const bool ch_ok = ch * 8 < p.D;
+        const int ch = lane % CH, key0 = lane / CH;
+        const char *slots = values ? cvb : ckb;
+        const long long ss = 2 * (values ? p.cv_ss : p.ck_ss);
+        if (base >= p.P && base + kChunk <= x1 && DP == p.D) {          // whole chunk of slots
+            const char *from = slots + (base - p.P + key0) * ss + ch * 16;
 #pragma unroll
-        for (int i = 0; i < kChunk / KPI; ++i) {
-            const int key = i * KPI + lane / CH;
-            const int x = base + key;
-            const bool ok = x < x1 && ch_ok;
-            const char *ks, *vs;
-            if (x < p.P) {
-                ks = pkb + (long long)x * p.pk_st * 2;
-                vs = pvb + (long long)x * p.pv_st * 2;
-            } else {
-                const int j = x - p.P;
-                ks = ckb + (long long)j * p.ck_ss * 2;
-                vs = cvb + (long long)j * p.cv_ss * 2;
+            for (int i = 0; i < kChunk / KPI; ++i) {
+                copy16(to + tile_off<DP>(i * KPI + key0, ch), from, true);
+                from += KPI * ss;
             }
-            const unsigned off = tile_off<DP>(key, ch);
-            copy16(stage + off, ok ? ks + ch * 16 : ckb, ok);
-            if (want_v)
-                copy16(stage + RowShape<DP>::kTile + off, ok ? vs + ch * 16 : cvb, ok);
+        } else {
+            const char *prompt = values ? pvb : pkb;
+            const long long st = 2 * (values ? p.pv_st : p.pk_st);
+            const bool ch_ok = ch * 8 < p.D;
+#pragma unroll 2
+            for (int i = 0; i < kChunk / KPI; ++i) {
+                const int key = i * KPI + key0;
+                const int x = base + key;
+                const bool ok = x < x1 && ch_ok;
+                const char *from = x < p.P ? prompt + x * st : slots + (x - p.P) * ss;
+                copy16(to + tile_off<DP>(key, ch), ok ? from + ch * 16 : slots, ok);
+            }
         }
-        if (ageb && lane < kChunk) {
+        if (!values && ageb && lane < kChunk) {
             const int j = base + lane - p.P;
             const bool ok = j >= 0 && base + lane < x1;
-            copy4(stage + 2 * RowShape<DP>::kTile + lane * 4, ok ? ageb + j : ageb, ok);
+            copy4(to + kChunk * DP * 2 + lane * 4, ok ? ageb + j : ageb, ok);
         }
     }
 };
 
-// x = scaled scores of 16 query rows against the chunk's 16 keys, in the
-// accumulator layout: x[n][0..1] = row lane / 4, keys 8 n + 2 (lane % 4) + 0..1;
-// x[n][2..3] = row lane / 4 + 8.  Keys a row does not see get -infinity.
-template <typename T, int DP>
-__device__ __forceinline__ void chunk_scores(float (&x)[2][4], const RowParams &p, unsigned sq,
-                                             unsigned stage, int rb, int lane, int base, int x1,
-                                             const int (&limit)[2], bool causal)
+// Query rows as the second operand of S' = K Q': fragments of k steps k and k + 1.
+template <int DP> __device__ __forceinline__ void query_pair(unsigned (&f)[4], unsigned sq, int n, int k, int lane)
+{
+    ldsm4(f, sq + tile_off<DP>(8 * n + (lane & 7), 2 * k + (lane >> 3)));
+}
+
+// x = scaled scores of the chunk's 16 keys against 8 NT query rows, in the accumulator layout:
+// x[n][0..1] = key lane / 4, rows 8 n + 2 (lane % 4) + 0..1; x[n][2..3] = key lane / 4 + 8.
+// `masked`: -infinity for keys past the list's end and, with `causal`, for slots younger than a
+// row's limit.
+template <typename T, int DP, int NT>
+__device__ __forceinline__ void chunk_scores(float (&x)[NT][4], const RowParams &p, const unsigned (&qf)[NT <= 2 ? NT : 1][DP / 16][2],
+                                             unsigned sq, unsigned keys, int lane, int base, int x1, const int (&limit)[NT][2],
+                                             bool masked, bool causal)
 {
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             x[n][e] = 0.f;
+    float y[NT][4];                                // odd k steps, so that the chains are half as long
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) {
-        unsigned a[4], b[4];
-        ldsm4(a, sq + tile_off<DP>(rb * 16 + (lane & 15), 2 * k + (lane >> 4)));
-        // matrices: keys 0-7 / 8-15 x the two 8-element halves of this k step
-        ldsm4(b, stage + tile_off<DP>((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
-        mma16816<T>(x[0], a, b[0], b[1]);
-        mma16816<T>(x[1], a, b[2], b[3]);
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            y[n][e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < DP / 16; k += 2) {
+        unsigned a[4], a2[4];
+        ldsm4(a, keys + tile_off<DP>(lane & 15, 2 * k + (lane >> 4)));
+        ldsm4(a2, keys + tile_off<DP>(lane & 15, 2 * k + 2 + (lane >> 4)));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (NT <= 2) {                         // (constant indices: qf has NT blocks then)
+                mma16816<T>(x[n], a, qf[NT <= 2 ? n : 0][k][0], qf[NT <= 2 ? n : 0][k][1]);
+                mma16816<T>(y[n], a2, qf[NT <= 2 ? n : 0][k + 1][0], qf[NT <= 2 ? n : 0][k + 1][1]);
+            } else {                               // too many to keep in registers
+                unsigned f[4];
+                query_pair<DP>(f, sq, n, k, lane);
+                mma16816<T>(x[n], a, f[0], f[1]);
+                mma16816<T>(y[n], a2, f[2], f[3]);
+            }
+        }
     }
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int key = 8 * n + 2 * (lane & 3) + (e & 1);
-            bool seen = base + key < x1;
-            if (limit[e >> 1] == INT_MIN)          // a query row that does not exist
-                seen = false;
-            else if (causal && base + key >= p.P) {
-                int age;
-                asm volatile("ld.shared.s32 %0, [%1];" : "=r"(age)
-                             : "r"(stage + 2 * RowShape<DP>::kTile + key * 4) : "memory");
-                seen = seen && age <= limit[e >> 1];
-            }
-            x[n][e] = seen ? x[n][e] * p.scale_log2 : -CUDART_INF_F;
-        }
+        for (int e = 0; e < 4; ++e)
+            x[n][e] = (x[n][e] + y[n][e]) * p.scale_log2;
+    if (!masked)
+        return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int key = 8 * h + (lane >> 2);
+        int age = INT_MIN;
+        if (causal && base + key >= p.P)
+            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(age) : "r"(keys + kChunk * DP * 2 + key * 4) : "memory");
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (base + key >= x1 || (causal && age > limit[n][e]))
+                    x[n][2 * h + e] = -CUDART_INF_F;
+    }
 }
 
 // A key that only some query rows see must not reach the others through 0 x NaN:
 // where such a key's value row holds something that is not finite, its products
 // are added one by one for the rows that see it, and the row is zeroed before
 // the matrix product.  At most the row's newest tokens are such keys.
-template <typename T, int DP, int RBT>
-__device__ __noinline__ void add_nonfinite_values(float (&o)[RBT][DP / 8][4], const float (&x)[RBT][2][4],
-                                                  char *vtile, int lane)
+// (Inlined: the accumulators must not have an address, or they live in memory.)
+template <typename T, int DP, int NT>
+__device__ __forceinline__ void add_nonfinite_values(float (&o)[NT][DP / 16][4], const float (&x)[NT][4], char *vtile,
+                                                     int lane)
 {
     unsigned bad = 0;
+#pragma unroll 1
     for (int i = lane; i < kChunk * DP / 8; i += 32) {
         const int key = i / (DP / 8), ch = i % (DP / 8);
         const uint4 v = *reinterpret_cast<const uint4 *>(vtile + tile_off<DP>(key, ch));
@@ -281,30 +326,27 @@ __device__ __noinline__ void add_nonfinite_values(float (&o)[RBT][DP / 8][4], co
                 bad |= 1u << key;
     }
     bad = __reduce_or_sync(0xffffffffu, bad);
+#pragma unroll 1
     for (; bad; bad &= bad - 1) {
         const int key = __ffs((int)bad) - 1;
-        const int src = (lane & ~3) | ((key & 7) >> 1);
+        const int src = ((key & 7) << 2) | (lane & 3);
 #pragma unroll
-        for (int rb = 0; rb < RBT; ++rb) {
-            const float p0 = __shfl_sync(0xffffffffu, x[rb][0][0], src), p1 = __shfl_sync(0xffffffffu, x[rb][0][1], src);
-            const float p2 = __shfl_sync(0xffffffffu, x[rb][1][0], src), p3 = __shfl_sync(0xffffffffu, x[rb][1][1], src);
-            const float p4 = __shfl_sync(0xffffffffu, x[rb][0][2], src), p5 = __shfl_sync(0xffffffffu, x[rb][0][3], src);
-            const float p6 = __shfl_sync(0xffffffffu, x[rb][1][2], src), p7 = __shfl_sync(0xffffffffu, x[rb][1][3], src);
-            const float lo = key < 8 ? (key & 1 ? p1 : p0) : (key & 1 ? p3 : p2);
-            const float hi = key < 8 ? (key & 1 ? p5 : p4) : (key & 1 ? p7 : p6);
+        for (int n = 0; n < NT; ++n) {
+            const float a0 = __shfl_sync(0xffffffffu, x[n][0], src), a1 = __shfl_sync(0xffffffffu, x[n][1], src);
+            const float b0 = __shfl_sync(0xffffffffu, x[n][2], src), b1 = __shfl_sync(0xffffffffu, x[n][3], src);
+            const float p0 = key < 8 ? a0 : b0, p1 = key < 8 ? a1 : b1;
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n) {
-                const unsigned u = *reinterpret_cast<const unsigned *>(vtile + tile_off<DP>(key, n) + (lane & 3) * 4);
-                const float2 v = Half2<T>::unpack(u);
-                if (lo != 0.f) {
-                    o[rb][n][0] += lo * v.x;
-                    o[rb][n][1] += lo * v.y;
+            for (int j = 0; j < DP / 16; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int d = 16 * j + 8 * h + (lane >> 2);
+                    const float v = Half2<T>::value(*reinterpret_cast<const unsigned short *>(
+                        vtile + tile_off<DP>(key, d >> 3) + (d & 7) * 2));
+                    if (p0 != 0.f)
+                        o[n][j][2 * h] += p0 * v;
+                    if (p1 != 0.f)
+                        o[n][j][2 * h + 1] += p1 * v;
                 }
-                if (hi != 0.f) {
-                    o[rb][n][2] += hi * v.x;
-                    o[rb][n][3] += hi * v.y;
-                }
-            }
         }
         __syncwarp();
         for (int ch = lane; ch < DP / 8; ch += 32)
@@ -313,19 +355,23 @@ __device__ __noinline__ void add_nonfinite_values(float (&o)[RBT][DP / 8][4], co
     }
 }
 
-template <typename T, int DP, int RBT>
-__global__ void __launch_bounds__(kWarps * 32)
+// NT: blocks of 8 query rows per pass
+template <typename T, int DP, int NT>
+__global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 4 : 2)
 row_attention_kernel(const __grid_constant__ RowParams p)
 {
-    constexpr int ROWS = 16 * RBT;
+    constexpr int ROWS = 8 * NT;
     using Shape = RowShape<DP>;
     extern __shared__ __align__(128) char smem[];
     char *s_q = smem;                                              // [ROWS][DP] of T
     float *s_stat = reinterpret_cast<float *>(s_q + ROWS * DP * 2); // [2 kWarps + 3][ROWS]
     char *s_ring = reinterpret_cast<char *>(s_stat + (2 * kWarps + 3) * ROWS);
-    float *s_o = reinterpret_cast<float *>(s_ring);                // [kWarps][ROWS][DP], after the loop
-    constexpr int kArea = Shape::kRing > kWarps * ROWS * DP * 4 ? Shape::kRing : kWarps * ROWS * DP * 4;
-    float *s_score = reinterpret_cast<float *>(s_ring + kArea);    // [ROWS][score_cap]
+    float *s_o = reinterpret_cast<float *>(s_ring);                // [kWarps][ROWS][kPitch], after the loop
+    constexpr int kOut = kWarps * ROWS * Shape::kPitch * 4;
+    constexpr int kArea = Shape::kRing > kOut ? Shape::kRing : kOut;
+    float *s_fac = reinterpret_cast<float *>(s_ring + kArea);      // [rows of a pass][max_parts]
+    float *s_score = s_fac + min(ROWS, p.G * p.T) * p.max_parts;   // [rows of a pass][score_cap]
+    __shared__ PartList s_parts[ROWS];
     float *s_m = s_stat, *s_l = s_stat + kWarps * ROWS;            // per warp
     float *s_cm = s_stat + 2 * kWarps * ROWS, *s_cl = s_cm + ROWS, *s_lse = s_cl + ROWS;
 
@@ -353,169 +399,196 @@ row_attention_kernel(const __grid_constant__ RowParams p)
         min(part * per * kChunk, total), min((part + 1) * per * kChunk, total)};
     const int n_chunks = (src.x1 - src.x0 + kChunk - 1) / kChunk;
     const int s0 = max(src.x0, p.P), s1 = max(src.x1, p.P);        // own slots: [s0 - P, s1 - P)
-    const bool keep = p.accumulate && s1 - s0 <= p.score_cap;
-    const unsigned ring = smem_addr(s_ring) + warp * kStages * Shape::kStage;
-    const unsigned sq = smem_addr(s_q);
+    // scores are kept from the chunk on in which the slots begin
+    const int kept0 = (s0 - src.x0) / kChunk * kChunk;
+    const bool keep = p.accumulate && n_chunks * kChunk - kept0 <= p.score_cap;
+    const int mine = n_chunks > warp ? (n_chunks - warp + kWarps - 1) / kWarps : 0;   // chunks of this warp
+    char *ring_ptr = s_ring + warp * kSlots * Shape::kUnit;
+    const unsigned ring = smem_addr(ring_ptr);
 
     for (int r0 = 0; r0 < R; r0 += ROWS) {
         const int nr = min(ROWS, R - r0);
-        for (int i = tid; i < ROWS * (DP / 8); i += kWarps * 32) {
-            const int r = i / (DP / 8), ch = i % (DP / 8);
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        // the queries and the first chunks are on their way together; unit 2 i is the keys of the
+        // warp's chunk i, unit 2 i + 1 its values
+        constexpr int kQ = (ROWS * (DP / 8) + kWarps * 32 - 1) / (kWarps * 32);
+        uint4 qv[kQ];
+#pragma unroll
+        for (int k = 0; k < kQ; ++k) {
+            const int i = tid + k * kWarps * 32, r = i / (DP / 8), ch = i % (DP / 8);
+            qv[k] = make_uint4(0u, 0u, 0u, 0u);
             if (r < nr && ch * 8 < p.D) {
-                const int t = (r0 + r) / p.G, g = (r0 + r) - t * p.G;
+                const int t = p.by_g(r0 + r), g = (r0 + r) - t * p.G;
                 const char *s = (const char *)p.q + ((long long)b * p.q_sb + (long long)t * p.q_st +
                                                      (long long)(kh * p.G + g) * p.q_sh) * 2;
-                v = *reinterpret_cast<const uint4 *>(s + ch * 16);
+                qv[k] = *reinterpret_cast<const uint4 *>(s + ch * 16);
             }
-            *reinterpret_cast<uint4 *>(s_q + tile_off<DP>(r, ch)) = v;
+        }
+        auto fetch = [&](int unit, int slot) {
+            if (unit < 2 * mine)
+                src.fetch(ring + slot * Shape::kUnit, unit & 1, src.x0 + ((unit >> 1) * kWarps + warp) * kChunk, lane);
+            copy_commit();
+        };
+#pragma unroll 1
+        for (int u = 0; u < kSlots; ++u)
+            fetch(u, u);
+#pragma unroll
+        for (int k = 0; k < kQ; ++k) {
+            const int i = tid + k * kWarps * 32;
+            if (i < ROWS * (DP / 8))
+                *reinterpret_cast<uint4 *>(s_q + tile_off<DP>(i / (DP / 8), i % (DP / 8))) = qv[k];
         }
         __syncthreads();
+        const unsigned sq = smem_addr(s_q);
+        unsigned qf[NT <= 2 ? NT : 1][DP / 16][2];
+#pragma unroll
+        for (int n = 0; n < (NT <= 2 ? NT : 0); ++n)
+#pragma unroll
+            for (int k = 0; k < DP / 16; k += 2) {
+                unsigned f[4];
+                query_pair<DP>(f, sq, n, k, lane);
+                qf[n][k][0] = f[0], qf[n][k][1] = f[1], qf[n][k + 1][0] = f[2], qf[n][k + 1][1] = f[3];
+            }
 
         // last position that each of this lane's query rows sees
-        int limit[RBT][2];
+        int limit[NT][2];
 #pragma unroll
-        for (int rb = 0; rb < RBT; ++rb)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = rb * 16 + h * 8 + (lane >> 2);
-                const int t = (r0 + r) / p.G;
-                limit[rb][h] = r < nr && t < nq ? (causal ? pos + t : 0) : INT_MIN;
-            }
+            for (int e = 0; e < 2; ++e)
+                limit[n][e] = pos + p.by_g(r0 + 8 * n + 2 * (lane & 3) + e);
 
-        float o[RBT][DP / 8][4], m[RBT][2], l[RBT][2];
+        float o[NT][DP / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
-        for (int rb = 0; rb < RBT; ++rb) {
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
+            for (int j = 0; j < DP / 16; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    o[rb][n][e] = 0.f;
-            m[rb][0] = m[rb][1] = -CUDART_INF_F;
-            l[rb][0] = l[rb][1] = 0.f;
+                    o[n][j][e] = 0.f;
+            m[n][0] = m[n][1] = -CUDART_INF_F;
+            l[n][0] = l[n][1] = 0.f;
         }
 
-#pragma unroll
-        for (int s = 0; s < kStages - 1; ++s) {
-            const int c = warp + s * kWarps;
-            if (c < n_chunks)
-                src.fetch(ring + s * Shape::kStage, src.x0 + c * kChunk, lane, true);
-            copy_commit();
-        }
         int slot = 0;
-        for (int c = warp; c < n_chunks; c += kWarps) {
-            {
-                const int ahead = c + (kStages - 1) * kWarps;
-                const int into = slot == 0 ? kStages - 1 : slot - 1;
-                if (ahead < n_chunks)
-                    src.fetch(ring + into * Shape::kStage, src.x0 + ahead * kChunk, lane, true);
-                copy_commit();
-            }
-            copy_wait<kStages - 1>();
+#pragma unroll 1
+        for (int i = 0; i < mine; ++i) {
+            copy_wait<kSlots - 1>();
             __syncwarp();
-            const unsigned stage = ring + slot * Shape::kStage;
-            const int base = src.x0 + c * kChunk;
-            float x[RBT][2][4];
-#pragma unroll
-            for (int rb = 0; rb < RBT; ++rb)
-                chunk_scores<T, DP>(x[rb], p, sq, stage, rb, lane, base, src.x1, limit[rb], causal);
-            if (keep) {
-#pragma unroll
-                for (int rb = 0; rb < RBT; ++rb)
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int r = rb * 16 + (e >> 1) * 8 + (lane >> 2);
-                            const int at = base + 8 * n + 2 * (lane & 3) + (e & 1);
-                            if (r < nr && at >= s0 && at < s1)
-                                s_score[r * p.score_cap + at - s0] = x[rb][n][e];
-                        }
+            const unsigned keys = ring + slot * Shape::kUnit;
+            const int base = src.x0 + (i * kWarps + warp) * kChunk;
+            float x[NT][4];
+            chunk_scores<T, DP, NT>(x, p, qf, sq, keys, lane, base, src.x1, limit, causal || base + kChunk > src.x1, causal);
+            bool partial = false;                    // a key seen by some rows of the call only
+            if (causal && p.T > 1) {
+                bool some = false;
+                if (lane < kChunk && base + lane >= p.P && base + lane < src.x1) {
+                    int age;
+                    asm volatile("ld.shared.s32 %0, [%1];" : "=r"(age) : "r"(keys + kChunk * DP * 2 + lane * 4) : "memory");
+                    some = age > pos;
+                }
+                partial = __any_sync(0xffffffffu, some);
             }
-            bool some = false;                       // a key seen by some rows of the call only
-            if (causal && p.T > 1 && lane < kChunk && base + lane >= p.P && base + lane < src.x1) {
-                int age;
-                asm volatile("ld.shared.s32 %0, [%1];" : "=r"(age)
-                             : "r"(stage + 2 * Shape::kTile + lane * 4) : "memory");
-                some = age > pos;
-            }
-            const bool partial = __any_sync(0xffffffffu, some);
+            __syncwarp();                            // the keys (and ages) have been read
+            fetch(2 * i + kSlots, slot);
+            slot = slot + 1 == kSlots ? 0 : slot + 1;
+            if (keep && base - src.x0 >= kept0) {
+                float *to = s_score + base - src.x0 - kept0 + (lane >> 2);
 #pragma unroll
-            for (int rb = 0; rb < RBT; ++rb) {
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float top = fmaxf(fmaxf(x[rb][0][2 * h], x[rb][0][2 * h + 1]),
-                                      fmaxf(x[rb][1][2 * h], x[rb][1][2 * h + 1]));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const float mn = fmaxf(m[rb][h], top);
-                    const float ref = mn == -CUDART_INF_F ? 0.f : mn;
-                    const float f = exp2_fast(m[rb][h] - ref);
-                    m[rb][h] = mn;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float &v = x[rb][n][2 * h + e];
-                            v = exp2_fast(v - ref);
-                            sum += v;
-                        }
-                    l[rb][h] = l[rb][h] * f + sum;
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n) {
-                        o[rb][n][2 * h] *= f;
-                        o[rb][n][2 * h + 1] *= f;
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 8 * n + 2 * (lane & 3) + (e & 1);
+                        if (r < nr)
+                            to[r * p.score_cap + 8 * (e >> 1)] = x[n][e];
                     }
-                }
             }
+            // the reference moves only when some score exceeds it by 2^8 (the first keys, rarely later):
+            // until then the probabilities stay below 2^8, in range of both 16-bit types
+            bool grow = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    grow = grow || fmaxf(x[n][e], x[n][2 + e]) > m[n][e] + kLazy;
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(x[n][e], x[n][2 + e]);
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                        const float mn = fmaxf(m[n][e], top);
+                        const float f = mn == -CUDART_INF_F ? 1.f : exp2_fast(m[n][e] - mn);
+                        m[n][e] = mn;
+                        l[n][e] *= f;
+#pragma unroll
+                        for (int j = 0; j < DP / 16; ++j) {
+                            o[n][j][e] *= f;
+                            o[n][j][2 + e] *= f;
+                        }
+                    }
+            }
+            // the probabilities enter the second product in the values' type: rounded to nearest, like
+            // the values themselves; the sum l keeps the unrounded ones
+            unsigned pf[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float ref = m[n][e & 1] == -CUDART_INF_F ? 0.f : m[n][e & 1];
+                    x[n][e] = exp2_fast(x[n][e] - ref);
+                    l[n][e & 1] += x[n][e];
+                }
+                pf[n][0] = transpose8(Half2<T>::pack(x[n][0], x[n][1]));
+                pf[n][1] = transpose8(Half2<T>::pack(x[n][2], x[n][3]));
+            }
+            copy_wait<kSlots - 1>();
+            __syncwarp();
+            const unsigned values = ring + slot * Shape::kUnit;
             if (partial)
-                add_nonfinite_values<T, DP, RBT>(o, x, s_ring + (warp * kStages + slot) * Shape::kStage + Shape::kTile, lane);
-            // the probabilities enter the second product in the values' type: rounded to nearest,
-            // like the values themselves; the sum l keeps the unrounded ones
-            unsigned a[RBT][4];
+                add_nonfinite_values<T, DP, NT>(o, x, ring_ptr + slot * Shape::kUnit, lane);
 #pragma unroll
-            for (int rb = 0; rb < RBT; ++rb) {
-                a[rb][0] = Half2<T>::pack(x[rb][0][0], x[rb][0][1]);
-                a[rb][1] = Half2<T>::pack(x[rb][0][2], x[rb][0][3]);
-                a[rb][2] = Half2<T>::pack(x[rb][1][0], x[rb][1][1]);
-                a[rb][3] = Half2<T>::pack(x[rb][1][2], x[rb][1][3]);
-            }
+            for (int j = 0; j < DP / 16; ++j) {
+                unsigned a[4];
+                ldsm4_trans(a, values + tile_off<DP>((lane & 7) + ((lane >> 4) << 3), 2 * j + ((lane >> 3) & 1)));
 #pragma unroll
-            for (int n2 = 0; n2 < DP / 16; ++n2) {
-                unsigned v[4];
-                ldsm4_trans(v, stage + Shape::kTile + tile_off<DP>(lane & 15, 2 * n2 + (lane >> 4)));
-#pragma unroll
-                for (int rb = 0; rb < RBT; ++rb) {
-                    mma16816<T>(o[rb][2 * n2], a[rb], v[0], v[1]);
-                    mma16816<T>(o[rb][2 * n2 + 1], a[rb], v[2], v[3]);
-                }
+                for (int n = 0; n < NT; ++n)
+                    mma16816<T>(o[n][j], a, pf[n][0], pf[n][1]);
             }
             __syncwarp();
-            slot = slot + 1 == kStages ? 0 : slot + 1;
+            fetch(2 * i + 1 + kSlots, slot);
+            slot = slot + 1 == kSlots ? 0 : slot + 1;
         }
         copy_wait<0>();
 
         // the warps' partial results meet in shared memory (the ring is free by now)
         __syncthreads();
 #pragma unroll
-        for (int rb = 0; rb < RBT; ++rb) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = rb * 16 + h * 8 + (lane >> 2);
-                float sum = l[rb][h];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                if ((lane & 3) == 0) {
-                    s_m[warp * ROWS + r] = m[rb][h];
-                    s_l[warp * ROWS + r] = sum;
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * n + 2 * (lane & 3) + e;
+                float sum = l[n][e];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                if (lane < 4) {
+                    // a token past n_query counts as one that sees nothing
+                    const bool real = r < nr && p.by_g(r0 + r) < nq;
+                    s_m[warp * ROWS + r] = real ? m[n][e] : -CUDART_INF_F;
+                    s_l[warp * ROWS + r] = real ? sum : 0.f;
                 }
+                if (r < nr) {
+                    float *to = s_o + (warp * ROWS + r) * Shape::kPitch + (lane >> 2);
 #pragma unroll
-                for (int n = 0; n < DP / 8; ++n)
-                    *reinterpret_cast<float2 *>(s_o + (warp * ROWS + r) * DP + n * 8 + 2 * (lane & 3)) =
-                        make_float2(o[rb][n][2 * h], o[rb][n][2 * h + 1]);
+                    for (int j = 0; j < DP / 16; ++j) {
+                        to[16 * j] = o[n][j][e];
+                        to[16 * j + 8] = o[n][j][2 + e];
+                    }
+                }
             }
-        }
         __syncthreads();
         for (int r = tid; r < nr; r += kWarps * 32) {
             float top = s_m[r];
@@ -536,19 +609,23 @@ row_attention_kernel(const __grid_constant__ RowParams p)
             s_cl[r] = sum;
         }
         __syncthreads();
-        for (int i = tid; i < nr * (DP / 2); i += kWarps * 32) {
-            const int r = i / (DP / 2), d = 2 * (i % (DP / 2));
-            float2 v = make_float2(0.f, 0.f);
+        auto axpy = [](float4 &v, float f, const float4 &u) {
+            v.x += f * u.x;
+            v.y += f * u.y;
+            v.z += f * u.z;
+            v.w += f * u.w;
+        };
+        for (int i = tid; i < nr * (DP / 4); i += kWarps * 32) {
+            const int r = i / (DP / 4), d = 4 * (i % (DP / 4));
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float f = s_m[w * ROWS + r];
-                const float2 u = *reinterpret_cast<const float2 *>(s_o + (w * ROWS + r) * DP + d);
-                if (f >= 0.f || f != f) {
-                    v.x += f * u.x;
-                    v.y += f * u.y;
-                }
+                const float4 u = *reinterpret_cast<const float4 *>(s_o + (w * ROWS + r) * Shape::kPitch + d);
+                if (!(f < 0.f))
+                    axpy(v, f, u);
             }
-            *reinterpret_cast<float2 *>(s_o + r * DP + d) = v;
+            *reinterpret_cast<float4 *>(s_o + r * Shape::kPitch + d) = v;
         }
         if (p.split > 1)
             cluster.sync();
@@ -559,62 +636,89 @@ row_attention_kernel(const __grid_constant__ RowParams p)
 
         // ... and the cluster's, through distributed shared memory; each CTA finishes a share
         // of the outputs and the weights of its own slots
-        for (int r = tid; r < nr; r += kWarps * 32) {
-            float top = -CUDART_INF_F;
-            for (int c = 0; c < p.split; ++c)
-                top = fmaxf(top, p.split > 1 ? *cluster.map_shared_rank(s_cm + r, c) : s_cm[r]);
-            const int t = (r0 + r) / p.G, g = (r0 + r) - t * p.G;
-            const bool real = t < nq;
-            const PartList parts = p.part_ml && real ? parts_of(p, kh, b * R + r0 + r) : PartList{0, 0, 0, 0};
-            for (int i = 0; i < parts.n; ++i)
-                top = fmaxf(top, p.part_ml[(parts.first + (long long)i * parts.step) * 128 + parts.row].x);
-            const float ref = top == -CUDART_INF_F ? 0.f : top;
-            float sum = 0.f;
-            for (int i = 0; i < parts.n; ++i) {
-                const float2 ml = p.part_ml[(parts.first + (long long)i * parts.step) * 128 + parts.row];
-                sum += exp2_fast(ml.x - ref) * ml.y;
+        for (int r = warp; r < nr; r += kWarps) {          // a warp per query row, lanes over the parts
+            const int t = p.by_g(r0 + r), g = (r0 + r) - t * p.G;
+            const PartList parts = p.part_ml && t < nq ? parts_of(p, kh, b * R + r0 + r) : PartList{0, 0, 0};
+            const float2 *ml = p.part_ml + (long long)parts.first * 128 + parts.row;
+            float2 first = make_float2(-CUDART_INF_F, 0.f);
+            if (lane < parts.n)
+                first = ml[(long long)lane * 256];
+            float cm = -CUDART_INF_F, cl = 0.f;
+            if (lane < p.split) {
+                cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, lane) : s_cm[r];
+                cl = p.split > 1 ? *cluster.map_shared_rank(s_cl + r, lane) : s_cl[r];
             }
-            for (int c = 0; c < p.split; ++c)
-                sum += p.split > 1 ? exp2_fast(*cluster.map_shared_rank(s_cm + r, c) - ref) * *cluster.map_shared_rank(s_cl + r, c)
-                                   : exp2_fast(s_cm[r] - ref) * s_cl[r];
+            float top = fmaxf(first.x, cm);
+            for (int i = lane + 32; i < parts.n; i += 32)
+                top = fmaxf(top, ml[(long long)i * 256].x);
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1)
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float ref = top == -CUDART_INF_F ? 0.f : top;
+            float sum = exp2_fast(cm - ref) * cl + exp2_fast(first.x - ref) * first.y;
+            for (int i = lane + 32; i < parts.n; i += 32)
+                sum += exp2_fast(ml[(long long)i * 256].x - ref) * ml[(long long)i * 256].y;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1)
+                sum += __shfl_xor_sync(0xffffffffu, sum, off);
             // nothing seen: +infinity, so that 2^(x - lse) is 0 for every key
             const float lse = sum == 0.f ? CUDART_INF_F : ref + log2f(sum);
-            s_lse[r] = lse;
-            if (part == 0 && p.lse_out)
-                p.lse_out[((long long)b * p.T + t) * p.Hq + kh * p.G + g] =
-                    sum == 0.f ? -CUDART_INF_F : lse * kLn2;
+            for (int i = lane; i < parts.n; i += 32) {
+                const float pm = i < 32 ? first.x : ml[(long long)i * 256].x;
+                // -1: a part that saw no key; it has no outputs
+                s_fac[r * p.max_parts + i] = pm == -CUDART_INF_F ? -1.f : exp2_fast(pm - lse);
+            }
+            if (lane == 0) {
+                s_lse[r] = lse;
+                s_parts[r] = parts;
+                if (part == 0 && p.lse_out)
+                    p.lse_out[((long long)b * p.T + t) * p.Hq + kh * p.G + g] =
+                        sum == 0.f ? -CUDART_INF_F : lse * kLn2;
+            }
         }
         __syncthreads();
-        // rows run fastest: the parts keep neighbouring rows side by side
+        // A group of `team` lanes per 4 outputs, each lane over every team-th part: as many lanes as
+        // there are for few rows, so that the parts are fetched side by side.  Rows run fastest: the
+        // parts keep neighbouring rows together.
         const int pieces = nr * (p.D / 4);
-        for (int i = part * kWarps * 32 + tid; i < pieces; i += p.split * kWarps * 32) {
+        int team = 1;
+        while (team < 32 && 2 * team * pieces <= p.split * kWarps * 32 && team < p.max_parts)
+            team *= 2;
+        const int sub = tid & (team - 1);
+        for (int i0 = part * (kWarps * 32 / team); i0 < pieces; i0 += p.split * (kWarps * 32 / team)) {
+            const int i = min(i0 + tid / team, pieces - 1);       // (all lanes of a warp stay for the sums)
             const int d4 = i / nr, r = i - d4 * nr;
-            const int t = (r0 + r) / p.G, g = (r0 + r) - t * p.G;
+            const int t = p.by_g(r0 + r), g = (r0 + r) - t * p.G;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            auto add = [&](float m, const float4 &u) {
-                const float f = exp2_fast(m - s_lse[r]);
-                if (m != -CUDART_INF_F) {
-                    v.x += f * u.x;
-                    v.y += f * u.y;
-                    v.z += f * u.z;
-                    v.w += f * u.w;
-                }
-            };
-            if (p.part_ml && t < nq) {
-                const PartList parts = parts_of(p, kh, b * R + r0 + r);
-                for (int k = 0; k < parts.n; ++k) {
-                    const long long block = parts.first + (long long)k * parts.step;
-                    const float m = p.part_ml[block * 128 + parts.row].x;
-                    // (a part without keys has no outputs)
-                    if (m != -CUDART_INF_F)
-                        add(m, p.part_o[(block * (DP / 4) + d4) * 128 + parts.row]);
-                }
+            const PartList parts = s_parts[r];
+            const float *fac = s_fac + r * p.max_parts;
+            const float4 *po = p.part_o + ((long long)parts.first * (DP / 4) + d4) * 128 + parts.row;
+#pragma unroll 1
+            for (int k0 = sub; k0 < parts.n; k0 += 8 * team) {     // eight loads in flight
+                float4 u[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k0 + k * team < parts.n)
+                        u[k] = po[(long long)(k0 + k * team) * (DP / 4) * 256];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k0 + k * team < parts.n && !(fac[k0 + k * team] < 0.f))
+                        axpy(v, fac[k0 + k * team], u[k]);
             }
-            for (int c = 0; c < p.split; ++c) {
+            for (int c = sub; c < p.split; c += team) {
                 const float *so = p.split > 1 ? cluster.map_shared_rank(s_o, c) : s_o;
-                const float m = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, c) : s_cm[r];
-                add(m, *reinterpret_cast<const float4 *>(so + r * DP + 4 * d4));
+                const float cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, c) : s_cm[r];
+                if (cm != -CUDART_INF_F)
+                    axpy(v, exp2_fast(cm - s_lse[r]), *reinterpret_cast<const float4 *>(so + r * Shape::kPitch + 4 * d4));
             }
+            for (int off = 1; off < team; off <<= 1) {
+                v.x += __shfl_xor_sync(0xffffffffu, v.x, off);
+                v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
+                v.z += __shfl_xor_sync(0xffffffffu, v.z, off);
+                v.w += __shfl_xor_sync(0xffffffffu, v.w, off);
+            }
+            if (sub != 0 || i0 + tid / team >= pieces)
+                continue;
             char *dst = (char *)p.out + ((long long)b * p.o_sb + (long long)t * p.o_st +
                                          (long long)(kh * p.G + g) * p.o_sh + 4 * d4) * 2;
             *reinterpret_cast<uint2 *>(dst) = make_uint2(Half2<T>::pack(v.x, v.y), Half2<T>::pack(v.z, v.w));
@@ -631,55 +735,41 @@ row_attention_kernel(const __grid_constant__ RowParams p)
                 for (int j = tid; j < s1 - s0; j += kWarps * 32) {
                     float w = 0.f;
                     for (int r = 0; r < nr; ++r)
-                        w += exp2_fast(s_score[r * p.score_cap + j] - s_lse[r]);
+                        if (p.by_g(r0 + r) < nq)
+                            w += exp2_fast(s_score[r * p.score_cap + (s0 - src.x0 - kept0) + j] - s_lse[r]);
                     const long long at = s0 - p.P + j;
                     if (CSTR_INB(p.oob, at, p.cap, CSTR_SITE_CACHE))
-                        wrow[at] += w;
+                        add_once(wrow + at, w);
                 }
             } else {                                // scores once more from the keys
-                float lse[RBT][2];
+                float lse[NT][2];
 #pragma unroll
-                for (int rb = 0; rb < RBT; ++rb)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int r = rb * 16 + h * 8 + (lane >> 2);
-                        lse[rb][h] = r < nr ? s_lse[r] : CUDART_INF_F;
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = 8 * n + 2 * (lane & 3) + e;
+                        lse[n][e] = r < nr && p.by_g(r0 + r) < nq ? s_lse[r] : CUDART_INF_F;
                     }
-                const int first = (s0 - src.x0) / kChunk;
-                for (int c = first + warp; c < n_chunks; c += kWarps) {
+                for (int c = kept0 / kChunk + warp; c < n_chunks; c += kWarps) {
                     const int base = src.x0 + c * kChunk;
-                    src.fetch(ring, base, lane, false);
+                    src.fetch(ring, false, base, lane);
                     copy_commit();
                     copy_wait<0>();
                     __syncwarp();
-                    float w[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+                    float x[NT][4], w[2] = {0.f, 0.f};
+                    chunk_scores<T, DP, NT>(x, p, qf, sq, ring, lane, base, src.x1, limit, true, causal);
 #pragma unroll
-                    for (int rb = 0; rb < RBT; ++rb) {
-                        float x[2][4];
-                        chunk_scores<T, DP>(x, p, sq, ring, rb, lane, base, src.x1, limit[rb], causal);
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int n = 0; n < 2; ++n)
+                        for (int e = 0; e < 4; ++e)
+                            w[e >> 1] += exp2_fast(x[n][e] - lse[n][e & 1]);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                w[n][e & 1] += exp2_fast(x[n][e] - lse[rb][e >> 1]);
-                    }
-#pragma unroll
-                    for (int off = 4; off < 32; off <<= 1)
-#pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            w[n][0] += __shfl_xor_sync(0xffffffffu, w[n][0], off);
-                            w[n][1] += __shfl_xor_sync(0xffffffffu, w[n][1], off);
-                        }
-                    if (lane < 4) {
-#pragma unroll
-                        for (int n = 0; n < 2; ++n)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int at = base + 8 * n + 2 * lane + e;
-                                if (at >= s0 && at < s1 &&
-                                    CSTR_INB(p.oob, at - p.P, p.cap, CSTR_SITE_CACHE))
-                                    wrow[at - p.P] += w[n][e];
-                            }
+                    for (int h = 0; h < 2; ++h) {
+                        w[h] += __shfl_xor_sync(0xffffffffu, w[h], 1);
+                        w[h] += __shfl_xor_sync(0xffffffffu, w[h], 2);
+                        const int at = base + 8 * h + (lane >> 2);
+                        if ((lane & 3) == 0 && at >= s0 && at < s1 && CSTR_INB(p.oob, at - p.P, p.cap, CSTR_SITE_CACHE))
+                            add_once(wrow + at - p.P, w[h]);
                     }
                     __syncwarp();
                 }
@@ -689,26 +779,28 @@ row_attention_kernel(const __grid_constant__ RowParams p)
     }
 }
 
-template <typename T, int DP, int RBT>
+template <typename T, int DP, int NT>
 int launch(const cstr_cache &c, RowParams p, cudaStream_t stream)
 {
     using Shape = RowShape<DP>;
-    constexpr int ROWS = 16 * RBT;
-    const int area = Shape::kRing > kWarps * ROWS * DP * 4 ? Shape::kRing : kWarps * ROWS * DP * 4;
-    const int fixed = ROWS * DP * 2 + (2 * kWarps + 3) * ROWS * 4 + area;
-    int smem = fixed;
+    constexpr int ROWS = 8 * NT;
+    constexpr int out = kWarps * ROWS * Shape::kPitch * 4;
+    const int fixed = ROWS * DP * 2 + (2 * kWarps + 3) * ROWS * 4 + (Shape::kRing > out ? Shape::kRing : out);
+    const int rows = p.G * p.T < ROWS ? p.G * p.T : ROWS;
+    int smem = fixed + rows * p.max_parts * 4;
     p.score_cap = 0;
     if (p.accumulate) {
-        const int rows = p.G * p.T < ROWS ? p.G * p.T : ROWS;
-        // own slots, at most: a CTA's share of the list may be slots alone
-        const long long share = ((long long)p.P + p.cap + p.split - 1) / p.split + kChunk;
-        const long long want = share < p.cap ? share : p.cap;
-        if (fixed + want * rows * 4 <= 220 * 1024) {
+        // own slots, at most: a CTA's share of the list may be slots alone.  Whole chunks; behind
+        // prefix keys the slots may begin within a chunk.
+        const long long share = ((long long)p.P + p.cap + p.split - 1) / p.split + (p.split > 1 ? kChunk : 0);
+        const long long own = (share < p.cap ? share : p.cap) + (p.P > 0 ? kChunk : 0);
+        const long long want = (own + kChunk - 1) / kChunk * kChunk;
+        if (smem + want * rows * 4 <= 220 * 1024) {
             p.score_cap = (int)want;
             smem += (int)(want * rows * 4);
         }
     }
-    auto kernel = row_attention_kernel<T, DP, RBT>;
+    auto kernel = row_attention_kernel<T, DP, NT>;
     CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
@@ -736,10 +828,13 @@ template <typename T>
 int launch_typed(const cstr_cache &c, const RowParams &p, cudaStream_t stream)
 {
     const bool wide = c.head_dim > 64;
-    // more than 16 query rows: two blocks of 16 per pass, so that the keys are read half as often
-    if (p.G * p.T > 16)
+    const int rows = p.G * p.T;
+    // as few passes over the keys as there are blocks of 32 query rows, and no wider than needed
+    if (rows <= 8)
+        return wide ? launch<T, 128, 1>(c, p, stream) : launch<T, 64, 1>(c, p, stream);
+    if (rows <= 16)
         return wide ? launch<T, 128, 2>(c, p, stream) : launch<T, 64, 2>(c, p, stream);
-    return wide ? launch<T, 128, 1>(c, p, stream) : launch<T, 64, 1>(c, p, stream);
+    return wide ? launch<T, 128, 4>(c, p, stream) : launch<T, 64, 4>(c, p, stream);
 }
 
 }  // namespace
@@ -769,6 +864,7 @@ int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, bool 
     p.Hq = c.n_heads;
     p.Hk = c.n_kv_heads;
     p.G = c.n_heads / c.n_kv_heads;
+    p.by_g.set(p.G);
     p.D = c.head_dim;
     p.cap = c.cap;
     p.P = with_prefix ? (int)c.prefix_len : 0;
@@ -779,14 +875,17 @@ int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, bool 
         p.pairs = s.pairs;
         p.tiles = s.tiles;
         p.grid = s.grid;
+        p.narrow = (long long)c.n_kv_heads * s.pairs * s.tiles * s.grid < 0x7fffffffLL;
+        p.max_parts = s.grid / (c.n_kv_heads * s.pairs) + 2;
     }
     p.scale_log2 = a.scale_log2;
     p.accumulate = a.accumulate;
     p.oob = CSTR_OOB_RECORD();
-    // share a row's keys among CTAs until there are two per SM, or 64 keys a CTA
+    // share a row's keys among CTAs while all of them still run at once (four per SM) and each has
+    // 64 keys
     const long long items = (long long)p.B * p.Hk;
     p.split = 1;
-    while (p.split < 8 && items * p.split < 2LL * c.sm_count &&
+    while (p.split < 8 && items * p.split * 2 <= 4LL * c.sm_count &&
            (long long)p.P + p.cap >= 2LL * p.split * 64)
         p.split *= 2;
     if (items * p.split > 0x7fffffffLL)

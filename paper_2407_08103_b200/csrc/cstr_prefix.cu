@@ -24,6 +24,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
+#include <math.h>
 #include <string.h>
 
 #include "cstr_cache.cuh"
@@ -45,14 +46,15 @@ template <int DP> struct Shape {
 
 struct PrefixParams {
     const void *q;
-    long long q_sb, q_st, q_sh;
+    int q_sb, q_st, q_sh;            // bytes / 16
     float *part_o;
     float2 *part_ml;
     int *status;
     int M, T, G, R, D, P, Hk;        // R = T G query rows of one batch row
     int tiles, pairs, grid;
-    float scale_log2;                // >= 0: a negative scale flips the queries' signs
-    int flip;
+    float scale_log2;                // >= 0: for a negative scale the first product negates the queries
+    unsigned negate;                 // bit of the instruction descriptor
+    cstr_divisor by_r, by_g;
 };
 
 __device__ __forceinline__ unsigned smem_addr(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -62,6 +64,30 @@ __device__ __forceinline__ float exp2_fast(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// two fp32 operations per instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\n"
+        "fma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n.reg .b64 x, y, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\n"
+        "add.rn.f32x2 w, x, y;\nmov.b64 {%0, %1}, w;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 template <typename T> __device__ __forceinline__ unsigned pack2(float lo, float hi);
@@ -152,35 +178,53 @@ __device__ __forceinline__ void tmem_st16(unsigned addr, const unsigned (&r)[16]
           "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Loads complete.  The registers are operands, so that no use of them moves before the wait.
+__device__ __forceinline__ void tmem_wait_ld(float (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
+                   "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]),
+                   "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]),
+                   "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
+                 :: "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-__device__ __forceinline__ void commit(unsigned bar)
+// The products are issued by one lane (`leader`) of a warp that runs through the loop as a whole:
+// every operand is then the same in all lanes and stays in the uniform registers that the
+// instructions take them from, instead of being moved there one by one.
+__device__ __forceinline__ void commit(unsigned leader, unsigned bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{\n.reg .pred l;\nsetp.ne.u32 l, %0, 0;\n"
+                 "@l tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n}\n"
+                 ::"r"(leader), "r"(bar) : "memory");
 }
 
-// Shared-memory operand with 128-byte rows in the 128-byte swizzle; `lead`: bytes between blocks of
-// 64 elements along the row dimension of a transposed operand.
-__device__ __forceinline__ unsigned long long operand(unsigned addr, unsigned lead)
+// Shared-memory operand with 128-byte rows in the 128-byte swizzle.  Low word: address and, for a
+// transposed operand, the bytes (kLead) between blocks of 64 elements along its row dimension;
+// high word: 1,024 bytes between groups of eight rows, version, swizzle.
+constexpr unsigned kOperandHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+constexpr unsigned kLead = kTile * 128;
+__device__ __forceinline__ unsigned operand(unsigned addr, unsigned lead)
 {
-    return (unsigned long long)((addr & 0x3ffffu) >> 4) | ((unsigned long long)(lead >> 4) << 16) |
-           ((unsigned long long)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+    return ((addr & 0x3ffffu) >> 4) | ((lead >> 4) << 16);
 }
 
-__device__ __forceinline__ void mma_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool add)
+__device__ __forceinline__ void mma_ss(unsigned leader, unsigned d, unsigned a, unsigned b, unsigned idesc, unsigned add)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add) : "memory");
+    asm volatile("{\n.reg .pred l, p;\n.reg .b64 x, y;\nsetp.ne.u32 l, %0, 0;\nsetp.ne.u32 p, %5, 0;\n"
+                 "mov.b64 x, {%2, %6};\nmov.b64 y, {%3, %6};\n"
+                 "@l tcgen05.mma.cta_group::1.kind::f16 [%1], x, y, %4, p;\n}\n"
+                 ::"r"(leader), "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(kOperandHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(unsigned d, unsigned a, unsigned long long b, unsigned idesc, bool add)
+__device__ __forceinline__ void mma_ts(unsigned leader, unsigned d, unsigned a, unsigned b, unsigned idesc, unsigned add)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((unsigned)add) : "memory");
+    asm volatile("{\n.reg .pred l, p;\n.reg .b64 y;\nsetp.ne.u32 l, %0, 0;\nsetp.ne.u32 p, %5, 0;\n"
+                 "mov.b64 y, {%3, %6};\n"
+                 "@l tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], y, %4, p;\n}\n"
+                 ::"r"(leader), "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(kOperandHigh) : "memory");
 }
 
 __device__ __forceinline__ void tma_tile(unsigned dst, const CUtensorMap *map, int x, int key, int head, unsigned bar)
@@ -209,7 +253,7 @@ struct Walk {
     {
         if (at >= end)
             return false;
-        s.item = (int)(at / p.tiles);
+        s.item = end < (1ll << 31) ? (int)((unsigned)at / (unsigned)p.tiles) : (int)(at / p.tiles);
         s.tile0 = (int)(at - (long long)s.item * p.tiles);
         s.tiles = (int)min((long long)(p.tiles - s.tile0), end - at);
         const int pair = s.item % p.pairs;
@@ -236,19 +280,19 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     using S = Shape<DP>;
     constexpr int kSlots = S::kSlots;
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) unsigned long long s_bar[2 * kSlots + 9];
+    __shared__ __align__(8) unsigned long long s_bar[2 * kSlots + 11];
+    __shared__ float2 s_ml[kTile];               // second stream's maximum and sum, one-tile segments
     __shared__ unsigned s_tmem;
     __shared__ int s_abort;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     const unsigned raw = smem_addr(smem_raw);
     const unsigned q_tile = (raw + 1023u) & ~1023u;              // [2][kTile][DP], swizzled
-    char *q_ptr = smem_raw + (q_tile - raw);
     const unsigned ring = q_tile + 2 * S::kTileBytes;
     const unsigned bars = smem_addr(s_bar);
     auto full = [&](int slot) { return bars + 8u * slot; };
     auto empty = [&](int slot) { return bars + 8u * (kSlots + slot); };
-    const unsigned q_full = bars + 8u * (2 * kSlots), drain = q_full + 56, q_free = q_full + 64;
+    const unsigned q_full = bars + 8u * (2 * kSlots), drain = q_full + 56, q_free = q_full + 64, ml_full = q_full + 72, ml_free = q_full + 80;
     auto s_full = [&](int s) { return q_full + 8u * (1 + s); };
     auto p_full = [&](int s) { return q_full + 8u * (3 + s); };
     auto o_full = [&](int s) { return q_full + 8u * (5 + s); };
@@ -269,6 +313,8 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         }
         bar_init(drain, 1);
         bar_init(q_free, 8);
+        bar_init(ml_full, 4);
+        bar_init(ml_free, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -315,74 +361,79 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {                                         // products
-            constexpr unsigned type = sizeof(T) && __is_same(T, __nv_bfloat16) ? 1u : 0u;
-            constexpr unsigned idesc = (1u << 4) | (type << 7) | (type << 10) | ((kTile / 16) << 24);
-            constexpr unsigned idesc_s = idesc | ((kTile / 8) << 17);
-            constexpr unsigned idesc_o = idesc | (1u << 16) | ((DP / 8) << 17);
-            unsigned base = 0, seg = 0, p_count[2] = {0, 0};
-            bool alive = true;
-            while (alive && walk.next(g)) {
-                const int lead = min(g.pair_rows ? 1 : 2, g.tiles);
-                const int visits = g.pair_rows ? 2 * g.tiles : g.tiles;
-                const int shift = g.pair_rows ? 1 : 0;
-                alive = bar_wait(q_full, seg & 1u, abort);
-                ++seg;
-                auto scores = [&](int n) {
-                    const unsigned at = base + place_k(n >> shift, lead);
-                    const int slot = at % kSlots;
-                    alive = alive && bar_wait(full(slot), (at / kSlots) & 1u, abort);
-                    if (!alive)
-                        return;
-                    fence_after();
-                    const int s = n & 1;
-                    const unsigned qa = q_tile + (g.pair_rows ? s : 0) * S::kTileBytes, ka = ring + slot * S::kTileBytes;
+        // products
+        constexpr unsigned type = __is_same(T, __nv_bfloat16) ? 1u : 0u;
+        constexpr unsigned idesc = (1u << 4) | (type << 7) | (type << 10) | ((kTile / 16) << 24);
+        const unsigned idesc_s = idesc | ((kTile / 8) << 17) | p.negate;
+        constexpr unsigned idesc_o = idesc | (1u << 16) | ((DP / 8) << 17);
+        unsigned leader;
+        asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(leader));
+        unsigned base = 0, seg = 0, p_count[2] = {0, 0};
+        bool alive = true;
+        auto wait = [&](unsigned bar, unsigned parity) {
+            alive = alive && __all_sync(0xffffffffu, bar_wait(bar, parity, abort));
+        };
+        while (alive && walk.next(g)) {
+            const int lead = min(g.pair_rows ? 1 : 2, g.tiles);
+            const int visits = g.pair_rows ? 2 * g.tiles : g.tiles;
+            const int shift = g.pair_rows ? 1 : 0;
+            wait(q_full, seg & 1u);
+            ++seg;
+            auto scores = [&](int n) {
+                const unsigned at = base + place_k(n >> shift, lead);
+                const int slot = at % kSlots;
+                wait(full(slot), (at / kSlots) & 1u);
+                if (!alive)
+                    return;
+                fence_after();
+                const int s = n & 1;
+                const unsigned qa = operand(q_tile + (g.pair_rows ? s : 0) * S::kTileBytes, 16);
+                const unsigned ka = operand(ring + slot * S::kTileBytes, 16);
 #pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
-                        const unsigned off = (k / 4) * (kTile * 128) + (k % 4) * 32;
-                        mma_ss(t_s + s * kTile, operand(qa + off, 16), operand(ka + off, 16), idesc_s, k > 0);
-                    }
-                    commit(s_full(s));
-                    if (!g.pair_rows || s == 1)
-                        commit(empty(slot));
-                };
-                if (alive)
-                    scores(0);
-                if (alive && visits > 1)
-                    scores(1);
-                for (int n = 0; n < visits && alive; ++n) {
-                    const int s = n & 1;
-                    const unsigned at = base + place_v(n >> shift, lead, g.tiles);
-                    const int slot = at % kSlots;
-                    alive = bar_wait(full(slot), (at / kSlots) & 1u, abort) && bar_wait(p_full(s), p_count[s] & 1u, abort);
-                    if (!alive)
-                        break;
-                    ++p_count[s];
-                    fence_after();
-                    const unsigned va = ring + slot * S::kTileBytes;
-#pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k)
-                        mma_ts(t_o + s * kTile, t_s + s * kTile + 8 * k, operand(va + k * 2048, kTile * 128), idesc_o,
-                               n >= 2 || k > 0);
-                    commit(o_full(s));
-                    if (!g.pair_rows || s == 1)
-                        commit(empty(slot));
-                    if (n + 2 < visits)
-                        scores(n + 2);
+                for (int k = 0; k < DP / 16; ++k) {
+                    const unsigned off = ((k / 4) * (kTile * 128) + (k % 4) * 32) >> 4;
+                    mma_ss(leader, t_s + s * kTile, qa + off, ka + off, idesc_s, k > 0);
                 }
-                base += 2 * g.tiles;
+                commit(leader, s_full(s));
+                if (!g.pair_rows || s == 1)
+                    commit(leader, empty(slot));
+            };
+            scores(0);
+            if (visits > 1)
+                scores(1);
+            for (int n = 0; n < visits; ++n) {
+                const int s = n & 1;
+                const unsigned at = base + place_v(n >> shift, lead, g.tiles);
+                const int slot = at % kSlots;
+                wait(full(slot), (at / kSlots) & 1u);
+                wait(p_full(s), p_count[s] & 1u);
+                if (!alive)
+                    break;
+                ++p_count[s];
+                fence_after();
+                const unsigned va = operand(ring + slot * S::kTileBytes, kLead);
+#pragma unroll
+                for (int k = 0; k < kTile / 16; ++k)
+                    mma_ts(leader, t_o + s * kTile, t_s + s * kTile + 8 * k, va + k * (2048 >> 4), idesc_o,
+                           k > 0 ? 1u : (unsigned)(n >= 2));
+                commit(leader, o_full(s));
+                if (!g.pair_rows || s == 1)
+                    commit(leader, empty(slot));
+                if (n + 2 < visits)
+                    scores(n + 2);
             }
-            if (*abort) {                                        // let the products in flight end
-                commit(drain);
-                for (unsigned k = 0; k < kWaitLimit && !bar_try(drain, 0); ++k) {}
-            }
+            base += 2 * g.tiles;
+        }
+        if (*abort) {                                            // let the products in flight end
+            commit(leader, drain);
+            for (unsigned k = 0; k < kWaitLimit && !bar_try(drain, 0); ++k) {}
         }
         __syncwarp();
     } else if (warp >= 4) {
         const int s = (warp - 4) >> 2, row = ((warp & 3) << 5) + lane;    // stream; row of its tile = TMEM lane
         const unsigned lane_base = (unsigned)((warp & 3) << 5) << 16;
         const unsigned my_s = t_s + s * kTile + lane_base, my_o = t_o + s * kTile + lane_base;
-        unsigned seg = 0, done = 0;                              // segments; visits of this stream so far
+        unsigned seg = 0, done = 0, joined = 0;                  // segments, visits of this stream, joins so far
         bool alive = true;
         while (alive && walk.next(g)) {
             // both streams have seen their last scores: the query tiles may be replaced
@@ -394,19 +445,19 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             ++seg;
             const int head = g.item / p.pairs, row0 = (g.item % p.pairs) * 2 * kTile;
             const int q_rows = g.pair_rows ? 2 * kTile : kTile;
-            for (int i = tid - 128; i < q_rows * (DP / 8); i += 256) {
-                const int r = i / (DP / 8), ch = i % (DP / 8);
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (r < g.rows && ch * 8 < p.D) {
-                    const int m = row0 + r, b = m / p.R, in = m - b * p.R, t = in / p.G, gh = in - t * p.G;
-                    v = *reinterpret_cast<const uint4 *>((const char *)p.q + 2 * ((long long)b * p.q_sb + (long long)t * p.q_st +
-                                                         (long long)(head * p.G + gh) * p.q_sh + ch * 8));
-                    if (p.flip)
-                        v.x ^= 0x80008000u, v.y ^= 0x80008000u, v.z ^= 0x80008000u, v.w ^= 0x80008000u;
-                }
-                *reinterpret_cast<uint4 *>(q_ptr + (r / kTile) * S::kTileBytes + (ch / 8) * (kTile * 128) +
-                                           (r % kTile) * 128 + (((ch ^ r) & 7) << 4)) = v;
+            constexpr int kPer = 256 / (DP / 8);                 // rows per pass of the 256 threads
+            const int ch = (tid - 128) % (DP / 8);
+#pragma unroll 2
+            for (int r = (tid - 128) / (DP / 8); r < q_rows; r += kPer) {
+                const bool ok = r < g.rows && ch * 8 < p.D;      // else zeroes
+                const int m = ok ? row0 + r : 0, b = p.by_r(m), in = m - b * p.R, t = p.by_g(in), gh = in - t * p.G;
+                const uint4 *from = reinterpret_cast<const uint4 *>(p.q) + ((long long)b * p.q_sb + (long long)t * p.q_st +
+                                    (long long)(head * p.G + gh) * p.q_sh + (ok ? ch : 0));
+                const unsigned to = q_tile + (r / kTile) * S::kTileBytes + (ch / 8) * (kTile * 128) + (r % kTile) * 128 +
+                                    (((ch ^ r) & 7) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(ok ? 16 : 0) : "memory");
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             bar_arrive(q_full);
 
@@ -420,34 +471,68 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                     break;
                 fence_after();
                 if (warp_on) {
-                    float x[4][32];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        tmem_ld32(x[c], my_s + 32 * c);
-                    tmem_wait_ld();
                     const int valid = p.P - (g.tile0 + (g.pair_rows ? n >> 1 : n)) * kTile;
-                    if (valid < kTile) {
+                    if (mine == 0) {                             // the first keys' maximum is the first reference
+                        float top = -CUDART_INF_F;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            float y[32];
+                            tmem_ld32(y, my_s + 32 * c);
+                            tmem_wait_ld(y);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (c * 32 + i >= valid)
-                                    x[c][i] = -CUDART_INF_F;
+                            for (int i = 0; i < 32; i += 2)
+                                top = max3(top, 32 * c + i < valid ? y[i] : -CUDART_INF_F,
+                                           32 * c + i + 1 < valid ? y[i + 1] : -CUDART_INF_F);
+                        }
+                        m = top * p.scale_log2;
                     }
-                    float top[4] = {x[0][0], x[1][0], x[2][0], x[3][0]};
+                    // One pass over the scores with the reference so far; only if some row's maximum
+                    // turns out to have grown by more than 2^8 (rarely) the reference moves and the
+                    // pass is taken again.  P replaces S afterwards.
+                    unsigned w[4][16];
+                    float sum;
+                    for (;;) {
+                        const float ref = m == -CUDART_INF_F ? 0.f : m;
+                        const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), ref2 = make_float2(-ref, -ref);
+                        float x[2][32];                          // a quarter is worked on, one on its way
+                        float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                        float top[2] = {-CUDART_INF_F, -CUDART_INF_F};
+                        tmem_ld32(x[0], my_s);
+                        tmem_wait_ld(x[0]);
 #pragma unroll
-                    for (int i = 1; i < 32; ++i)
+                        for (int c = 0; c < 4; ++c) {
+                            float (&y)[32] = x[c & 1], (&next)[32] = x[(c + 1) & 1];
+                            if (c < 3)
+                                tmem_ld32(next, my_s + 32 * (c + 1));
+                            if (valid < 32 * c + 32) {           // keys past the prompt's end
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            top[c] = fmaxf(top[c], x[c][i]);
-                    const float seen = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
-                    const bool grow = seen > m + kLazy || (m == -CUDART_INF_F && seen > m);
-                    if (__any_sync(0xffffffffu, grow)) {
+                                for (int i = 0; i < 32; ++i)
+                                    if (32 * c + i >= valid)
+                                        y[i] = -CUDART_INF_F;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                top[(i >> 1) & 1] = max3(top[(i >> 1) & 1], y[i], y[i + 1]);
+                                float2 e = fma2(make_float2(y[i], y[i + 1]), scale2, ref2);
+                                e.x = exp2_fast(e.x);
+                                e.y = exp2_fast(e.y);
+                                sum2[(i >> 1) & 1] = add2(sum2[(i >> 1) & 1], e);
+                                // rounded to the values' type for the second product; the sum is not
+                                w[c][i / 2] = pack2<T>(e.x, e.y);
+                            }
+                            if (c < 3)
+                                tmem_wait_ld(next);
+                        }
+                        sum = (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
+                        const float seen = fmaxf(top[0], top[1]) * p.scale_log2;
+                        const bool grow = seen > m + kLazy;
+                        if (!__any_sync(0xffffffffu, grow))
+                            break;
                         const float to = grow ? seen : m;
                         const float f = m == to ? 1.f : exp2_fast(m - to);
                         l *= f;
                         m = to;
-                        if (mine > 0) {                          // O so far counts from the old maximum
+                        if (mine > 0) {                          // O so far counts from the old reference
                             if (!(alive = __all_sync(0xffffffffu, bar_wait(o_full(s), (done - 1) & 1u, abort))))
                                 break;
                             fence_after();
@@ -455,7 +540,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                             for (int c = 0; c < DP / 32; ++c) {
                                 float o[32];
                                 tmem_ld32(o, my_o + 32 * c);
-                                tmem_wait_ld();
+                                tmem_wait_ld(o);
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
                                     o[i] *= f;
@@ -463,23 +548,12 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                             }
                         }
                     }
-                    const float ref = m == -CUDART_INF_F ? 0.f : m;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (!alive)
+                        break;
+                    l += sum;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        unsigned w[16];
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const float a = exp2_fast(fmaf(x[c][i], p.scale_log2, -ref));
-                            const float b = exp2_fast(fmaf(x[c][i + 1], p.scale_log2, -ref));
-                            sum[i & 2] += a;
-                            sum[(i & 2) + 1] += b;
-                            // rounded to the values' type for the second product; the sum is not
-                            w[i / 2] = pack2<T>(a, b);
-                        }
-                        tmem_st16(my_s + 16 * c, w);
-                    }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    for (int c = 0; c < 4; ++c)
+                        tmem_st16(my_s + 16 * c, w[c]);
                     tmem_wait_st();
                 }
                 fence_before();
@@ -489,30 +563,70 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             }
             if (!alive)
                 break;
-            // this segment's part: O as [DP / 4][128][4], so that a warp's rows are adjacent
-            const long long block = ((long long)blockIdx.x + g.item) * 2 + s;
             if (mine > 0) {
                 if (!(alive = __all_sync(0xffffffffu, bar_wait(o_full(s), (done - 1) & 1u, abort))))
                     break;
                 fence_after();
             }
-            if (warp_on) {
-                if (mine > 0) {
+            // One-tile segments: the first stream takes the second one's O (the same tensor memory
+            // lanes) and statistics, and writes one part for both.
+            float m1 = -CUDART_INF_F, l1 = 0.f;
+            if (!g.pair_rows) {
+                if (s == 1) {
+                    s_ml[row] = make_float2(m, l);
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0)
+                        bar_arrive(ml_full);
+                    alive = __all_sync(0xffffffffu, bar_wait(ml_free, joined & 1u, abort));
+                    fence_after();
+                } else {
+                    if (!(alive = __all_sync(0xffffffffu, bar_wait(ml_full, joined & 1u, abort))))
+                        break;
+                    fence_after();
+                    m1 = s_ml[row].x;
+                    l1 = s_ml[row].y;
+                }
+                ++joined;
+            }
+            if (s == 0 || g.pair_rows) {
+                const float top = fmaxf(m, m1), ref = top == -CUDART_INF_F ? 0.f : top;
+                const float f0 = exp2_fast(m - ref), f1 = exp2_fast(m1 - ref);
+                const bool both = !g.pair_rows && visits > 1;
+                // O as [DP / 4][128][4], so that a warp's rows are adjacent
+                const long long block = ((long long)blockIdx.x + g.item) * 2 + s;
+                if (warp_on) {
                     float4 *dst = reinterpret_cast<float4 *>(p.part_o) + block * (DP / 4) * kTile + row;
 #pragma unroll
                     for (int c = 0; c < DP / 32; ++c) {
                         float o[32];
                         tmem_ld32(o, my_o + 32 * c);
-                        tmem_wait_ld();
+                        tmem_wait_ld(o);
+                        if (both) {
+                            float o1[32];
+                            tmem_ld32(o1, my_o + kTile + 32 * c);
+                            tmem_wait_ld(o1);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                o[i] = f0 * o[i] + f1 * o1[i];
+                        }
                         if (my_row < g.rows)
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
                                 dst[(c * 8 + i) * kTile] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     }
+                    if (my_row < g.rows)
+                        p.part_ml[block * kTile + row] = both ? make_float2(top, f0 * l + f1 * l1) : make_float2(m, l);
                 }
-                if (my_row < g.rows)
-                    p.part_ml[block * kTile + row] = make_float2(m, l);
+                if (!g.pair_rows) {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0)
+                        bar_arrive(ml_free);
+                }
             }
+            if (!alive)
+                break;
             fence_before();
         }
     }
@@ -551,7 +665,10 @@ cstr_prefix_plan cstr_plan_prefix(const cstr_cache &c, int tokens)
     s.pairs = (int)((rows + 2 * kTile - 1) / (2 * kTile));
     s.tiles = (int)((c.prefix_len + kTile - 1) / kTile);
     const long long units = (long long)c.n_kv_heads * s.pairs * s.tiles;
-    s.grid = (int)(units < c.sm_count ? units : c.sm_count);
+    // With two tiles of query rows a segment leaves 128 KB of parts, as much as two key tiles read:
+    // a CTA gets two units at least.
+    const long long most = rows > kTile ? (units + 1) / 2 : units;
+    s.grid = (int)(most < c.sm_count ? most : c.sm_count);
     return s;
 }
 
@@ -595,7 +712,7 @@ int cstr_launch_prefix(const cstr_cache &c, const cstr_row_args &a, cudaStream_t
     memset(&p, 0, sizeof p);
     const cstr_prefix_plan s = cstr_plan_prefix(c, a.tokens);
     p.q = a.q;
-    p.q_sb = a.q_sb, p.q_st = a.q_st, p.q_sh = a.q_sh;
+    p.q_sb = (int)(a.q_sb / 8), p.q_st = (int)(a.q_st / 8), p.q_sh = (int)(a.q_sh / 8);
     p.part_o = c.part_o;
     p.part_ml = (float2 *)c.part_ml;
     p.status = c.status;
@@ -603,14 +720,16 @@ int cstr_launch_prefix(const cstr_cache &c, const cstr_row_args &a, cudaStream_t
     p.G = c.n_heads / c.n_kv_heads;
     p.R = p.T * p.G;
     p.M = c.batch * p.R;
+    p.by_r.set(p.R);
+    p.by_g.set(p.G);
     p.D = c.head_dim;
     p.P = (int)c.prefix_len;
     p.Hk = c.n_kv_heads;
     p.tiles = s.tiles;
     p.pairs = s.pairs;
     p.grid = s.grid;
-    p.flip = a.scale_log2 < 0.f;
-    p.scale_log2 = p.flip ? -a.scale_log2 : a.scale_log2;
+    p.negate = a.scale_log2 < 0.f ? 1u << 13 : 0u;
+    p.scale_log2 = fabsf(a.scale_log2);
     const bool wide = c.head_dim > 64;
     if (c.dtype == CSTR_BF16)
         return wide ? launch<__nv_bfloat16, 128>(c, p, stream) : launch<__nv_bfloat16, 64>(c, p, stream);
