@@ -11,23 +11,26 @@ namespace {
 
 // ---- insertion -------------------------------------------------------------
 //
-// One CTA per row and key / value head.  Entries are ordered by (protected,
+// Per row and key / value head ("item"), entries are ordered by (protected,
 // weight, slot); their 32-bit keys are order-preserving bits of the weight, all
-// ones when protected, 0 for NaN.
-//   One entry to evict (a decoding step with a full cache): the smallest (key,
-// slot) pair, found while the row is read.
-//   More: the keys are put into shared memory, the e-th smallest is found by
-// three passes over digits of 11, 11 and 10 bits (counts per digit, then a scan),
-// and ties at that key are taken in slot order.  Evicted slots below the new
-// length, and surviving ones past it, are listed in slot order: each warp counts
-// its own range, the counts are added up across warps, and the warp writes from
-// there.  The i-th free place gets the i-th mover.
+// ones when protected, 0 for NaN.  The e-th smallest key is found, ties at it are
+// taken in slot order, evicted slots below the new length and surviving ones past
+// it are listed in slot order, and the i-th free place gets the i-th mover.
 // All of it is counting, so no result depends on the order of atomics.
 //
 // Bound: 8 bytes per entry (weight, age) are read; only new tokens, and
-// survivors past the new length, are copied.
-constexpr int kMaxThreads = 256;
-constexpr int kBins = 2048;
+// survivors past the new length, are copied.  What costs time beyond that is the
+// chain of dependent steps of one item, so the variants differ in who
+// works on it:
+//   single tokens, up to 2,048 slots: a warp per item.  It evicts one entry (a
+//     decoding step with a full cache): the smallest (key, slot) pair, found
+//     while the row is read, without a barrier;
+//   else a CTA per item, 256 threads up to 4,096 slots (so that several items share
+//     an SM), 1,024 beyond; keys in shared memory (or scratch, past 24,576), the
+//     e-th smallest from counts per 11-bit digit.
+constexpr int kMaxThreads = 1024;
+constexpr int kMaxWarps = kMaxThreads / 32;
+
 
 struct InsertParams {
     const char *k_new, *v_new;
@@ -40,6 +43,7 @@ struct InsertParams {
     unsigned int *ticket;
     int32_t *list;       // null: keys and places live in shared memory
     int B, Hk, D, cap, T, budget, recent;
+    int bits;            // of a digit: 11 (8 KB of bins) or 8 (1 KB, for CTAs that hardly ever count)
     int wide;            // weight and age rows can be read 16 bytes at a time
     unsigned long long *oob;
 };
@@ -54,117 +58,98 @@ __device__ __forceinline__ unsigned evict_key(float w, int age, int protect_from
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// f(slot, key) for the slots [0, len) of a row, each by one thread of the CTA
+constexpr unsigned kZeroKey = 0x80000000u;    // evict_key of weight 0
+
+// f(slot, key) for the slots [0, len) of a row, each by one of `step` threads
 template <typename F>
 __device__ __forceinline__ void for_keys(const InsertParams &p, const float *weight, const int32_t *age, int len,
-                                         int protect_from, F f)
+                                         int protect_from, int tid, int step, F f)
 {
     if (p.wide) {
-#pragma unroll 4
-        for (int j = threadIdx.x * 4; j < len; j += blockDim.x * 4) {
-            const float4 w = *reinterpret_cast<const float4 *>(weight + j);
-            const int4 a = *reinterpret_cast<const int4 *>(age + j);
-            f(j, evict_key(w.x, a.x, protect_from));
-            if (j + 1 < len)
-                f(j + 1, evict_key(w.y, a.y, protect_from));
-            if (j + 2 < len)
-                f(j + 2, evict_key(w.z, a.z, protect_from));
-            if (j + 3 < len)
-                f(j + 3, evict_key(w.w, a.w, protect_from));
+#pragma unroll 1
+        for (int j0 = tid * 4; j0 < len; j0 += step * 16) {       // eight loads in flight
+            float4 w[4];
+            int4 a[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = j0 + i * step * 4;
+                if (j < len) {
+                    w[i] = *reinterpret_cast<const float4 *>(weight + j);
+                    a[i] = *reinterpret_cast<const int4 *>(age + j);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = j0 + i * step * 4;
+                if (j < len)
+                    f(j, evict_key(w[i].x, a[i].x, protect_from));
+                if (j + 1 < len)
+                    f(j + 1, evict_key(w[i].y, a[i].y, protect_from));
+                if (j + 2 < len)
+                    f(j + 2, evict_key(w[i].z, a[i].z, protect_from));
+                if (j + 3 < len)
+                    f(j + 3, evict_key(w[i].w, a[i].w, protect_from));
+            }
         }
     } else {
 #pragma unroll 4
-        for (int j = threadIdx.x; j < len; j += blockDim.x)
+        for (int j = tid; j < len; j += step)
             f(j, evict_key(weight[j], age[j], protect_from));
     }
 }
 
-// Lists the free places below new_len (ascending, from place[0]) and the surviving slots at or past
-// it (ascending, from place[cap - 1] downwards); returns the number of the latter.  `evict` >= 2.
-__device__ __forceinline__ int choose(const InsertParams &p, const unsigned *keys, int *place, int *s_bin, int *s_word,
-                                      int len, int new_len, int evict)
+template <bool WARP> __device__ __forceinline__ void team_sync()
 {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-    unsigned prefix = 0, fixed = 0;                               // digits found so far, and their mask
-    int want = evict;                                             // rank among the keys with this prefix
-#pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-        const unsigned digits = pass == 2 ? 1023u : 2047u;
-        for (int i = tid; i < kBins; i += blockDim.x)
-            s_bin[i] = 0;
+    if (WARP)
+        __syncwarp();
+    else
         __syncthreads();
-        for (int j = tid; j - lane < len; j += blockDim.x) {      // whole warps
-            const unsigned k = j < len ? keys[j] : 0u;
-            const bool in = j < len && (k & fixed) == prefix;
-            const unsigned d = in ? (k >> shift) & digits : 0xffffffffu;
-            int same;
-            __match_all_sync(0xffffffffu, d, &same);              // e.g. nothing weighed yet: all zero
-            if (same) {
-                if (in && lane == 0)
-                    atomicAdd(&s_bin[d], 32);
-            } else if (in)
-                atomicAdd(&s_bin[d], 1);
-        }
-        __syncthreads();
-        // first digit whose running count reaches `want`: a thread adds up its bins, the warps scan
-        const int per = kBins / (int)blockDim.x;
-        int sum = 0;
-        for (int i = 0; i < per; ++i)
-            sum += s_bin[tid * per + i];
-        int upto = sum;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, upto, off);
-            upto += lane >= off ? o : 0;
-        }
-        if (lane == 31)
-            s_word[warp] = upto;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w)
-            upto += s_word[w];
-        if (upto >= want && upto - sum < want) {                  // one thread
-            int below = upto - sum, d = tid * per;
-            while (below + s_bin[d] < want)
-                below += s_bin[d++];
-            s_word[kMaxThreads / 32] = d;
-            s_word[kMaxThreads / 32 + 1] = below;
-        }
-        __syncthreads();
-        prefix |= (unsigned)s_word[kMaxThreads / 32] << shift;
-        fixed |= digits << shift;
-        want -= s_word[kMaxThreads / 32 + 1];
-        __syncthreads();
-    }
-    // evicted: key < prefix, and the first `want` slots with key == prefix
-    const int span = ((len + warps - 1) / warps + 31) & ~31;      // slots of a warp
-    const int lo = min(warp * span, len), hi = min(lo + span, len);
-    int ties = 0;
-    for (int j = lo + lane; j - lane < hi; j += 32)
-        ties += __popc(__ballot_sync(0xffffffffu, j < hi && keys[j] == prefix));
-    if (lane == 0)
-        s_word[warp] = ties;
-    __syncthreads();
+}
+
+// Evicted: key < limit, and the first `want` slots with key == limit (`all_equal`: all of them, so that
+// they need no counting).  Lists the free places below
+// new_len (ascending, from place[0]) and the surviving slots at or past it (ascending, from
+// place[cap - 1] downwards); returns the number of the latter.  The team is a warp or the CTA; its
+// warps own contiguous spans [lo, hi) of slots.
+template <bool WARP>
+__device__ __forceinline__ int list_places(const InsertParams &p, const unsigned *keys, int *place, int *s_word, int len, int new_len,
+                                           unsigned limit, int want, bool all_equal, int lo, int hi)
+{
+    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5;
+    const int warps = WARP ? 1 : blockDim.x >> 5, tid = WARP ? lane : threadIdx.x, step = WARP ? 32 : blockDim.x;
+    const unsigned below = (1u << lane) - 1u;
     int tie0 = 0;
-    for (int w = 0; w < warp; ++w)
-        tie0 += s_word[w];
-    __syncthreads();
+    if (!all_equal) {
+        int ties = 0;
+#pragma unroll 4
+        for (int j = lo + lane; j - lane < hi; j += 32)
+            ties += __popc(__ballot_sync(0xffffffffu, j < hi && keys[j] == limit));
+        if (lane == 0)
+            s_word[warp] = ties;
+        team_sync<WARP>();
+        if (!WARP)
+            tie0 = __reduce_add_sync(0xffffffffu, lane < warp ? s_word[lane] : 0);
+        team_sync<WARP>();
+    }
     int holes = 0, movers = 0;
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {                     // count, then write
         int hole0 = 0, mover0 = 0, tie = tie0;
         if (round == 1) {
             if (lane == 0)
-                s_word[warp] = holes, s_word[kMaxThreads / 32 + warp] = movers;
-            __syncthreads();
-            for (int w = 0; w < warp; ++w)
-                hole0 += s_word[w], mover0 += s_word[kMaxThreads / 32 + w];
+                s_word[warp] = holes, s_word[kMaxWarps + warp] = movers;
+            team_sync<WARP>();
+            if (!WARP) {
+                hole0 = __reduce_add_sync(0xffffffffu, lane < warp ? s_word[lane] : 0);
+                mover0 = __reduce_add_sync(0xffffffffu, lane < warp ? s_word[kMaxWarps + lane] : 0);
+            }
         }
         holes = movers = 0;
+#pragma unroll 4
         for (int j = lo + lane; j - lane < hi; j += 32) {
-            const unsigned k = j < hi ? keys[j] : 0xffffffffu, below = (1u << lane) - 1u;
-            const unsigned equal = __ballot_sync(0xffffffffu, j < hi && k == prefix);
-            const bool gone = j < hi && (k < prefix || (k == prefix && tie + __popc(equal & below) < want));
+            const unsigned k = j < hi ? keys[j] : 0xffffffffu;
+            const unsigned equal = __ballot_sync(0xffffffffu, j < hi && k == limit);
+            const bool gone = j < hi && (k < limit || (k == limit && (all_equal || tie + __popc(equal & below) < want)));
             tie += __popc(equal);
             const unsigned hole = __ballot_sync(0xffffffffu, gone && j < new_len);
             const unsigned mover = __ballot_sync(0xffffffffu, j < hi && !gone && j >= new_len);
@@ -178,43 +163,177 @@ __device__ __forceinline__ int choose(const InsertParams &p, const unsigned *key
             movers += __popc(mover);
         }
         if (round == 1 && warp == warps - 1 && lane == 0) {       // totals
-            s_word[2 * (kMaxThreads / 32)] = hole0 + holes;
-            s_word[2 * (kMaxThreads / 32) + 1] = mover0 + movers;
+            s_word[2 * kMaxWarps] = hole0 + holes;
+            s_word[2 * kMaxWarps + 1] = mover0 + movers;
         }
     }
-    __syncthreads();
-    const int all = s_word[2 * (kMaxThreads / 32)];
-    for (int j = len + tid; j < new_len; j += blockDim.x)         // free places past the old length
+    team_sync<WARP>();
+    const int all = s_word[2 * kMaxWarps];
+    for (int j = len + tid; j < new_len; j += step)               // free places past the old length
         place[all + j - len] = j;
-    __syncthreads();
-    return s_word[2 * (kMaxThreads / 32) + 1];
+    team_sync<WARP>();
+    return s_word[2 * kMaxWarps + 1];
 }
 
-__global__ void __launch_bounds__(kMaxThreads)
+// Reads a row, leaves its keys in keys[0 .. len), and finds the `evict` smallest: those below the
+// returned limit and the first `want` (in slot order) of the `equal` ones at it; where all of these
+// belong to them, the limit may be any larger key below the next one.  Counts per digit of p.bits
+// bits, the most significant first (that one while the row is read).
+template <bool WARP>
+__device__ __forceinline__ unsigned select_by_digits(const InsertParams &p, const float *weight, const int32_t *age,
+                                                     int protect_from, unsigned *keys, int *s_bin, int *s_word,
+                                                     int len, int evict, int &want, int &equal)
+{
+    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5;
+    const int tid = WARP ? lane : threadIdx.x, step = WARP ? 32 : blockDim.x;
+    const int per = (1 << p.bits) / step;                         // bins of a thread, side by side
+    int *mine = s_bin + tid * per;
+    unsigned prefix = 0, fixed = 0;                               // digits found so far, and their mask
+    want = evict;                                                 // rank among the keys with this prefix
+    auto clear = [&] {                                            // (per is 2, 8 or 64; bins are aligned)
+        if (per % 4 == 0)
+            for (int i = 0; i < per; i += 4)
+                *reinterpret_cast<int4 *>(mine + i) = make_int4(0, 0, 0, 0);
+        else
+            for (int i = 0; i < per; ++i)
+                mine[i] = 0;
+    };
+    clear();
+    team_sync<WARP>();
+#pragma unroll 1
+    for (int left = 32; left > 0; left -= p.bits) {
+        const int shift = max(left - p.bits, 0);
+        const unsigned digits = (1u << (left - shift)) - 1u;
+        // Protected entries, and tokens that nothing has attended to yet, are many: they would queue up
+        // at one bin.  The former are left out, the latter are counted aside.
+        int zeros = 0;
+        auto count = [&](unsigned k) {
+            if (k == kZeroKey)
+                ++zeros;
+            else if (k != 0xffffffffu)
+                atomicAdd(&s_bin[(k >> shift) & digits], 1);
+        };
+        if (left == 32) {
+            for_keys(p, weight, age, len, protect_from, tid, step, [&](int j, unsigned k) {
+                keys[j] = k;
+                count(k);
+            });
+        } else {
+#pragma unroll 4
+            for (int j = tid; j < len; j += step) {
+                const unsigned k = keys[j];
+                if ((k & fixed) == prefix)
+                    count(k);
+            }
+        }
+        __syncwarp();
+        zeros = __reduce_add_sync(0xffffffffu, zeros);
+        if (lane == 0 && zeros)
+            atomicAdd(&s_bin[(kZeroKey >> shift) & digits], zeros);
+        team_sync<WARP>();
+        // first digit whose running count reaches `want`: a thread adds up its bins, the warps scan
+        int sum = 0;
+        if (per % 4 == 0)
+            for (int i = 0; i < per; i += 4) {
+                const int4 c = *reinterpret_cast<const int4 *>(mine + i);
+                sum += c.x + c.y + c.z + c.w;
+            }
+        else
+            for (int i = 0; i < per; ++i)
+                sum += mine[i];
+        int upto = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, upto, off);
+            upto += lane >= off ? o : 0;
+        }
+        if (!WARP) {
+            if (lane == 31)
+                s_word[warp] = upto;
+            __syncthreads();
+            upto += __reduce_add_sync(0xffffffffu, lane < warp ? s_word[lane] : 0);
+        }
+        if (upto >= want && upto - sum < want) {                  // one thread, if any
+            int before = upto - sum, i = 0;
+            while (before + mine[i] < want)
+                before += mine[i++];
+            s_word[kMaxWarps] = tid * per + i;
+            s_word[kMaxWarps + 1] = before;
+            s_word[kMaxWarps + 2] = mine[i];
+        }
+        if (tid == step - 1 && upto < want)                       // protected entries have to go, too
+            s_word[kMaxWarps] = -1, s_word[kMaxWarps + 1] = upto;
+        clear();                                                  // for the next digit
+        team_sync<WARP>();
+        const int d = s_word[kMaxWarps];
+        want -= s_word[kMaxWarps + 1];
+        if (d < 0) {
+            prefix = 0xffffffffu;
+            equal = -1;
+            break;
+        }
+        prefix |= (unsigned)d << shift;
+        fixed |= digits << shift;
+        equal = s_word[kMaxWarps + 2];
+        if (equal == want) {                                      // no need to tell these apart
+            prefix |= ~fixed;
+            break;
+        }
+    }
+    team_sync<WARP>();
+    return prefix;
+}
+
+template <bool WARP>
+__global__ void __launch_bounds__(WARP ? 128 : kMaxThreads, WARP ? 8 : 1)
 cache_insert_kernel(const __grid_constant__ InsertParams p)
 {
-    extern __shared__ int s_dyn[];
-    __shared__ int s_word[2 * (kMaxThreads / 32) + 2];
-    __shared__ unsigned long long s_least[kMaxThreads / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int b = blockIdx.x / p.Hk, kh = blockIdx.x - b * p.Hk;
+    constexpr int kWords = 2 * kMaxWarps + 2;
+    extern __shared__ __align__(16) int s_dyn[];                  // bins, keys, places
+    __shared__ int s_words[(WARP ? 4 : 1) * kWords];
+    __shared__ unsigned long long s_least[kMaxWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tid = WARP ? lane : threadIdx.x, step = WARP ? 32 : blockDim.x;
+    const int item = WARP ? blockIdx.x * 4 + warp : blockIdx.x;
+    if (item >= p.B * p.Hk)
+        return;                                                   // (a whole warp; no CTA barrier follows)
+    const int b = item / p.Hk, kh = item - b * p.Hk;
     const int len = min(max(p.lens[b], 0), p.cap);
     const int n = p.n_new ? min(max(p.n_new[b], 0), p.T) : p.T;
     const int pos = p.pos[b];
     const int new_len = min(len + n, p.budget);
     const int evict = len + n - new_len;
-    const long long entry0 = ((long long)b * p.Hk + kh) * p.cap;
+    const int protect_from = pos + n - p.recent;
+    const long long entry0 = (long long)item * p.cap;
     float *weight = p.weight + entry0;
     int32_t *age = p.age + entry0;
-    int *s_bin = s_dyn;
-    unsigned *keys = reinterpret_cast<unsigned *>(p.list ? p.list + entry0 * 2 : s_dyn + kBins);
+    int *s_bin = s_dyn + (WARP ? warp << p.bits : 0), *s_word = s_words + (WARP ? warp * kWords : 0);
+    unsigned *keys = reinterpret_cast<unsigned *>(p.list ? p.list + entry0 * 2 : s_dyn + (1 << p.bits));
     int *place = reinterpret_cast<int *>(keys + p.cap);
     int n_old = 0;                                                // survivors past the new length
-    int only = len;                                               // the place, where there is one to fill
+    int only = len;                                               // evict == 1: the evicted slot
+    const bool listed = evict > 1;
 
-    if (evict == 1) {
+    if (listed) {
+        if (!WARP) {                                              // the new tokens are on their way meanwhile
+            const int lines = (p.D * 2 + 127) / 128;
+            for (int i = tid; i < n * lines; i += step) {
+                const int t = i / lines, line = i - t * lines;
+                const char *k = p.k_new + ((long long)b * p.nk_sb + (long long)t * p.nk_st + (long long)kh * p.nk_sh) * 2;
+                const char *v = p.v_new + ((long long)b * p.nv_sb + (long long)t * p.nv_st + (long long)kh * p.nv_sh) * 2;
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(k + line * 128));
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(v + line * 128));
+            }
+        }
+        int want, equal;
+        const unsigned limit = select_by_digits<WARP>(p, weight, age, protect_from, keys, s_bin, s_word, len, evict,
+                                                      want, equal);
+        const int warps = WARP ? 1 : blockDim.x >> 5, span = ((len + warps - 1) / warps + 31) & ~31;
+        const int lo = WARP ? 0 : min(warp * span, len), hi = min(lo + span, len);
+        n_old = list_places<WARP>(p, keys, place, s_word, len, new_len, limit, want, equal == want, lo, hi);
+    } else if (evict == 1) {
         unsigned long long least = ~0ull;
-        for_keys(p, weight, age, len, pos + n - p.recent, [&](int j, unsigned k) {
+        for_keys(p, weight, age, len, protect_from, tid, step, [&](int j, unsigned k) {
             const unsigned long long at = ((unsigned long long)k << 32) | (unsigned)j;
             least = at < least ? at : least;
         });
@@ -223,25 +342,19 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
             const unsigned long long o = __shfl_xor_sync(0xffffffffu, least, off);
             least = o < least ? o : least;
         }
-        if (lane == 0)
-            s_least[warp] = least;
-        __syncthreads();
-        for (int w = 0; w < (int)(blockDim.x >> 5); ++w)
-            least = s_least[w] < least ? s_least[w] : least;
+        if (!WARP) {
+            if (lane == 0)
+                s_least[warp] = least;
+            __syncthreads();
+            for (int w = 0; w < (int)(blockDim.x >> 5); ++w)
+                least = s_least[w] < least ? s_least[w] : least;
+        }
         only = (int)(unsigned)least;
+        // with nothing added the last entry lies past the new length, and fills the evicted slot
+        // unless it is the evicted one itself
+        n_old = n == 0 && only < new_len ? 1 : 0;
     }
-    // One token into one place, or a row that only grows: no list.  (evict == 1: the free places are
-    // the evicted slot and [len, new_len); with n == 0 the last entry moves into the evicted slot
-    // unless it is that slot.)
-    const bool listed = evict > 1;
-    if (listed) {
-        for_keys(p, weight, age, len, pos + n - p.recent, [&](int j, unsigned k) { keys[j] = k; });
-        __syncthreads();
-        n_old = choose(p, keys, place, s_bin, s_word, len, new_len, evict);
-    } else if (evict == 1) {
-        // the last entry stays but lies past the new length: only when nothing is added
-        n_old = new_len < len && only < new_len ? 1 : 0;
-    }
+    // free places: the list; or the evicted slot and then [len, new_len); or [len, new_len)
     const int moves = n_old + n;
     auto place_of = [&](int mv) {
         if (listed)
@@ -251,7 +364,7 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
     auto mover = [&](int mv) { return listed ? place[p.cap - 1 - mv] : len - 1; };
 
     // copies: 16 bytes a thread, keys and values of four places in flight
-    const int per = p.D / 8, at_once = (int)blockDim.x / per;     // pieces of a row; places side by side
+    const int per = p.D / 8, at_once = step / per;                // pieces of a row; places side by side
     const int piece = tid % per;
     char *ck = p.ck + ((long long)b * p.ck_sb + (long long)kh * p.ck_sh) * 2 + piece * 16;
     char *cv = p.cv + ((long long)b * p.cv_sb + (long long)kh * p.cv_sh) * 2 + piece * 16;
@@ -287,7 +400,7 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
             }
         }
     }
-    for (int mv = tid; mv < moves; mv += blockDim.x) {
+    for (int mv = tid; mv < moves; mv += step) {
         const int dst = place_of(mv);
         if (!CSTR_INB(p.oob, dst, p.cap, CSTR_SITE_CACHE))
             continue;
@@ -301,8 +414,8 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
         }
     }
 
-    // every CTA of the row has read lens[b] when it arrives here; the last one replaces it
-    __syncthreads();
+    // every team of the row has read lens[b] when it arrives here; the last one replaces it
+    team_sync<WARP>();
     if (tid == 0) {
         const unsigned prev = atomicAdd(p.ticket + b, 1u);
         if (prev == (unsigned)p.Hk - 1u) {
@@ -352,19 +465,23 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
     p.budget = a.budget;
     p.recent = a.recent;
     p.oob = CSTR_OOB_RECORD();
-    // Single tokens evict at most one entry (unless the budget has just been lowered): small CTAs,
-    // so that all rows are in flight at once, and the list's memory in the handle's scratch.
-    const bool single = a.tokens <= 1;
-    const bool shared = !single && c.cap <= CSTR_INSERT_SMEM_SLOTS;
-    if (shared)
-        p.list = nullptr;
     p.wide = c.cap % 4 == 0 && aligned16(c.weight) && aligned16(c.age);
-    const int threads = single && c.cap <= 2048 ? 64 : kMaxThreads;
-    const int smem = kBins * 4 + (shared ? c.cap * 8 : 0);
-    if (smem > 48 * 1024)
-        CSTR_CUDA_TRY(cudaFuncSetAttribute(cache_insert_kernel,
-                                           cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    cache_insert_kernel<<<(unsigned)(c.batch * c.n_kv_heads), threads, smem, stream>>>(p);
+    const unsigned items = (unsigned)(c.batch * c.n_kv_heads);
+    if (a.tokens == 1 && c.cap <= 2048) {
+        p.bits = 8;
+        cache_insert_kernel<true><<<(items + 3) / 4, 128, 4 * (4 << p.bits), stream>>>(p);
+    } else {
+        const bool shared = c.cap <= CSTR_INSERT_SMEM_SLOTS;
+        if (shared)
+            p.list = nullptr;
+        p.bits = 11;
+        const int smem = (4 << p.bits) + (shared ? c.cap * 8 : 0);
+        static std::atomic<int> allowed[64];
+        const int rc = smem > 48 * 1024 ? cstr_allow_smem(cache_insert_kernel<false>, allowed, c.device, smem) : CSTR_OK;
+        if (rc)
+            return rc;
+        cache_insert_kernel<false><<<items, c.cap <= 4096 ? 256 : kMaxThreads, smem, stream>>>(p);
+    }
     CSTR_CUDA_TRY(cudaGetLastError());
     return CSTR_OK;
 }

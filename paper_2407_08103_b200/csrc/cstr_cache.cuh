@@ -1,7 +1,22 @@
 // Internal definitions of the key / value cache and its attention (not part of the ABI).
 #pragma once
 
+#include <atomic>
+
 #include "cstr_internal.cuh"
+
+// Allows `kernel` that much dynamic shared memory on `device`; `allowed` (one array per kernel)
+// remembers what it has been given, so that a decoding loop does not ask again.
+template <typename K>
+int cstr_allow_smem(K kernel, std::atomic<int> (&allowed)[64], int device, int bytes)
+{
+    if (device >= 0 && device < 64 && allowed[device].load(std::memory_order_relaxed) >= bytes)
+        return CSTR_OK;
+    CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (device >= 0 && device < 64)
+        allowed[device].store(bytes, std::memory_order_relaxed);
+    return CSTR_OK;
+}
 
 // What cstr_cache_create recorded: caller-owned arrays and their strides (in
 // elements), and the scratch that the handle's calls share.

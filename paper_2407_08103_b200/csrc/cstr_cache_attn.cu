@@ -801,7 +801,10 @@ int launch(const cstr_cache &c, RowParams p, cudaStream_t stream)
         }
     }
     auto kernel = row_attention_kernel<T, DP, NT>;
-    CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static std::atomic<int> allowed[64];
+    const int rc = cstr_allow_smem(kernel, allowed, c.device, smem);
+    if (rc)
+        return rc;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     cfg.gridDim = dim3((unsigned)((long long)p.B * p.Hk * p.split));

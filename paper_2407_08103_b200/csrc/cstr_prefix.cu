@@ -643,7 +643,10 @@ template <typename T, int DP>
 int launch(const cstr_cache &c, const PrefixParams &p, cudaStream_t stream)
 {
     auto kernel = prefix_attention_kernel<T, DP>;
-    CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kSmem));
+    static std::atomic<int> allowed[64];
+    const int rc = cstr_allow_smem(kernel, allowed, c.device, Shape<DP>::kSmem);
+    if (rc)
+        return rc;
     CUtensorMap k, v;
     memcpy(&k, c.map_k, sizeof k);
     memcpy(&v, c.map_v, sizeof v);

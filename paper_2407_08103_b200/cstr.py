@@ -619,11 +619,19 @@ def cstr_pda_step_status(ws: PdaWorkspace, stream=None):
     return tuple(int(v.value) for v in vals)
 
 
+def _raw_stream(stream, device):
+    """Address of a stream of ``device`` (None: its current one)."""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return stream.cuda_stream
+
+
 def _rows_arg(name, t, batch, device, dtype):
     """Checked per-row vector -> address (None -> NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() < batch or not t.is_contiguous() or t.device != device:
+    if t.dtype != dtype or t.numel() < batch or t.device != device or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor with one entry per row on %s"
                          % (name, dtype, device))
     return t.data_ptr()
@@ -678,6 +686,7 @@ def cstr_cache_create(cache_k, cache_v, lens, n_heads: int, prefix_k=None, prefi
     c.arrays = (cache_k, cache_v, prefix_k, prefix_v, lens, weight, age)
     c.batch, c.n_heads, c.n_kv_heads, c.head_dim = batch, n_heads, heads, dim
     c.dtype, c.device = cache_k.dtype, cache_k.device
+    c.strides = {}            # C arrays of the stride sets seen (a program has a few)
     return c
 
 
@@ -696,6 +705,13 @@ def _tokens_arg(name, t, cache, tokens, heads):
     return t.data_ptr(), st
 
 
+def _c_strides(cache, strides):
+    c = cache.strides.get(strides)
+    if c is None:
+        c = cache.strides[strides] = (ctypes.c_int64 * len(strides))(*strides)
+    return c
+
+
 def cstr_cache_insert(cache: Cache, k_new, v_new, pos, budget: int, recent: int = 0, n_new=None,
                       stream=None) -> None:
     """Put ``k_new`` / ``v_new`` ``[B][T][n_kv_heads][D]`` (None: only shrink) into the rows' caches;
@@ -711,13 +727,13 @@ def cstr_cache_insert(cache: Cache, k_new, v_new, pos, budget: int, recent: int 
         tokens = k_new.shape[1] if k_new.dim() == 4 else -1
         kp, ks = _tokens_arg("k_new", k_new, cache, tokens, cache.n_kv_heads)
         vp, vs = _tokens_arg("v_new", v_new, cache, tokens, cache.n_kv_heads)
-        strides = (ctypes.c_int64 * 6)(ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
+        strides = _c_strides(cache, (*ks[:3], *vs[:3]))
     if pos is None:
         raise ValueError("pos is required")
     rc = lib().cstr_cache_insert(cache.ptr, kp, vp, strides, tokens,
                                  _rows_arg("n_new", n_new, cache.batch, cache.device, torch.int32),
                                  _rows_arg("pos", pos, cache.batch, cache.device, torch.int32),
-                                 budget, recent, _stream_ptr(stream))
+                                 budget, recent, _raw_stream(stream, cache.device))
     if rc:
         _check(rc)
 
@@ -736,11 +752,11 @@ def cstr_cache_attention(cache: Cache, q, out, scale: float | None = None, pos=N
     if lse_out is not None:
         lp = _rows_arg("lse_out", lse_out, cache.batch * tokens * cache.n_heads, cache.device, torch.float32)
     rc = lib().cstr_cache_attention(
-        cache.ptr, qp, (ctypes.c_int64 * 3)(qs[0], qs[1], qs[2]), tokens,
+        cache.ptr, qp, _c_strides(cache, qs[:3]), tokens,
         _rows_arg("pos", pos, cache.batch, cache.device, torch.int32),
         _rows_arg("n_query", n_query, cache.batch, cache.device, torch.int32),
         cache.head_dim ** -0.5 if scale is None else scale, 1 if accumulate else 0, op,
-        (ctypes.c_int64 * 3)(os_[0], os_[1], os_[2]), lp, _stream_ptr(stream))
+        _c_strides(cache, os_[:3]), lp, _raw_stream(stream, cache.device))
     if rc:
         _check(rc)
 
@@ -800,7 +816,7 @@ def cstr_policy_loss(tables, logits, states, actions, old_logp, advantages, loss
         _rows_arg("advantages", advantages, n, device, f32),
         _rows_arg("weight", weight, n, device, f32), clip_low, clip_high, kl_coef,
         _rows_arg("loss_out", loss_out, n, device, f32), _rows_arg("logp_out", logp_out, n, device, f32),
-        dp, n, _stream_ptr(stream))
+        dp, n, _raw_stream(stream, device))
     if rc:
         _check(rc)
 

@@ -253,6 +253,13 @@ def test_insert_beyond_the_shared_memory_size():
     check_insert(*random_insert(7, 2, 1, 8, 24576 + 700, 0, 300, 50, "odd"))
 
 
+@pytest.mark.parametrize("cap", [2049, 4097, 8192, 8193, 12000])
+def test_insert_sizes_at_which_the_kernel_changes(cap):
+    check_insert(*random_insert(9, 3, 1, 8, cap, 70, cap - 50, 90, "ties"))
+    check_insert(*random_insert(10, 3, 1, 8, cap, 1, cap - 3, 90, "full"))
+    check_insert(*random_insert(11, 3, 2, 8, cap, 0, cap // 2, 0, "odd"))
+
+
 def test_insert_repeated_steps_stay_within_budget():
     rng = np.random.default_rng(8)
     B, Hk, D, cap, budget = 3, 2, 16, 24, 20
