@@ -2,7 +2,8 @@
 
 Holds the per-batch device state (one automaton state per row, Algorithm 2's
 ``q``) and the step workspace; every step is one ``cstr_step`` call.  The LM
-that produces the logits is outside this package.
+that produces the logits is outside this package; ``SharedPromptCache`` is the
+attention of one of its layers for a batch that answers one prompt.
 """
 
 from __future__ import annotations
@@ -98,3 +99,45 @@ class PushdownDecoder:
         """(inactive rows other than finished ones, rows without an allowed token,
         rows whose stack outgrew ``stack_cap``) since the last call."""
         return cstr.cstr_pda_step_status(self.ws, stream)
+
+
+class SharedPromptCache:
+    """Keys, values and attention of one layer for ``batch`` rows that answer one prompt.
+
+    ``prefix_k`` / ``prefix_v`` ``[P][n_kv_heads][D]`` (bfloat16 or float16) are the prompt's, held
+    once; every row has ``budget`` slots for its own tokens.  A row that would exceed its budget
+    loses the tokens that have received the least attention, its last ``recent`` ones excepted."""
+
+    def __init__(self, prefix_k, prefix_v, batch: int, n_heads: int, budget: int, recent: int = 0,
+                 max_tokens: int = 1):
+        heads, dim = prefix_k.shape[1:]
+        dev = prefix_k.device
+        self.batch, self.budget, self.recent = batch, budget, recent
+        self.k = torch.empty((batch, budget, heads, dim), dtype=prefix_k.dtype, device=dev)
+        self.v = torch.empty_like(self.k)
+        self.weight = torch.empty((batch, heads, budget), dtype=torch.float32, device=dev)
+        self.age = torch.empty((batch, heads, budget), dtype=torch.int32, device=dev)
+        self.lens = torch.zeros(batch, dtype=torch.int32, device=dev)
+        self.pos = torch.zeros(batch, dtype=torch.int32, device=dev)
+        self.handle = cstr.cstr_cache_create(self.k, self.v, self.lens, n_heads, prefix_k=prefix_k,
+                                             prefix_v=prefix_v, weight=self.weight, age=self.age,
+                                             max_tokens=max_tokens)
+
+    def reset(self):
+        """Forget every row's own tokens; the prompt stays."""
+        self.lens.zero_()
+        self.pos.zero_()
+
+    def step(self, q, k, v, n_new=None, scale=None, stream=None):
+        """Put the new tokens' ``k`` / ``v`` ``[B][T][n_kv_heads][D]`` into the rows' caches and return
+        the attention of ``q`` ``[B][T][n_heads][D]`` over the prompt and the caches.  ``n_new`` int32
+        ``[B]``: tokens that a row really has (a finished row has 0); None: all ``T``."""
+        tokens = q.shape[1]
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        cstr.cstr_cache_insert(self.handle, k, v, self.pos, self.budget, self.recent, n_new=n_new,
+                               stream=stream)
+        cstr.cstr_cache_attention(self.handle, q, out, scale=scale, n_query=n_new, accumulate=True,
+                                  pos=self.pos if tokens > 1 else None, stream=stream)
+        with torch.cuda.stream(stream or torch.cuda.current_stream(self.pos.device)):
+            self.pos += tokens if n_new is None else n_new
+        return out

@@ -1,0 +1,50 @@
+"""Training on constrained answers: the policy loss as a differentiable torch function.
+
+The loss is over the constrained distribution (disallowed logits are -infinity, as
+in Algorithm 2's loop body), because that is the distribution the answers were sampled from.
+"""
+
+from __future__ import annotations
+
+import torch
+
+from . import cstr
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, actions, old_logp, advantages, ref_logp, weight, args):
+        n = logits.shape[0]
+        loss, logp = (torch.empty(n, dtype=torch.float32, device=logits.device) for _ in range(2))
+        cstr.cstr_policy_loss(args["tables"], logits, args["states"], actions, old_logp, advantages,
+                              loss, logp, ref_logp=ref_logp, weight=weight, **args["options"])
+        ctx.save_for_backward(logits, actions, old_logp, advantages, ref_logp, weight)
+        ctx.args = args
+        ctx.mark_non_differentiable(logp)
+        return loss, logp
+
+    @staticmethod
+    def backward(ctx, grad_loss, _):
+        # the gradient of row n is linear in its weight, so the upstream gradient enters there;
+        # nothing but the logits is kept in between
+        logits, actions, old_logp, advantages, ref_logp, weight = ctx.saved_tensors
+        grad = grad_loss.float()
+        grad = grad.contiguous() if weight is None else grad * weight
+        dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype,
+                                      device=logits.device)
+        loss, logp = torch.empty_like(grad), torch.empty_like(grad)
+        cstr.cstr_policy_loss(ctx.args["tables"], logits, ctx.args["states"], actions, old_logp,
+                              advantages, loss, logp, ref_logp=ref_logp, weight=grad,
+                              dlogits=dlogits, **ctx.args["options"])
+        return dlogits, None, None, None, None, None, None
+
+
+def constrained_policy_loss(logits, actions, old_logp, advantages, tables=None, states=None,
+                            ref_logp=None, weight=None, row_table=None, clip_low: float = 0.2,
+                            clip_high: float = 0.2, kl_coef: float = 0.0, temperature: float = 1.0):
+    """``(loss [N], logp [N])`` of ``cstr_policy_loss``; the loss is differentiable in ``logits``
+    (float32 or bfloat16 ``[N][V]``), the log probabilities are not."""
+    args = dict(tables=tables, states=states,
+                options=dict(row_table=row_table, clip_low=clip_low, clip_high=clip_high,
+                             kl_coef=kl_coef, temperature=temperature))
+    return _PolicyLoss.apply(logits, actions, old_logp, advantages, ref_logp, weight, args)
