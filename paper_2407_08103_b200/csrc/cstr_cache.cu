@@ -292,6 +292,8 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
     extern __shared__ __align__(16) int s_dyn[];                  // bins, keys, places
     __shared__ int s_words[(WARP ? 4 : 1) * kWords];
     __shared__ unsigned long long s_least[kMaxWarps];
+    cstr_wait_for_earlier_kernels();
+    cstr_let_next_kernel_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tid = WARP ? lane : threadIdx.x, step = WARP ? 32 : blockDim.x;
     const int item = WARP ? blockIdx.x * 4 + warp : blockIdx.x;
@@ -469,7 +471,7 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
     const unsigned items = (unsigned)(c.batch * c.n_kv_heads);
     if (a.tokens == 1 && c.cap <= 2048) {
         p.bits = 8;
-        cache_insert_kernel<true><<<(items + 3) / 4, 128, 4 * (4 << p.bits), stream>>>(p);
+        return cstr_launch(cache_insert_kernel<true>, (items + 3) / 4, 128, 1, 4 * (4 << p.bits), stream, p);
     } else {
         const bool shared = c.cap <= CSTR_INSERT_SMEM_SLOTS;
         if (shared)
@@ -480,10 +482,8 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
         const int rc = smem > 48 * 1024 ? cstr_allow_smem(cache_insert_kernel<false>, allowed, c.device, smem) : CSTR_OK;
         if (rc)
             return rc;
-        cache_insert_kernel<false><<<items, c.cap <= 4096 ? 256 : kMaxThreads, smem, stream>>>(p);
+        return cstr_launch(cache_insert_kernel<false>, items, c.cap <= 4096 ? 256 : kMaxThreads, 1, smem, stream, p);
     }
-    CSTR_CUDA_TRY(cudaGetLastError());
-    return CSTR_OK;
 }
 
 extern "C" void cstr_free_cache(cstr_cache_t *c)

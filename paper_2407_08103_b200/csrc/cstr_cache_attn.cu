@@ -375,6 +375,10 @@ row_attention_kernel(const __grid_constant__ RowParams p)
     float *s_m = s_stat, *s_l = s_stat + kWarps * ROWS;            // per warp
     float *s_cm = s_stat + 2 * kWarps * ROWS, *s_cl = s_cm + ROWS, *s_lse = s_cl + ROWS;
 
+    if (!p.part_ml) {                              // (else the prefix kernel has waited)
+        cstr_wait_for_earlier_kernels();
+        cstr_let_next_kernel_start();
+    }
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int item = blockIdx.x / p.split, part = blockIdx.x - item * p.split;
@@ -631,44 +635,53 @@ row_attention_kernel(const __grid_constant__ RowParams p)
             cluster.sync();
         else
             __syncthreads();
-        if (p.part_ml)
-            asm volatile("griddepcontrol.wait;" ::: "memory");      // the prefix kernel has finished
+        if (p.part_ml) {
+            cstr_wait_for_earlier_kernels();       // the prefix kernel has finished
+            cstr_let_next_kernel_start();
+        }
 
         // ... and the cluster's, through distributed shared memory; each CTA finishes a share
         // of the outputs and the weights of its own slots
-        for (int r = warp; r < nr; r += kWarps) {          // a warp per query row, lanes over the parts
-            const int t = p.by_g(r0 + r), g = (r0 + r) - t * p.G;
-            const PartList parts = p.part_ml && t < nq ? parts_of(p, kh, b * R + r0 + r) : PartList{0, 0, 0};
+        // eight lanes per query row, over its parts (there are about eight at most, unless few rows share
+        // a long prompt: then lane i takes parts i, i + 8, ...)
+        for (int r = tid >> 3; r < (nr + 3 & ~3); r += kWarps * 4) {   // (whole warps: shuffles below)
+            const bool on = r < nr;
+            const int sub = tid & 7, t = p.by_g(r0 + (on ? r : 0)), g = (r0 + r) - t * p.G;
+            const PartList parts = p.part_ml && on && t < nq ? parts_of(p, kh, b * R + r0 + r) : PartList{0, 0, 0};
             const float2 *ml = p.part_ml + (long long)parts.first * 128 + parts.row;
             float2 first = make_float2(-CUDART_INF_F, 0.f);
-            if (lane < parts.n)
-                first = ml[(long long)lane * 256];
+            if (sub < parts.n)
+                first = ml[(long long)sub * 256];
             float cm = -CUDART_INF_F, cl = 0.f;
-            if (lane < p.split) {
-                cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, lane) : s_cm[r];
-                cl = p.split > 1 ? *cluster.map_shared_rank(s_cl + r, lane) : s_cl[r];
+            if (on && sub < p.split) {
+                cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, sub) : s_cm[r];
+                cl = p.split > 1 ? *cluster.map_shared_rank(s_cl + r, sub) : s_cl[r];
             }
             float top = fmaxf(first.x, cm);
-            for (int i = lane + 32; i < parts.n; i += 32)
+#pragma unroll 4
+            for (int i = sub + 8; i < parts.n; i += 8)
                 top = fmaxf(top, ml[(long long)i * 256].x);
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1)
+            for (int off = 4; off > 0; off >>= 1)
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             const float ref = top == -CUDART_INF_F ? 0.f : top;
             float sum = exp2_fast(cm - ref) * cl + exp2_fast(first.x - ref) * first.y;
-            for (int i = lane + 32; i < parts.n; i += 32)
-                sum += exp2_fast(ml[(long long)i * 256].x - ref) * ml[(long long)i * 256].y;
+#pragma unroll 4
+            for (int i = sub + 8; i < parts.n; i += 8) {
+                const float2 x = ml[(long long)i * 256];
+                sum += exp2_fast(x.x - ref) * x.y;
+            }
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1)
+            for (int off = 4; off > 0; off >>= 1)
                 sum += __shfl_xor_sync(0xffffffffu, sum, off);
             // nothing seen: +infinity, so that 2^(x - lse) is 0 for every key
             const float lse = sum == 0.f ? CUDART_INF_F : ref + log2f(sum);
-            for (int i = lane; i < parts.n; i += 32) {
-                const float pm = i < 32 ? first.x : ml[(long long)i * 256].x;
+            for (int i = sub; i < parts.n; i += 8) {
+                const float pm = i < 8 ? first.x : ml[(long long)i * 256].x;
                 // -1: a part that saw no key; it has no outputs
                 s_fac[r * p.max_parts + i] = pm == -CUDART_INF_F ? -1.f : exp2_fast(pm - lse);
             }
-            if (lane == 0) {
+            if (on && sub == 0) {
                 s_lse[r] = lse;
                 s_parts[r] = parts;
                 if (part == 0 && p.lse_out)
@@ -805,26 +818,7 @@ int launch(const cstr_cache &c, RowParams p, cudaStream_t stream)
     const int rc = cstr_allow_smem(kernel, allowed, c.device, smem);
     if (rc)
         return rc;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3((unsigned)((long long)p.B * p.Hk * p.split));
-    cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = p.split;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (p.part_ml) {                     // may start beside the prefix kernel, and waits for its parts
-        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[1].val.programmaticStreamSerializationAllowed = 1;
-        cfg.numAttrs = 2;
-    }
-    CSTR_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
-    return CSTR_OK;
+    return cstr_launch(kernel, (long long)p.B * p.Hk * p.split, kWarps * 32, p.split, smem, stream, p);
 }
 
 template <typename T>
@@ -837,6 +831,8 @@ int launch_typed(const cstr_cache &c, const RowParams &p, cudaStream_t stream)
         return wide ? launch<T, 128, 1>(c, p, stream) : launch<T, 64, 1>(c, p, stream);
     if (rows <= 16)
         return wide ? launch<T, 128, 2>(c, p, stream) : launch<T, 64, 2>(c, p, stream);
+    if (rows <= 24)
+        return wide ? launch<T, 128, 3>(c, p, stream) : launch<T, 64, 3>(c, p, stream);
     return wide ? launch<T, 128, 4>(c, p, stream) : launch<T, 64, 4>(c, p, stream);
 }
 

@@ -71,6 +71,38 @@ __device__ __forceinline__ bool cstr_in_bounds(unsigned long long *rec, long lon
 #define CSTR_OOB_RECORD() ((unsigned long long *)nullptr)
 #endif
 
+// Kernels launched by cstr_launch may be set up while the previous kernel of the stream still runs:
+// they call the first function before they touch anything that an earlier kernel may write, and the
+// second to allow the same to the kernel after them.
+__device__ __forceinline__ void cstr_wait_for_earlier_kernels()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+__device__ __forceinline__ void cstr_let_next_kernel_start()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename K, typename... A>
+int cstr_launch(K kernel, long long blocks, int threads, int cluster, int smem, cudaStream_t stream, const A &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    CSTR_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return CSTR_OK;
+}
+
 // State ids inside the builder's tables are permuted within blocks of 256:
 // state 256 b + 8 l + j sits at slot 256 b + 32 j + l.  A warp whose lane l
 // owns the 8 consecutive states 8 l .. 8 l + 7 then reads 32 consecutive slots

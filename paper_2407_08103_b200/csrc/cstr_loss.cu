@@ -209,6 +209,8 @@ policy_loss_kernel(const __grid_constant__ LossParams p)
     __shared__ MaxSum s_part[kMaxCluster];       // every CTA's, written by its owner
     __shared__ float s_row[6];                   // old_logp, ref_logp, advantage, weight, action's logit, valid
     __shared__ float s_result[3];                // hot, coef, maximum
+    cstr_wait_for_earlier_kernels();
+    cstr_let_next_kernel_start();
     cg::cluster_group cluster = cg::this_cluster();
     const int size = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -373,20 +375,7 @@ int launch(void (*kernel)(LossParams), const LossParams &p, int size, cudaStream
 {
     if (size > 8)
         CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3((unsigned)((long long)p.rows * size));
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = size;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    CSTR_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
-    return CSTR_OK;
+    return cstr_launch(kernel, (long long)p.rows * size, kThreads, size, 0, stream, p);
 }
 
 }  // namespace

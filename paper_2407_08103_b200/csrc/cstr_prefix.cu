@@ -284,8 +284,6 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     __shared__ float2 s_ml[kTile];               // second stream's maximum and sum, one-tile segments
     __shared__ unsigned s_tmem;
     __shared__ int s_abort;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
     const unsigned raw = smem_addr(smem_raw);
     const unsigned q_tile = (raw + 1023u) & ~1023u;              // [2][kTile][DP], swizzled
     const unsigned ring = q_tile + 2 * S::kTileBytes;
@@ -324,6 +322,10 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     }
     __syncthreads();
     fence_after();
+    // Up to here nothing that an earlier kernel may still write has been read.  The row kernel may start
+    // from here on; it waits for this one's parts.
+    cstr_wait_for_earlier_kernels();
+    cstr_let_next_kernel_start();
     const unsigned tmem = s_tmem;
     const unsigned t_s = tmem, t_o = tmem + 2 * kTile;           // S (and P over it), O: + stream * 128
 
@@ -650,9 +652,7 @@ int launch(const cstr_cache &c, const PrefixParams &p, cudaStream_t stream)
     CUtensorMap k, v;
     memcpy(&k, c.map_k, sizeof k);
     memcpy(&v, c.map_v, sizeof v);
-    kernel<<<p.grid, kThreads, Shape<DP>::kSmem, stream>>>(k, v, p);
-    CSTR_CUDA_TRY(cudaGetLastError());
-    return CSTR_OK;
+    return cstr_launch(kernel, p.grid, kThreads, 1, Shape<DP>::kSmem, stream, k, v, p);
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -668,10 +668,14 @@ cstr_prefix_plan cstr_plan_prefix(const cstr_cache &c, int tokens)
     s.pairs = (int)((rows + 2 * kTile - 1) / (2 * kTile));
     s.tiles = (int)((c.prefix_len + kTile - 1) / kTile);
     const long long units = (long long)c.n_kv_heads * s.pairs * s.tiles;
-    // With two tiles of query rows a segment leaves 128 KB of parts, as much as two key tiles read:
-    // a CTA gets two units at least.
-    const long long most = rows > kTile ? (units + 1) / 2 : units;
-    s.grid = (int)(most < c.sm_count ? most : c.sm_count);
+    // Every CTA leaves a part of up to 128 KB per row group that it works for, as much as two key tiles
+    // read, and the row kernel has to join them.  So with two tiles of query rows a CTA gets two units
+    // (but a row group a CTA at least), and a row group at most 40 CTAs.
+    const long long items = (long long)c.n_kv_heads * s.pairs;
+    long long grid = rows > kTile ? (units + 1) / 2 : units;
+    grid = grid < items ? items : grid;
+    grid = grid > 40 * items ? 40 * items : grid;
+    s.grid = (int)(grid < c.sm_count ? grid : c.sm_count);
     return s;
 }
 
