@@ -14,7 +14,8 @@
 // While the 128 threads of one stream turn its S into probabilities P, the
 // tensor cores work for the other stream.  One thread issues all products,
 // S = Q K^T (both operands from shared memory) and O += P V (P from tensor
-// memory, over its own S), one thread issues the copies into a ring of tiles.
+// memory, over its own S), one thread issues the copies into a ring of tiles, and
+// two warps bring the next row group's queries while the last one is finished.
 //
 // Split: the units (key tile x group of 256 query rows) are dealt out evenly and
 // contiguously to one CTA per SM, so a CTA starts or ends within a row group and
@@ -31,7 +32,7 @@
 
 namespace {
 
-constexpr int kThreads = 384;        // warps 0-3: copies, products, tensor memory, -; 4-7, 8-11: streams
+constexpr int kThreads = 384;        // warps 0-3: copies, products, query tiles (two); 4-7, 8-11: streams
 constexpr int kTile = 128;           // query rows and keys of a tile
 // A maximum that grew by less than 2^8 keeps the old reference: P stays below 2^8, in range of
 // both 16-bit types, and the rescaling of O (a round trip through registers) is left out.
@@ -280,7 +281,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     using S = Shape<DP>;
     constexpr int kSlots = S::kSlots;
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) unsigned long long s_bar[2 * kSlots + 11];
+    __shared__ __align__(8) unsigned long long s_bar[2 * kSlots + 12];
     __shared__ float2 s_ml[kTile];               // second stream's maximum and sum, one-tile segments
     __shared__ unsigned s_tmem;
     __shared__ int s_abort;
@@ -290,7 +291,8 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const unsigned bars = smem_addr(s_bar);
     auto full = [&](int slot) { return bars + 8u * slot; };
     auto empty = [&](int slot) { return bars + 8u * (kSlots + slot); };
-    const unsigned q_full = bars + 8u * (2 * kSlots), drain = q_full + 56, q_free = q_full + 64, ml_full = q_full + 72, ml_free = q_full + 80;
+    const unsigned q_full = bars + 8u * (2 * kSlots), drain = q_full + 56, q_free = q_full + 64, ml_full = q_full + 72, ml_free = q_full + 80,
+                   q_first = q_full + 88;
     auto s_full = [&](int s) { return q_full + 8u * (1 + s); };
     auto p_full = [&](int s) { return q_full + 8u * (3 + s); };
     auto o_full = [&](int s) { return q_full + 8u * (5 + s); };
@@ -303,14 +305,15 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             bar_init(full(i), 1);
             bar_init(empty(i), 1);
         }
-        bar_init(q_full, 256);
+        bar_init(q_full, 64);
+        bar_init(q_first, 320);
         for (int s = 0; s < 2; ++s) {
             bar_init(s_full(s), 1);
             bar_init(p_full(s), 4);
             bar_init(o_full(s), 1);
         }
         bar_init(drain, 1);
-        bar_init(q_free, 8);
+        bar_init(q_free, 1);
         bar_init(ml_full, 4);
         bar_init(ml_free, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -328,6 +331,25 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     cstr_let_next_kernel_start();
     const unsigned tmem = s_tmem;
     const unsigned t_s = tmem, t_o = tmem + 2 * kTile;           // S (and P over it), O: + stream * 128
+
+    // a segment's query rows into the swizzled tiles; thread `index` of `threads`
+    auto load_queries = [&](const Segment &g, int index, int threads) {
+        const int head = g.item / p.pairs, row0 = (g.item % p.pairs) * 2 * kTile;
+        const int q_rows = g.pair_rows ? 2 * kTile : kTile;
+        const int ch = index % (DP / 8);
+#pragma unroll 4
+        for (int r = index / (DP / 8); r < q_rows; r += threads / (DP / 8)) {
+            const bool ok = r < g.rows && ch * 8 < p.D;          // else zeroes
+            const int m = ok ? row0 + r : 0, b = p.by_r(m), in = m - b * p.R, t = p.by_g(in), gh = in - t * p.G;
+            const uint4 *from = reinterpret_cast<const uint4 *>(p.q) + ((long long)b * p.q_sb + (long long)t * p.q_st +
+                                (long long)(head * p.G + gh) * p.q_sh + (ok ? ch : 0));
+            const unsigned to = q_tile + (r / kTile) * S::kTileBytes + (ch / 8) * (kTile * 128) + (r % kTile) * 128 +
+                                (((ch ^ r) & 7) << 4);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(ok ? 16 : 0) : "memory");
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    };
 
     Walk walk(p);
     Segment g;
@@ -379,7 +401,10 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             const int lead = min(g.pair_rows ? 1 : 2, g.tiles);
             const int visits = g.pair_rows ? 2 * g.tiles : g.tiles;
             const int shift = g.pair_rows ? 1 : 0;
-            wait(q_full, seg & 1u);
+            if (seg == 0)
+                wait(q_first, 0);
+            else
+                wait(q_full, (seg - 1) & 1u);
             ++seg;
             auto scores = [&](int n) {
                 const unsigned at = base + place_k(n >> shift, lead);
@@ -399,6 +424,8 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                 commit(leader, s_full(s));
                 if (!g.pair_rows || s == 1)
                     commit(leader, empty(slot));
+                if (n == visits - 1)
+                    commit(leader, q_free);
             };
             scores(0);
             if (visits > 1)
@@ -431,38 +458,30 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             for (unsigned k = 0; k < kWaitLimit && !bar_try(drain, 0); ++k) {}
         }
         __syncwarp();
-    } else if (warp >= 4) {
+    } else if (warp < 4) {                                       // query tiles, by two warps
+        unsigned seg = 0;
+        bool alive = true;
+        for (; alive && walk.next(g); ++seg) {
+            // the previous segment's last scores have been computed: its tiles may be replaced
+            if (seg > 0 && !(alive = __all_sync(0xffffffffu, bar_wait(q_free, (seg - 1) & 1u, abort))))
+                break;
+            // (the first segment's with the streams' help)
+            load_queries(g, tid - 64, seg == 0 ? 320 : 64);
+            bar_arrive(seg == 0 ? q_first : q_full);
+        }
+        __syncwarp();
+    } else {
         const int s = (warp - 4) >> 2, row = ((warp & 3) << 5) + lane;    // stream; row of its tile = TMEM lane
         const unsigned lane_base = (unsigned)((warp & 3) << 5) << 16;
         const unsigned my_s = t_s + s * kTile + lane_base, my_o = t_o + s * kTile + lane_base;
-        unsigned seg = 0, done = 0, joined = 0;                  // segments, visits of this stream, joins so far
-        bool alive = true;
+        unsigned done = 0, joined = 0;                           // visits of this stream, joins so far
+        bool alive = true, started = false;
         while (alive && walk.next(g)) {
-            // both streams have seen their last scores: the query tiles may be replaced
-            __syncwarp();
-            if (lane == 0)
-                bar_arrive(q_free);
-            if (!(alive = __all_sync(0xffffffffu, bar_wait(q_free, seg & 1u, abort))))
-                break;
-            ++seg;
-            const int head = g.item / p.pairs, row0 = (g.item % p.pairs) * 2 * kTile;
-            const int q_rows = g.pair_rows ? 2 * kTile : kTile;
-            constexpr int kPer = 256 / (DP / 8);                 // rows per pass of the 256 threads
-            const int ch = (tid - 128) % (DP / 8);
-#pragma unroll 2
-            for (int r = (tid - 128) / (DP / 8); r < q_rows; r += kPer) {
-                const bool ok = r < g.rows && ch * 8 < p.D;      // else zeroes
-                const int m = ok ? row0 + r : 0, b = p.by_r(m), in = m - b * p.R, t = p.by_g(in), gh = in - t * p.G;
-                const uint4 *from = reinterpret_cast<const uint4 *>(p.q) + ((long long)b * p.q_sb + (long long)t * p.q_st +
-                                    (long long)(head * p.G + gh) * p.q_sh + (ok ? ch : 0));
-                const unsigned to = q_tile + (r / kTile) * S::kTileBytes + (ch / 8) * (kTile * 128) + (r % kTile) * 128 +
-                                    (((ch ^ r) & 7) << 4);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(ok ? 16 : 0) : "memory");
+            if (!started) {
+                load_queries(g, tid - 64, 320);
+                bar_arrive(q_first);
+                started = true;
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            bar_arrive(q_full);
-
             const int my_row = g.pair_rows ? s * kTile + row : row;      // row of the group
             const bool warp_on = my_row - lane < g.rows;
             const int visits = g.pair_rows ? 2 * g.tiles : g.tiles;
