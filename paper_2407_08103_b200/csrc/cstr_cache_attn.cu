@@ -697,44 +697,70 @@ row_attention_kernel(const __grid_constant__ RowParams p)
         int team = 1;
         while (team < 32 && 2 * team * pieces <= p.split * kWarps * 32 && team < p.max_parts)
             team *= 2;
-        const int sub = tid & (team - 1);
-        for (int i0 = part * (kWarps * 32 / team); i0 < pieces; i0 += p.split * (kWarps * 32 / team)) {
-            const int i = min(i0 + tid / team, pieces - 1);       // (all lanes of a warp stay for the sums)
-            const int d4 = i / nr, r = i - d4 * nr;
-            const int t = p.by_g(r0 + r), g = (r0 + r) - t * p.G;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            const PartList parts = s_parts[r];
-            const float *fac = s_fac + r * p.max_parts;
-            const float4 *po = p.part_o + ((long long)parts.first * (DP / 4) + d4) * 128 + parts.row;
+        const int sub = tid & (team - 1), at_once = kWarps * 32 / team;
+        // two pieces at a time with four parts of each in flight, or the last one with eight (a lane
+        // without a piece works on the last one, for the warp's sums)
+        for (int i0 = part * at_once; i0 < pieces; i0 += 2 * p.split * at_once) {
+            const bool two = i0 + p.split * at_once < pieces;
+            const int skip = two ? 0 : 4 * team, step = two ? 4 * team : 8 * team;
+            int r[2], d4[2], n = 0;
+            const float4 *po[2];
+            float4 v[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = min(i0 + (two ? h * p.split * at_once : 0) + tid / team, pieces - 1);
+                d4[h] = i / nr;
+                r[h] = i - d4[h] * nr;
+                const PartList parts = s_parts[r[h]];
+                po[h] = p.part_o + ((long long)parts.first * (DP / 4) + d4[h]) * 128 + parts.row;
+                v[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+                n = max(n, parts.n);
+            }
 #pragma unroll 1
-            for (int k0 = sub; k0 < parts.n; k0 += 8 * team) {     // eight loads in flight
-                float4 u[8];
+            for (int k0 = sub; k0 < n; k0 += step) {
+                float4 u[2][4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k0 + k * team < parts.n)
-                        u[k] = po[(long long)(k0 + k * team) * (DP / 4) * 256];
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k0 + k * team < parts.n && !(fac[k0 + k * team] < 0.f))
-                        axpy(v, fac[k0 + k * team], u[k]);
+                    for (int k = 0; k < 4; ++k)
+                        if (k0 + h * skip + k * team < s_parts[r[h]].n)
+                            u[h][k] = po[h][(long long)(k0 + h * skip + k * team) * (DP / 4) * 256];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k0 + h * skip + k * team < s_parts[r[h]].n) {
+                            const float f = s_fac[r[h] * p.max_parts + k0 + h * skip + k * team];
+                            if (!(f < 0.f))
+                                axpy(v[h], f, u[h][k]);
+                        }
             }
-            for (int c = sub; c < p.split; c += team) {
-                const float *so = p.split > 1 ? cluster.map_shared_rank(s_o, c) : s_o;
-                const float cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r, c) : s_cm[r];
-                if (cm != -CUDART_INF_F)
-                    axpy(v, exp2_fast(cm - s_lse[r]), *reinterpret_cast<const float4 *>(so + r * Shape::kPitch + 4 * d4));
+            if (!two)
+                axpy(v[0], 1.f, v[1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h == 1 && !two)
+                    break;
+                for (int c = sub; c < p.split; c += team) {
+                    const float *so = p.split > 1 ? cluster.map_shared_rank(s_o, c) : s_o;
+                    const float cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r[h], c) : s_cm[r[h]];
+                    if (cm != -CUDART_INF_F)
+                        axpy(v[h], exp2_fast(cm - s_lse[r[h]]),
+                             *reinterpret_cast<const float4 *>(so + r[h] * Shape::kPitch + 4 * d4[h]));
+                }
+                for (int off = 1; off < team; off <<= 1) {
+                    v[h].x += __shfl_xor_sync(0xffffffffu, v[h].x, off);
+                    v[h].y += __shfl_xor_sync(0xffffffffu, v[h].y, off);
+                    v[h].z += __shfl_xor_sync(0xffffffffu, v[h].z, off);
+                    v[h].w += __shfl_xor_sync(0xffffffffu, v[h].w, off);
+                }
+                if (sub != 0 || i0 + h * p.split * at_once + tid / team >= pieces)
+                    continue;
+                const int t = p.by_g(r0 + r[h]), g = (r0 + r[h]) - t * p.G;
+                char *dst = (char *)p.out + ((long long)b * p.o_sb + (long long)t * p.o_st +
+                                             (long long)(kh * p.G + g) * p.o_sh + 4 * d4[h]) * 2;
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(Half2<T>::pack(v[h].x, v[h].y), Half2<T>::pack(v[h].z, v[h].w));
             }
-            for (int off = 1; off < team; off <<= 1) {
-                v.x += __shfl_xor_sync(0xffffffffu, v.x, off);
-                v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
-                v.z += __shfl_xor_sync(0xffffffffu, v.z, off);
-                v.w += __shfl_xor_sync(0xffffffffu, v.w, off);
-            }
-            if (sub != 0 || i0 + tid / team >= pieces)
-                continue;
-            char *dst = (char *)p.out + ((long long)b * p.o_sb + (long long)t * p.o_st +
-                                         (long long)(kh * p.G + g) * p.o_sh + 4 * d4) * 2;
-            *reinterpret_cast<uint2 *>(dst) = make_uint2(Half2<T>::pack(v.x, v.y), Half2<T>::pack(v.z, v.w));
         }
         // the next rows reuse the memory that peers read, and a CTA must not leave while they do.
         // (Every CTA of the cluster takes the same number of cluster barriers: what follows has none.)
@@ -745,14 +771,24 @@ row_attention_kernel(const __grid_constant__ RowParams p)
         if (p.accumulate) {
             float *wrow = p.weight + ((long long)b * p.Hk + kh) * p.cap;
             if (keep) {
-                for (int j = tid; j < s1 - s0; j += kWarps * 32) {
-                    float w = 0.f;
-                    for (int r = 0; r < nr; ++r)
-                        if (p.by_g(r0 + r) < nq)
-                            w += exp2_fast(s_score[r * p.score_cap + (s0 - src.x0 - kept0) + j] - s_lse[r]);
-                    const long long at = s0 - p.P + j;
-                    if (CSTR_INB(p.oob, at, p.cap, CSTR_SITE_CACHE))
-                        add_once(wrow + at, w);
+                const float *score = s_score + (s0 - src.x0 - kept0);
+                const int real = min(nr, nq * p.G - r0);           // rows of tokens below n_query
+                for (int j0 = tid; j0 < s1 - s0; j0 += 4 * kWarps * 32) {      // four slots at a time
+                    float w[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+                    for (int r = 0; r < real; ++r) {
+                        const float lse = s_lse[r];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if (j0 + u * kWarps * 32 < s1 - s0)
+                                w[u] += exp2_fast(score[r * p.score_cap + j0 + u * kWarps * 32] - lse);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const long long at = s0 - p.P + j0 + u * kWarps * 32;
+                        if (j0 + u * kWarps * 32 < s1 - s0 && real > 0 && CSTR_INB(p.oob, at, p.cap, CSTR_SITE_CACHE))
+                            add_once(wrow + at, w[u]);
+                    }
                 }
             } else {                                // scores once more from the keys
                 float lse[NT][2];
