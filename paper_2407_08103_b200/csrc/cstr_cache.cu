@@ -671,7 +671,13 @@ extern "C" int cstr_cache_attention(cstr_cache_t *c, const void *q, const int64_
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.accumulate = accumulate ? 1 : 0;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    const bool tensor = c->has_maps && c->prefix_len >= 128;
+    // On the tensor cores the prompt costs a launch and the join of its parts, about 10 us; in the row kernel
+    // every row reads it by itself, from the L2 cache mostly, and few rows in a long serial chain each.
+    // So: from 512 tokens on, or where the rows read 16 MiB of it together.  Measured, tensor / row, 8 key /
+    // value heads: 4 x 128 tokens 10.5 / 9.4 us, 8 x 256 tokens 11.2 / 10.8, 16 x 256 (16 MiB) 11.8 / 11.9,
+    // 64 x 256 16.3 / 21.5, 4 x 512 11.1 / 12.0, 1 x 1,024 11.8 / 13.1, 64 x 4,096 34 / 217.
+    const bool tensor = c->has_maps && c->prefix_len >= 128 &&
+                        (c->prefix_len >= 512 || (long long)c->batch * c->n_kv_heads * c->prefix_len * c->head_dim * 4 >= 16 << 20);
     if (tensor) {
         rc = cstr_launch_prefix(*c, a, stream);
         if (rc)

@@ -29,7 +29,6 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kSlots = 3;        // units (keys or values of a chunk) in a warp's ring
 constexpr int kChunk = 16;       // keys per step of a warp
 constexpr float kLazy = 8.f;
 constexpr float kLn2 = 0.693147180559945309f;
@@ -190,7 +189,12 @@ template <int DP> __device__ __forceinline__ unsigned tile_off(int r, int ch)
     return (unsigned)(r * DP * 2 + ((ch ^ (r & 7)) << 4));
 }
 
-template <int DP> struct RowShape {
+// kSlots: units (keys or values of a chunk) in a warp's ring.  Two for few query rows of wide heads (512
+// rows of 1,024 slots, head_dim 128: 369 us, with three 376 us, with four 470 us, three CTAs per SM then);
+// three where a unit is half as large (head_dim 64: 265 us, with two 275 us) or is worked on for longer
+// (64 rows x 20 query rows: 88.7 us, with two 90.5 us).
+template <int DP, int NT> struct RowShape {
+    static constexpr int kSlots = DP == 128 && NT == 1 ? 2 : 3;
     static constexpr int kUnit = kChunk * DP * 2 + kChunk * 4;   // keys (or values) of a chunk, ages
     static constexpr int kRing = kWarps * kSlots * kUnit;
     static constexpr int kPitch = DP + 4;                        // floats per row of the partial outputs
@@ -361,7 +365,8 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 4 : 2)
 row_attention_kernel(const __grid_constant__ RowParams p)
 {
     constexpr int ROWS = 8 * NT;
-    using Shape = RowShape<DP>;
+    using Shape = RowShape<DP, NT>;
+    constexpr int kSlots = Shape::kSlots;
     extern __shared__ __align__(128) char smem[];
     char *s_q = smem;                                              // [ROWS][DP] of T
     float *s_stat = reinterpret_cast<float *>(s_q + ROWS * DP * 2); // [2 kWarps + 3][ROWS]
@@ -603,8 +608,9 @@ row_attention_kernel(const __grid_constant__ RowParams p)
             float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                // -1: the warp saw no key of this row; whatever its sums hold does not count
-                const bool none = s_m[w * ROWS + r] == -CUDART_INF_F;
+                // -1: the warp saw no key of this row; whatever its sums hold does not count.  (Scores that
+                // are all NaN leave no maximum either, but a sum of NaN.)
+                const bool none = s_m[w * ROWS + r] == -CUDART_INF_F && s_l[w * ROWS + r] == 0.f;
                 const float f = exp2_fast(s_m[w * ROWS + r] - ref);
                 sum += f * s_l[w * ROWS + r];
                 s_m[w * ROWS + r] = none ? -1.f : f;
@@ -674,12 +680,12 @@ row_attention_kernel(const __grid_constant__ RowParams p)
 #pragma unroll
             for (int off = 4; off > 0; off >>= 1)
                 sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            // nothing seen: +infinity, so that 2^(x - lse) is 0 for every key
+            // nothing seen: +infinity, so that 2^(x - lse) is 0 for every key; NaN makes all outputs NaN
             const float lse = sum == 0.f ? CUDART_INF_F : ref + log2f(sum);
             for (int i = sub; i < parts.n; i += 8) {
                 const float pm = i < 8 ? first.x : ml[(long long)i * 256].x;
                 // -1: a part that saw no key; it has no outputs
-                s_fac[r * p.max_parts + i] = pm == -CUDART_INF_F ? -1.f : exp2_fast(pm - lse);
+                s_fac[r * p.max_parts + i] = pm == -CUDART_INF_F && lse == lse ? -1.f : exp2_fast(pm - lse);
             }
             if (on && sub == 0) {
                 s_lse[r] = lse;
@@ -744,7 +750,7 @@ row_attention_kernel(const __grid_constant__ RowParams p)
                 for (int c = sub; c < p.split; c += team) {
                     const float *so = p.split > 1 ? cluster.map_shared_rank(s_o, c) : s_o;
                     const float cm = p.split > 1 ? *cluster.map_shared_rank(s_cm + r[h], c) : s_cm[r[h]];
-                    if (cm != -CUDART_INF_F)
+                    if (cm != -CUDART_INF_F || s_lse[r[h]] != s_lse[r[h]])
                         axpy(v[h], exp2_fast(cm - s_lse[r[h]]),
                              *reinterpret_cast<const float4 *>(so + r[h] * Shape::kPitch + 4 * d4[h]));
                 }
@@ -831,7 +837,7 @@ row_attention_kernel(const __grid_constant__ RowParams p)
 template <typename T, int DP, int NT>
 int launch(const cstr_cache &c, RowParams p, cudaStream_t stream)
 {
-    using Shape = RowShape<DP>;
+    using Shape = RowShape<DP, NT>;
     constexpr int ROWS = 8 * NT;
     constexpr int out = kWarps * ROWS * Shape::kPitch * 4;
     const int fixed = ROWS * DP * 2 + (2 * kWarps + 3) * ROWS * 4 + (Shape::kRing > out ? Shape::kRing : out);

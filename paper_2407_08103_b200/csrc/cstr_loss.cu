@@ -407,6 +407,9 @@ extern "C" int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tab
     if (!logits || !actions || !old_logp || !advantages || !loss_out || !logp_out ||
         (n_tables > 0 && (!tables || !states)))
         return cstr_fail(CSTR_ERR_NULL, "cstr_policy_loss: null pointer");
+    const uintptr_t element = dtype == CSTR_BF16 ? 2 : 4;
+    if ((uintptr_t)logits % element || (uintptr_t)dlogits % element)
+        return cstr_fail(CSTR_ERR_SHAPE, "cstr_policy_loss: logits and dlogits must start on whole elements");
     int device = -1;
     CSTR_CUDA_TRY(cudaGetDevice(&device));
     LossParams p;
@@ -453,8 +456,7 @@ extern "C" int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tab
         return cstr_fail(CSTR_ERR_SHAPE, "cstr_policy_loss: rows x vocabulary too large for one launch");
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     // rows of both buffers begin at the same place of their 16 bytes
-    const bool together = (!dlogits || (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15u) == 0) &&
-                          (uintptr_t)logits % (bf16 ? 2 : 4) == 0;
+    const bool together = !dlogits || (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15u) == 0;
     // 64 KB of a row per CTA; smaller shares, down to 2,048 tokens, while there are fewer CTAs than
     // two per SM
     static std::atomic<int> known[64];

@@ -53,7 +53,7 @@ struct PrefixParams {
     int *status;
     int M, T, G, R, D, P, Hk;        // R = T G query rows of one batch row
     int tiles, pairs, grid;
-    float scale_log2;                // >= 0: for a negative scale the first product negates the queries
+    float scale_log2;                // > 0: for a negative scale the first product negates the queries
     unsigned negate;                 // bit of the instruction descriptor
     cstr_divisor by_r, by_g;
 };
@@ -755,7 +755,9 @@ int cstr_launch_prefix(const cstr_cache &c, const cstr_row_args &a, cudaStream_t
     p.pairs = s.pairs;
     p.grid = s.grid;
     p.negate = a.scale_log2 < 0.f ? 1u << 13 : 0u;
-    p.scale_log2 = fabsf(a.scale_log2);
+    // A scale of 0 would turn the -infinity of keys past the prompt's end into NaN.  2^-126 in its place
+    // leaves every weight at 1 to 2^-26 for scores below 2^100.
+    p.scale_log2 = fmaxf(fabsf(a.scale_log2), 0x1p-126f);
     const bool wide = c.head_dim > 64;
     if (c.dtype == CSTR_BF16)
         return wide ? launch<__nv_bfloat16, 128>(c, p, stream) : launch<__nv_bfloat16, 64>(c, p, stream);

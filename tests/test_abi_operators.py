@@ -53,6 +53,7 @@ def test_null_range_and_type_errors(lib):
         assert loss(**kw) == -2, kw
     assert loss(logits=None) == -1 and loss(act=None) == -1
     assert loss(n_tables=1) == -1 and loss(n_tables=1, states=p) == -1
+    assert loss(logits=ctypes.c_void_p(p.value + 2)) == -6 and loss(logits=ctypes.c_void_p(p.value + 1), dtype=1) == -6
 
 
 def test_binding_refuses_before_the_library(monkeypatch):

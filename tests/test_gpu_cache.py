@@ -81,6 +81,22 @@ def test_attention_nonfinite_values_reach_only_the_tokens_that_see_them(value, d
     assert torch.isfinite(c.out[:, :3]).all() and torch.isfinite(c.lse[:, :3]).all()
 
 
+@pytest.mark.parametrize("B,P,cap", [(1, 0, 900), (2, 100, 40), (3, 700, 50), (40, 700, 5)])
+def test_attention_of_a_query_that_is_not_a_number(B, P, cap):
+    # its own row is NaN and no other
+    c = AttentionCase(18, B, 2, 4, 2, 64, P, cap, BF, causal=True)
+    c.w0 = None
+    c.dev()
+    c.run()
+    want, lse = c.out.clone(), c.lse.clone()
+    c.q[0, 1, 2] = math.nan
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.isnan(c.out[0, 1, 2]).all() and torch.isnan(c.lse[0, 1, 2])
+    c.out[0, 1, 2], c.lse[0, 1, 2] = want[0, 1, 2], lse[0, 1, 2]
+    assert torch.equal(c.out, want) and torch.equal(c.lse, lse)
+
+
 def test_attention_large_scores_and_lowest_values():
     c = AttentionCase(11, 2, 1, 4, 2, 64, 50, 60, BF, lens=[60, 7], sigma=20.0)
     c.ck[0, 3] = torch.finfo(BF).min                       # scores overflow to an infinity of either sign
