@@ -10,7 +10,10 @@
  *          mask[q] bit v = (next[q][v] != -1)
  *      for every DFA state q and vocabulary token v;
  *   2. the per-step recipe: mask from the current state, penalise the logits
- *      with -infinity, select a token, advance the state - for a whole batch.
+ *      with -infinity, select a token, advance the state - for a whole batch;
+ *   3. what a batch of constrained rows needs of the model around that step:
+ *      attention over a prompt that all rows share and each row's own cache, the
+ *      cache's upkeep, and the policy loss over the constrained distribution.
  *
  * Conventions
  *   - Every function returns 0 (CSTR_OK) or a negative CSTR_ERR_* code and
@@ -632,8 +635,10 @@ int cstr_cache_status(cstr_cache_t *cache, void *cuda_stream, int64_t *gave_up);
  *   dlogits     DEVICE [rows][ld] of dtype or NULL (no gradient); may be the same buffer
  *               as logits; columns >= vocab_size are not written
  * A row whose state is -1 or out of range, whose table index or action is out of
- * range, or whose action is not allowed or has a logit of -infinity, gets loss 0, logp -infinity, gradient 0; a row of weight 0 gets loss 0 and gradient 0
- * whatever its logits hold.  Other rows propagate NaN.
+ * range, or whose action is not allowed or has a logit of -infinity, gets loss 0,
+ * logp -infinity, gradient 0; a row of weight 0 gets loss 0 and gradient 0
+ * whatever its logits hold.  Other rows propagate NaN.  logits and dlogits start on
+ * whole elements (else CSTR_ERR_SHAPE).
  * Only enqueues one kernel on cuda_stream; no allocation, no host synchronisation.
  */
 int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,

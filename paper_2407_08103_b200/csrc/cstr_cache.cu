@@ -24,10 +24,15 @@ namespace {
 // works on it:
 //   single tokens, up to 2,048 slots: a warp per item.  It evicts one entry (a
 //     decoding step with a full cache): the smallest (key, slot) pair, found
-//     while the row is read, without a barrier;
+//     while the row is read, without a barrier.  512 rows x 8 heads of 1,024 slots
+//     10.8 us (33.7 MB, 3.1 TB/s; a CTA per item 30.2 us), of 2,048 17.2 us (33.6);
+//     past that the CTA wins: 128 x 8 of 4,096 13.2 us, a warp 18.3 us;
 //   else a CTA per item, 256 threads up to 4,096 slots (so that several items share
-//     an SM), 1,024 beyond; keys in shared memory (or scratch, past 24,576), the
-//     e-th smallest from counts per 11-bit digit.
+//     an SM), 1,024 beyond: 64 rows x 8 heads of 2,304 slots, 256 tokens 31.7 us (75 MB,
+//     2.4 TB/s; with 1,024 threads 43.4 us), of 8,192 slots 62.6 us (with 256 65.6 us),
+//     4 x 8 of 20,000 8.6 us (10.4).  Keys in shared memory (or scratch, past 24,576:
+//     at 8,192 slots 69.5 us, at 2,304 32.6 us), the e-th smallest from counts per
+//     11-bit digit.
 constexpr int kMaxThreads = 1024;
 constexpr int kMaxWarps = kMaxThreads / 32;
 

@@ -16,6 +16,11 @@
 // instruction, and its 8 columns are query rows, so that the usual 4 or 8 query
 // rows of a key / value head waste nothing (the other way round they would fill
 // a quarter or a half of 16).
+//
+// Measured: 512 rows x 8 heads of up to 1,024 slots, head_dim 128, bf16, weights added
+// up, behind 128 prompt tokens: 256 us for 1.64 GB, 6.4 TB/s; behind 16,384 tokens it
+// joins the prefix kernel's parts as well (380 us together, of them 141 the prefix
+// kernel's).  Few rows: bound by one CTA's chain of chunks, hence the split.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -190,7 +195,7 @@ template <int DP> __device__ __forceinline__ unsigned tile_off(int r, int ch)
 }
 
 // kSlots: units (keys or values of a chunk) in a warp's ring.  Two for few query rows of wide heads (512
-// rows of 1,024 slots, head_dim 128: 369 us, with three 376 us, with four 470 us, three CTAs per SM then);
+// rows of 1,024 slots, head_dim 128: 380 us, with three 385 us, with four 486 us);
 // three where a unit is half as large (head_dim 64: 265 us, with two 275 us) or is worked on for longer
 // (64 rows x 20 query rows: 88.7 us, with two 90.5 us).
 template <int DP, int NT> struct RowShape {
@@ -844,6 +849,8 @@ int launch(const cstr_cache &c, RowParams p, cudaStream_t stream)
     const int rows = p.G * p.T < ROWS ? p.G * p.T : ROWS;
     int smem = fixed + rows * p.max_parts * 4;
     p.score_cap = 0;
+    // the scores stay in shared memory for the weights, if they fit (512 rows 380 us, 505 us where they are
+    // computed from the keys again; 64 rows 33.5 / 36.9 us)
     if (p.accumulate) {
         // own slots, at most: a CTA's share of the list may be slots alone.  Whole chunks; behind
         // prefix keys the slots may begin within a chunk.
@@ -868,7 +875,9 @@ int launch_typed(const cstr_cache &c, const RowParams &p, cudaStream_t stream)
 {
     const bool wide = c.head_dim > 64;
     const int rows = p.G * p.T;
-    // as few passes over the keys as there are blocks of 32 query rows, and no wider than needed
+    // as few passes over the keys as there are blocks of 32 query rows, and no wider than needed: the
+    // widest for all costs registers and shared memory (64 rows of 4 query rows 47.0 us, 33.5 us so;
+    // 512 rows 558 / 380 us; 64 rows of 20 query rows 96.9 / 88.9 us)
     if (rows <= 8)
         return wide ? launch<T, 128, 1>(c, p, stream) : launch<T, 64, 1>(c, p, stream);
     if (rows <= 16)
@@ -923,7 +932,8 @@ int cstr_launch_row_attention(const cstr_cache &c, const cstr_row_args &a, bool 
     p.accumulate = a.accumulate;
     p.oob = CSTR_OOB_RECORD();
     // share a row's keys among CTAs while all of them still run at once (four per SM) and each has
-    // 64 keys
+    // 64 keys (6 rows x 4 heads of 512 slots behind 65,000 tokens: 39.2 us, unshared 48.8 us, by four
+    // at most 41.3 us; the batches of 64 and 512 rows are not shared)
     const long long items = (long long)p.B * p.Hk;
     p.split = 1;
     while (p.split < 8 && items * p.split * 2 <= 4LL * c.sm_count &&

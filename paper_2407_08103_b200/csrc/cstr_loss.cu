@@ -11,7 +11,8 @@
 // Bound: the row is read from memory once and the gradient written once; the
 // second pass finds the row in the L2 cache.  For that the rows in flight have to
 // fit there: a cluster of up to 16 CTAs shares a row, 64 KB each (512 x 256,000
-// fp32: 243 us, 1.04 GB of DRAM traffic; with 8 CTAs of 128 KB 270 us).  All 2,048
+// fp32: 242 us, 1.05 GB of DRAM traffic, 4.4 TB/s; with 8 CTAs of 128 KB 270 us; 2,048 x
+// 32,000 bf16 69 us, 3.9 TB/s, where 23 instructions an element weigh as much).  All 2,048
 // threads of an SM are used, at 32 registers, since what is left is the latency
 // of the passes and of the join between them.  Measured and dropped: the row held
 // in registers between the passes (344 us), and persistent CTAs with a ring of
@@ -197,8 +198,8 @@ __device__ __forceinline__ bool row_mask(const LossParams &p, int row, int a, co
 // The 16-byte vectors begin at the row's first aligned token; the tokens before and after them ("edge",
 // at most 2 (N - 1)) belong to the first threads of the first CTA.  WIDE is false where the rows of the
 // two buffers do not share their alignment: then every token is an edge token, dealt out over all threads.
-// kUnroll: vectors of a thread in flight; 2 where the logits are only read (300 x 128,256 fp32 38.5 us,
-// with one 44.0 us), 1 with a gradient (2,048 x 32,000 bf16 71 us, with two 77 us: registers).
+// kUnroll: vectors of a thread in flight; 2 where the logits are only read (300 x 128,256 fp32 36.7 us,
+// 4.2 TB/s; with one about 5 us more), 1 with a gradient (2,048 x 32,000 bf16, two: 6 us more, registers).
 template <bool BF16, bool WIDE, int kUnroll>
 __global__ void __launch_bounds__(kThreads, 8)
 policy_loss_kernel(const __grid_constant__ LossParams p)
@@ -458,7 +459,7 @@ extern "C" int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tab
     // rows of both buffers begin at the same place of their 16 bytes
     const bool together = !dlogits || (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15u) == 0;
     // 64 KB of a row per CTA; smaller shares, down to 2,048 tokens, while there are fewer CTAs than
-    // two per SM
+    // two per SM (4 x 32,000 fp32 6.5 us, unshared 13.5 us; 16 x 128,256 11.9 / 18.8 us)
     static std::atomic<int> known[64];
     int sms = device >= 0 && device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
     if (sms == 0) {
