@@ -133,11 +133,11 @@ class SharedPromptCache:
         the attention of ``q`` ``[B][T][n_heads][D]`` over the prompt and the caches.  ``n_new`` int32
         ``[B]``: tokens that a row really has (a finished row has 0); None: all ``T``."""
         tokens = q.shape[1]
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        cstr.cstr_cache_insert(self.handle, k, v, self.pos, self.budget, self.recent, n_new=n_new,
-                               stream=stream)
-        cstr.cstr_cache_attention(self.handle, q, out, scale=scale, n_query=n_new, accumulate=True,
-                                  pos=self.pos if tokens > 1 else None, stream=stream)
-        with torch.cuda.stream(stream or torch.cuda.current_stream(self.pos.device)):
+        with torch.cuda.stream(stream or torch.cuda.current_stream(self.pos.device)):   # (its memory, too)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            cstr.cstr_cache_insert(self.handle, k, v, self.pos, self.budget, self.recent, n_new=n_new,
+                                   stream=stream)
+            cstr.cstr_cache_attention(self.handle, q, out, scale=scale, n_query=n_new, accumulate=True,
+                                      pos=self.pos if tokens > 1 else None, stream=stream)
             self.pos += tokens if n_new is None else n_new
         return out
