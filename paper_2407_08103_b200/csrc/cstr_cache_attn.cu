@@ -315,10 +315,11 @@ __device__ __forceinline__ void chunk_scores(float (&x)[NT][4], const RowParams 
     }
 }
 
-// A key that only some query rows see must not reach the others through 0 x NaN:
-// where such a key's value row holds something that is not finite, its products
-// are added one by one for the rows that see it, and the row is zeroed before
-// the matrix product.  At most the row's newest tokens are such keys.
+// A key that only some query rows see, or none, must not reach the others through
+// 0 x NaN: where such a key's value row holds something that is not finite, its
+// products are added one by one for the rows that see it, and the row is zeroed
+// before the matrix product.  The row's newest tokens are such keys, and with a
+// single token every slot that is younger than it.
 // (Inlined: the accumulators must not have an address, or they live in memory.)
 template <typename T, int DP, int NT>
 __device__ __forceinline__ void add_nonfinite_values(float (&o)[NT][DP / 16][4], const float (&x)[NT][4], char *vtile,
@@ -492,8 +493,8 @@ row_attention_kernel(const __grid_constant__ RowParams p)
             const int base = src.x0 + (i * kWarps + warp) * kChunk;
             float x[NT][4];
             chunk_scores<T, DP, NT>(x, p, qf, sq, keys, lane, base, src.x1, limit, causal || base + kChunk > src.x1, causal);
-            bool partial = false;                    // a key seen by some rows of the call only
-            if (causal && p.T > 1) {
+            bool partial = false;                    // a key that some query rows, or all, do not see
+            if (causal) {
                 bool some = false;
                 if (lane < kChunk && base + lane >= p.P && base + lane < src.x1) {
                     int age;
