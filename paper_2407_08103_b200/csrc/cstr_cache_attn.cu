@@ -823,7 +823,8 @@ row_attention_kernel(const __grid_constant__ RowParams p)
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            w[e >> 1] += exp2_fast(x[n][e] - lse[n][e & 1]);
+                            // (a select: what a row past n_query scores, its queries being anything, may be NaN)
+                            w[e >> 1] += lse[n][e & 1] == CUDART_INF_F ? 0.f : exp2_fast(x[n][e] - lse[n][e & 1]);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         w[h] += __shfl_xor_sync(0xffffffffu, w[h], 1);

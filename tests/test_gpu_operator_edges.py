@@ -27,3 +27,17 @@ def test_a_single_token_is_not_reached_by_slots_it_does_not_see(dtype, value, P,
     c.run()
     c.check()
     assert torch.isfinite(c.out).all() and torch.isfinite(c.d_w).all()
+
+
+# long caches of one row whose weights are computed from the keys again (63 and 8 query rows), and
+# one whose scores are kept
+@pytest.mark.parametrize("P,cap,T,G,D", [(100, 10000, 9, 7, 128), (600, 10000, 9, 7, 128), (100, 48000, 4, 2, 128),
+                                         (0, 300, 9, 7, 64)])
+@pytest.mark.parametrize("value", [math.nan, math.inf, 3e38])
+def test_queries_past_n_query_do_not_reach_the_weights(value, P, cap, T, G, D):
+    c = AttentionCase(52, 1, T, G, 1, D, P, cap, BF, causal=True, lens=[cap - 7], n_query=[2])
+    c.q[0, 2:] = value                                     # padding: may hold anything
+    c.dev()
+    c.run()
+    c.check()
+    assert torch.isfinite(c.d_w).all()
