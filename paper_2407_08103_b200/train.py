@@ -18,24 +18,31 @@ class _PolicyLoss(torch.autograd.Function):
         loss, logp = (torch.empty(n, dtype=torch.float32, device=logits.device) for _ in range(2))
         cstr.cstr_policy_loss(args["tables"], logits, args["states"], actions, old_logp, advantages,
                               loss, logp, ref_logp=ref_logp, weight=weight, **args["options"])
-        ctx.save_for_backward(logits, actions, old_logp, advantages, ref_logp, weight)
+        # The backward pass takes the loss again.  The library writes states and tokens in place through
+        # their addresses (a decoder that steps on), which autograd's versions do not show: so the
+        # per-row arrays are kept as copies, a few bytes a row.
+        if ctx.needs_input_grad[0]:
+            rows = (args["states"], actions, old_logp, advantages, ref_logp, weight, args["options"]["row_table"])
+            ctx.save_for_backward(logits, *(None if t is None else t.clone() for t in rows))
         ctx.args = args
         ctx.mark_non_differentiable(logp)
         return loss, logp
 
     @staticmethod
     def backward(ctx, grad_loss, _):
+        if not ctx.needs_input_grad[0]:
+            return (None,) * 7
         # the gradient of row n is linear in its weight, so the upstream gradient enters there;
         # nothing but the logits is kept in between
-        logits, actions, old_logp, advantages, ref_logp, weight = ctx.saved_tensors
+        logits, states, actions, old_logp, advantages, ref_logp, weight, row_table = ctx.saved_tensors
         grad = grad_loss.float()
         grad = grad.contiguous() if weight is None else grad * weight
         dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype,
                                       device=logits.device)
         loss, logp = torch.empty_like(grad), torch.empty_like(grad)
-        cstr.cstr_policy_loss(ctx.args["tables"], logits, ctx.args["states"], actions, old_logp,
-                              advantages, loss, logp, ref_logp=ref_logp, weight=grad,
-                              dlogits=dlogits, **ctx.args["options"])
+        cstr.cstr_policy_loss(ctx.args["tables"], logits, states, actions, old_logp, advantages, loss, logp,
+                              ref_logp=ref_logp, weight=grad, dlogits=dlogits,
+                              **dict(ctx.args["options"], row_table=row_table))
         return dlogits, None, None, None, None, None, None
 
 
