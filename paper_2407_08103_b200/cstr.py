@@ -165,6 +165,7 @@ class Vocab(_Handle):
 class Table(_Handle):
     _free = "cstr_free_table"
     vocab = None  # keeps the vocabulary handle alive
+    builds = 0    # times that it has been built again
 
 
 class Workspace(_Handle):
@@ -246,11 +247,13 @@ def cstr_table_create(vocab: Vocab, max_states: int) -> Table:
 
 
 def cstr_table_build(table: Table, dfa: Dfa, eos_id: int = -1, stream=None) -> None:
+    table.builds += 1
     _check(lib().cstr_table_build(table.ptr, dfa.ptr, ctypes.c_int32(eos_id), _stream_ptr(stream)))
 
 
 def cstr_table_build_dense(table: Table, dfa: Dfa, eos_id: int = -1, stream=None) -> None:
     """The same table by the per-token walk without shared prefixes (measurement baseline)."""
+    table.builds += 1
     _check(lib().cstr_table_build_dense(table.ptr, dfa.ptr, ctypes.c_int32(eos_id),
                                         _stream_ptr(stream)))
 

@@ -11,6 +11,10 @@ import torch
 from . import cstr
 
 
+def _builds(tables):
+    return [t.builds for t in tables]
+
+
 class _PolicyLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, actions, old_logp, advantages, ref_logp, weight, args):
@@ -24,6 +28,7 @@ class _PolicyLoss(torch.autograd.Function):
         if ctx.needs_input_grad[0]:
             rows = (args["states"], actions, old_logp, advantages, ref_logp, weight, args["options"]["row_table"])
             ctx.save_for_backward(logits, *(None if t is None else t.clone() for t in rows))
+            ctx.builds = _builds(args["tables"])
         ctx.args = args
         ctx.mark_non_differentiable(logp)
         return loss, logp
@@ -32,6 +37,8 @@ class _PolicyLoss(torch.autograd.Function):
     def backward(ctx, grad_loss, _):
         if not ctx.needs_input_grad[0]:
             return (None,) * 7
+        if _builds(ctx.args["tables"]) != ctx.builds:
+            raise RuntimeError("a table of this loss was built again before its backward pass")
         # the gradient of row n is linear in its weight, so the upstream gradient enters there;
         # nothing but the logits is kept in between
         logits, states, actions, old_logp, advantages, ref_logp, weight, row_table = ctx.saved_tensors
@@ -51,6 +58,7 @@ def constrained_policy_loss(logits, actions, old_logp, advantages, tables=None, 
                             clip_high: float = 0.2, kl_coef: float = 0.0, temperature: float = 1.0):
     """``(loss [N], logp [N])`` of ``cstr_policy_loss``; the loss is differentiable in ``logits``
     (float32 or bfloat16 ``[N][V]``), the log probabilities are not."""
+    tables = [tables] if isinstance(tables, cstr.Table) else list(tables or [])
     args = dict(tables=tables, states=states,
                 options=dict(row_table=row_table, clip_low=clip_low, clip_high=clip_high,
                              kl_coef=kl_coef, temperature=temperature))

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2407_08103_b200 import cstr
 from paper_2407_08103_b200.train import constrained_policy_loss
 from synth.configs import config_dfas, config_vocab
 
@@ -60,3 +61,17 @@ def test_logits_without_gradient():
     assert torch.equal(loss.detach(), constrained_policy_loss(**a)[0])
     loss.sum().backward()                                  # differentiable in the logits only
     assert w.grad is None
+
+
+def test_a_table_built_again_before_the_backward_pass_is_refused():
+    vb, vo = config_vocab("api_1k")
+    dfa = config_dfas("api_1k")[0]
+    vocab, d = cstr.cstr_load_vocab(vb, vo), cstr.cstr_load_dfa(*dfa)
+    table = cstr.cstr_table_create(vocab, dfa[0].shape[0])
+    cstr.cstr_table_build(table, d)
+    a = dict(batch(), tables=[table], row_table=None)
+    assert torch.equal(gradient(a), gradient(dict(a, tables=table)))
+    for again in (cstr.cstr_table_build, cstr.cstr_table_build_dense):
+        with pytest.raises(RuntimeError, match="built again"):
+            gradient(a, lambda: again(table, d))
+    gradient(a)                                            # a loss taken after that is fine
