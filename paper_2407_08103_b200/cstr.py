@@ -165,7 +165,7 @@ class Vocab(_Handle):
 class Table(_Handle):
     _free = "cstr_free_table"
     vocab = None  # keeps the vocabulary handle alive
-    builds = 0    # times that it has been built again
+    builds = 0    # calls of cstr_table_build and cstr_table_build_dense
 
 
 class Workspace(_Handle):

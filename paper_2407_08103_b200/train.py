@@ -7,6 +7,7 @@ in Algorithm 2's loop body), because that is the distribution the answers were s
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import cstr
 
@@ -34,6 +35,7 @@ class _PolicyLoss(torch.autograd.Function):
         return loss, logp
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_loss, _):
         if not ctx.needs_input_grad[0]:
             return (None,) * 7

@@ -75,3 +75,12 @@ def test_a_table_built_again_before_the_backward_pass_is_refused():
         with pytest.raises(RuntimeError, match="built again"):
             gradient(a, lambda: again(table, d))
     gradient(a)                                            # a loss taken after that is fine
+
+
+def test_second_derivatives_are_refused():
+    a = batch()
+    x = a["logits"].clone().requires_grad_()
+    loss, _ = constrained_policy_loss(**dict(a, logits=x))
+    (g,) = torch.autograd.grad(loss.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (g * x).sum().backward()                           # (the term through g must not be left out)
