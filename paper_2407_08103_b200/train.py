@@ -45,7 +45,7 @@ class _PolicyLoss(torch.autograd.Function):
         # nothing but the logits is kept in between
         logits, states, actions, old_logp, advantages, ref_logp, weight, row_table = ctx.saved_tensors
         grad = grad_loss.float()
-        grad = grad.contiguous() if weight is None else grad * weight
+        grad = grad.contiguous() if weight is None else grad * weight.flatten()[:grad.shape[0]]
         dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype,
                                       device=logits.device)
         loss, logp = torch.empty_like(grad), torch.empty_like(grad)

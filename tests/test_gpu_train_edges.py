@@ -84,3 +84,14 @@ def test_second_derivatives_are_refused():
     (g,) = torch.autograd.grad(loss.sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         (g * x).sum().backward()                           # (the term through g must not be left out)
+
+
+@pytest.mark.parametrize("name", ["weight", "states", "actions", "old_logp", "advantages", "ref_logp", "row_table"])
+def test_per_row_arrays_of_other_shapes(name):
+    # one entry per row is what counts: a column, or an array with entries to spare
+    a = batch()
+    want, up = gradient(a), torch.rand(24, device=DEV)
+    want_up = gradient(a, up=up)
+    for other in (a[name][:, None], torch.cat([a[name], a[name]])):
+        assert torch.equal(gradient(dict(a, **{name: other})), want)
+        assert torch.equal(gradient(dict(a, **{name: other}), up=up), want_up)
