@@ -7,13 +7,24 @@ in Algorithm 2's loop body), because that is the distribution the answers were s
 from __future__ import annotations
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import cstr
 
 
 def _builds(tables):
     return [t.builds for t in tables]
+
+
+class _Once(torch.autograd.Function):
+    """A gradient whose own derivative is not there."""
+
+    @staticmethod
+    def forward(ctx, gradient, *inputs):
+        return gradient
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("constrained_policy_loss is differentiable once only")
 
 
 class _PolicyLoss(torch.autograd.Function):
@@ -35,7 +46,6 @@ class _PolicyLoss(torch.autograd.Function):
         return loss, logp
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, grad_loss, _):
         if not ctx.needs_input_grad[0]:
             return (None,) * 7
@@ -52,6 +62,8 @@ class _PolicyLoss(torch.autograd.Function):
         cstr.cstr_policy_loss(ctx.args["tables"], logits, states, actions, old_logp, advantages, loss, logp,
                               ref_logp=ref_logp, weight=grad, dlogits=dlogits,
                               **dict(ctx.args["options"], row_table=row_table))
+        if torch.is_grad_enabled():              # create_graph: the gradient is a function of these, too
+            dlogits = _Once.apply(dlogits, logits, grad_loss)
         return dlogits, None, None, None, None, None, None
 
 

@@ -82,7 +82,8 @@ def test_second_derivatives_are_refused():
     x = a["logits"].clone().requires_grad_()
     loss, _ = constrained_policy_loss(**dict(a, logits=x))
     (g,) = torch.autograd.grad(loss.sum(), x, create_graph=True)
-    with pytest.raises(RuntimeError):
+    assert torch.equal(g, gradient(a))
+    with pytest.raises(RuntimeError, match="once only"):
         (g * x).sum().backward()                           # (the term through g must not be left out)
 
 
