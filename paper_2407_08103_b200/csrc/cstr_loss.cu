@@ -214,6 +214,8 @@ policy_loss_kernel(const __grid_constant__ LossParams p)
     cstr_let_next_kernel_start();
     cg::cluster_group cluster = cg::this_cluster();
     const int size = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    if (size > 1)                                // this CTA runs: its shared memory may be written from now on
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row = blockIdx.x / size;
     const char *x_row = (const char *)p.logits + (long long)row * p.ld * ESZ;
@@ -290,6 +292,8 @@ policy_loss_kernel(const __grid_constant__ LossParams p)
     if (lane == 0)
         s_warp[warp] = r;
     __syncthreads();
+    if (size > 1)                                // the others run, too (they said so before their first pass)
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (warp == 0 && size > 1) {
         r = join_lanes(lane < kWarps ? s_warp[lane] : none);
         if (lane < size)                         // to every CTA; after the barrier nobody reads remotely

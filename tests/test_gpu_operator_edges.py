@@ -5,7 +5,9 @@ import numpy as np
 import pytest
 import torch
 
-from operator_cases import AttentionCase
+from paper_2407_08103_b200 import cstr
+
+from operator_cases import DEV, AttentionCase
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -41,3 +43,22 @@ def test_queries_past_n_query_do_not_reach_the_weights(value, P, cap, T, G, D):
     c.run()
     c.check()
     assert torch.isfinite(c.d_w).all()
+
+
+# rows shared by clusters of 2 to 16 blocks, the last ones with short shares or (narrow rows) none
+@pytest.mark.parametrize("N,V", [(1, 8193), (2, 16385), (1, 65537), (40, 32769), (9, 131073), (300, 16390)])
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_loss_of_rows_shared_by_a_cluster(dtype, N, V):
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.randn(N, V, generator=g, device=DEV).to(dtype)
+    act = torch.randint(0, V, (N,), generator=g, device=DEV, dtype=torch.int32)
+    adv = torch.ones(N, device=DEV)
+    want = torch.log_softmax(x.double(), 1).gather(1, act.long()[:, None])[:, 0]
+    runs = []
+    for _ in range(20):
+        loss, logp, d = torch.empty(N, device=DEV), torch.empty(N, device=DEV), torch.empty_like(x)
+        cstr.cstr_policy_loss(None, x, None, act, want.float(), adv, loss, logp, dlogits=d)
+        runs.append((loss, logp, d))
+    assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(runs[0], r))
+    # logits below 8 and log probabilities below 32 in 32 bits, the sum of the exponentials to 2^-18
+    assert (runs[0][1].double() - want).abs().max() <= 2.0 ** -21 * 41 + 2.0 ** -18
