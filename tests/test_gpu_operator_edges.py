@@ -62,3 +62,30 @@ def test_loss_of_rows_shared_by_a_cluster(dtype, N, V):
     assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(runs[0], r))
     # logits below 8 and log probabilities below 32 in 32 bits, the sum of the exponentials to 2^-18
     assert (runs[0][1].double() - want).abs().max() <= 2.0 ** -21 * 41 + 2.0 ** -18
+
+
+# logits far from zero: a model's own masks of -1e9 or -1e30 over all that the constraint allows, or a common offset
+@pytest.mark.parametrize("offset", [0.0, 1e4, -1e4, 1e6, -1e9, 1e9, -1e30, 1e30])
+@pytest.mark.parametrize("temperature", [1.0, 0.25])
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_loss_of_logits_with_a_large_offset(dtype, temperature, offset):
+    N, V = 6, 5000
+    g = torch.Generator().manual_seed(5)
+    x = (2.0 * torch.randn(N, V, generator=g, dtype=torch.float64) + offset).to(dtype).to(DEV)
+    act = x.argmax(1).int()
+    soft = torch.log_softmax(x.double() / temperature, 1)
+    want = soft.gather(1, act.long()[:, None])[:, 0]
+    old, adv = want.float(), torch.ones(N, device=DEV)
+    loss, logp, d = torch.empty(N, device=DEV), torch.empty(N, device=DEV), torch.empty_like(x)
+    cstr.cstr_policy_loss(None, x, None, act, old, adv, loss, logp, dlogits=d, temperature=temperature)
+    # Differences of logits to the maximum that weigh (32 below it at most) in one rounding, scaled in another:
+    # 32 x 2^-22 of an exponent, and 2^-21 a step for the exponential, their sum, its logarithm (below 16)
+    tol = 2.0 ** -17 + 2.0 ** -18
+    assert (logp.double() - want).abs().max() <= tol
+    ratio = torch.exp(want - old.double())[:, None]
+    hot = torch.zeros_like(soft).scatter_(1, act.long()[:, None], 1.0)
+    grad = -ratio * (hot - soft.exp()) / temperature
+    size = ratio * (hot + soft.exp()) / temperature
+    unit = 2.0 ** -8 if dtype == BF else 2.0 ** -23
+    assert ((d.double() - grad).abs() <= unit * grad.abs() + 4 * tol * size + 1e-12).all()
+    assert ((loss.double() + ratio[:, 0]).abs() <= 2 * tol).all()
