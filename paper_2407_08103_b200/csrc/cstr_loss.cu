@@ -176,9 +176,10 @@ __device__ __forceinline__ RowResult row_result(const LossParams &p, bool valid,
             r.loss = plain > clipped ? -clipped : -plain;
             float g = plain > clipped ? 0.f : -plain;
             if (p.ref_logp) {
-                const float diff = ref_logp - r.logp, k = expf(diff);
-                r.loss += p.kl * (k - diff - 1.f);
-                g += p.kl * (1.f - k);
+                // exp(diff) - 1 as one function: near the reference policy the term is about diff^2 / 2
+                const float diff = ref_logp - r.logp, k1 = expm1f(diff);
+                r.loss += p.kl * (k1 - diff);
+                g -= p.kl * k1;
             }
             r.loss *= w;
             r.hot = g * w * p.inv_temp;

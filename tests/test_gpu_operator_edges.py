@@ -89,3 +89,25 @@ def test_loss_of_logits_with_a_large_offset(dtype, temperature, offset):
     unit = 2.0 ** -8 if dtype == BF else 2.0 ** -23
     assert ((d.double() - grad).abs() <= unit * grad.abs() + 4 * tol * size + 1e-12).all()
     assert ((loss.double() + ratio[:, 0]).abs() <= 2 * tol).all()
+
+
+@pytest.mark.parametrize("step", [1e-6, 1e-4, -1e-3, 1e-2, -0.3, 5.0])
+def test_kl_term_near_the_reference_policy(step):
+    # the term is about d^2 / 2 there, of summands about 1
+    N, V = 64, 1000
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn(N, V, generator=g).to(DEV)
+    act = torch.randint(0, V, (N,), generator=g).int().to(DEV)
+    lp = torch.log_softmax(x.double(), 1).gather(1, act.long()[:, None])[:, 0]
+    loss, logp, d = torch.empty(N, device=DEV), torch.empty(N, device=DEV), torch.empty_like(x)
+    ref = (lp + step).float()
+    cstr.cstr_policy_loss(None, x, None, act, lp.float(), torch.zeros(N, device=DEV), loss, logp, ref_logp=ref,
+                          kl_coef=1.0, dlogits=d)
+    diff = ref.double() - logp.double()                    # exact: both have 24 bits
+    want = torch.expm1(diff) - diff
+    # the difference in 32 bits, then exp(d) - 1 to two units of its last place, then one subtraction
+    size = diff.abs() + torch.expm1(diff).abs()
+    assert ((loss.double() - want).abs() <= 2.0 ** -21 * size).all()
+    hot = d.gather(1, act.long()[:, None])[:, 0].double()
+    p = logp.double().exp()
+    assert ((hot + torch.expm1(diff) * (1 - p)).abs() <= 2.0 ** -18 * size + 1e-12).all()
