@@ -627,6 +627,7 @@ int cstr_cache_status(cstr_cache_t *cache, void *cuda_stream, int64_t *gave_up);
  *   states      DEVICE int32 [rows]: state before the token (NULL exactly when n_tables is 0)
  *   logits      DEVICE [rows][ld] of dtype CSTR_F32 or CSTR_BF16;  ld >= vocab_size
  *   vocab_size  equal to the tables' V
+ *   temperature finite, above 4.3e-39 (its reciprocal times log2(e) is a float)
  *   actions     DEVICE int32 [rows]: the sampled token a
  *   old_logp, advantages   DEVICE float [rows]
  *   ref_logp    DEVICE float [rows] or NULL (no KL term; kl_coef is ignored)

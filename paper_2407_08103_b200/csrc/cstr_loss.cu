@@ -410,7 +410,8 @@ extern "C" int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tab
         return cstr_fail(CSTR_ERR_DTYPE, "cstr_policy_loss: unknown dtype %d", dtype);
     if (rows < 0 || vocab_size < 1)
         return cstr_fail(CSTR_ERR_ARG, "cstr_policy_loss: rows = %d, vocab_size = %d", rows, vocab_size);
-    if (!(temperature > 0.f) || !isfinite(temperature) || !(clip_low >= 0.f) || !(clip_high >= 0.f) ||
+    const float scale_log2 = (float)(1.4426950408889634 / temperature);
+    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(scale_log2) || !(clip_low >= 0.f) || !(clip_high >= 0.f) ||
         !isfinite(kl_coef))
         return cstr_fail(CSTR_ERR_ARG, "cstr_policy_loss: temperature = %g, clip = %g / %g, kl = %g",
                          temperature, clip_low, clip_high, kl_coef);
@@ -454,7 +455,7 @@ extern "C" int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tab
     p.ld = ld;
     p.V = vocab_size;
     p.rows = rows;
-    p.c = (float)(1.4426950408889634 / temperature);
+    p.c = scale_log2;
     p.inv_temp = 1.f / temperature;
     p.old_logp = old_logp;
     p.ref_logp = ref_logp;
