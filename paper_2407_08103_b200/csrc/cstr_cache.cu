@@ -483,8 +483,9 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
             p.list = nullptr;
         p.bits = 11;
         const int smem = (4 << p.bits) + (shared ? c.cap * 8 : 0);
-        static std::atomic<int> allowed[64];
-        const int rc = smem > 48 * 1024 ? cstr_allow_smem(cache_insert_kernel<false>, allowed, c.device, smem) : CSTR_OK;
+        static std::atomic<bool> allowed[64];
+        const int rc = cstr_allow_smem(cache_insert_kernel<false>, allowed, c.device,
+                                       (4 << p.bits) + CSTR_INSERT_SMEM_SLOTS * 8);
         if (rc)
             return rc;
         return cstr_launch(cache_insert_kernel<false>, items, c.cap <= 4096 ? 256 : kMaxThreads, 1, smem, stream, p);

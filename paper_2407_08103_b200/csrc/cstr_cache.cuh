@@ -5,16 +5,17 @@
 
 #include "cstr_internal.cuh"
 
-// Allows `kernel` that much dynamic shared memory on `device`; `allowed` (one array per kernel)
-// remembers what it has been given, so that a decoding loop does not ask again.
+// Allows `kernel` its dynamic shared memory on `device`.  `most` is the largest amount that any call asks
+// for, the same every time: threads that launch the kernel side by side never lower each other's limit.
+// `allowed` (one array per kernel) remembers where it has been done, so that a decoding loop does not ask again.
 template <typename K>
-int cstr_allow_smem(K kernel, std::atomic<int> (&allowed)[64], int device, int bytes)
+int cstr_allow_smem(K kernel, std::atomic<bool> (&allowed)[64], int device, int most)
 {
-    if (device >= 0 && device < 64 && allowed[device].load(std::memory_order_relaxed) >= bytes)
+    if (device >= 0 && device < 64 && allowed[device].load(std::memory_order_relaxed))
         return CSTR_OK;
-    CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     if (device >= 0 && device < 64)
-        allowed[device].store(bytes, std::memory_order_relaxed);
+        allowed[device].store(true, std::memory_order_relaxed);
     return CSTR_OK;
 }
 

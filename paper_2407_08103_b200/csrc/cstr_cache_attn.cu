@@ -35,6 +35,7 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kChunk = 16;       // keys per step of a warp
+constexpr int kMostSmem = 220 * 1024;   // dynamic shared memory of a CTA, the scores it keeps included
 constexpr float kLazy = 8.f;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -859,14 +860,14 @@ int launch(const cstr_cache &c, RowParams p, cudaStream_t stream)
         const long long share = ((long long)p.P + p.cap + p.split - 1) / p.split + (p.split > 1 ? kChunk : 0);
         const long long own = (share < p.cap ? share : p.cap) + (p.P > 0 ? kChunk : 0);
         const long long want = (own + kChunk - 1) / kChunk * kChunk;
-        if (smem + want * rows * 4 <= 220 * 1024) {
+        if (smem + want * rows * 4 <= kMostSmem) {
             p.score_cap = (int)want;
             smem += (int)(want * rows * 4);
         }
     }
     auto kernel = row_attention_kernel<T, DP, NT>;
-    static std::atomic<int> allowed[64];
-    const int rc = cstr_allow_smem(kernel, allowed, c.device, smem);
+    static std::atomic<bool> allowed[64];
+    const int rc = cstr_allow_smem(kernel, allowed, c.device, kMostSmem);
     if (rc)
         return rc;
     return cstr_launch(kernel, (long long)p.B * p.Hk * p.split, kWarps * 32, p.split, smem, stream, p);

@@ -673,7 +673,7 @@ template <typename T, int DP>
 int launch(const cstr_cache &c, const PrefixParams &p, cudaStream_t stream)
 {
     auto kernel = prefix_attention_kernel<T, DP>;
-    static std::atomic<int> allowed[64];
+    static std::atomic<bool> allowed[64];
     const int rc = cstr_allow_smem(kernel, allowed, c.device, Shape<DP>::kSmem);
     if (rc)
         return rc;

@@ -1,5 +1,6 @@
 """Edges of the cache and loss operators at which a call once went wrong."""
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -111,3 +112,35 @@ def test_kl_term_near_the_reference_policy(step):
     hot = d.gather(1, act.long()[:, None])[:, 0].double()
     p = logp.double().exp()
     assert ((hot + torch.expm1(diff) * (1 - p)).abs() <= 2.0 ** -18 * size + 1e-12).all()
+
+
+def test_handles_of_several_threads_side_by_side():
+    # handles of different sizes launch the same kernels, each from its own thread and stream
+    cases = [(cap, AttentionCase(60 + i, 2, 1, 4, 2, 64, 33, cap, BF, lens=[cap, cap - 1]))
+             for i, cap in enumerate((40, 3000, 9000, 20000))]
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(c, cap):
+        try:
+            side = torch.cuda.Stream()
+            c.run(stream=side)
+            k, v = (torch.zeros(2, 2, 2, 64, dtype=BF, device=DEV) for _ in range(2))
+            pos = torch.full((2,), cap, dtype=torch.int32, device=DEV)
+            torch.cuda.current_stream().synchronize()
+            for _ in range(50):
+                cstr.cstr_cache_attention(c.cache, c.q, c.out, stream=side)
+            big = cstr.cstr_cache_create(c.ck, c.cv, c.d_lens, 4, weight=c.d_w.clone(), age=c.d_age, max_tokens=2)
+            side.synchronize()
+            for _ in range(20):
+                cstr.cstr_cache_insert(big, k, v, pos, cap, 2, stream=side)
+            side.synchronize()
+        except Exception as e:                             # (an assertion in a thread would pass unseen)
+            failed.append(e)
+    for _ in range(3):
+        threads = [threading.Thread(target=work, args=(c, cap)) for cap, c in cases]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    assert not failed
