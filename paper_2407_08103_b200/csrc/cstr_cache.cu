@@ -573,13 +573,21 @@ extern "C" int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, 
     if (e == cudaSuccess)
         e = cudaMalloc((void **)&c->ticket, (size_t)batch * 4);
     if (e == cudaSuccess)
-        e = cudaMemset(c->ticket, 0, (size_t)batch * 4);
-    if (e == cudaSuccess)
         e = cudaMalloc((void **)&c->status, 4);
-    if (e == cudaSuccess)
-        e = cudaMemset(c->status, 0, 4);
     if (e == cudaSuccess && weight && age)
         e = cudaMalloc((void **)&c->list, (size_t)batch * n_kv_heads * cap * 8);
+    // zeroed before the handle is out, whatever stream it is used on and whatever the default stream has queued
+    cudaStream_t own = nullptr;
+    if (e == cudaSuccess)
+        e = cudaStreamCreateWithFlags(&own, cudaStreamNonBlocking);
+    if (e == cudaSuccess)
+        e = cudaMemsetAsync(c->ticket, 0, (size_t)batch * 4, own);
+    if (e == cudaSuccess)
+        e = cudaMemsetAsync(c->status, 0, 4, own);
+    if (e == cudaSuccess)
+        e = cudaStreamSynchronize(own);
+    if (own)
+        cudaStreamDestroy(own);
     if (e != cudaSuccess) {
         rc = cstr_fail(e == cudaErrorMemoryAllocation ? CSTR_ERR_NOMEM : CSTR_ERR_CUDA,
                        "cstr_cache_create: %s", cudaGetErrorString(e));

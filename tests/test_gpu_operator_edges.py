@@ -6,9 +6,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import operators as ref
 from paper_2407_08103_b200 import cstr
 
-from operator_cases import DEV, AttentionCase
+from operator_cases import DEV, AttentionCase, f8, random_cache, ranked_ages
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -101,10 +102,10 @@ def test_kl_term_near_the_reference_policy(step):
     act = torch.randint(0, V, (N,), generator=g).int().to(DEV)
     lp = torch.log_softmax(x.double(), 1).gather(1, act.long()[:, None])[:, 0]
     loss, logp, d = torch.empty(N, device=DEV), torch.empty(N, device=DEV), torch.empty_like(x)
-    ref = (lp + step).float()
-    cstr.cstr_policy_loss(None, x, None, act, lp.float(), torch.zeros(N, device=DEV), loss, logp, ref_logp=ref,
+    near = (lp + step).float()
+    cstr.cstr_policy_loss(None, x, None, act, lp.float(), torch.zeros(N, device=DEV), loss, logp, ref_logp=near,
                           kl_coef=1.0, dlogits=d)
-    diff = ref.double() - logp.double()                    # exact: both have 24 bits
+    diff = near.double() - logp.double()                    # exact: both have 24 bits
     want = torch.expm1(diff) - diff
     # the difference in 32 bits, then exp(d) - 1 to two units of its last place, then one subtraction
     size = diff.abs() + torch.expm1(diff).abs()
@@ -144,3 +145,26 @@ def test_handles_of_several_threads_side_by_side():
         for t in threads:
             t.join()
     assert not failed
+
+
+def test_a_new_handle_is_ready_on_any_stream():
+    # while the default stream is busy, on a stream that does not wait for it
+    rng = np.random.default_rng(4)
+    side = torch.cuda.Stream()
+    for i in range(3):
+        B, Hk, cap = 50, 8, 40
+        ck, cv = random_cache(rng, B, Hk, 64, cap, None)
+        k, v = random_cache(rng, B, Hk, 64, 2, None)
+        lens = np.full(B, cap, np.int32)
+        age, w = ranked_ages(rng, lens, Hk, cap), rng.random((B, Hk, cap)).astype(np.float32)
+        d = [torch.from_numpy(a).to(DEV) for a in (w, age, lens)]
+        pos = torch.full((B,), cap, dtype=torch.int32, device=DEV)
+        want = ref.insert(f8(ck), f8(cv), w, age, lens, f8(k), f8(v), lens, cap - 3, 5)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(200_000_000)                     # about 0.1 s
+        cache = cstr.cstr_cache_create(ck, cv, d[2], Hk, weight=d[0], age=d[1], max_tokens=2)
+        cstr.cstr_cache_insert(cache, k, v, pos, cap - 3, 5, stream=side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert np.array_equal(d[2].cpu().numpy(), want[4]) and (want[4] == cap - 3).all()
+        assert np.array_equal(d[1].cpu().numpy(), want[3]) and np.array_equal(f8(ck), want[0])
