@@ -1,6 +1,8 @@
 // Internal definitions of the key / value cache and its attention (not part of the ABI).
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include <atomic>
 
 #include "cstr_internal.cuh"
@@ -18,6 +20,18 @@ int cstr_allow_smem(K kernel, std::atomic<bool> (&allowed)[64], int device, int 
         allowed[device].store(true, std::memory_order_relaxed);
     return CSTR_OK;
 }
+
+// Reference of an online softmax (base 2) whose probabilities enter a product in a 16-bit type.  It is set
+// kBelow under the maximum and moves when a score exceeds it by more than kLag, so that most keys need no
+// rescaling of the sums (the running maximum of Milakov and Gimelshein, arXiv:1805.02867, with a lag).  The
+// probabilities stay below 2^kLag, in range of the type.  Half precision has few bits below 2^-14 and none
+// below 2^-24: lifting its probabilities by 2^7 keeps all bits down to 2^-21 of the largest one.
+template <typename T> struct cstr_softmax_reference {
+    static constexpr float kBelow = 0.f, kLag = 8.f;          // bfloat16: the exponents of fp32
+};
+template <> struct cstr_softmax_reference<__half> {
+    static constexpr float kBelow = 7.f, kLag = 15.f;
+};
 
 // What cstr_cache_create recorded: caller-owned arrays and their strides (in
 // elements), and the scratch that the handle's calls share.

@@ -36,7 +36,6 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kChunk = 16;       // keys per step of a warp
 constexpr int kMostSmem = 220 * 1024;   // dynamic shared memory of a CTA, the scores it keeps included
-constexpr float kLazy = 8.f;
 constexpr float kLn2 = 0.693147180559945309f;
 
 struct RowParams {
@@ -373,6 +372,7 @@ row_attention_kernel(const __grid_constant__ RowParams p)
 {
     constexpr int ROWS = 8 * NT;
     using Shape = RowShape<DP, NT>;
+    using Ref = cstr_softmax_reference<T>;
     constexpr int kSlots = Shape::kSlots;
     extern __shared__ __align__(128) char smem[];
     char *s_q = smem;                                              // [ROWS][DP] of T
@@ -518,14 +518,14 @@ row_attention_kernel(const __grid_constant__ RowParams p)
                             to[r * p.score_cap + 8 * (e >> 1)] = x[n][e];
                     }
             }
-            // the reference moves only when some score exceeds it by 2^8 (the first keys, rarely later):
-            // until then the probabilities stay below 2^8, in range of both 16-bit types
+            // the reference moves only when some score exceeds it by more than the lag (the first keys,
+            // rarely later)
             bool grow = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    grow = grow || fmaxf(x[n][e], x[n][2 + e]) > m[n][e] + kLazy;
+                    grow = grow || fmaxf(x[n][e], x[n][2 + e]) > m[n][e] + Ref::kLag;
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -535,7 +535,7 @@ row_attention_kernel(const __grid_constant__ RowParams p)
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                        const float mn = fmaxf(m[n][e], top);
+                        const float mn = fmaxf(m[n][e], top - Ref::kBelow);
                         const float f = mn == -CUDART_INF_F ? 1.f : exp2_fast(m[n][e] - mn);
                         m[n][e] = mn;
                         l[n][e] *= f;

@@ -43,9 +43,6 @@ namespace {
 
 constexpr int kThreads = 384;        // warps 0-3: copies, products, query tiles (two); 4-7, 8-11: streams
 constexpr int kTile = 128;           // query rows and keys of a tile
-// A maximum that grew by less than 2^8 keeps the old reference: P stays below 2^8, in range of
-// both 16-bit types, and the rescaling of O (a round trip through registers) is left out.
-constexpr float kLazy = 8.f;
 constexpr unsigned kWaitLimit = 1u << 22;
 
 template <int DP> struct Shape {
@@ -288,6 +285,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                         const __grid_constant__ PrefixParams p)
 {
     using S = Shape<DP>;
+    using Ref = cstr_softmax_reference<T>;       // (moving it costs a round trip of O through registers)
     constexpr int kSlots = S::kSlots;
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) unsigned long long s_bar[2 * kSlots + 12];
@@ -502,7 +500,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                 fence_after();
                 if (warp_on) {
                     const int valid = p.P - (g.tile0 + (g.pair_rows ? n >> 1 : n)) * kTile;
-                    if (mine == 0) {                             // the first keys' maximum is the first reference
+                    if (mine == 0) {                             // the first keys' maximum sets the first reference
                         float top = -CUDART_INF_F;
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
@@ -514,10 +512,10 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                                 top = max3(top, 32 * c + i < valid ? y[i] : -CUDART_INF_F,
                                            32 * c + i + 1 < valid ? y[i + 1] : -CUDART_INF_F);
                         }
-                        m = top * p.scale_log2;
+                        m = top * p.scale_log2 - Ref::kBelow;
                     }
                     // One pass over the scores with the reference so far; only if some row's maximum
-                    // turns out to have grown by more than 2^8 (rarely) the reference moves and the
+                    // turns out to exceed it by more than the lag (rarely) the reference moves and the
                     // pass is taken again.  P replaces S afterwards.
                     unsigned w[4][16];
                     float sum;
@@ -555,10 +553,10 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                         }
                         sum = (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
                         const float seen = fmaxf(top[0], top[1]) * p.scale_log2;
-                        const bool grow = seen > m + kLazy;
+                        const bool grow = seen > m + Ref::kLag;
                         if (!__any_sync(0xffffffffu, grow))
                             break;
-                        const float to = grow ? seen : m;
+                        const float to = grow ? seen - Ref::kBelow : m;
                         const float f = m == to ? 1.f : exp2_fast(m - to);
                         l *= f;
                         m = to;

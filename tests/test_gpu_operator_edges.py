@@ -168,3 +168,28 @@ def test_a_new_handle_is_ready_on_any_stream():
         torch.cuda.synchronize()
         assert np.array_equal(d[2].cpu().numpy(), want[4]) and (want[4] == cap - 3).all()
         assert np.array_equal(d[1].cpu().numpy(), want[3]) and np.array_equal(f8(ck), want[0])
+
+
+# the row kernel alone, and behind one and two tiles of query rows on the tensor cores
+@pytest.mark.parametrize("P,B", [(100, 2), (600, 2), (2000, 40)])
+@pytest.mark.parametrize("x", [14.5, 18.3, 20.4, 22.6, 24.3, 26.0])
+def test_half_precision_keeps_small_probabilities(x, P, B):
+    # one key with nearly all of the weight, which has value 0; all others 2^-x of it each
+    c = AttentionCase(53, B, 1, 4, 1, 64, P, 4, HF, lens=[2] * B, weights=False)
+    c.q.zero_()
+    c.q[..., 0] = 1.0
+    c.pk.zero_()
+    c.pk[1:, 0, 0] = -x * math.log(2.0)
+    c.pv[:] = 64.0
+    c.pv[0] = 0.0
+    c.ck[:, :2], c.cv[:, :2] = 0.0, 0.0
+    c.ck[:, :2, 0, 0] = -30.0
+    c.dev()
+    c.run(scale=1.0)
+    torch.cuda.synchronize()
+    e = np.exp(f8(c.pk)[:, 0, 0])
+    want = 64.0 * e[1:].sum() / (e.sum() + 2 * math.exp(-30.0))
+    # the same rounding in every probability and one of the output, 2^-11 each; probabilities count in
+    # multiples of 2^-24 below 2^-14, and enter the product multiplied by 2^7 at least
+    tol = want * (2.0 ** -10 + 2.0 ** (x - 32) + 2.0 ** -14)
+    assert np.abs(f8(c.out) - want).max() <= tol
