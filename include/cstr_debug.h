@@ -39,6 +39,13 @@ int cstr_debug_bounds_status(uint64_t *out, int32_t reset);
  */
 int cstr_test_set_group_hash_bits(int32_t bits);
 
+/*
+ * Tries (-1: the usual number) that each bounded wait of the attention over the
+ * prompt gets before its thread block gives up and counts in cstr_cache_status;
+ * 0: one look, without the pause that a try takes.  Affects calls made afterwards.
+ */
+int cstr_test_set_wait_limit(int32_t tries);
+
 #ifdef __cplusplus
 }
 #endif

@@ -43,7 +43,7 @@ namespace {
 
 constexpr int kThreads = 384;        // warps 0-3: copies, products, query tiles (two); 4-7, 8-11: streams
 constexpr int kTile = 128;           // query rows and keys of a tile
-constexpr unsigned kWaitLimit = 1u << 22;
+constexpr int kWaitLimit = 1 << 22;
 
 template <int DP> struct Shape {
     static constexpr int kTileBytes = kTile * DP * 2;
@@ -62,7 +62,12 @@ struct PrefixParams {
     float scale_log2;                // > 0: for a negative scale the first product negates the queries
     unsigned negate;                 // bit of the instruction descriptor
     cstr_divisor by_r, by_g;
+    int wait_limit;                  // kWaitLimit but in tests
 };
+
+#ifdef CSTR_TESTING
+int g_test_wait_limit = kWaitLimit;
+#endif
 
 __device__ __forceinline__ unsigned smem_addr(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
 
@@ -111,7 +116,7 @@ template <> __device__ __forceinline__ unsigned pack2<__half>(float lo, float hi
     return u;
 }
 
-// ---- barriers: every wait ends, after kWaitLimit tries with the CTA's abort flag set ----
+// ---- barriers: every wait ends, after abort[1] tries with the CTA's abort flag, abort[0], set ----
 
 __device__ __forceinline__ void bar_init(unsigned bar, unsigned count)
 {
@@ -134,17 +139,26 @@ __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity)
 }
 __device__ __noinline__ bool bar_wait_slow(unsigned bar, unsigned parity, volatile int *abort)
 {
-    for (unsigned i = 0; i < kWaitLimit; ++i) {
+    const int limit = abort[1];
+    for (int i = 0; i < limit; ++i) {
         if (bar_try(bar, parity))
             return true;
-        if (*abort)
+        if (abort[0])
             return false;
     }
-    *abort = 1;
+    abort[0] = 1;
     return false;
 }
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile int *abort)
 {
+#ifdef CSTR_TESTING
+    if (abort[1] == 0) {                         // one look, without the pause of a try
+        unsigned ok;
+        asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}\n"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        return ok || bar_wait_slow(bar, parity, abort);
+    }
+#endif
     return bar_try(bar, parity) || bar_wait_slow(bar, parity, abort);
 }
 
@@ -198,6 +212,14 @@ __device__ __forceinline__ void tmem_wait_ld(float (&r)[32])
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 1 in one lane of the warp, the same one every time
+__device__ __forceinline__ unsigned elected()
+{
+    unsigned leader;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(leader));
+    return leader;
+}
 
 // The products are issued by one lane (`leader`) of a warp that runs through the loop as a whole:
 // every operand is then the same in all lanes and stays in the uniform registers that the
@@ -291,7 +313,8 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     __shared__ __align__(8) unsigned long long s_bar[2 * kSlots + 12];
     __shared__ float2 s_ml[kTile];               // second stream's maximum and sum, one-tile segments
     __shared__ unsigned s_tmem;
-    __shared__ int s_abort;
+    __shared__ int s_abort[2];                   // a wait has run out; tries of a wait
+    __shared__ unsigned s_copies;                // tiles that were sent for (in shared memory, not in everyone's registers)
     const unsigned raw = smem_addr(smem_raw);
     const unsigned q_tile = (raw + 1023u) & ~1023u;              // [2][kTile][DP], swizzled
     const unsigned ring = q_tile + 2 * S::kTileBytes;
@@ -305,9 +328,10 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     auto o_full = [&](int s) { return q_full + 8u * (5 + s); };
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    volatile int *abort = &s_abort;
+    volatile int *abort = s_abort;
     if (tid == 0) {
-        s_abort = 0;
+        s_abort[0] = 0;
+        s_abort[1] = p.wait_limit;
         for (int i = 0; i < kSlots; ++i) {
             bar_init(full(i), 1);
             bar_init(empty(i), 1);
@@ -362,18 +386,18 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     Segment g;
     if (warp == 0) {
         if (lane == 0) {                                         // copies
-            unsigned count = 0;
+            unsigned copies = 0;
             bool alive = true;
             auto put = [&](const CUtensorMap *map, int key_tile, int head) {
-                const int slot = count % kSlots;
-                alive = alive && bar_wait(empty(slot), ((count / kSlots) & 1u) ^ 1u, abort);
+                const int slot = copies % kSlots;
+                alive = alive && bar_wait(empty(slot), ((copies / kSlots) & 1u) ^ 1u, abort);
                 if (!alive)
                     return;
                 bar_expect(full(slot), S::kTileBytes);
 #pragma unroll
                 for (int x = 0; x < DP / 64; ++x)
                     tma_tile(ring + slot * S::kTileBytes + x * (kTile * 128), map, x * 64, key_tile * kTile, head, full(slot));
-                ++count;
+                ++copies;
             };
             while (alive && walk.next(g)) {
                 const int head = g.item / p.pairs;
@@ -386,9 +410,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                         put(&map_k, g.tile0 + i + lead, head);
                 }
             }
-            if (*abort)                                          // let the copies in flight land
-                for (unsigned i = count > kSlots ? count - kSlots : 0; i < count; ++i)
-                    for (unsigned k = 0; k < kWaitLimit && !bar_try(full(i % kSlots), (i / kSlots) & 1u); ++k) {}
+            s_copies = copies;
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -397,8 +419,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         constexpr unsigned idesc = (1u << 4) | (type << 7) | (type << 10) | ((kTile / 16) << 24);
         const unsigned idesc_s = idesc | ((kTile / 8) << 17) | p.negate;
         constexpr unsigned idesc_o = idesc | (1u << 16) | ((DP / 8) << 17);
-        unsigned leader;
-        asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(leader));
+        const unsigned leader = elected();
         unsigned base = 0, seg = 0, p_count[2] = {0, 0};
         bool alive = true;
         auto wait = [&](unsigned bar, unsigned parity) {
@@ -459,10 +480,6 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
                     scores(n + 2);
             }
             base += 2 * g.tiles;
-        }
-        if (*abort) {                                            // let the products in flight end
-            commit(leader, drain);
-            for (unsigned k = 0; k < kWaitLimit && !bar_try(drain, 0); ++k) {}
         }
         __syncwarp();
     } else if (warp < 4) {                                       // query tiles, by two warps
@@ -659,8 +676,20 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         }
     }
     __syncthreads();
-    if (tid == 0 && s_abort)
-        atomicAdd(p.status, 1);
+    if (abort[0]) {                              // (nobody sets it any more)
+        // No role waits for what it has in flight when another one gives up, so it ends here, before the
+        // CTA leaves its shared and tensor memory.
+        if (tid == 0) {
+            const unsigned copies = s_copies;
+            for (unsigned i = copies > kSlots ? copies - kSlots : 0; i < copies; ++i)
+                for (int k = 0; k < kWaitLimit && !bar_try(full(i % kSlots), (i / kSlots) & 1u); ++k) {}
+            atomicAdd(p.status, 1);
+        } else if (warp == 1) {
+            commit(elected(), drain);
+            for (int k = 0; k < kWaitLimit && !bar_try(drain, 0); ++k) {}
+        }
+        __syncthreads();
+    }
     if (warp == 2) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
@@ -763,6 +792,10 @@ int cstr_launch_prefix(const cstr_cache &c, const cstr_row_args &a, cudaStream_t
     p.tiles = s.tiles;
     p.pairs = s.pairs;
     p.grid = s.grid;
+    p.wait_limit = kWaitLimit;
+#ifdef CSTR_TESTING
+    p.wait_limit = g_test_wait_limit;
+#endif
     p.negate = a.scale_log2 < 0.f ? 1u << 13 : 0u;
     // A scale of 0 would turn the -infinity of keys past the prompt's end into NaN.  2^-126 in its place
     // leaves every weight at 1 to 2^-26 for scores below 2^100.
@@ -772,3 +805,13 @@ int cstr_launch_prefix(const cstr_cache &c, const cstr_row_args &a, cudaStream_t
         return wide ? launch<__nv_bfloat16, 128>(c, p, stream) : launch<__nv_bfloat16, 64>(c, p, stream);
     return wide ? launch<__half, 128>(c, p, stream) : launch<__half, 64>(c, p, stream);
 }
+
+#ifdef CSTR_TESTING
+extern "C" int cstr_test_set_wait_limit(int32_t tries)
+{
+    if (tries < -1)
+        return cstr_fail(CSTR_ERR_ARG, "cstr_test_set_wait_limit: tries = %d, need -1 or more", tries);
+    g_test_wait_limit = tries < 0 ? kWaitLimit : tries;
+    return CSTR_OK;
+}
+#endif

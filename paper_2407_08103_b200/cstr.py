@@ -39,7 +39,7 @@ EXPORTS = [
 ]
 
 # entry points of the checking build only (include/cstr_debug.h)
-DEBUG_EXPORTS = ["cstr_debug_bounds_status", "cstr_test_set_group_hash_bits"]
+DEBUG_EXPORTS = ["cstr_debug_bounds_status", "cstr_test_set_group_hash_bits", "cstr_test_set_wait_limit"]
 
 _lib = None
 _libs = {}            # path -> loaded library
@@ -113,6 +113,14 @@ def cstr_test_set_group_hash_bits(bits: int) -> None:
     if not getattr(L, "is_check_build", False):
         raise RuntimeError("cstr_test_set_group_hash_bits needs the checking build")
     _check(L.cstr_test_set_group_hash_bits(ctypes.c_int32(bits)))
+
+
+def cstr_test_set_wait_limit(tries: int) -> None:
+    """Checking build only: tries of a bounded wait of the attention over the prompt (-1: the usual)."""
+    L = lib()
+    if not getattr(L, "is_check_build", False):
+        raise RuntimeError("cstr_test_set_wait_limit needs the checking build")
+    _check(L.cstr_test_set_wait_limit(ctypes.c_int32(tries)))
 
 
 def _check(rc):

@@ -193,3 +193,27 @@ def test_half_precision_keeps_small_probabilities(x, P, B):
     # multiples of 2^-24 below 2^-14, and enter the product multiplied by 2^7 at least
     tol = want * (2.0 ** -10 + 2.0 ** (x - 32) + 2.0 ** -14)
     assert np.abs(f8(c.out) - want).max() <= tol
+
+
+# one tile of query rows and two; the waits of the attention over the prompt get no second try
+@pytest.mark.parametrize("B,dim", [(3, 64), (70, 128)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_waits_that_run_out_are_counted_and_leave_the_device_usable(dtype, B, dim):
+    cstr.use_check_library(True)
+    try:
+        c = AttentionCase(70, B, 1, 8, 2, dim, 2000, 20, dtype, weights=False)
+        c.run()
+        want, lse = c.out.clone(), c.lse.clone()
+        assert cstr.cstr_cache_status(c.cache) == 0
+        cstr.cstr_test_set_wait_limit(0)
+        try:
+            for _ in range(3):
+                cstr.cstr_cache_attention(c.cache, c.q, c.out, lse_out=c.lse)
+                assert cstr.cstr_cache_status(c.cache) > 0
+        finally:
+            cstr.cstr_test_set_wait_limit(-1)
+        cstr.cstr_cache_attention(c.cache, c.q, c.out, lse_out=c.lse)
+        assert cstr.cstr_cache_status(c.cache) == 0
+        assert torch.equal(c.out, want) and torch.equal(c.lse, lse)
+    finally:
+        cstr.use_check_library(False)
