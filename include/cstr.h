@@ -603,7 +603,8 @@ int cstr_cache_attention(cstr_cache_t *cache, const void *q, const int64_t *q_st
 
 /*
  * Thread blocks of cstr_cache_attention calls since the last status call whose
- * bounded waits gave up (the outputs are then not valid; never expected: 0).
+ * bounded waits gave up (never expected: 0).  The rows and heads that such a
+ * block worked for get NaN in out, in lse_out and in the weights they add to.
  * Synchronises cuda_stream, then resets the count.
  */
 int cstr_cache_status(cstr_cache_t *cache, void *cuda_stream, int64_t *gave_up);

@@ -688,6 +688,12 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
             commit(elected(), drain);
             for (int k = 0; k < kWaitLimit && !bar_try(drain, 0); ++k) {}
         }
+        // its parts become NaN, and with them their rows' outputs: what an earlier call left in their
+        // place must not pass for an answer
+        Walk again(p);
+        while (again.next(g))
+            for (int r = tid; r < g.rows; r += kThreads)
+                p.part_ml[(((long long)blockIdx.x + g.item) * 2 + r / kTile) * kTile + r % kTile] = make_float2(0.f, CUDART_NAN_F);
         __syncthreads();
     }
     if (warp == 2) {

@@ -217,3 +217,29 @@ def test_waits_that_run_out_are_counted_and_leave_the_device_usable(dtype, B, di
         assert torch.equal(c.out, want) and torch.equal(c.lse, lse)
     finally:
         cstr.use_check_library(False)
+
+
+@pytest.mark.parametrize("B,dim", [(3, 64), (70, 128), (300, 64)])
+def test_no_answer_comes_of_a_block_that_gave_up(B, dim):
+    # what the call before left in the scratch is not taken for this call's parts
+    cstr.use_check_library(True)
+    try:
+        c = AttentionCase(71, B, 1, 8, 2, dim, 2000, 20, BF, weights=False)
+        other = c.q.clone().neg_()
+        c.run()
+        right, right_lse = c.out.clone(), c.lse.clone()
+        cstr.cstr_cache_attention(c.cache, other, c.out)   # (its parts are what would be left)
+        cstr.cstr_test_set_wait_limit(0)
+        try:
+            for _ in range(5):
+                c.out.zero_()
+                c.lse.zero_()
+                cstr.cstr_cache_attention(c.cache, c.q, c.out, lse_out=c.lse)
+                assert cstr.cstr_cache_status(c.cache) > 0
+                lost = c.lse.isnan()
+                assert lost.any() and (c.out.isnan().all(-1) == lost).all()
+                assert torch.equal(c.out[~lost], right[~lost]) and torch.equal(c.lse[~lost], right_lse[~lost])
+        finally:
+            cstr.cstr_test_set_wait_limit(-1)
+    finally:
+        cstr.use_check_library(False)
