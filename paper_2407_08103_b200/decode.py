@@ -139,5 +139,6 @@ class SharedPromptCache:
                                    stream=stream)
             cstr.cstr_cache_attention(self.handle, q, out, scale=scale, n_query=n_new, accumulate=True,
                                       pos=self.pos if tokens > 1 else None, stream=stream)
-            self.pos += tokens if n_new is None else n_new
+            # (n_new as the kernels take it)
+            self.pos += tokens if n_new is None else n_new.flatten()[:self.batch].clamp(0, tokens)
         return out
