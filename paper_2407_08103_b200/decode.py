@@ -128,10 +128,23 @@ class SharedPromptCache:
         self.lens.zero_()
         self.pos.zero_()
 
+    def _check_step(self, q, k, v, scale):
+        """What the attention would refuse only after the insertion has taken place."""
+        if not q.dim() == k.dim() == v.dim() == 4 or not 1 <= q.shape[1] == k.shape[1] == v.shape[1]:
+            raise ValueError("q, k and v must be [B][T][heads][D] of the same T >= 1")
+        address, strides = cstr._tokens_arg("q", q, self.handle, q.shape[1], self.handle.n_heads)
+        if address % 16 or any(s % 8 or abs(s) > 1 << 33 for s in strides[:3]):
+            raise ValueError("q must start on 16 bytes, with strides that are multiples of 8 up to 2^33")
+        scale = self.handle.head_dim ** -0.5 if scale is None else float(scale)
+        if not abs(scale) <= torch.finfo(torch.float32).max:
+            raise ValueError("scale is not a finite float32")
+        return scale
+
     def step(self, q, k, v, n_new=None, scale=None, stream=None):
         """Put the new tokens' ``k`` / ``v`` ``[B][T][n_kv_heads][D]`` into the rows' caches and return
         the attention of ``q`` ``[B][T][n_heads][D]`` over the prompt and the caches.  ``n_new`` int32
         ``[B]``: tokens that a row really has (a finished row has 0); None: all ``T``."""
+        scale = self._check_step(q, k, v, scale)
         tokens = q.shape[1]
         with torch.cuda.stream(stream or torch.cuda.current_stream(self.pos.device)):   # (its memory, too)
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
