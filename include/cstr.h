@@ -555,8 +555,9 @@ void cstr_free_cache(cstr_cache_t *cache);
  * key / value head, with n = n_new[b] tokens and len = lens[b]:
  *   evicted   the max(0, len + n - budget) first entries in the order
  *             (protected, weight, slot), protected = age >= pos[b] + n - recent:
- *             the row's last `recent` tokens, the new ones among them; a NaN
- *             weight comes before every other
+ *             the row's last `recent` tokens, the new ones among them, which go
+ *             last and by slot alone; among the others a NaN weight comes before
+ *             every other, and -0 counts as 0
  *   new length  min(len + n, budget)
  *   moves     old entries that stay but lie past the new length, then the new
  *             tokens, take the free slots below it (evicted ones, or at and past

@@ -9,7 +9,7 @@ import torch
 from oracle import operators as ref
 from paper_2407_08103_b200 import cstr
 
-from operator_cases import DEV, AttentionCase, f8, random_cache, ranked_ages
+from operator_cases import DEV, AttentionCase, check_insert, f8, random_cache, ranked_ages
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -243,3 +243,17 @@ def test_no_answer_comes_of_a_block_that_gave_up(B, dim):
             cstr.cstr_test_set_wait_limit(-1)
     finally:
         cstr.use_check_library(False)
+
+
+# one entry to evict or several, by a warp and by a block
+@pytest.mark.parametrize("T,budget", [(1, 40), (1, 30), (3, 38), (0, 20), (70, 3000)])
+def test_protected_entries_that_have_to_go_do_so_by_slot(T, budget):
+    rng = np.random.default_rng(T)
+    cap = 3000 if T == 70 else 40
+    lens = np.array([cap, cap - 1, budget], np.int32)
+    ck, cv = random_cache(rng, 3, 2, 16, cap, None)
+    k, v = random_cache(rng, 3, 2, 16, T, None) if T else (None, None)
+    age = ranked_ages(rng, lens, 2, cap)
+    pos = np.array([5, 0, 8], np.int32)                    # entries at and past it count as recent
+    w = rng.random((3, 2, cap)).astype(np.float32)
+    check_insert(rng, ck, cv, w, age, lens, k, v, pos, budget, 2)
