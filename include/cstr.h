@@ -540,7 +540,9 @@ int cstr_step_static(const cstr_table_t *const *tables, int32_t n_tables,
  * Strides count elements and are multiples of 8, and arrays of keys and values
  * start on 16 bytes (else CSTR_ERR_SHAPE); the head_dim elements are adjacent.
  * The caller keeps the arrays; slots at and past lens[b] are never read.  A handle
- * serves one stream at a time.  Allocates device memory.
+ * serves one stream at a time.  Allocates device memory: behind a prompt 528 bytes
+ * (head_dim up to 64: 272) for each of batch x max_tokens x n_heads queries and 20 MB;
+ * with weight and age 8 bytes a slot and head where cap is up to 2,048 or above 24,576.
  */
 int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, int32_t n_kv_heads,
                       int32_t head_dim, int32_t max_tokens, const void *prefix_k,
@@ -585,7 +587,9 @@ int cstr_cache_insert(cstr_cache_t *cache, const void *k_new, const void *v_new,
  * (pos NULL: all; else age[b][.][j] <= pos[b] + t, so that drafted tokens do not
  * see later ones):
  *   lse = log sum_x exp(scale q.k_x),   out = sum_x exp(scale q.k_x - lse) v_x
- * accumulated in 32 bits, rounded once.  A token that sees nothing, and every
+ * with sums, maxima and weights in 32 bits; the exponentials enter the second
+ * product rounded to dtype (their sum holds them unrounded), and out is rounded
+ * to it once more.  A token that sees nothing, and every
  * token t >= n_query[b], gets out = 0 and lse = -infinity; what lies in keys and
  * values that a token does not see (NaN, infinity) does not reach it.
  *   q, out        DEVICE [batch][n_tokens][n_heads][head_dim]; strides HOST int64 [3]: row,

@@ -474,7 +474,7 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
     p.oob = CSTR_OOB_RECORD();
     p.wide = c.cap % 4 == 0 && aligned16(c.weight) && aligned16(c.age);
     const unsigned items = (unsigned)(c.batch * c.n_kv_heads);
-    if (a.tokens == 1 && c.cap <= 2048) {
+    if (a.tokens == 1 && c.cap <= CSTR_INSERT_WARP_SLOTS) {
         p.bits = 8;
         return cstr_launch(cache_insert_kernel<true>, (items + 3) / 4, 128, 1, 4 * (4 << p.bits), stream, p);
     } else {
@@ -574,7 +574,7 @@ extern "C" int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, 
         e = cudaMalloc((void **)&c->ticket, (size_t)batch * 4);
     if (e == cudaSuccess)
         e = cudaMalloc((void **)&c->status, 4);
-    if (e == cudaSuccess && weight && age)
+    if (e == cudaSuccess && weight && age && (cap <= CSTR_INSERT_WARP_SLOTS || cap > CSTR_INSERT_SMEM_SLOTS))
         e = cudaMalloc((void **)&c->list, (size_t)batch * n_kv_heads * cap * 8);
     // zeroed before the handle is out, whatever stream it is used on and whatever the default stream has queued
     cudaStream_t own = nullptr;

@@ -115,3 +115,6 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
 // Largest cap whose keys and places fit the insert kernel's shared memory (8 bytes a slot beside
 // 8 KB of bins).
 #define CSTR_INSERT_SMEM_SLOTS 24576
+// Largest cap whose single tokens a warp per item inserts; where it has more than one entry to evict
+// (a shrinking row), its keys and places are in scratch, too.
+#define CSTR_INSERT_WARP_SLOTS 2048

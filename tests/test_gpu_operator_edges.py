@@ -257,3 +257,17 @@ def test_protected_entries_that_have_to_go_do_so_by_slot(T, budget):
     pos = np.array([5, 0, 8], np.int32)                    # entries at and past it count as recent
     w = rng.random((3, 2, cap)).astype(np.float32)
     check_insert(rng, ck, cv, w, age, lens, k, v, pos, budget, 2)
+
+
+@pytest.mark.parametrize("cap,scratch", [(2048, True), (2049, False), (24576, False), (24577, True)])
+def test_scratch_of_the_insertion_only_where_it_is_used(cap, scratch):
+    B, Hk = (64 << 20) // (cap * 4 * 8), 4                 # 64 MB of it
+    ck = torch.zeros(8, dtype=BF, device=DEV).expand(B, cap, Hk, 8)      # (not read)
+    w, age = torch.zeros(B, Hk, cap, device=DEV), torch.zeros(B, Hk, cap, dtype=torch.int32, device=DEV)
+    lens = torch.zeros(B, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    cache = cstr.cstr_cache_create(ck, ck, lens, Hk, weight=w, age=age)
+    used = before - torch.cuda.mem_get_info()[0]
+    cache.close()
+    assert (used > 48 << 20) == scratch, used
