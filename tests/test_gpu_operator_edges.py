@@ -1,4 +1,5 @@
 """Edges of the cache and loss operators at which a call once went wrong."""
+import ctypes
 import math
 import threading
 
@@ -9,7 +10,7 @@ import torch
 from oracle import operators as ref
 from paper_2407_08103_b200 import cstr
 
-from operator_cases import DEV, AttentionCase, check_insert, f8, random_cache, ranked_ages
+from operator_cases import DEV, AttentionCase, check_insert, check_loss, f8, random_cache, ranked_ages
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -271,3 +272,56 @@ def test_scratch_of_the_insertion_only_where_it_is_used(cap, scratch):
     used = before - torch.cuda.mem_get_info()[0]
     cache.close()
     assert (used > 48 << 20) == scratch, used
+
+
+# many new tokens at once: several passes of 32 query rows over the slots, tiles of 128 that start within a row
+@pytest.mark.parametrize("B,T,Hq,Hk,D,P,cap", [(2, 33, 2, 1, 64, 0, 300), (1, 64, 4, 2, 128, 700, 90), (2, 129, 2, 2, 64, 130, 400),
+                                               (1, 256, 4, 1, 128, 600, 1500), (3, 65, 8, 1, 40, 513, 70)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_attention_of_a_long_new_input(dtype, B, T, Hq, Hk, D, P, cap):
+    c = AttentionCase(80, B, T, Hq, Hk, D, P, cap, dtype, causal=True, lens=[cap] + [max(T, cap - 5)] * (B - 1),
+                      n_query=[T] + [T // 2 + 1] * (B - 1))
+    c.run()
+    c.check()
+    assert cstr.cstr_cache_status(c.cache) == 0
+
+
+# long prompts of few key / value heads
+@pytest.mark.parametrize("B,T,Hq,Hk,D,P", [(1, 1, 8, 1, 128, 30000), (16, 1, 8, 1, 64, 9000), (2, 2, 16, 2, 128, 20001), (40, 1, 8, 2, 64, 6000)])
+def test_attention_of_few_heads_over_a_long_prompt(B, T, Hq, Hk, D, P):
+    c = AttentionCase(81, B, T, Hq, Hk, D, P, 12, BF, causal=T > 1)
+    c.run()
+    c.check()
+    assert cstr.cstr_cache_status(c.cache) == 0
+
+
+def test_prompts_that_the_copy_engine_cannot_read():
+    # one head's keys for all heads (a stride of 0), and tokens stored last to first (a negative one)
+    c = AttentionCase(82, 3, 1, 8, 2, 64, 700, 20, BF)
+    c.pk = c.pk[:, :1].expand(700, 2, 64)
+    c.run()
+    c.check()
+    c = AttentionCase(83, 3, 2, 8, 2, 64, 700, 20, HF, causal=True)
+    pk, pv = c.pk.flip(0).contiguous(), c.pv.flip(0).contiguous()
+    out = ctypes.c_void_p()
+    at = lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    cstr._check(cstr.lib().cstr_cache_create(
+        2, 3, 8, 2, 64, 2, at(pk[-1]), at(pv[-1]), ctypes.c_int64(700), (ctypes.c_int64 * 4)(-128, 64, -128, 64),
+        at(c.ck), at(c.cv), 20, (ctypes.c_int64 * 6)(*c.ck.stride()[:3], *c.cv.stride()[:3]),
+        at(c.d_w), at(c.d_age), at(c.d_lens), ctypes.byref(out)))
+    cache = cstr.Cache(out)
+    c.run()                                                # (a handle of the prompt in its usual order)
+    c.check()
+    cache.batch, cache.n_heads, cache.n_kv_heads, cache.head_dim = 3, 8, 2, 64
+    cache.dtype, cache.device, cache.strides = HF, c.ck.device, {}
+    c.d_w.copy_(torch.from_numpy(c.w0))
+    cstr.cstr_cache_attention(cache, c.q, c.out, pos=c.d_pos, accumulate=True, lse_out=c.lse)
+    c.check()
+
+
+@pytest.mark.parametrize("N,V", [(3, 1003), (5, 32000), (2, 128256)])
+def test_scoring_of_bfloat16_logits(N, V):
+    rng = np.random.default_rng(V)
+    x = torch.randn(N, V, generator=torch.Generator().manual_seed(V)).mul_(3.0).to(BF).to(DEV)
+    ok = np.ones((N, V), bool)
+    check_loss(x, ok, rng.integers(0, V, N), np.full(N, -9.0, np.float32), rng.standard_normal(N).astype(np.float32), gradient=False)
