@@ -687,11 +687,17 @@ extern "C" int cstr_cache_attention(cstr_cache_t *c, const void *q, const int64_
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     // On the tensor cores the prompt costs a launch and the join of its parts, about 10 us; in the row kernel
     // every row reads it by itself, from the L2 cache mostly, and few rows in a long serial chain each.
-    // So: from 512 tokens on, or where the rows read 16 MiB of it together.  Measured, tensor / row, 8 key /
-    // value heads: 4 x 128 tokens 10.5 / 9.4 us, 8 x 256 tokens 11.2 / 10.8, 16 x 256 (16 MiB) 11.8 / 11.9,
-    // 64 x 256 16.3 / 21.5, 4 x 512 11.1 / 12.0, 1 x 1,024 11.8 / 13.1, 64 x 4,096 34 / 217.
+    // So: from 512 tokens on, or where the rows read 16 MiB of it together, 32 MiB if they have no more than 8
+    // query rows for it.  Measured in us, tensor / row, head_dim 128:
+    //   8 query rows, 8 key / value heads: 4 x 512 tokens 12.2 / 12.9, 1 x 1,024 12.9 / 13.7, 64 x 256 17.3 / 22.5
+    //   (64 MiB); 2 heads: 64 x 256 (16 MiB) 16.6 / 12.7, 128 x 256 (32 MiB) 16.8 / 15.9, 256 x 256 17.3 / 22.5,
+    //   64 x 512 16.8 / 16.1, 64 x 1,024 17.2 / 22.7; 1 head: 128 x 384 (24 MiB) 21.3 / 13.6
+    //   16 query rows, 16 MiB: 128 x 1 head x 256 18.0 / 23.2, 16 x 8 x 256 18.2 / 23.6
+    // What the rule misses: one row of 16 to 32 query rows, 512 to 4,096 tokens (1 x 4,096 26.2 / 23.1, 39.0 / 32.9).
+    const long long reads = (long long)c->batch * c->n_kv_heads * c->prefix_len * c->head_dim * 4;
+    const bool narrow = (long long)n_tokens * (c->n_heads / c->n_kv_heads) <= 8;
     const bool tensor = c->has_maps && c->prefix_len >= 128 &&
-                        (c->prefix_len >= 512 || (long long)c->batch * c->n_kv_heads * c->prefix_len * c->head_dim * 4 >= 16 << 20);
+                        (c->prefix_len >= 512 || reads >= (narrow ? 32 << 20 : 16 << 20));
     if (tensor) {
         rc = cstr_launch_prefix(*c, a, stream);
         if (rc)

@@ -731,9 +731,12 @@ cstr_prefix_plan cstr_plan_prefix(const cstr_cache &c, int tokens)
     const long long units = (long long)c.n_kv_heads * s.pairs * s.tiles;
     // Every CTA leaves a part of up to 128 KB per row group that it works for, as much as two key tiles
     // read, and the row kernel has to join them.  So with two tiles of query rows a CTA gets two units
-    // (64 rows x 4,096 tokens 34.2 us, with one unit 35.7 us), but there is a CTA per row group at least.
-    // No row group gets more than 40 CTAs: the row kernel keeps a factor per part (same time without
-    // that limit, 39.2 us for 6 rows x 65,000 tokens).
+    // (64 rows x 32 / 8 heads, 4,096 tokens 34.2 us, with one unit 35.7 us; 64 rows x 4 tokens x 8 / 1 heads,
+    // 2,048: 26.3 / 38.1; only the shortest prompts lose, 64 rows x 16 / 2 heads, 1,024: 17.4 / 16.3), but there
+    // is a CTA per row group at least.  For the same reason no row group gets more than 40 CTAs, though one to
+    // three key / value heads leave SMs idle by that: 65,000 tokens, 8 query heads a key / value head, 1 row x
+    // 1 head 30.3 us, without the limit 47.2; 1 x 2 32.5 / 39.0; 4 rows x 4 tokens x 1 head 55.2 / 134.9,
+    // x 3 heads 66.0 / 79.4; from four heads on it does not act.
     const long long items = (long long)c.n_kv_heads * s.pairs;
     long long grid = rows > kTile ? (units + 1) / 2 : units;
     grid = grid < items ? items : grid;
