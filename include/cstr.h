@@ -581,6 +581,22 @@ int cstr_cache_insert(cstr_cache_t *cache, const void *k_new, const void *v_new,
                       const int32_t *pos, int32_t budget, int32_t recent, void *cuda_stream);
 
 /*
+ * Take tokens back: the entries whose age is pos[b] or more leave the rows'
+ * caches.  For drafted tokens that verification rejected (cstr_accept_draft):
+ * pos = position of the first rejected one, where the next token goes.
+ *   leaving   in every head of a row as many entries as the head with the most
+ *             such entries has; heads that an insertion since has evicted some
+ *             from lose their least attended entries instead (a NaN weight first)
+ *   new length  len - that number; surviving entries past it take the freed
+ *             slots in ascending order, every other entry keeps its slot
+ * What was evicted when the tokens came in does not come back.
+ *   pos           DEVICE int32 [batch]
+ * Needs weight and age (else CSTR_ERR_NULL).  Enqueues two kernels on cuda_stream;
+ * no allocation, no host synchronisation.
+ */
+int cstr_cache_truncate(cstr_cache_t *cache, const int32_t *pos, void *cuda_stream);
+
+/*
  * Attention of every row's newest tokens over the shared prompt and the row's
  * cache (which holds them already).  For row b, token t, head h, with the keys
  * k_x of the prompt and of the slots j < lens[b] that t may see

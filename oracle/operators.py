@@ -82,6 +82,30 @@ def insert(cache_k, cache_v, weight, age, lens, k_new, v_new, pos, budget, recen
     return ck, cv, w, a, ln
 
 
+def truncate(cache_k, cache_v, weight, age, lens, pos):
+    """Copies of (cache_k, cache_v, weight, age, lens) after the entries of age ``pos`` or more have left."""
+    ck, cv, w, a, ln = (np.array(x) for x in (cache_k, cache_v, weight, age, lens))
+    B, cap, Hk = ck.shape[:3]
+    for b in range(B):
+        old = min(max(int(lens[b]), 0), cap)
+        gone = max(int((age[b, c, :old] >= pos[b]).sum()) for c in range(Hk))
+        for c in range(Hk):
+            def order(j):
+                x = float(weight[b, c, j])
+                if age[b, c, j] >= pos[b]:
+                    return (0, 0.0, j)
+                return (1, 0.0, j) if x != x else (2, x, j)
+            out = set(sorted(range(old), key=order)[:gone])
+            movers = [j for j in range(old - gone, old) if j not in out]
+            free = [j for j in range(old - gone) if j in out]
+            assert len(movers) == len(free)
+            for j, dst in zip(movers, free):
+                ck[b, dst, c], cv[b, dst, c] = cache_k[b, j, c], cache_v[b, j, c]
+                w[b, c, dst], a[b, c, dst] = weight[b, c, j], age[b, c, j]
+        ln[b] = old - gone
+    return ck, cv, w, a, ln
+
+
 def policy_loss(logits, allowed, actions, old_logp, advantages, ref_logp=None, weight=None,
                 clip_low=0.2, clip_high=0.2, kl_coef=0.0, temperature=1.0):
     """float64 ``logits`` [N][V]; ``allowed`` bool [N][V] (a row of False: inactive).  Returns

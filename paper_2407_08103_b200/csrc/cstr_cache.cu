@@ -1,5 +1,6 @@
 // Key / value cache of a batch with a shared prompt: handle, argument checks,
-// and the insertion of new tokens with eviction by accumulated attention weight.
+// the insertion of new tokens with eviction by accumulated attention weight, and
+// the removal of tokens that are taken back.
 #include <math.h>
 #include <string.h>
 
@@ -33,6 +34,8 @@ namespace {
 //     4 x 8 of 20,000 8.6 us (10.4).  Keys in shared memory (or scratch, past 24,576:
 //     at 8,192 slots 69.5 us, at 2,304 32.6 us), the e-th smallest from counts per
 //     11-bit digit.
+// Tokens that are taken back leave by the same kernel, a CTA per item, with keys that put them first; a
+// kernel before it counts them per row (512 rows x 8 heads of 1,024 slots, three tokens: 17 us together).
 constexpr int kMaxThreads = 1024;
 constexpr int kMaxWarps = kMaxThreads / 32;
 
@@ -46,6 +49,7 @@ struct InsertParams {
     int32_t *age, *lens;
     const int32_t *n_new, *pos;
     unsigned int *ticket;
+    int32_t *gone;       // tokens taken back: entries that leave each row (null: insertion)
     int32_t *list;       // null: keys and places live in shared memory
     int B, Hk, D, cap, T, budget, recent;
     int bits;            // of a digit: 11 (8 KB of bins) or 8 (1 KB, for CTAs that hardly ever count)
@@ -65,11 +69,21 @@ __device__ __forceinline__ unsigned evict_key(float w, int age, int protect_from
 
 constexpr unsigned kZeroKey = 0x80000000u;    // evict_key of weight 0
 
-// f(slot, key) for the slots [0, len) of a row, each by one of `step` threads
-template <typename F>
+// Tokens taken back: entries of age `from` or more are the first to leave.
+__device__ __forceinline__ unsigned back_key(float w, int age, int from)
+{
+    return age >= from ? 0u : max(evict_key(w, age, INT_MAX), 1u);      // (INT_MAX is `from` or more)
+}
+
+// f(slot, key) for the slots [0, len) of a row, each by one of `step` threads; BACK: the keys of back_key, with
+// `from` in the place of protect_from
+template <bool BACK, typename F>
 __device__ __forceinline__ void for_keys(const InsertParams &p, const float *weight, const int32_t *age, int len,
                                          int protect_from, int tid, int step, F f)
 {
+    auto evict_key = [](float w, int age, int limit) {
+        return BACK ? back_key(w, age, limit) : ::evict_key(w, age, limit);
+    };
     if (p.wide) {
 #pragma unroll 1
         for (int j0 = tid * 4; j0 < len; j0 += step * 16) {       // eight loads in flight
@@ -184,7 +198,7 @@ __device__ __forceinline__ int list_places(const InsertParams &p, const unsigned
 // returned limit and the first `want` (in slot order) of the `equal` ones at it; where all of these
 // belong to them, the limit may be any larger key below the next one.  Counts per digit of p.bits
 // bits, the most significant first (that one while the row is read).
-template <bool WARP>
+template <bool WARP, bool BACK>
 __device__ __forceinline__ unsigned select_by_digits(const InsertParams &p, const float *weight, const int32_t *age,
                                                      int protect_from, unsigned *keys, int *s_bin, int *s_word,
                                                      int len, int evict, int &want, int &equal)
@@ -219,7 +233,7 @@ __device__ __forceinline__ unsigned select_by_digits(const InsertParams &p, cons
                 atomicAdd(&s_bin[(k >> shift) & digits], 1);
         };
         if (left == 32) {
-            for_keys(p, weight, age, len, protect_from, tid, step, [&](int j, unsigned k) {
+            for_keys<BACK>(p, weight, age, len, protect_from, tid, step, [&](int j, unsigned k) {
                 keys[j] = k;
                 count(k);
             });
@@ -289,7 +303,8 @@ __device__ __forceinline__ unsigned select_by_digits(const InsertParams &p, cons
     return prefix;
 }
 
-template <bool WARP>
+// BACK: no new tokens; p.gone[row] entries leave, those of age p.pos[row] or more first
+template <bool WARP, bool BACK>
 __global__ void __launch_bounds__(WARP ? 128 : kMaxThreads, WARP ? 8 : 1)
 cache_insert_kernel(const __grid_constant__ InsertParams p)
 {
@@ -306,11 +321,11 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
         return;                                                   // (a whole warp; no CTA barrier follows)
     const int b = item / p.Hk, kh = item - b * p.Hk;
     const int len = min(max(p.lens[b], 0), p.cap);
-    const int n = p.n_new ? min(max(p.n_new[b], 0), p.T) : p.T;
+    const int n = BACK ? 0 : p.n_new ? min(max(p.n_new[b], 0), p.T) : p.T;
     const int pos = p.pos[b];
-    const int new_len = min(len + n, p.budget);
+    const int new_len = BACK ? len - p.gone[b] : min(len + n, p.budget);
     const int evict = len + n - new_len;
-    const int protect_from = pos + n - p.recent;
+    const int protect_from = BACK ? pos : pos + n - p.recent;
     const long long entry0 = (long long)item * p.cap;
     float *weight = p.weight + entry0;
     int32_t *age = p.age + entry0;
@@ -333,14 +348,14 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
             }
         }
         int want, equal;
-        const unsigned limit = select_by_digits<WARP>(p, weight, age, protect_from, keys, s_bin, s_word, len, evict,
+        const unsigned limit = select_by_digits<WARP, BACK>(p, weight, age, protect_from, keys, s_bin, s_word, len, evict,
                                                       want, equal);
         const int warps = WARP ? 1 : blockDim.x >> 5, span = ((len + warps - 1) / warps + 31) & ~31;
         const int lo = WARP ? 0 : min(warp * span, len), hi = min(lo + span, len);
         n_old = list_places<WARP>(p, keys, place, s_word, len, new_len, limit, want, equal == want, lo, hi);
     } else if (evict == 1) {
         unsigned long long least = ~0ull;
-        for_keys(p, weight, age, len, protect_from, tid, step, [&](int j, unsigned k) {
+        for_keys<BACK>(p, weight, age, len, protect_from, tid, step, [&](int j, unsigned k) {
             const unsigned long long at = ((unsigned long long)k << 32) | (unsigned)j;
             least = at < least ? at : least;
         });
@@ -432,6 +447,34 @@ cache_insert_kernel(const __grid_constant__ InsertParams p)
     }
 }
 
+// gone[row] = entries of age pos[row] or more in the head that has the most of them; a block per row
+__global__ void __launch_bounds__(256)
+cache_count_kernel(const __grid_constant__ InsertParams p)
+{
+    __shared__ int s_most[8];
+    cstr_wait_for_earlier_kernels();
+    cstr_let_next_kernel_start();
+    const int b = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int len = min(max(p.lens[b], 0), p.cap), pos = p.pos[b];
+    int most = 0;
+    for (int kh = warp; kh < p.Hk; kh += 8) {
+        const int32_t *age = p.age + ((long long)b * p.Hk + kh) * p.cap;
+        int n = 0;
+#pragma unroll 8
+        for (int j = lane; j < len; j += 32)
+            n += age[j] >= pos;
+        most = max(most, __reduce_add_sync(0xffffffffu, n));
+    }
+    if (lane == 0)
+        s_most[warp] = most;
+    __syncthreads();
+    if (warp == 0) {
+        most = __reduce_max_sync(0xffffffffu, lane < 8 ? s_most[lane] : 0);
+        if (lane == 0)
+            p.gone[b] = most;
+    }
+}
+
 int strides_ok(const char *what, const int64_t *s, int n)
 {
     for (int i = 0; i < n; ++i)
@@ -442,6 +485,27 @@ int strides_ok(const char *what, const int64_t *s, int n)
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+}  // namespace
+
+namespace {
+
+// a block per item
+template <bool BACK>
+int launch_blocks(const cstr_cache &c, InsertParams &p, unsigned items, cudaStream_t stream)
+{
+    const bool shared = c.cap <= CSTR_INSERT_SMEM_SLOTS;
+    if (shared)
+        p.list = nullptr;
+    p.bits = 11;
+    const int smem = (4 << p.bits) + (shared ? c.cap * 8 : 0);
+    static std::atomic<bool> allowed[64];
+    const int rc = cstr_allow_smem(cache_insert_kernel<false, BACK>, allowed, c.device,
+                                   (4 << p.bits) + CSTR_INSERT_SMEM_SLOTS * 8);
+    if (rc)
+        return rc;
+    return cstr_launch(cache_insert_kernel<false, BACK>, items, c.cap <= 4096 ? 256 : kMaxThreads, 1, smem, stream, p);
+}
 
 }  // namespace
 
@@ -474,22 +538,16 @@ int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStrea
     p.oob = CSTR_OOB_RECORD();
     p.wide = c.cap % 4 == 0 && aligned16(c.weight) && aligned16(c.age);
     const unsigned items = (unsigned)(c.batch * c.n_kv_heads);
+    if (a.back) {
+        p.gone = c.gone;
+        const int rc = cstr_launch(cache_count_kernel, c.batch, 256, 1, 0, stream, p);
+        return rc ? rc : launch_blocks<true>(c, p, items, stream);
+    }
     if (a.tokens == 1 && c.cap <= CSTR_INSERT_WARP_SLOTS) {
         p.bits = 8;
-        return cstr_launch(cache_insert_kernel<true>, (items + 3) / 4, 128, 1, 4 * (4 << p.bits), stream, p);
-    } else {
-        const bool shared = c.cap <= CSTR_INSERT_SMEM_SLOTS;
-        if (shared)
-            p.list = nullptr;
-        p.bits = 11;
-        const int smem = (4 << p.bits) + (shared ? c.cap * 8 : 0);
-        static std::atomic<bool> allowed[64];
-        const int rc = cstr_allow_smem(cache_insert_kernel<false>, allowed, c.device,
-                                       (4 << p.bits) + CSTR_INSERT_SMEM_SLOTS * 8);
-        if (rc)
-            return rc;
-        return cstr_launch(cache_insert_kernel<false>, items, c.cap <= 4096 ? 256 : kMaxThreads, 1, smem, stream, p);
+        return cstr_launch(cache_insert_kernel<true, false>, (items + 3) / 4, 128, 1, 4 * (4 << p.bits), stream, p);
     }
+    return launch_blocks<false>(c, p, items, stream);
 }
 
 extern "C" void cstr_free_cache(cstr_cache_t *c)
@@ -571,7 +629,8 @@ extern "C" int cstr_cache_create(int32_t dtype, int32_t batch, int32_t n_heads, 
     if (e == cudaSuccess)
         e = cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
     if (e == cudaSuccess)
-        e = cudaMalloc((void **)&c->ticket, (size_t)batch * 4);
+        e = cudaMalloc((void **)&c->ticket, (size_t)batch * 8);
+    c->gone = (int32_t *)(c->ticket + batch);
     if (e == cudaSuccess)
         e = cudaMalloc((void **)&c->status, 4);
     if (e == cudaSuccess && weight && age && (cap <= CSTR_INSERT_WARP_SLOTS || cap > CSTR_INSERT_SMEM_SLOTS))
@@ -640,6 +699,22 @@ extern "C" int cstr_cache_insert(cstr_cache_t *c, const void *k_new, const void 
     a.pos = pos;
     a.budget = budget;
     a.recent = recent;
+    return cstr_launch_insert(*c, a, (cudaStream_t)cuda_stream);
+}
+
+extern "C" int cstr_cache_truncate(cstr_cache_t *c, const int32_t *pos, void *cuda_stream)
+{
+    if (!c || !pos)
+        return cstr_fail(CSTR_ERR_NULL, "cstr_cache_truncate: null pointer");
+    if (!c->weight || !c->age)
+        return cstr_fail(CSTR_ERR_NULL, "cstr_cache_truncate: the cache was created without weight or age");
+    const int rc = cstr_check_device(c->device, "cache");
+    if (rc)
+        return rc;
+    cstr_insert_args a;
+    memset(&a, 0, sizeof a);
+    a.pos = pos;
+    a.back = 1;
     return cstr_launch_insert(*c, a, (cudaStream_t)cuda_stream);
 }
 

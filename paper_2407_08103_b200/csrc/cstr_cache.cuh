@@ -48,6 +48,7 @@ struct cstr_cache {
     int32_t *age;        // DEVICE [batch][n_kv_heads][cap] or null
     int32_t *lens;       // DEVICE [batch]
     unsigned int *ticket;   // DEVICE [batch]: arrivals of a row's insert CTAs, left zero by each call
+    int32_t *gone;          // DEVICE [batch], behind ticket: entries that a truncation takes from each row
     // attention of the whole batch over the prompt on the tensor cores (cstr_prefix.cu)
     int has_maps;        // the copy engine can read the prompt: maps and scratch below are there
     alignas(64) unsigned char map_k[128], map_v[128];     // tensor maps of prefix_k, prefix_v
@@ -109,6 +110,7 @@ struct cstr_insert_args {
     int32_t tokens;
     const int32_t *n_new, *pos;
     int32_t budget, recent;
+    int32_t back;        // no insertion: entries of age pos or more leave
 };
 int cstr_launch_insert(const cstr_cache &c, const cstr_insert_args &a, cudaStream_t stream);
 

@@ -33,8 +33,8 @@ EXPORTS = [
     "cstr_pda_workspace_create",
     "cstr_free_pda_workspace", "cstr_pda_step", "cstr_pda_step_history",
     "cstr_pda_accept_draft", "cstr_pda_step_status",
-    "cstr_cache_create", "cstr_free_cache", "cstr_cache_insert", "cstr_cache_attention",
-    "cstr_cache_status",
+    "cstr_cache_create", "cstr_free_cache", "cstr_cache_insert", "cstr_cache_truncate",
+    "cstr_cache_attention", "cstr_cache_status",
     "cstr_policy_loss",
 ]
 
@@ -71,6 +71,7 @@ def _load(path, debug):
         # called once per layer and decoding step: declared, so that plain ints can be passed
         ptr, i32, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
         L.cstr_cache_insert.argtypes = [ptr, ptr, ptr, ptr, i32, ptr, ptr, i32, i32, ptr]
+        L.cstr_cache_truncate.argtypes = [ptr, ptr, ptr]
         L.cstr_cache_attention.argtypes = [ptr, ptr, ptr, i32, ptr, ptr, f32, i32, ptr, ptr, ptr, ptr]
         L.cstr_policy_loss.argtypes = [ptr, i32, ptr, ptr, ptr, i32, ctypes.c_int64, i32, f32, ptr, ptr,
                                        ptr, ptr, ptr, f32, f32, f32, ptr, ptr, ptr, i32, ptr]
@@ -747,6 +748,15 @@ def cstr_cache_insert(cache: Cache, k_new, v_new, pos, budget: int, recent: int 
                                  budget, recent, _raw_stream(stream, cache.device))
     if rc:
         _check(rc)
+
+
+def cstr_cache_truncate(cache: Cache, pos, stream=None) -> None:
+    """Take tokens back: entries of age ``pos`` (int32 ``[B]``) or more leave the rows' caches."""
+    import torch
+    if pos is None:
+        raise ValueError("pos is required")
+    _check(lib().cstr_cache_truncate(cache.ptr, _rows_arg("pos", pos, cache.batch, cache.device, torch.int32),
+                                     _raw_stream(stream, cache.device)))
 
 
 def cstr_cache_attention(cache: Cache, q, out, scale: float | None = None, pos=None, n_query=None,

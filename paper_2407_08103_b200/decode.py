@@ -128,6 +128,13 @@ class SharedPromptCache:
         self.lens.zero_()
         self.pos.zero_()
 
+    def take_back(self, n, stream=None):
+        """Forget each row's newest ``n`` tokens (int32 ``[B]``): drafts that verification rejected.
+        Entries that were evicted for them do not come back."""
+        with torch.cuda.stream(stream or torch.cuda.current_stream(self.pos.device)):
+            self.pos.copy_((self.pos - n.flatten()[:self.batch].clamp(min=0)).clamp(min=0))
+            cstr.cstr_cache_truncate(self.handle, self.pos, stream=stream)
+
     def _check_step(self, q, k, v, scale):
         """What the attention would refuse only after the insertion has taken place."""
         if not q.dim() == k.dim() == v.dim() == 4 or not 1 <= q.shape[1] == k.shape[1] == v.shape[1]:

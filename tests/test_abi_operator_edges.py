@@ -20,3 +20,8 @@ def test_temperature_whose_reciprocal_overflows(lib, temperature):
     assert lib.cstr_policy_loss(None, 0, None, None, p, 0, 8, 8, temperature, p, p, None, p, None, 0.2, 0.2, 0.0,
                                 p, p, None, 2, None) == -2
     assert b"temperature" in lib.cstr_last_error()
+
+
+def test_truncation_of_nothing(lib):
+    p = ctypes.c_void_p(np.zeros(8, dtype=np.int64).ctypes.data)
+    assert lib.cstr_cache_truncate(None, p, None) == -1
