@@ -612,6 +612,7 @@ int cstr_cache_truncate(cstr_cache_t *cache, const int32_t *pos, void *cuda_stre
  *                 token, head (multiples of 8; 16-byte aligned); must not overlap
  *   n_tokens      1 .. max_tokens; n_query  DEVICE int32 [batch] or NULL: all n_tokens
  *   pos           DEVICE int32 [batch]: position of token 0, or NULL
+ *   scale         below 2.358e38 in size (its product with log2(e) is a float)
  *   accumulate    non-zero: weight[b][h / group][j] += exp(scale q.k_j - lse), summed over
  *                 the row's tokens and the heads of the group in a fixed order
  *   lse_out       DEVICE float [batch][n_tokens][n_heads] or NULL

@@ -732,8 +732,9 @@ extern "C" int cstr_cache_attention(cstr_cache_t *c, const void *q, const int64_
     if (n_tokens < 1 || n_tokens > c->max_tokens)
         return cstr_fail(CSTR_ERR_ARG, "cstr_cache_attention: n_tokens = %d, need 1..%d", n_tokens,
                          c->max_tokens);
-    if (!isfinite(scale))
-        return cstr_fail(CSTR_ERR_ARG, "cstr_cache_attention: scale is not finite");
+    const float scale_log2 = (float)((double)scale * 1.4426950408889634);
+    if (!isfinite(scale_log2))
+        return cstr_fail(CSTR_ERR_ARG, "cstr_cache_attention: scale x log2(e) = %g is not finite", scale_log2);
     int rc = strides_ok("cstr_cache_attention", q_strides, 3);
     if (!rc)
         rc = strides_ok("cstr_cache_attention", out_strides, 3);
@@ -757,7 +758,7 @@ extern "C" int cstr_cache_attention(cstr_cache_t *c, const void *q, const int64_
     a.tokens = n_tokens;
     a.pos = pos;
     a.n_query = n_query;
-    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.scale_log2 = scale_log2;
     a.accumulate = accumulate ? 1 : 0;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     // On the tensor cores the prompt costs a launch and the join of its parts, about 10 us; in the row kernel

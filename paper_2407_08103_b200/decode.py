@@ -143,8 +143,8 @@ class SharedPromptCache:
         if address % 16 or any(s % 8 or abs(s) > 1 << 33 for s in strides[:3]):
             raise ValueError("q must start on 16 bytes, with strides that are multiples of 8 up to 2^33")
         scale = self.handle.head_dim ** -0.5 if scale is None else float(scale)
-        if not abs(scale) <= torch.finfo(torch.float32).max:
-            raise ValueError("scale is not a finite float32")
+        if not abs(scale) < 2.358e38:             # (times log2(e) a float)
+            raise ValueError("scale is not finite or too large")
         return scale
 
     def step(self, q, k, v, n_new=None, scale=None, stream=None):

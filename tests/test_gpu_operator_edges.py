@@ -325,3 +325,12 @@ def test_scoring_of_bfloat16_logits(N, V):
     x = torch.randn(N, V, generator=torch.Generator().manual_seed(V)).mul_(3.0).to(BF).to(DEV)
     ok = np.ones((N, V), bool)
     check_loss(x, ok, rng.integers(0, V, N), np.full(N, -9.0, np.float32), rng.standard_normal(N).astype(np.float32), gradient=False)
+
+
+def test_a_scale_that_overflows_with_log2_e_is_refused():
+    c = AttentionCase(84, 2, 1, 4, 2, 64, 8, 10, BF)
+    c.run(scale=2.3e38)                                    # the largest ones are not
+    for scale in (2.5e38, -3.4e38):
+        with pytest.raises(cstr.CstrError) as e:
+            cstr.cstr_cache_attention(c.cache, c.q, c.out, scale=scale)
+        assert e.value.code == -2
