@@ -26,14 +26,14 @@ namespace {
 //   single tokens, up to 2,048 slots: a warp per item.  It evicts one entry (a
 //     decoding step with a full cache): the smallest (key, slot) pair, found
 //     while the row is read, without a barrier.  512 rows x 8 heads of 1,024 slots
-//     10.8 us (33.7 MB, 3.1 TB/s; a CTA per item 30.2 us), of 2,048 17.2 us (33.6);
-//     past that the CTA wins: 128 x 8 of 4,096 13.2 us, a warp 18.3 us;
+//     10.3 us (33.7 MB, 3.3 TB/s; a CTA per item 27.3 us), of 2,048 17.4 us (33.7);
+//     past that the CTA wins: 128 x 8 of 4,096 11.4 us, a warp 16.2 us;
 //   else a CTA per item, 256 threads up to 4,096 slots (so that several items share
-//     an SM), 1,024 beyond: 64 rows x 8 heads of 2,304 slots, 256 tokens 31.7 us (75 MB,
-//     2.4 TB/s; with 1,024 threads 43.4 us), of 8,192 slots 62.6 us (with 256 65.6 us),
-//     4 x 8 of 20,000 8.6 us (10.4).  Keys in shared memory (or scratch, past 24,576:
-//     at 8,192 slots 69.5 us, at 2,304 32.6 us), the e-th smallest from counts per
-//     11-bit digit.
+//     an SM), 1,024 beyond: 64 rows x 8 heads of 2,304 slots, 256 tokens 31.0 us (75 MB,
+//     2.4 TB/s; with 1,024 threads 43.8 us), of 8,192 slots 62.4 us (with 256 60.2 us),
+//     few rows of more, 4 x 8 of 20,000, 64 tokens 25.8 us (48.5).  Keys in shared memory
+//     (or scratch, past 24,576: at 8,192 slots 65.1 us, at 2,304 32.3 us), the e-th
+//     smallest from counts per 11-bit digit.
 // Tokens that are taken back leave by the same kernel, a CTA per item, with keys that put them first; a
 // kernel before it counts them per row (512 rows x 8 heads of 1,024 slots, three tokens: 17 us together).
 constexpr int kMaxThreads = 1024;

@@ -19,8 +19,9 @@
 //
 // Measured: 512 rows x 8 heads of up to 1,024 slots, head_dim 128, bf16, weights added
 // up, behind 128 prompt tokens: 256 us for 1.64 GB, 6.4 TB/s; behind 16,384 tokens it
-// joins the prefix kernel's parts as well (380 us together, of them 141 the prefix
-// kernel's).  Few rows: bound by one CTA's chain of chunks, hence the split.
+// joins the prefix kernel's parts as well (380 - 388 us together, of them 139 the prefix
+// kernel's).  Where ages decide what a token sees, looking for slots it does not see
+// costs 2.5 us of 269.  Few rows: bound by one CTA's chain of chunks, hence the split.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -11,8 +11,8 @@
 // Bound: the row is read from memory once and the gradient written once; the
 // second pass finds the row in the L2 cache.  For that the rows in flight have to
 // fit there: a cluster of up to 16 CTAs shares a row, 64 KB each (512 x 256,000
-// fp32: 242 us, 1.05 GB of DRAM traffic, 4.4 TB/s; with 8 CTAs of 128 KB 270 us; 2,048 x
-// 32,000 bf16 69 us, 3.9 TB/s, where 23 instructions an element weigh as much).  All 2,048
+// fp32: 241 us, 1.05 GB of DRAM traffic, 4.4 TB/s; with 8 CTAs of 128 KB 270 us; 2,048 x
+// 32,000 bf16 69 us, 3.9 TB/s, where 22 instructions an element weigh as much).  All 2,048
 // threads of an SM are used, at 32 registers, since what is left is the latency
 // of the passes and of the join between them.  Measured and dropped: the row held
 // in registers between the passes (344 us), and persistent CTAs with a ring of
@@ -207,8 +207,8 @@ __device__ __forceinline__ bool row_mask(const LossParams &p, int row, int a, co
 // The 16-byte vectors begin at the row's first aligned token; the tokens before and after them ("edge",
 // at most 2 (N - 1)) belong to the first threads of the first CTA.  WIDE is false where the rows of the
 // two buffers do not share their alignment: then every token is an edge token, dealt out over all threads.
-// kUnroll: vectors of a thread in flight; 2 where the logits are only read (300 x 128,256 fp32 36.7 us,
-// 4.2 TB/s; with one about 5 us more), 1 with a gradient (2,048 x 32,000 bf16, two: 6 us more, registers).
+// kUnroll: vectors of a thread in flight; 2 where the logits are only read (300 x 128,256 fp32 36.1 us,
+// 4.3 TB/s; with one about 5 us more), 1 with a gradient (2,048 x 32,000 bf16, two: 6 us more, registers).
 template <bool BF16, bool WIDE, int kUnroll>
 __global__ void __launch_bounds__(kThreads, 8)
 policy_loss_kernel(const __grid_constant__ LossParams p)

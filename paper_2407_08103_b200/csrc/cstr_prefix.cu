@@ -18,12 +18,12 @@
 // two warps bring the next row group's queries while the last one is finished.
 //
 // Split: the units (key tile x group of 256 query rows) are dealt out evenly and
-// contiguously to one CTA per SM, so a CTA starts or ends within a row group and
-// no SM idles in a last wave, whatever the sizes; each (CTA, row group) segment
+// contiguously, to one CTA per SM where there are enough, so a CTA starts or ends
+// within a row group and no SM idles in a last wave; each (CTA, row group) segment
 // leaves one part.
 //
 // Bound: at 512 rows x 4 heads a key / value head, 8 of these, 16,384 tokens, head_dim
-// 128, bf16 (137 GFLOP) it takes 141 us, 970 TFLOP/s; the tensor cores wait for the
+// 128, bf16 (137 GFLOP) it takes 139 us, 990 TFLOP/s; the tensor cores wait for the
 // chain scores -> probabilities -> second product of the two streams, about 3,300
 // cycles per 128 keys x 256 rows.  It is not the exponentials alone: taking 2 to 4
 // of 8 pairs of them on the multiply-add units instead was slower (+3 to +21 us).
