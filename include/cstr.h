@@ -631,6 +631,67 @@ int cstr_cache_attention(cstr_cache_t *cache, const void *q, const int64_t *q_st
  */
 int cstr_cache_status(cstr_cache_t *cache, void *cuda_stream, int64_t *gave_up);
 
+/* ------------------------------------- whole distributions under constraints */
+
+#define CSTR_MAX_ROW 8388608    /* most tokens of a row in the calls of this section      */
+#define CSTR_MAX_TOP 1024       /* longest record of most likely tokens                   */
+
+/*
+ * Draw a token of every row's constrained distribution from one uniform number a row, and advance the
+ * row: the step's recipe (Section 1) with the third part as serving systems have it.  With A = the tokens
+ * that the row's state allows (as in cstr_step; all tokens when n_tables is 0) whose logits are neither NaN
+ * nor -infinity, ordered by (logit descending, id ascending):
+ *   p_v    = softmax over A of logits / temperature
+ *   kept   = the longest prefix of the order that lies within all of
+ *              the first top_k tokens                         (top_k 0 or below: all)
+ *              the tokens with p_v >= min_p * the largest p    (min_p 0 or below: all)
+ *              the shortest prefix that holds top_p of the probability which the two cuts above leave
+ *                                                              (top_p 1 or above: all)
+ *            and the first token in any case
+ *   token  = the first kept token by id for which the sum of p over the kept tokens up to it exceeds
+ *            uniform * the sum of p over all kept tokens
+ *   state  = next[state][token]
+ * The weights that decide are taken and added in 64 bits.  temperature 0: the first token of the order
+ * (as cstr_step without noise), logp 0, kept 1.  Infinite logits share the probability equally.  Where A is
+ * empty, an allowed -infinity still beats none: the lowest such id, logp -infinity, kept 0.
+ *   tables, n_tables, row_table   as in cstr_step; n_tables 0 .. CSTR_MAX_TABLES
+ *   states_in, states_out  DEVICE int32 [rows], may be the same array; NULL when n_tables is 0
+ *   logits      DEVICE [rows][ld] of dtype CSTR_F32 or CSTR_BF16, on whole elements;  ld >= vocab_size
+ *   vocab_size  equal to the tables' V, up to CSTR_MAX_ROW
+ *   uniform     DEVICE float [rows], in [0, 1) (others are taken as the nearest number in there)
+ *   temperature, top_p, min_p  DEVICE float [rows] or NULL (1, 1, 0);  top_k  DEVICE int32 [rows] or NULL (0)
+ *   tokens_out  DEVICE int32 [rows]
+ *   logp_out    DEVICE float [rows] or NULL: log p of the token, before any cut - what cstr_policy_loss
+ *               calls logp; less log(kept) it is the log probability with which the token was drawn
+ *   kept_out    DEVICE float [rows] or NULL: sum of p over the kept tokens
+ *   accept_out  DEVICE uint8 [rows] or NULL: 1 iff the new state is accepting
+ * A row whose state is -1 or out of range, whose table index is out of range, whose temperature is negative,
+ * infinite or below 4.3e-39 without being 0, or any of whose settings is NaN, and a row without an allowed
+ * token that is not NaN, gets token -1, state -1, logp -infinity, kept 0.
+ * Only enqueues one kernel on cuda_stream; no allocation, no host synchronisation.
+ */
+int cstr_sample(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                const int32_t *states_in, int32_t *states_out, const void *logits, int32_t dtype,
+                int64_t ld, int32_t vocab_size, const float *uniform, const float *temperature,
+                const int32_t *top_k, const float *top_p, const float *min_p, int32_t *tokens_out,
+                float *logp_out, float *kept_out, uint8_t *accept_out, int32_t rows, void *cuda_stream);
+
+/*
+ * The n most likely tokens of every row's constrained distribution with their log probabilities: what
+ * answers show as alternatives, and a teacher's record of a position for cstr_distill_loss.
+ *   ids_out     DEVICE int32 [rows][n]: the first n tokens of the order of cstr_sample, in that order
+ *   logp_out    DEVICE float [rows][n]: their log p;  n 1 .. CSTR_MAX_TOP
+ *   lse_out     DEVICE float [rows] or NULL: log sum over A of exp(logits / temperature)
+ *   temperature finite, above 4.3e-39 (its reciprocal times log2(e) is a float)
+ * Entries past the tokens of A hold id -1 and logp -infinity, and so does all of an inactive row (lse
+ * -infinity).  Other arguments as in cstr_sample; states NULL exactly when n_tables is 0.
+ * Only enqueues one kernel on cuda_stream; no allocation, no host synchronisation.
+ */
+int cstr_top_logprobs(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                      const int32_t *states, const void *logits, int32_t dtype, int64_t ld,
+                      int32_t vocab_size, float temperature, int32_t n, int32_t *ids_out,
+                      float *logp_out, float *lse_out, int32_t rows, void *cuda_stream);
+
 /* ------------------------------------------------- loss under constraints */
 
 /*

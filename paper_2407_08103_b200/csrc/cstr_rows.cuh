@@ -1,0 +1,188 @@
+// Rows of logits under their automaton states, as the operators on whole distributions read them:
+// the tables' descriptors and their host checks, a row's mask, masked vectors of logits, the next
+// state, and exponentials in 64 bits.
+#pragma once
+
+#include <math_constants.h>
+
+#include "cstr_internal.cuh"
+
+namespace cstr_rows {
+
+constexpr unsigned kFull = 0xffffffffu;
+
+struct TableDesc {
+    const uint32_t *mask;
+    const void *next;        // token-major: next[token * lds + internal state]
+    const uint8_t *accept;
+    const int32_t *rank;     // caller's state id -> internal one, or null (identity)
+    const int32_t *unrank;   // and back
+    long long lds, ldw;
+    int n_states, wide, code_shift;
+};
+
+struct Tables {
+    TableDesc tab[CSTR_MAX_TABLES];
+    int n;                   // 0: every token is allowed
+    const int32_t *row_table, *states;
+};
+
+// Checks of the arguments that the row operators share; fills `out`.
+inline int take_tables(const char *name, const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                       const int32_t *states, int32_t vocab_size, int device, Tables &out)
+{
+    out.n = n_tables;
+    out.row_table = row_table;
+    out.states = states;
+    for (int32_t i = 0; i < n_tables; ++i) {
+        const cstr_table *t = tables[i];
+        if (!t)
+            return cstr_fail(CSTR_ERR_NULL, "%s: tables[%d] is null", name, i);
+        if (t->device != device)
+            return cstr_fail(CSTR_ERR_DEVICE, "%s: tables[%d] is on device %d, device %d is current", name, i,
+                             t->device, device);
+        if (t->n_states < 1)
+            return cstr_fail(CSTR_ERR_ARG, "%s: tables[%d] has not been built", name, i);
+        if (t->V != vocab_size)
+            return cstr_fail(CSTR_ERR_SHAPE, "%s: tables[%d] has V = %d, vocab_size is %d", name, i, t->V, vocab_size);
+        TableDesc &d = out.tab[i];
+        d.mask = t->mask;
+        d.next = t->next;
+        d.accept = t->accept;
+        d.rank = t->renumbered ? t->rank : nullptr;
+        d.unrank = t->renumbered ? t->unrank : nullptr;
+        d.lds = t->lds;
+        d.ldw = t->ldw;
+        d.n_states = t->n_states;
+        d.wide = t->wide;
+        d.code_shift = t->code_shift;
+    }
+    return CSTR_OK;
+}
+
+// The row's table and state; false: an inactive row.  mrow: its mask, null where everything is allowed.
+__device__ __forceinline__ bool row_state(const Tables &a, int row, int &table, int &state, const uint32_t *&mrow)
+{
+    mrow = nullptr;
+    table = 0;
+    state = -1;
+    if (a.n == 0)
+        return true;
+    table = a.row_table ? a.row_table[row] : 0;
+    state = a.states[row];
+    if (table < 0 || table >= a.n || state < 0 || state >= a.tab[table].n_states)
+        return false;
+    mrow = a.tab[table].mask + (long long)state * a.tab[table].ldw;
+    return true;
+}
+
+// State after an allowed token (next holds codes of internal ids; its sink means "no edge").
+__device__ __forceinline__ int next_state(const TableDesc &t, int state, int token)
+{
+    const long long at = (long long)token * t.lds + (t.rank ? t.rank[state] : state);
+    int q = t.wide ? ((const int32_t *)t.next)[at] : (int)((const uint16_t *)t.next)[at];
+    q = CSTR_UNPERM(q >> t.code_shift);
+    return q == t.n_states ? CSTR_DEAD : t.unrank ? t.unrank[q] : q;
+}
+
+// A row as 16-byte vectors from the 16-byte boundary at or before its first logit: vector v holds the
+// tokens v * N - head .. + N - 1, those outside [0, V) read as disallowed and not touched.
+template <bool BF16> struct RowView {
+    static constexpr int N = BF16 ? 8 : 4, ESZ = BF16 ? 2 : 4;
+    const char *row;         // first logit
+    const uint32_t *mrow;    // allowed tokens, or null
+    int head, V;
+
+    __device__ __forceinline__ RowView(const void *logits, long long offset, int V_, const uint32_t *m)
+        : row((const char *)logits + offset * ESZ), mrow(m), V(V_)
+    {
+        head = (int)((unsigned)(uintptr_t)row & 15u) / ESZ;
+    }
+    __device__ __forceinline__ int vectors() const { return (V + head + N - 1) / N; }
+    __device__ __forceinline__ int token(int v) const { return v * N - head; }
+    __device__ __forceinline__ bool inside(int v) const { return token(v) >= 0 && token(v) + N <= V; }
+    __device__ __forceinline__ bool allowed(int tok) const { return !mrow || ((__ldg(mrow + (tok >> 5)) >> (tok & 31)) & 1u); }
+    __device__ __forceinline__ float one(int tok) const
+    {
+        return BF16 ? __uint_as_float((unsigned)__ldg((const unsigned short *)row + tok) << 16) : __ldg((const float *)row + tok);
+    }
+    // allowed bits of a vector that is inside
+    __device__ __forceinline__ unsigned bits(int v) const
+    {
+        if (!mrow)
+            return kFull;
+        const int tok = token(v);
+        const unsigned lo = __ldg(mrow + (tok >> 5));
+        return __funnelshift_r(lo, (tok & 31) + N > 32 ? __ldg(mrow + (tok >> 5) + 1) : 0u, tok & 31);
+    }
+    // raw vector with -infinity where the token is disallowed
+    static __device__ __forceinline__ uint4 mask(uint4 u, unsigned bits)
+    {
+        unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (BF16)
+                w[i] = __byte_perm((bits >> (2 * i)) & 1u ? w[i] : 0xff80ff80u, (bits >> (2 * i + 1)) & 1u ? w[i] : 0xff80ff80u, 0x7610);
+            else
+                w[i] = (bits >> i) & 1u ? w[i] : 0xff800000u;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ uint4 edge(int v) const       // a vector that is partly (or not) inside
+    {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = BF16 ? 0xff80ff80u : 0xff800000u;
+#pragma unroll
+            for (int h = 0; h < N / 4; ++h) {
+                const int tok = token(v) + i * (N / 4) + h;
+                if (tok >= 0 && tok < V && allowed(tok)) {
+                    const unsigned f = __float_as_uint(one(tok));
+                    w[i] = BF16 ? __byte_perm(w[i], f >> 16, h ? 0x5410 : 0x3254) : f;
+                }
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ uint4 masked(int v) const
+    {
+        return inside(v) ? mask(__ldg(reinterpret_cast<const uint4 *>(row - head * ESZ) + v), bits(v)) : edge(v);
+    }
+    // Logit e of a raw vector; NaN reads as -infinity.
+    static __device__ __forceinline__ float value(uint4 u, int e)
+    {
+        const unsigned w[4] = {u.x, u.y, u.z, u.w};
+        const float f = BF16 ? __uint_as_float(e & 1 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16) : __uint_as_float(w[e % 4]);
+        return fmaxf(f, -CUDART_INF_F);
+    }
+};
+
+// 2^t for t <= 0 to 1.2e-12: t = n + f, the polynomial of degree 8 that meets 2^f at the nine
+// Chebyshev points of [-1/2, 1/2] (1.1e-12 at most, exact at 0), the exponent by integer addition.
+__device__ __forceinline__ double exp2_64(double t)
+{
+    if (!(t > -1000.0))
+        return 0.0;
+    const double shift = 6755399441055744.0;                 // 1.5 * 2^52: adding it rounds to a whole number
+    const double r = t + shift, f = t - (r - shift);
+    double p = 1.3255224887502117e-06;
+    p = fma(p, f, 1.531007940254368e-05);
+    p = fma(p, f, 0.0001540345585240991);
+    p = fma(p, f, 0.0013333450567999414);
+    p = fma(p, f, 0.009618129159402628);
+    p = fma(p, f, 0.05550410941205934);
+    p = fma(p, f, 0.2402265069581299);
+    p = fma(p, f, 0.6931471805459335);
+    p = fma(p, f, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
+}
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+}  // namespace cstr_rows

@@ -1,0 +1,786 @@
+// Sampling under the constraint with temperature, top-k, top-p and min-p from one uniform number a
+// row, and the most likely allowed tokens with their log probabilities, each in one kernel.
+//
+// Mathematics.  The allowed tokens of a row are ordered by (logit descending, id ascending); each of the
+// three cuts keeps a prefix of that order, so all of them together keep "logit > x, or logit = x and id <= i"
+// for one pair (x, i).  With weights w_v = 2^(c (x_v - m)), c = log2(e) / temperature, m the row's maximum, the
+// token is the first one by id whose running sum over the kept weights exceeds u times their sum.  Borders
+// between tokens lie 1 / V apart, so that sums in 32 bits would take a neighbour now and then: the weights that
+// decide are taken in 64 bits and added as whole numbers of 2^-s (s = 62 - log2 V), whose sums are exact
+// whatever their order - atomics included - so a row's token does not depend on the launch.
+//
+// A cluster of up to 16 CTAs shares a row.  The row's maximum and sum come from one pass over memory; what
+// follows reads the row from the L2 cache: the pair (x, i) by counts or masses of three digits of the logit's
+// ordered bits, the token by sums of chunks of 128 vectors.
+#include <cooperative_groups.h>
+#include <math.h>
+#include <string.h>
+
+#include <atomic>
+
+#include "cstr_rows.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+using namespace cstr_rows;
+typedef unsigned long long u64;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 16;
+constexpr int kU = 4;                     // vectors of a lane in flight; a chunk is 32 * kU vectors
+constexpr int kBins = 2048;               // digits of a selection round; entries of the list
+constexpr int kNone = 0x7fffffff;
+
+struct SampleParams {
+    Tables t;
+    const void *logits;
+    long long ld;
+    int V, rows;
+    int per;                              // chunks of a CTA, at most
+    int scale_bits;                       // s
+    u64 *oob;
+    // sampling
+    const float *uniform, *temperature, *top_p, *min_p;
+    const int32_t *top_k;
+    int32_t *states_out, *tokens;
+    float *logp, *kept;
+    uint8_t *accept_out;
+    // most likely tokens
+    int n;
+    double c;                             // log2(e) / temperature
+    int32_t *ids;
+    float *lse;
+};
+
+// Ascending for descending logits; -0 and +0 are one value.
+__device__ __forceinline__ unsigned order_of(float x)
+{
+    const unsigned u = __float_as_uint(x + 0.0f);
+    return (u & 0x80000000u) ? u : ~(u | 0x80000000u);
+}
+__device__ __forceinline__ float logit_of(unsigned o)
+{
+    return __uint_as_float((o & 0x80000000u) ? o : ~o & 0x7fffffffu);
+}
+
+// The whole number at or above (below) a * f, for 0 <= f < 1: f is a whole number of 2^-150.
+__device__ __forceinline__ u64 part_of(u64 a, float f, bool up)
+{
+    const unsigned b = __float_as_uint(f);
+    const int e = (int)(b >> 23);
+    const u64 mant = (b & 0x7fffffu) | (e ? 0x800000u : 0u);
+    const int shift = 150 - (e ? e : 1);                     // f = mant * 2^-shift, shift >= 24
+    const u64 lo = a * mant, hi = __umul64hi(a, mant);
+    if (shift >= 128)
+        return up && (lo | hi) ? 1 : 0;
+    u64 whole, rest;
+    if (shift >= 64) {
+        whole = shift == 64 ? hi : hi >> (shift - 64);
+        rest = lo | (shift == 64 ? 0 : hi << (128 - shift));
+    } else {
+        whole = (lo >> shift) | (hi << (64 - shift));
+        rest = lo << (64 - shift);
+    }
+    return whole + (up && rest ? 1 : 0);
+}
+
+__device__ __forceinline__ u64 inclusive_scan(u64 v, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const u64 o = __shfl_up_sync(kFull, v, off);
+        v += lane >= off ? o : 0;
+    }
+    return v;
+}
+__device__ __forceinline__ u64 warp_sum(u64 v)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        v += __shfl_xor_sync(kFull, v, off);
+    return v;
+}
+__device__ __forceinline__ double warp_sum(double v)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        v += __shfl_xor_sync(kFull, v, off);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        v = fmaxf(v, __shfl_xor_sync(kFull, v, off));
+    return v;
+}
+
+// What the CTAs of a cluster tell each other.
+struct Word {
+    double sum;
+    u64 mass;
+    float m;
+    int token;
+};
+
+// A prefix of the row's order: logits above x, and those equal to x with ids up to `last`.
+struct Cut {
+    float x;
+    int last;
+    __device__ __forceinline__ bool keeps(float v, int tok) const { return v > x || (v == x && tok <= last); }
+    __device__ __forceinline__ bool tighter_than(const Cut &o) const { return x > o.x || (x == o.x && last < o.last); }
+};
+
+template <bool BF16> struct Row {
+    using View = RowView<BF16>;
+    static constexpr int N = View::N;
+    cg::cluster_group cluster;
+    View view;
+    int size, part, tid, lane, warp;
+    int c0, c1;                           // this CTA's chunks
+    double c;                             // log2(e) / temperature
+    float m;
+    double unit;                          // 2^s
+    u64 *bins, *chunk_mass;
+    float *chunk_max;
+    Word *word;                           // two, in turn
+    u64 *scratch;                         // kWarps + 4
+    int phase;
+    u64 before, mine;                     // mass of the lower parts, of this one (after a mass pass)
+
+    __device__ __forceinline__ void barrier()
+    {
+        if (size > 1)
+            cluster.sync();
+        else
+            __syncthreads();
+    }
+    // Every CTA's word, one per lane; thread 0's `w` is this CTA's.
+    __device__ __forceinline__ Word exchange(const Word &w)
+    {
+        Word *slot = word + phase;
+        phase ^= 1;
+        if (tid == 0)
+            *slot = w;
+        barrier();
+        Word r = {0.0, 0, -CUDART_INF_F, -1};
+        if (lane < size)
+            r = *cluster.map_shared_rank(slot, lane);
+        return r;
+    }
+    template <class T> __device__ __forceinline__ T block_sum(T v)
+    {
+        v = warp_sum(v);
+        T *s = reinterpret_cast<T *>(scratch);
+        __syncthreads();
+        if (lane == 0)
+            s[warp] = v;
+        __syncthreads();
+        T r = s[0];
+#pragma unroll
+        for (int i = 1; i < kWarps; ++i)
+            r += s[i];
+        return r;
+    }
+    __device__ __forceinline__ u64 weight(float x) const
+    {
+        const double w = x == m ? 1.0 : exp2_64(((double)x - (double)m) * c);
+        return (u64)__double2ll_rn(w * unit);
+    }
+    // f(logit, token) for every allowed logit above -infinity of this CTA's chunks
+    template <class F> __device__ __forceinline__ void each(F f)
+    {
+        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
+            uint4 raw[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                raw[u] = view.masked((ch * kU + u) * 32 + lane);
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int tok = view.token((ch * kU + u) * 32 + lane);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = View::value(raw[u], e);
+                    if (x > -CUDART_INF_F)
+                        f(x, tok + e);
+                }
+            }
+        }
+    }
+    // This CTA's and the row's sums of the chunks' masses; returns the row's.
+    __device__ __forceinline__ u64 share_masses()
+    {
+        u64 s = 0;
+        for (int i = tid; i < c1 - c0; i += kThreads)
+            s += chunk_mass[i];
+        mine = block_sum(s);
+        const Word r = exchange({0.0, mine, 0.f, 0});
+        before = warp_sum(lane < part ? r.mass : 0);
+        return warp_sum(lane < size ? r.mass : 0);
+    }
+    // Sums of f(logit, token) by chunk; returns the row's.
+    template <class F> __device__ __forceinline__ u64 mass_pass(F f)
+    {
+        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
+            u64 s = 0;
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int v = (ch * kU + u) * 32 + lane;
+                const uint4 raw = view.masked(v);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = View::value(raw, e);
+                    if (x > -CUDART_INF_F)
+                        s += f(x, view.token(v) + e);
+                }
+            }
+            s = warp_sum(s);
+            if (lane == 0)
+                chunk_mass[ch - c0] = s;
+        }
+        __syncthreads();
+        return share_masses();
+    }
+    // After a mass pass over f: the first token by id whose running sum exceeds t, in warp 0 of the CTA
+    // that holds it, -1 everywhere else.
+    template <class F> __device__ __forceinline__ int find(F f, u64 t)
+    {
+        if (warp != 0 || t < before || t >= before + mine)
+            return -1;
+        u64 base = before;
+        int ch = c0;
+        for (;; ch += 32) {                              // (ends: the sum of all chunks exceeds t)
+            const u64 w = ch + lane < c1 ? chunk_mass[ch - c0 + lane] : 0;
+            const u64 upto = base + inclusive_scan(w, lane);
+            const unsigned over = __ballot_sync(kFull, upto > t);
+            if (over) {
+                const int l = __ffs((int)over) - 1;
+                base = __shfl_sync(kFull, upto - w, l);
+                ch += l;
+                break;
+            }
+            base = __shfl_sync(kFull, upto, 31);
+            if (ch + 32 >= c1)
+                break;
+        }
+        int last = -1;                                   // last token with any weight
+        for (int u = 0; u < kU; ++u) {
+            const int v = (ch * kU + u) * 32 + lane;
+            const uint4 raw = view.masked(v);
+            u64 s = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float x = View::value(raw, e);
+                const u64 w = x > -CUDART_INF_F ? f(x, view.token(v) + e) : 0;
+                s += w;
+                last = w ? view.token(v) + e : last;
+            }
+            const u64 upto = base + inclusive_scan(s, lane);
+            const unsigned over = __ballot_sync(kFull, upto > t);
+            if (over) {
+                const int l = __ffs((int)over) - 1;
+                u64 at = upto - s;
+                int tok = -1;
+                for (int e = 0; e < N; ++e) {
+                    const float x = View::value(raw, e);
+                    at += x > -CUDART_INF_F ? f(x, view.token(v) + e) : 0;
+                    if (tok < 0 && at > t)
+                        tok = view.token(v) + e;
+                }
+                return __shfl_sync(kFull, tok, l);
+            }
+            base = __shfl_sync(kFull, upto, 31);
+        }
+        // the chunk's mass and its tokens' differ by rounding (masses taken from the first pass)
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1)
+            last = max(last, __shfl_xor_sync(kFull, last, off));
+        return last;
+    }
+    // The shortest prefix of the row's order whose sum of f reaches `target` (>= 1); false: the whole row
+    // does not.  Equal logits have equal f.
+    template <class F> __device__ __forceinline__ bool select(F f, u64 target, Cut &cut)
+    {
+        unsigned prefix = 0;
+        u64 sum = 0, at = 0;                             // mass before the digit, mass of the digit
+        const int shifts[4] = {32, 21, 10, 0};
+#pragma unroll 1
+        for (int round = 0; round < 3; ++round) {
+            const int shift = shifts[round + 1], above = shifts[round];
+            const unsigned digits = 1u << (above - shift);
+            for (int i = tid; i < kBins; i += kThreads)
+                bins[i] = 0;
+            __syncthreads();
+            each([&](float x, int tok) {
+                const unsigned o = order_of(x);
+                if (round == 0 || (o >> above) == prefix)
+                    atomicAdd(bins + ((o >> shift) & (digits - 1)), f(x, tok));
+            });
+            barrier();
+            u64 w[kBins / kThreads], s = 0;
+#pragma unroll
+            for (int i = 0; i < kBins / kThreads; ++i) {
+                w[i] = 0;
+                for (int r = 0; r < size; ++r)
+                    w[i] += *cluster.map_shared_rank(bins + tid * (kBins / kThreads) + i, r);
+                s += w[i];
+            }
+            const u64 upto = inclusive_scan(s, lane);
+            __syncthreads();
+            if (lane == 31)
+                scratch[warp] = upto;
+            if (tid == 0)
+                scratch[kWarps] = ~0ull;
+            __syncthreads();
+            u64 base = sum;
+            for (int i = 0; i < warp; ++i)
+                base += scratch[i];
+            if (base + upto >= target && base + upto - s < target) {
+                u64 b = base + upto - s;
+                int i = 0;
+                while (i < kBins / kThreads - 1 && b + w[i] < target)
+                    b += w[i++];
+                scratch[kWarps] = tid * (kBins / kThreads) + i;
+                scratch[kWarps + 1] = b;
+                scratch[kWarps + 2] = w[i];
+            }
+            __syncthreads();
+            const u64 digit = scratch[kWarps];
+            sum = scratch[kWarps + 1];
+            at = scratch[kWarps + 2];
+            barrier();                                   // the bins have been read
+            if (digit == ~0ull)
+                return false;
+            prefix = (prefix << (above - shift)) | (unsigned)digit;
+        }
+        cut.x = logit_of(prefix);
+        cut.last = kNone;
+        const u64 one = f(cut.x, 0), r = (target - sum + one - 1) / one;      // equal logits that are kept
+        if (r * one < at) {
+            const float x = cut.x;
+            auto tie = [x](float v, int) { return (u64)(v == x); };
+            mass_pass(tie);
+            const int tok = find(tie, r - 1);
+            cut.last = everybody(tok);
+        }
+        return true;
+    }
+    // The largest of the CTAs' (warp 0's) tokens, for all
+    __device__ __forceinline__ int everybody(int tok)
+    {
+        const Word r = exchange({0.0, 0, 0.f, tok});
+        return __reduce_max_sync(kFull, r.token);
+    }
+};
+
+// Bitonic sort of n (a power of two) numbers in shared memory.
+__device__ __forceinline__ void sort_list(u64 *list, int n)
+{
+    for (int k = 2; k <= n; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+                const int a = 2 * i - (i & (j - 1)), b = a + j;
+                const u64 x = list[a], y = list[b];
+                if ((x > y) == ((a & k) == 0)) {
+                    list[a] = y;
+                    list[b] = x;
+                }
+            }
+        }
+    __syncthreads();
+}
+
+template <bool BF16, bool TOP>
+__global__ void __launch_bounds__(kThreads, 4)
+sample_kernel(const __grid_constant__ SampleParams p)
+{
+    using View = RowView<BF16>;
+    constexpr int N = View::N;
+    extern __shared__ u64 s_dynamic[];                   // bins, then masses and maxima of the chunks
+    __shared__ Word s_word[2];
+    __shared__ u64 s_scratch[kWarps + 4];
+    __shared__ int s_count;
+    cstr_wait_for_earlier_kernels();
+    cstr_let_next_kernel_start();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int size = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int row = blockIdx.x / size;
+    int table, state;
+    const uint32_t *mrow;
+    bool active = row_state(p.t, row, table, state, mrow);
+
+    // the row's settings
+    float u = 0.f, top_p = 1.f, min_p = 0.f;
+    int top_k = 0;
+    double c = p.c;
+    bool cold = false;                                   // temperature 0
+    if (!TOP) {
+        const float temperature = p.temperature ? p.temperature[row] : 1.f;
+        u = p.uniform[row];
+        top_p = p.top_p ? p.top_p[row] : 1.f;
+        min_p = p.min_p ? p.min_p[row] : 0.f;
+        top_k = p.top_k ? p.top_k[row] : 0;
+        cold = temperature == 0.f;
+        c = cold ? 1.0 : 1.4426950408889634 / (double)temperature;
+        if (!(temperature >= 0.f) || temperature == CUDART_INF_F || !((float)c < CUDART_INF_F) || u != u ||
+            top_p != top_p || min_p != min_p)
+            active = false;
+        u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
+    }
+    // token and state of a row, by one thread
+    auto finish = [&](int token, float logp, float kept) {
+        int next = CSTR_DEAD;
+        if (token >= 0 && p.t.n > 0)
+            next = next_state(p.t.tab[table], state, token);
+        p.tokens[row] = token;
+        if (p.states_out)
+            p.states_out[row] = next;
+        if (p.logp)
+            p.logp[row] = logp;
+        if (p.kept)
+            p.kept[row] = kept;
+        if (p.accept_out)
+            p.accept_out[row] = next >= 0 ? (uint8_t)(p.t.tab[table].accept[next] != 0) : (uint8_t)0;
+    };
+    if (!active) {
+        if (part == 0) {
+            if (TOP) {
+                for (int i = tid; i < p.n; i += kThreads) {
+                    p.ids[(long long)row * p.n + i] = -1;
+                    p.logp[(long long)row * p.n + i] = -CUDART_INF_F;
+                }
+                if (tid == 0 && p.lse)
+                    p.lse[row] = -CUDART_INF_F;
+            } else if (tid == 0)
+                finish(-1, -CUDART_INF_F, 0.f);
+        }
+        return;
+    }
+
+    Row<BF16> r = {cluster, View(p.logits, (long long)row * p.ld, p.V, mrow), size, part, tid, lane, warp};
+    const int chunks = (r.view.vectors() + 32 * kU - 1) / (32 * kU), per = (chunks + size - 1) / size;
+    r.c0 = min(part * per, chunks);
+    r.c1 = min(r.c0 + per, chunks);
+    r.c = c;
+    r.unit = __hiloint2double((1023 + p.scale_bits) << 20, 0);
+    r.bins = s_dynamic;
+    r.chunk_mass = s_dynamic + kBins;
+    r.chunk_max = reinterpret_cast<float *>(r.chunk_mass + p.per);
+    r.word = s_word;
+    r.scratch = s_scratch;
+    r.phase = 0;
+    if (tid == 0)
+        s_count = 0;
+
+    // One pass over memory: maximum of every chunk, sum of its weights relative to it (bits of a double).
+    const bool plain = !TOP && !cold && top_k <= 0 && top_p >= 1.f && min_p <= 0.f;
+    const float c32 = (float)c;
+    for (int ch = r.c0 + warp; ch < r.c1; ch += kWarps) {
+        uint4 raw[kU];
+#pragma unroll
+        for (int i = 0; i < kU; ++i)
+            raw[i] = r.view.masked((ch * kU + i) * 32 + lane);
+        float top = -CUDART_INF_F;
+#pragma unroll
+        for (int i = 0; i < kU; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                top = fmaxf(top, View::value(raw[i], e));
+        top = warp_max(top);
+        double sum = 0.0;
+        if (top == CUDART_INF_F || (plain && top > -CUDART_INF_F)) {
+#pragma unroll
+            for (int i = 0; i < kU; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = View::value(raw[i], e);
+                    sum += x == top ? 1.0 : exp2_64(((double)x - (double)top) * c);
+                }
+        } else if (top > -CUDART_INF_F) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < kU; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    s += exp2_fast((View::value(raw[i], e) - top) * c32);
+            sum = s;
+        }
+        sum = warp_sum(sum);
+        if (lane == 0) {
+            r.chunk_max[ch - r.c0] = top;
+            r.chunk_mass[ch - r.c0] = (u64)__double_as_longlong(sum);
+        }
+    }
+    __syncthreads();
+    auto chunk_sum = [&](int i, float ref) {              // relative to ref
+        const float top = r.chunk_max[i];
+        const double s = __longlong_as_double((long long)r.chunk_mass[i]);
+        return top == ref ? s : s * exp2_64(((double)top - (double)ref) * c);
+    };
+    float m = -CUDART_INF_F;
+    for (int i = tid; i < r.c1 - r.c0; i += kThreads)
+        m = fmaxf(m, r.chunk_max[i]);
+    m = warp_max(m);
+    if (lane == 0)
+        reinterpret_cast<float *>(s_scratch)[warp] = m;
+    __syncthreads();
+    m = warp_max(lane < kWarps ? reinterpret_cast<float *>(s_scratch)[lane] : -CUDART_INF_F);
+    double sum = 0.0;
+    if (m > -CUDART_INF_F)
+        for (int i = tid; i < r.c1 - r.c0; i += kThreads)
+            sum += chunk_sum(i, m);
+    sum = r.block_sum(sum);
+    const Word all = r.exchange({sum, 0, m, 0});
+    const float own_max = m;
+    m = warp_max(lane < size ? all.m : -CUDART_INF_F);
+    r.m = m;
+    double total = 0.0;                                   // of the row, relative to m
+    if (lane < size && all.sum > 0.0)
+        total = all.m == m ? all.sum : all.sum * exp2_64(((double)all.m - (double)m) * c);
+    total = warp_sum(total);
+
+    if (TOP) {
+        if (tid == 0 && part == 0 && p.lse)
+            p.lse[row] = m == -CUDART_INF_F ? m : (float)((double)m * c * 0.6931471805599453 + log(total));
+        int found = 0;
+        if (m == -CUDART_INF_F)
+            r.barrier();                                  // (the words have been read)
+        else {
+            Cut cut = {-CUDART_INF_F, kNone};
+            r.select([](float, int) { return (u64)1; }, (u64)p.n, cut);
+            // every CTA's kept tokens into the list of the first one
+            u64 *list = cluster.map_shared_rank(r.bins, 0);
+            int *count = cluster.map_shared_rank(&s_count, 0);
+            r.each([&](float x, int tok) {
+                if (cut.keeps(x, tok)) {
+                    const int at = atomicAdd(count, 1);
+                    if (at < kBins)
+                        list[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
+                }
+            });
+            r.barrier();
+            found = min(s_count, p.n);
+        }
+        if (part != 0)
+            return;
+        int power = 1;
+        while (power < found)
+            power <<= 1;
+        for (int i = found + tid; i < power; i += kThreads)
+            r.bins[i] = ~0ull;
+        sort_list(r.bins, power);
+        const double log_total = log(total);
+        for (int i = tid; i < p.n; i += kThreads) {
+            const u64 e = i < found ? r.bins[i] : 0;
+            const float x = logit_of((unsigned)(e >> 32));
+            const double z = x == m ? 0.0 : ((double)x - (double)m) * c * 0.6931471805599453;
+            p.ids[(long long)row * p.n + i] = i < found ? (int)(unsigned)e : -1;
+            p.logp[(long long)row * p.n + i] = i < found ? (float)(z - log_total) : -CUDART_INF_F;
+        }
+        return;
+    }
+
+    int token = -1;                                       // in warp 0 of one CTA of the cluster
+    u64 mass = 0;
+    if (m == -CUDART_INF_F) {
+        // nothing above -infinity: the first allowed token that is not NaN, if there is one
+        int first = kNone;
+        for (int i = r.c0 * kU * 32 * N - r.view.head + tid; i < min(p.V, r.c1 * kU * 32 * N - r.view.head); i += kThreads)
+            if (i >= 0 && i < first && r.view.allowed(i) && r.view.one(i) == -CUDART_INF_F)
+                first = i;
+        first = __reduce_min_sync(kFull, first);
+        __syncthreads();
+        if (lane == 0)
+            reinterpret_cast<int *>(s_scratch)[warp] = first;
+        __syncthreads();
+        first = __reduce_min_sync(kFull, lane < kWarps ? reinterpret_cast<int *>(s_scratch)[lane] : kNone);
+        const Word w = r.exchange({0.0, 0, 0.f, first});
+        first = __reduce_min_sync(kFull, lane < size ? w.token : kNone);
+        if (tid == 0 && part == 0)
+            finish(first == kNone ? -1 : first, -CUDART_INF_F, 0.f);
+        r.barrier();
+        return;
+    }
+    const bool greedy = cold || top_k == 1 || !(top_p > 0.f) || min_p > 1.f;
+    if (greedy) {
+        // the first chunk with the maximum, of the first CTA that has one
+        auto best = [m](float x, int) { return (u64)(x == m); };
+        for (int i = tid; i < r.c1 - r.c0; i += kThreads)
+            r.chunk_mass[i] = r.chunk_max[i] == m ? 1 : 0;
+        __syncthreads();
+        r.mine = own_max == m ? 1 : 0;
+        r.before = __any_sync(kFull, lane < part && all.m == m) ? 1 : 0;
+        token = r.find(best, 0);
+        if (warp == 0 && lane == 0 && token >= 0)
+            finish(token, cold ? 0.f : (float)-log(total), cold ? 1.f : (float)(1.0 / total));
+        r.barrier();
+        return;
+    }
+    Cut cut = {-CUDART_INF_F, kNone};
+    auto tighten = [&](const Cut &o) {
+        if (o.tighter_than(cut))
+            cut = o;
+    };
+    auto kept_weight = [&](float x, int tok) { return cut.keeps(x, tok) ? r.weight(x) : (u64)0; };
+    if (plain) {
+        for (int i = tid; i < r.c1 - r.c0; i += kThreads)
+            r.chunk_mass[i] = r.chunk_max[i] > -CUDART_INF_F ? (u64)__double2ll_rn(chunk_sum(i, m) * r.unit) : 0;
+        __syncthreads();
+        mass = r.share_masses();
+    } else {
+        if (min_p > 0.f) {
+            const float x = m == CUDART_INF_F ? m : fminf(m, __double2float_ru((double)m + log((double)min_p) * (1.4426950408889634 / c)));
+            tighten({x, kNone});
+        }
+        if (top_k > 0) {
+            Cut k;
+            if (r.select([](float, int) { return (u64)1; }, (u64)top_k, k))
+                tighten(k);
+        }
+        mass = r.mass_pass(kept_weight);
+        if (top_p < 1.f) {
+            Cut k;
+            if (r.select([&](float x, int) { return r.weight(x); }, part_of(mass, top_p, true), k))
+                tighten(k);
+            mass = r.mass_pass(kept_weight);
+        }
+    }
+    token = r.find(kept_weight, part_of(mass, u, false));
+    if (warp == 0 && lane == 0 && token >= 0) {
+        const float x = r.view.one(token);
+        const double z = x == m ? 0.0 : ((double)x - (double)m) * c * 0.6931471805599453;
+        const double sums = plain ? (double)mass / r.unit : total;
+        finish(token, (float)(z - log(sums)), plain ? 1.f : (float)((double)mass / r.unit / sums));
+    }
+    r.barrier();
+}
+
+}  // namespace
+
+namespace {
+
+// CTAs of a row: 64 chunks each, smaller shares, down to 8, while there are fewer CTAs than two per SM
+int cluster_size(int rows, int chunks, int sms)
+{
+    int size = 1;
+    while (size < kMaxCluster && (chunks > 64 * size || (rows * (long long)size <= sms && chunks >= 16 * size)))
+        size *= 2;
+    return size;
+}
+
+// Checks and launch shared by both operators; `p` holds what is theirs alone.
+template <bool TOP>
+int run(const char *name, const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+        const int32_t *states, const void *logits, int32_t dtype, int64_t ld, int32_t vocab_size, int32_t rows,
+        SampleParams &p, cudaStream_t stream)
+{
+    if ((uintptr_t)logits % (dtype == CSTR_BF16 ? 2 : 4))
+        return cstr_fail(CSTR_ERR_SHAPE, "%s: logits must start on whole elements", name);
+    int device = -1;
+    CSTR_CUDA_TRY(cudaGetDevice(&device));
+    if (const int rc = cstr_rows::take_tables(name, tables, n_tables, row_table, states, vocab_size, device, p.t))
+        return rc;
+    static std::atomic<int> known[64];
+    int sms = device >= 0 && device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+    if (sms == 0) {
+        CSTR_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+        if (device >= 0 && device < 64)
+            known[device].store(sms, std::memory_order_relaxed);
+    }
+    p.logits = logits;
+    p.ld = ld;
+    p.V = vocab_size;
+    p.rows = rows;
+    p.oob = CSTR_OOB_RECORD();
+    const bool bf16 = dtype == CSTR_BF16;
+    const int n = bf16 ? 8 : 4;
+    const int chunks = (vocab_size + n - 1 + 32 * kU * n - 1) / (32 * kU * n);       // (a row may begin inside a vector)
+    const int size = cluster_size(rows, chunks, sms);
+    if ((long long)rows * size > 0x7fffffffLL)
+        return cstr_fail(CSTR_ERR_SHAPE, "%s: rows x vocabulary too large for one launch", name);
+    p.per = (chunks + size - 1) / size;
+    p.scale_bits = 62;
+    while ((1LL << (62 - p.scale_bits)) < vocab_size)
+        --p.scale_bits;
+    const int smem = (kBins + p.per) * 8 + p.per * 4;
+    void (*kernel)(SampleParams) = bf16 ? sample_kernel<true, TOP> : sample_kernel<false, TOP>;
+    if (size > 8)
+        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (smem > 48 * 1024)
+        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    return cstr_launch(kernel, (long long)rows * size, kThreads, size, smem, stream, p);
+}
+
+int check_rows(const char *name, int32_t n_tables, int32_t dtype, int64_t ld, int32_t vocab_size, int32_t rows)
+{
+    if (n_tables < 0 || n_tables > CSTR_MAX_TABLES)
+        return cstr_fail(CSTR_ERR_ARG, "%s: n_tables = %d, need 0..%d", name, n_tables, CSTR_MAX_TABLES);
+    if (dtype != CSTR_F32 && dtype != CSTR_BF16)
+        return cstr_fail(CSTR_ERR_DTYPE, "%s: unknown dtype %d", name, dtype);
+    if (rows < 0 || vocab_size < 1 || vocab_size > CSTR_MAX_ROW)
+        return cstr_fail(CSTR_ERR_ARG, "%s: rows = %d, vocab_size = %d", name, rows, vocab_size);
+    if (ld < vocab_size)
+        return cstr_fail(CSTR_ERR_SHAPE, "%s: ld = %lld is below V = %d", name, (long long)ld, vocab_size);
+    return CSTR_OK;
+}
+
+}  // namespace
+
+extern "C" int cstr_sample(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                           const int32_t *states_in, int32_t *states_out, const void *logits, int32_t dtype,
+                           int64_t ld, int32_t vocab_size, const float *uniform, const float *temperature,
+                           const int32_t *top_k, const float *top_p, const float *min_p, int32_t *tokens_out,
+                           float *logp_out, float *kept_out, uint8_t *accept_out, int32_t rows, void *cuda_stream)
+{
+    if (const int rc = check_rows("cstr_sample", n_tables, dtype, ld, vocab_size, rows))
+        return rc;
+    if (rows == 0)
+        return CSTR_OK;
+    if (!logits || !uniform || !tokens_out || (n_tables > 0 && (!tables || !states_in || !states_out)))
+        return cstr_fail(CSTR_ERR_NULL, "cstr_sample: null pointer");
+    SampleParams p;
+    memset(&p, 0, sizeof p);
+    p.uniform = uniform;
+    p.temperature = temperature;
+    p.top_k = top_k;
+    p.top_p = top_p;
+    p.min_p = min_p;
+    p.states_out = n_tables > 0 ? states_out : nullptr;
+    p.tokens = tokens_out;
+    p.logp = logp_out;
+    p.kept = kept_out;
+    p.accept_out = accept_out;
+    return run<false>("cstr_sample", tables, n_tables, row_table, states_in, logits, dtype, ld, vocab_size, rows, p,
+                      (cudaStream_t)cuda_stream);
+}
+
+extern "C" int cstr_top_logprobs(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                                 const int32_t *states, const void *logits, int32_t dtype, int64_t ld,
+                                 int32_t vocab_size, float temperature, int32_t n, int32_t *ids_out,
+                                 float *logp_out, float *lse_out, int32_t rows, void *cuda_stream)
+{
+    if (const int rc = check_rows("cstr_top_logprobs", n_tables, dtype, ld, vocab_size, rows))
+        return rc;
+    if (n < 1 || n > CSTR_MAX_TOP)
+        return cstr_fail(CSTR_ERR_ARG, "cstr_top_logprobs: n = %d, need 1..%d", n, CSTR_MAX_TOP);
+    const double c = 1.4426950408889634 / temperature;
+    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite((float)c))
+        return cstr_fail(CSTR_ERR_ARG, "cstr_top_logprobs: temperature = %g", temperature);
+    if (rows == 0)
+        return CSTR_OK;
+    if (!logits || !ids_out || !logp_out || (n_tables > 0 && (!tables || !states)))
+        return cstr_fail(CSTR_ERR_NULL, "cstr_top_logprobs: null pointer");
+    SampleParams p;
+    memset(&p, 0, sizeof p);
+    p.n = n;
+    p.c = c;
+    p.ids = ids_out;
+    p.logp = logp_out;
+    p.lse = lse_out;
+    return run<true>("cstr_top_logprobs", tables, n_tables, row_table, states, logits, dtype, ld, vocab_size, rows, p,
+                     (cudaStream_t)cuda_stream);
+}

@@ -20,6 +20,7 @@ CSTR_BF16 = 1
 CSTR_F16 = 2
 CSTR_MAX_TABLES = 16
 CSTR_STATIC_MAX_BATCH = 4096
+CSTR_MAX_TOP = 1024
 
 EXPORTS = [
     "cstr_load_dfa", "cstr_load_dfa_terminals", "cstr_free_dfa", "cstr_load_vocab",
@@ -36,6 +37,7 @@ EXPORTS = [
     "cstr_cache_create", "cstr_free_cache", "cstr_cache_insert", "cstr_cache_truncate",
     "cstr_cache_attention", "cstr_cache_status",
     "cstr_policy_loss",
+    "cstr_sample", "cstr_top_logprobs",
 ]
 
 # entry points of the checking build only (include/cstr_debug.h)
@@ -75,6 +77,9 @@ def _load(path, debug):
         L.cstr_cache_attention.argtypes = [ptr, ptr, ptr, i32, ptr, ptr, f32, i32, ptr, ptr, ptr, ptr]
         L.cstr_policy_loss.argtypes = [ptr, i32, ptr, ptr, ptr, i32, ctypes.c_int64, i32, f32, ptr, ptr,
                                        ptr, ptr, ptr, f32, f32, f32, ptr, ptr, ptr, i32, ptr]
+        i64 = ctypes.c_int64
+        L.cstr_sample.argtypes = [ptr, i32, ptr, ptr, ptr, ptr, i32, i64, i32] + [ptr] * 9 + [i32, ptr]
+        L.cstr_top_logprobs.argtypes = [ptr, i32, ptr, ptr, ptr, i32, i64, i32, f32, i32, ptr, ptr, ptr, i32, ptr]
         L.is_check_build = debug
         _libs[path] = L
     return _libs[path]
@@ -838,6 +843,83 @@ def cstr_policy_loss(tables, logits, states, actions, old_logp, advantages, loss
         _rows_arg("weight", weight, n, device, f32), clip_low, clip_high, kl_coef,
         _rows_arg("loss_out", loss_out, n, device, f32), _rows_arg("logp_out", logp_out, n, device, f32),
         dp, n, _raw_stream(stream, device))
+    if rc:
+        _check(rc)
+
+
+def _logit_rows(tables, logits, states):
+    """Checks of the operators over whole rows -> (C array of tables or None, their number, address,
+    dtype code, ld, rows, vocabulary, device)."""
+    import torch
+    if isinstance(tables, Table):
+        tables = [tables]
+    tables = tables or []
+    if logits.dtype == torch.float32:
+        dtype = CSTR_F32
+    elif logits.dtype == torch.bfloat16:
+        dtype = CSTR_BF16
+    else:
+        raise TypeError("logits must be float32 or bfloat16")
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [N][V] with unit inner stride")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor")
+    if bool(tables) != (states is not None):
+        raise ValueError("states go with tables")
+    n, vocab = logits.shape
+    ld = logits.stride(0) if n > 1 else max(vocab, logits.stride(0))
+    arr = (ctypes.c_void_p * len(tables))(*[t.ptr.value for t in tables]) if tables else None
+    return arr, len(tables), logits.data_ptr(), dtype, ld, n, vocab, logits.device
+
+
+def cstr_sample(tables, logits, states, tokens_out, uniform, temperature=None, top_k=None, top_p=None,
+                min_p=None, logp_out=None, kept_out=None, row_table=None, accept_out=None, states_out=None,
+                stream=None) -> None:
+    """Draw a token of every row's constrained distribution and advance the rows.  CUDA tensors:
+    ``logits`` ``[N][V]`` float32 or bfloat16; ``uniform``, ``temperature``, ``top_p``, ``min_p``,
+    ``logp_out``, ``kept_out`` float32 ``[N]`` and ``top_k``, ``states``, ``tokens_out``, ``row_table``,
+    ``states_out`` int32 ``[N]``, ``accept_out`` uint8 ``[N]``; all but ``uniform`` and ``tokens_out`` may be
+    None.  Without ``states_out`` the rows advance in place.  ``tables`` None or empty (with ``states``
+    None): unconstrained."""
+    import torch
+    arr, count, address, dtype, ld, n, vocab, device = _logit_rows(tables, logits, states)
+    for name, t in (("uniform", uniform), ("tokens_out", tokens_out)):
+        if t is None:
+            raise ValueError("%s is required" % name)
+    if states is None and states_out is not None:
+        raise ValueError("states_out goes with states")
+    f32, i32 = torch.float32, torch.int32
+
+    def rows(name, t, dt):
+        return _rows_arg(name, t, n, device, dt)
+    before = rows("states", states, i32)
+    rc = lib().cstr_sample(
+        arr, count, rows("row_table", row_table, i32), before,
+        before if states_out is None else rows("states_out", states_out, i32), address, dtype, ld, vocab,
+        rows("uniform", uniform, f32), rows("temperature", temperature, f32), rows("top_k", top_k, i32),
+        rows("top_p", top_p, f32), rows("min_p", min_p, f32), rows("tokens_out", tokens_out, i32),
+        rows("logp_out", logp_out, f32), rows("kept_out", kept_out, f32),
+        rows("accept_out", accept_out, torch.uint8), n, _raw_stream(stream, device))
+    if rc:
+        _check(rc)
+
+
+def cstr_top_logprobs(tables, logits, states, ids_out, logp_out, temperature: float = 1.0, lse_out=None,
+                      row_table=None, stream=None) -> None:
+    """The most likely tokens of every row's constrained distribution.  CUDA tensors: ``ids_out`` int32 and
+    ``logp_out`` float32 ``[N][n]`` contiguous (``n`` up to ``CSTR_MAX_TOP``), ``lse_out`` float32 ``[N]`` or
+    None; the others as in ``cstr_sample``."""
+    import torch
+    arr, count, address, dtype, ld, n, vocab, device = _logit_rows(tables, logits, states)
+    for name, t, dt in (("ids_out", ids_out, torch.int32), ("logp_out", logp_out, torch.float32)):
+        if t is None or t.dtype != dt or t.dim() != 2 or t.shape[0] != n or t.shape != ids_out.shape \
+                or not t.is_contiguous() or t.device != device:
+            raise ValueError("%s must be a contiguous %s tensor [N][n] on %s" % (name, dt, device))
+    rc = lib().cstr_top_logprobs(
+        arr, count, _rows_arg("row_table", row_table, n, device, torch.int32),
+        _rows_arg("states", states, n, device, torch.int32), address, dtype, ld, vocab, temperature,
+        ids_out.shape[1], ids_out.data_ptr(), logp_out.data_ptr(),
+        _rows_arg("lse_out", lse_out, n, device, torch.float32), n, _raw_stream(stream, device))
     if rc:
         _check(rc)
 
