@@ -734,6 +734,40 @@ int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tables, const 
                      float *loss_out, float *logp_out, void *dlogits, int32_t rows,
                      void *cuda_stream);
 
+/*
+ * Divergence of a student's constrained distribution from a teacher's record of its most likely tokens
+ * (cstr_top_logprobs), and its gradient, for `rows` positions.  With A as in cstr_policy_loss and
+ * q = softmax over A of logits / temperature, the entries i of a row's record with an id in [0, vocab_size)
+ * and t_i = exp(teacher_logp[i]) > 0, and of these the ones whose token is in A with a logit above -infinity:
+ *   CSTR_TAIL_DROP    loss = w sum_i t_i (log t_i - log q_i)
+ *   CSTR_TAIL_RENORM  the same with t_i / sum t: the record is a distribution of its own (teacher_logp may
+ *                     then be logits, and may be an unconstrained teacher's: what A does not hold is left out)
+ *   CSTR_TAIL_LUMP    CSTR_TAIL_DROP, and all other tokens of A are one more event with the teacher's
+ *                     r = max(0, 1 - the sum of exp over all entries with an id) and the student's Q = sum of q over
+ *                     the tokens of A without an entry:  + w r (log r - log Q), nothing where r or Q is 0
+ *   dlogits[v] = d loss / d logits[v]: 0 outside A
+ * An id that is listed twice counts with both entries.  Sums over the record are taken in 64 bits, those over
+ * the vocabulary in 32; dlogits is rounded once to its type.
+ *   teacher_ids   DEVICE int32 [rows][k];  teacher_logp  DEVICE float [rows][k];  k 1 .. CSTR_MAX_TOP
+ *   weight        DEVICE float [rows] or NULL (1): w, e.g. 1 / tokens, 0 for padding
+ *   loss_out      DEVICE float [rows]
+ *   dlogits       DEVICE [rows][ld] of dtype or NULL (no gradient); may be the same buffer as logits;
+ *                 columns >= vocab_size are not written
+ *   temperature   of the student; finite, above 4.3e-39 (its reciprocal times log2(e) is a float)
+ * A row whose state is -1 or out of range or whose table index is out of range, a row of weight 0, and a row
+ * whose allowed logits are all -infinity, get loss 0 and gradient 0; a record without an entry that counts gives
+ * 0 but for the lumped tail.  Other rows propagate NaN.  Other arguments as in cstr_policy_loss; vocab_size up to
+ * CSTR_MAX_ROW.  Only enqueues one kernel on cuda_stream; no allocation, no host synchronisation.
+ */
+#define CSTR_TAIL_DROP 0
+#define CSTR_TAIL_RENORM 1
+#define CSTR_TAIL_LUMP 2
+int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                      const int32_t *states, const void *logits, int32_t dtype, int64_t ld,
+                      int32_t vocab_size, float temperature, const int32_t *teacher_ids,
+                      const float *teacher_logp, int32_t k, int32_t tail, const float *weight,
+                      float *loss_out, void *dlogits, int32_t rows, void *cuda_stream);
+
 /* Message for the calling thread's most recent error ("" if none). */
 const char *cstr_last_error(void);
 

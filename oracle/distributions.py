@@ -81,3 +81,47 @@ def top(x, allowed, n, temperature=1.0):
             logp[i, :k] = np.log(w[:k] / w.sum()) if x[i][mine[0]] == np.inf \
                 else (x[i][mine[:k]] - x[i][mine[0]]) / temperature - np.log(w.sum())
     return ids, logp, lse
+
+
+DROP, RENORM, LUMP = 0, 1, 2
+
+
+def distill(x, allowed, ids, teacher, tail, weight=None, temperature=1.0):
+    """(loss [N], dlogits [N][V]) of float64 logits ``x``; ``allowed`` bool (a row of False: inactive);
+    ``ids`` / ``teacher`` [N][k].  The gradient comes from the events' probabilities, not from the loss."""
+    N, V = x.shape
+    loss, grad = np.zeros(N), np.zeros((N, V))
+    for i in range(N):
+        w = 1.0 if weight is None else float(weight[i])
+        z = np.where(allowed[i], x[i] / temperature, -np.inf)
+        if w == 0.0 or not allowed[i].any() or (z == -np.inf).all():
+            continue
+        with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
+            top = np.nanmax(np.where(np.isnan(z), -np.inf, z))
+            e = np.where(z == -np.inf, 0.0, np.exp(z - top))
+            q = e / e.sum()
+            logq = z - top - np.log(e.sum())
+            real = [(v, g) for v, g in zip(ids[i], teacher[i]) if 0 <= v < V and g != -np.inf]
+            entries = [(v, g) for v, g in real if z[v] != -np.inf]
+            scale = max([g for _, g in entries], default=0.0) if tail == RENORM else 0.0
+            t = np.array([np.exp(g - scale) for _, g in entries])
+            logt = np.array([g - scale for _, g in entries])
+            if tail == RENORM and len(t):
+                logt, t = logt - np.log(t.sum()), t / t.sum()
+            value = float(sum(t[j] * (logt[j] - logq[v]) for j, (v, _) in enumerate(entries)))
+            wanted = np.zeros(V)
+            for j, (v, _) in enumerate(entries):
+                wanted[v] += t[j]
+            if tail == LUMP:
+                inside = np.zeros(V, bool)
+                inside[[v for v, _ in real]] = True
+                rest = np.where(inside, -np.inf, z)
+                r = max(0.0, 1.0 - sum(np.exp(g) for _, g in real)) if not any(np.isnan(g) for _, g in real) else np.nan
+                if not (rest == -np.inf).all() and r != 0.0:
+                    low = np.nanmax(np.where(np.isnan(rest), -np.inf, rest))
+                    er = np.where(rest == -np.inf, 0.0, np.exp(rest - low))
+                    value += r * (np.log(r) - (np.log(er.sum() / e.sum()) + (low - top)))
+                    wanted += r * er / er.sum()
+            loss[i] = w * value
+            grad[i] = np.where(z == -np.inf, 0.0, w / temperature * (q * wanted.sum() - wanted))
+    return loss, grad

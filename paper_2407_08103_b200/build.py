@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libcstr.so")
 CHECK_LIB_PATH = os.path.join(PKG_DIR, "libcstr_check.so")
 CHECK_FLAGS = ["-DCSTR_BOUNDS_CHECK", "-DCSTR_TESTING"]
 SOURCES = ["cstr_host.cu", "cstr_build.cu", "cstr_step.cu", "cstr_pda.cu", "cstr_cache.cu",
-           "cstr_cache_attn.cu", "cstr_prefix.cu", "cstr_loss.cu", "cstr_sample.cu"]
+           "cstr_cache_attn.cu", "cstr_prefix.cu", "cstr_loss.cu", "cstr_sample.cu",
+           "cstr_distill.cu"]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,462 @@
+// Divergence of a student's constrained distribution from a teacher's record of its most likely tokens,
+// forward and gradient, in one kernel.
+//
+// Mathematics, with c = log2(e) / temperature, e_v = 2^(c (x_v - m)): the record's tokens are kept out of the
+// running sum of the others, so that what the others hold together is a sum of its own and no small difference
+// (the record often holds all but 1e-4).  With t the record, T = sum t, r the rest of the teacher, S = sum e:
+//   loss = sum t_i (log t_i - log e_i / S) + r (log r - log rest / S)
+//   d loss / d z_v = (T + r) e_v / S - (v in the record: t_v, else r e_v / rest)
+// The sums over the record are taken in 64 bits (a divergence is a small difference of them), those over the
+// vocabulary in 32.
+//
+// Bound: logits read once, gradient written once; the second pass finds the row in the L2 cache, as in the
+// policy loss: a cluster of up to 16 CTAs shares a row.  A bitmap in shared memory marks the record's tokens of
+// a CTA's share; their gradients are written behind the others'.
+#include <cooperative_groups.h>
+#include <math.h>
+#include <string.h>
+
+#include <atomic>
+
+#include "cstr_rows.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+using namespace cstr_rows;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 16;
+
+struct DistillParams {
+    Tables t;
+    const void *logits;
+    void *dlogits;
+    long long ld;
+    int V, rows, k, tail;
+    float c;                         // log2(e) / temperature
+    double inv_temp;
+    const int32_t *ids;
+    const float *teacher, *weight;
+    float *loss;
+    unsigned words;                  // of a CTA's bitmap
+};
+
+struct MaxSum {
+    float m, s;
+};
+
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c)
+{
+    MaxSum r;
+    r.m = fmaxf(a.m, b.m);
+    const float ref = r.m == -CUDART_INF_F ? 0.f : r.m;
+    r.s = a.s * exp2_fast((a.m - ref) * c) + b.s * exp2_fast((b.m - ref) * c);
+    return r;
+}
+
+// A CTA's part of the record.  Weights are relative to exp(ref), logits to x, their largest: t = sum t_i,
+// t_log = sum t_i log t_i, t_x = sum t_i (x_i - x), e = sum of the distinct tokens' 2^(c (x_i - x)).
+struct Record {
+    double t, t_log, t_x, given;
+    float ref, x, e;
+};
+__device__ __forceinline__ Record join(const Record &a, const Record &b, float c)
+{
+    Record r = {0.0, 0.0, 0.0, a.given + b.given, fmaxf(a.ref, b.ref), fmaxf(a.x, b.x), 0.f};
+    auto add = [&](const Record &o) {
+        if (o.t == 0.0 && o.e == 0.f)            // (nothing in it; its references are -infinity)
+            return;
+        const double down = o.ref == r.ref ? 0.0 : (double)o.ref - (double)r.ref, f = down == 0.0 ? 1.0 : exp(down);
+        r.t += f * o.t;
+        r.t_log += f == 0.0 ? 0.0 : f * (o.t_log + o.t * down);
+        r.t_x += f * (o.x == r.x ? o.t_x : o.t_x + o.t * ((double)o.x - (double)r.x));
+        r.e += o.x == r.x ? o.e : o.e * exp2_fast((o.x - r.x) * c);
+    };
+    add(a);
+    add(b);
+    return r;
+}
+
+// What a CTA knows of its share of the row.
+struct Share {
+    MaxSum rest;
+    Record record;
+};
+
+template <class T> __device__ __forceinline__ T from_lane(const T &v, int off)
+{
+    T r;
+    const int n = sizeof(T) / 4;
+    const int *a = reinterpret_cast<const int *>(&v);
+    int *b = reinterpret_cast<int *>(&r);
+#pragma unroll
+    for (int i = 0; i < n; ++i)
+        b[i] = __shfl_xor_sync(kFull, a[i], off);
+    return r;
+}
+
+template <bool BF16> __device__ __forceinline__ void store_one(char *row, int tok, float x)
+{
+    if (BF16) {
+        unsigned u;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(0.f), "f"(x));
+        ((unsigned short *)row)[tok] = (unsigned short)u;
+    } else
+        ((float *)row)[tok] = x;
+}
+
+template <bool BF16> __device__ __forceinline__ float raw_value(uint4 u, int e)
+{
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+    return BF16 ? __uint_as_float(e & 1 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16) : __uint_as_float(w[e % 4]);
+}
+
+template <bool BF16> __device__ __forceinline__ uint4 narrow(const float *d)
+{
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (BF16)
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(d[BF16 ? 2 * i + 1 : i]), "f"(d[BF16 ? 2 * i : i]));
+        else
+            w[i] = __float_as_uint(d[i]);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// WIDE: rows of both buffers begin at the same place of their 16 bytes (or there is no gradient)
+template <bool BF16, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 6)
+distill_kernel(const __grid_constant__ DistillParams p)
+{
+    using View = RowView<BF16>;
+    constexpr int N = View::N;
+    extern __shared__ unsigned s_dynamic[];              // bitmap, then ids, weights and logits of the record
+    __shared__ Share s_warp[kWarps], s_share;
+    __shared__ float s_top[2][kWarps];                   // largest teacher value, largest logit of the record's part
+    __shared__ float s_result[5];                        // factors of e in the rest, in the record, of t; maxima
+    __shared__ float s_ref;
+    __shared__ int s_twice;
+    unsigned *bitmap = s_dynamic;
+    int *s_id = reinterpret_cast<int *>(bitmap + p.words);
+    float *s_t = reinterpret_cast<float *>(s_id + p.k), *s_x = s_t + p.k;
+    cstr_wait_for_earlier_kernels();
+    cstr_let_next_kernel_start();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int size = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int row = blockIdx.x / size;
+    int table, state;
+    const uint32_t *mrow;
+    const bool active = row_state(p.t, row, table, state, mrow);
+    const float w = p.weight ? p.weight[row] : 1.f;
+    const View view(p.logits, (long long)row * p.ld, p.V, mrow);
+    char *d_row = (char *)p.dlogits + (long long)row * p.ld * View::ESZ;
+    const int vectors = view.vectors(), per = (vectors + size - 1) / size;
+    const int v0 = min(part * per, vectors), v1 = min(v0 + per, vectors);
+    const int lo = max(view.token(v0), 0), hi = min(view.token(v1), p.V);        // this CTA's tokens
+    auto put = [&](int v, const float *d) {
+        if (WIDE && view.inside(v))
+            __stcs(reinterpret_cast<uint4 *>(d_row - view.head * View::ESZ) + v, narrow<BF16>(d));
+        else
+            for (int e = 0; e < N; ++e)
+                if (view.token(v) + e >= 0 && view.token(v) + e < p.V)
+                    store_one<BF16>(d_row, view.token(v) + e, d[e]);
+    };
+    auto nothing = [&]() {
+        const float zero[N] = {};
+        if (p.dlogits)
+            for (int v = v0 + tid; v < v1; v += kThreads)
+                put(v, zero);
+        if (part == 0 && tid == 0)
+            p.loss[row] = 0.f;
+    };
+    if (!active || w == 0.f) {
+        nothing();
+        return;
+    }
+
+    // the record's tokens of this share
+    const int32_t *ids = p.ids + (long long)row * p.k;
+    const float *teacher = p.teacher + (long long)row * p.k;
+    for (int i = tid; i < (int)p.words; i += kThreads)
+        bitmap[i] = 0;
+    if (tid == 0)
+        s_twice = 0;
+    __syncthreads();
+    const bool renorm = p.tail == CSTR_TAIL_RENORM;
+    Record rec = {0.0, 0.0, 0.0, 0.0, -CUDART_INF_F, -CUDART_INF_F, 0.f};
+    for (int i = tid; i < p.k; i += kThreads) {
+        const int id = ids[i];
+        const float g = teacher[i];
+        s_id[i] = -1;
+        if (id < lo || id >= hi || g == -CUDART_INF_F)
+            continue;
+        const float x = view.allowed(id) ? view.one(id) : -CUDART_INF_F;
+        const int bit = id - view.token(v0);
+        const unsigned old = atomicOr(bitmap + (bit >> 5), 1u << (bit & 31));
+        if ((old >> (bit & 31)) & 1u)
+            s_twice = 1;
+        s_id[i] = id;
+        s_x[i] = x;
+        s_t[i] = g;
+        if (p.tail == CSTR_TAIL_LUMP)
+            rec.given += exp((double)g);
+        if (x != -CUDART_INF_F) {
+            rec.ref = fmaxf(rec.ref, g);
+            rec.x = fmaxf(rec.x, x);
+        }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        rec.ref = fmaxf(rec.ref, __shfl_xor_sync(kFull, rec.ref, off));
+        rec.x = fmaxf(rec.x, __shfl_xor_sync(kFull, rec.x, off));
+    }
+    if (lane == 0) {
+        s_top[0][warp] = rec.ref;
+        s_top[1][warp] = rec.x;
+    }
+    __syncthreads();
+    for (int i = 0; i < kWarps; ++i) {
+        rec.ref = fmaxf(rec.ref, s_top[0][i]);
+        rec.x = fmaxf(rec.x, s_top[1][i]);
+    }
+    if (!renorm)
+        rec.ref = 0.f;
+    const bool twice = s_twice != 0;
+    // an id's first entry in the record
+    auto first = [&](int i) {
+        if (twice)
+            for (int j = 0; j < i; ++j)
+                if (s_id[j] == s_id[i])
+                    return false;
+        return true;
+    };
+    for (int i = tid; i < p.k; i += kThreads) {
+        if (s_id[i] < 0 || s_x[i] == -CUDART_INF_F)
+            continue;
+        const double log_t = (double)s_t[i] - (double)rec.ref, t = exp(log_t);
+        rec.t += t;
+        rec.t_log += t == 0.0 ? 0.0 : t * log_t;
+        rec.t_x += t * ((double)s_x[i] - (double)rec.x);
+        if (first(i))
+            rec.e += exp2_fast((s_x[i] - rec.x) * p.c);
+    }
+
+    // the others
+    auto bits_of = [&](int v) {
+        const int bit = (v - v0) * N;
+        return ~(bitmap[bit >> 5] >> (bit & 31));
+    };
+    MaxSum rest = {-CUDART_INF_F, 0.f};
+    for (int v = v0 + tid; v < v1; v += kThreads) {
+        const uint4 raw = View::mask(view.masked(v), bits_of(v));
+        float x[N], top = -CUDART_INF_F;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            x[e] = raw_value<BF16>(raw, e);
+            top = fmaxf(top, x[e]);
+        }
+        if (top > rest.m) {
+            rest.s *= exp2_fast((rest.m - top) * p.c);
+            rest.m = top;
+        }
+        const float ref = rest.m == -CUDART_INF_F ? 0.f : rest.m;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            rest.s += exp2_fast((x[e] - ref) * p.c);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        rest = join(rest, from_lane(rest, off), p.c);
+        rec.t += __shfl_xor_sync(kFull, rec.t, off);
+        rec.t_log += __shfl_xor_sync(kFull, rec.t_log, off);
+        rec.t_x += __shfl_xor_sync(kFull, rec.t_x, off);
+        rec.given += __shfl_xor_sync(kFull, rec.given, off);
+        rec.e += __shfl_xor_sync(kFull, rec.e, off);
+    }
+    if (lane == 0)
+        s_warp[warp] = {rest, rec};
+    __syncthreads();
+    if (tid == 0) {
+        Share s = s_warp[0];
+        for (int i = 1; i < kWarps; ++i) {
+            const Share &o = s_warp[i];                  // (all with the same references)
+            s.rest = join(s.rest, o.rest, p.c);
+            s.record.t += o.record.t;
+            s.record.t_log += o.record.t_log;
+            s.record.t_x += o.record.t_x;
+            s.record.given += o.record.given;
+            s.record.e += o.record.e;
+        }
+        s_share = s;
+    }
+    if (size > 1)
+        cluster.sync();
+    else
+        __syncthreads();
+    if (warp == 0) {
+        Share s = {{-CUDART_INF_F, 0.f}, {0.0, 0.0, 0.0, 0.0, -CUDART_INF_F, -CUDART_INF_F, 0.f}};
+        if (lane < size)
+            s = *cluster.map_shared_rank(&s_share, lane);
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) {
+            s.rest = join(s.rest, from_lane(s.rest, off), p.c);
+            s.record = join(s.record, from_lane(s.record, off), p.c);
+        }
+        if (lane == 0) {
+            Record r = s.record;
+            const MaxSum all = join(s.rest, {r.x, r.e}, p.c);
+            if (r.ref == CUDART_INF_F)
+                r.t = CUDART_NAN;                // a record with infinite logits is none
+            float loss = 0.f, f_rest = 0.f, f_listed = 0.f, f_t = 0.f;
+            if (all.m != -CUDART_INF_F || all.s != 0.f) {
+                const double inv = p.inv_temp, total = all.s;
+                // log S relative to the record's largest logit
+                const double log_all = log(total) + (r.x == all.m ? 0.0 : ((double)all.m - (double)r.x) * inv);
+                // the rest's tokens are counted from their own maximum: they may lie far below the record's
+                const double down = s.rest.m == all.m ? 0.0 : ((double)s.rest.m - (double)all.m) * inv;
+                double value = r.t == 0.0 ? 0.0 : r.t_log - r.t_x * inv + r.t * log_all, sum = r.t, left = 0.0;
+                if (renorm) {
+                    value = r.t != 0.0 ? value / r.t - log(r.t) : 0.0;
+                    sum = r.t != 0.0 ? r.t / r.t : 0.0;
+                }
+                if (p.tail == CSTR_TAIL_LUMP && s.rest.s != 0.f) {
+                    left = 1.0 - r.given;
+                    left = left < 0.0 ? 0.0 : left;
+                    if (left != 0.0)
+                        value += left * (log(left) - (log((double)s.rest.s / total) + down));
+                }
+                const double wt = (double)w * inv;
+                loss = (float)((double)w * value);
+                f_listed = (float)(wt * (sum + left) / total);
+                f_rest = s.rest.s != 0.f ? (float)(wt * ((sum + left) * exp(down) / total - left / (double)s.rest.s)) : 0.f;
+                f_t = (float)(renorm ? (r.t != 0.0 ? wt / r.t : 0.0) : wt);
+            }
+            if (part == 0)
+                p.loss[row] = loss;
+            s_result[0] = f_rest;
+            s_result[1] = f_listed;
+            s_result[2] = f_t;
+            s_result[3] = all.m;
+            s_result[4] = s.rest.m;
+            s_ref = r.ref;
+        }
+    }
+    if (size > 1)
+        cluster.sync();                          // the shares have been read
+    else
+        __syncthreads();
+    if (!p.dlogits)
+        return;
+    const float f_rest = s_result[0], f_listed = s_result[1], f_t = s_result[2], ref = s_result[3], low = s_result[4];
+    for (int v = v0 + tid; v < v1; v += kThreads) {
+        const uint4 raw = View::mask(view.masked(v), bits_of(v));
+        float d[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float x = raw_value<BF16>(raw, e);
+            d[e] = x == -CUDART_INF_F ? 0.f : f_rest * exp2_fast((x - low) * p.c);
+        }
+        put(v, d);
+    }
+    __syncthreads();                             // behind the zeros in their places
+    const double t_ref = s_ref;                          // 0 unless the record is renormalised
+    for (int i = tid; i < p.k; i += kThreads) {
+        if (s_id[i] < 0 || !first(i))
+            continue;
+        float d = 0.f;
+        if (s_x[i] != -CUDART_INF_F) {
+            double t = 0.0;
+            for (int j = i; j < (twice ? p.k : i + 1); ++j)
+                if (s_id[j] == s_id[i])
+                    t += exp((double)s_t[j] - t_ref);
+            d = f_listed * exp2_fast((s_x[i] - ref) * p.c) - (float)(t * (double)f_t);
+        }
+        store_one<BF16>(d_row, s_id[i], d);
+    }
+}
+
+int launch(void (*kernel)(DistillParams), const DistillParams &p, int size, int smem, cudaStream_t stream)
+{
+    if (size > 8)
+        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (smem > 40 * 1024)
+        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    return cstr_launch(kernel, (long long)p.rows * size, kThreads, size, smem, stream, p);
+}
+
+}  // namespace
+
+extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
+                                 const int32_t *states, const void *logits, int32_t dtype, int64_t ld,
+                                 int32_t vocab_size, float temperature, const int32_t *teacher_ids,
+                                 const float *teacher_logp, int32_t k, int32_t tail, const float *weight,
+                                 float *loss_out, void *dlogits, int32_t rows, void *cuda_stream)
+{
+    if (n_tables < 0 || n_tables > CSTR_MAX_TABLES)
+        return cstr_fail(CSTR_ERR_ARG, "cstr_distill_loss: n_tables = %d, need 0..%d", n_tables, CSTR_MAX_TABLES);
+    if (dtype != CSTR_F32 && dtype != CSTR_BF16)
+        return cstr_fail(CSTR_ERR_DTYPE, "cstr_distill_loss: unknown dtype %d", dtype);
+    if (rows < 0 || vocab_size < 1 || vocab_size > CSTR_MAX_ROW)
+        return cstr_fail(CSTR_ERR_ARG, "cstr_distill_loss: rows = %d, vocab_size = %d", rows, vocab_size);
+    if (k < 1 || k > CSTR_MAX_TOP)
+        return cstr_fail(CSTR_ERR_ARG, "cstr_distill_loss: k = %d, need 1..%d", k, CSTR_MAX_TOP);
+    if (tail != CSTR_TAIL_DROP && tail != CSTR_TAIL_RENORM && tail != CSTR_TAIL_LUMP)
+        return cstr_fail(CSTR_ERR_ARG, "cstr_distill_loss: unknown tail %d", tail);
+    const float c = (float)(1.4426950408889634 / temperature);
+    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(c))
+        return cstr_fail(CSTR_ERR_ARG, "cstr_distill_loss: temperature = %g", temperature);
+    if (ld < vocab_size)
+        return cstr_fail(CSTR_ERR_SHAPE, "cstr_distill_loss: ld = %lld is below V = %d", (long long)ld, vocab_size);
+    if (rows == 0)
+        return CSTR_OK;
+    if (!logits || !teacher_ids || !teacher_logp || !loss_out || (n_tables > 0 && (!tables || !states)))
+        return cstr_fail(CSTR_ERR_NULL, "cstr_distill_loss: null pointer");
+    const bool bf16 = dtype == CSTR_BF16;
+    const uintptr_t element = bf16 ? 2 : 4;
+    if ((uintptr_t)logits % element || (uintptr_t)dlogits % element)
+        return cstr_fail(CSTR_ERR_SHAPE, "cstr_distill_loss: logits and dlogits must start on whole elements");
+    int device = -1;
+    CSTR_CUDA_TRY(cudaGetDevice(&device));
+    DistillParams p;
+    memset(&p, 0, sizeof p);
+    if (const int rc = cstr_rows::take_tables("cstr_distill_loss", tables, n_tables, row_table, states, vocab_size, device, p.t))
+        return rc;
+    p.logits = logits;
+    p.dlogits = dlogits;
+    p.ld = ld;
+    p.V = vocab_size;
+    p.rows = rows;
+    p.k = k;
+    p.tail = tail;
+    p.c = c;
+    p.inv_temp = 1.0 / (double)temperature;
+    p.ids = teacher_ids;
+    p.teacher = teacher_logp;
+    p.weight = weight;
+    p.loss = loss_out;
+    static std::atomic<int> known[64];
+    int sms = device >= 0 && device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+    if (sms == 0) {
+        CSTR_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+        if (device >= 0 && device < 64)
+            known[device].store(sms, std::memory_order_relaxed);
+    }
+    const long long share = bf16 ? 32768 : 16384;
+    int size = 1;
+    while (size < kMaxCluster && (vocab_size > share * size ||
+                                  (rows * (long long)size <= sms && vocab_size >= 4096LL * size)))
+        size *= 2;
+    if ((long long)rows * size > 0x7fffffffLL)
+        return cstr_fail(CSTR_ERR_SHAPE, "cstr_distill_loss: rows x vocabulary too large for one launch");
+    const int n = bf16 ? 8 : 4;
+    const int vectors = (vocab_size + 2 * n - 2) / n, per = (vectors + size - 1) / size;   // (a row may begin inside a vector)
+    p.words = (unsigned)((per * (long long)n + 31) / 32);
+    const int smem = (int)p.words * 4 + k * 12;
+    const bool together = !dlogits || (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15u) == 0;
+    void (*kernel)(DistillParams) = bf16 ? (together ? distill_kernel<true, true> : distill_kernel<true, false>)
+                                         : (together ? distill_kernel<false, true> : distill_kernel<false, false>);
+    return launch(kernel, p, size, smem, (cudaStream_t)cuda_stream);
+}

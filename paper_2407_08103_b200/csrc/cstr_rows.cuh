@@ -104,7 +104,7 @@ template <bool BF16> struct RowView {
     __device__ __forceinline__ bool allowed(int tok) const { return !mrow || ((__ldg(mrow + (tok >> 5)) >> (tok & 31)) & 1u); }
     __device__ __forceinline__ float one(int tok) const
     {
-        return BF16 ? __uint_as_float((unsigned)__ldg((const unsigned short *)row + tok) << 16) : __ldg((const float *)row + tok);
+        return BF16 ? __uint_as_float((unsigned)((const unsigned short *)row)[tok] << 16) : ((const float *)row)[tok];
     }
     // allowed bits of a vector that is inside
     __device__ __forceinline__ unsigned bits(int v) const
@@ -147,7 +147,7 @@ template <bool BF16> struct RowView {
     }
     __device__ __forceinline__ uint4 masked(int v) const
     {
-        return inside(v) ? mask(__ldg(reinterpret_cast<const uint4 *>(row - head * ESZ) + v), bits(v)) : edge(v);
+        return inside(v) ? mask(reinterpret_cast<const uint4 *>(row - head * ESZ)[v], bits(v)) : edge(v);
     }
     // Logit e of a raw vector; NaN reads as -infinity.
     static __device__ __forceinline__ float value(uint4 u, int e)

@@ -21,6 +21,9 @@ CSTR_F16 = 2
 CSTR_MAX_TABLES = 16
 CSTR_STATIC_MAX_BATCH = 4096
 CSTR_MAX_TOP = 1024
+CSTR_TAIL_DROP = 0
+CSTR_TAIL_RENORM = 1
+CSTR_TAIL_LUMP = 2
 
 EXPORTS = [
     "cstr_load_dfa", "cstr_load_dfa_terminals", "cstr_free_dfa", "cstr_load_vocab",
@@ -37,7 +40,7 @@ EXPORTS = [
     "cstr_cache_create", "cstr_free_cache", "cstr_cache_insert", "cstr_cache_truncate",
     "cstr_cache_attention", "cstr_cache_status",
     "cstr_policy_loss",
-    "cstr_sample", "cstr_top_logprobs",
+    "cstr_sample", "cstr_top_logprobs", "cstr_distill_loss",
 ]
 
 # entry points of the checking build only (include/cstr_debug.h)
@@ -80,6 +83,7 @@ def _load(path, debug):
         i64 = ctypes.c_int64
         L.cstr_sample.argtypes = [ptr, i32, ptr, ptr, ptr, ptr, i32, i64, i32] + [ptr] * 9 + [i32, ptr]
         L.cstr_top_logprobs.argtypes = [ptr, i32, ptr, ptr, ptr, i32, i64, i32, f32, i32, ptr, ptr, ptr, i32, ptr]
+        L.cstr_distill_loss.argtypes = [ptr, i32, ptr, ptr, ptr, i32, i64, i32, f32, ptr, ptr, i32, i32, ptr, ptr, ptr, i32, ptr]
         L.is_check_build = debug
         _libs[path] = L
     return _libs[path]
@@ -920,6 +924,39 @@ def cstr_top_logprobs(tables, logits, states, ids_out, logp_out, temperature: fl
         _rows_arg("states", states, n, device, torch.int32), address, dtype, ld, vocab, temperature,
         ids_out.shape[1], ids_out.data_ptr(), logp_out.data_ptr(),
         _rows_arg("lse_out", lse_out, n, device, torch.float32), n, _raw_stream(stream, device))
+    if rc:
+        _check(rc)
+
+
+def cstr_distill_loss(tables, logits, states, teacher_ids, teacher_logp, loss_out, weight=None, dlogits=None,
+                      tail: int = CSTR_TAIL_RENORM, temperature: float = 1.0, row_table=None, stream=None) -> None:
+    """Divergence of the rows' constrained distributions from a teacher's records; with ``dlogits`` also the
+    gradient.  CUDA tensors: ``logits`` / ``dlogits`` ``[N][V]`` float32 or bfloat16 (may be the same tensor),
+    ``teacher_ids`` int32 and ``teacher_logp`` float32 ``[N][k]`` contiguous (``k`` up to ``CSTR_MAX_TOP``),
+    ``states`` / ``row_table`` int32 ``[N]``, ``loss_out`` / ``weight`` float32 ``[N]``.  ``tail``: one of
+    ``CSTR_TAIL_DROP``, ``CSTR_TAIL_RENORM``, ``CSTR_TAIL_LUMP``.  ``tables`` None or empty (with ``states``
+    None): unconstrained."""
+    import torch
+    arr, count, address, dtype, ld, n, vocab, device = _logit_rows(tables, logits, states)
+    dp = None
+    if dlogits is not None:
+        if dlogits.dtype != logits.dtype:
+            raise TypeError("dlogits must have the dtype of logits")
+        if dlogits.shape != logits.shape or dlogits.stride() != logits.stride() or dlogits.device != device:
+            raise ValueError("dlogits must have the layout of logits")
+        dp = dlogits.data_ptr()
+    for name, t, dt in (("teacher_ids", teacher_ids, torch.int32), ("teacher_logp", teacher_logp, torch.float32)):
+        if t is None or t.dtype != dt or t.dim() != 2 or t.shape[0] != n or t.shape != teacher_ids.shape \
+                or not t.is_contiguous() or t.device != device:
+            raise ValueError("%s must be a contiguous %s tensor [N][k] on %s" % (name, dt, device))
+    if loss_out is None:
+        raise ValueError("loss_out is required")
+    rc = lib().cstr_distill_loss(
+        arr, count, _rows_arg("row_table", row_table, n, device, torch.int32),
+        _rows_arg("states", states, n, device, torch.int32), address, dtype, ld, vocab, temperature,
+        teacher_ids.data_ptr(), teacher_logp.data_ptr(), teacher_ids.shape[1], tail,
+        _rows_arg("weight", weight, n, device, torch.float32),
+        _rows_arg("loss_out", loss_out, n, device, torch.float32), dp, n, _raw_stream(stream, device))
     if rc:
         _check(rc)
 

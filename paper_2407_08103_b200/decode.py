@@ -30,6 +30,9 @@ class ConstrainedDecoder:
         self.states = torch.empty(batch, dtype=torch.int32, device=self.device)
         self.tokens = torch.empty(batch, dtype=torch.int32, device=self.device)
         self.accept = torch.empty(batch, dtype=torch.uint8, device=self.device)
+        self.logp = torch.empty(batch, dtype=torch.float32, device=self.device)
+        self.kept = torch.empty(batch, dtype=torch.float32, device=self.device)
+        self._settings = {}                       # per-row tensors of settings given as numbers
         self._start = self._start_states()
         self.reset()
 
@@ -53,6 +56,40 @@ class ConstrainedDecoder:
                        noise=noise, row_table=self.row_table, accept_out=self.accept,
                        stream=stream)
         return self.tokens, masked_out
+
+    def sample(self, logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None):
+        """One decoding step that draws each row's token from one uniform number (float32 ``[B]``) under
+        ``cstr_sample``'s cuts; returns ``(tokens, logp)`` (device tensors, reused by the next call), and
+        ``self.kept`` holds the probability that the cuts left.  A setting is a number, or a tensor with one
+        entry per row."""
+        cstr.cstr_sample(self.tables, logits, self.states, self.tokens, uniform,
+                         temperature=self._setting("temperature", temperature, 1.0, torch.float32),
+                         top_k=self._setting("top_k", top_k, 0, torch.int32),
+                         top_p=self._setting("top_p", top_p, 1.0, torch.float32),
+                         min_p=self._setting("min_p", min_p, 0.0, torch.float32),
+                         logp_out=self.logp, kept_out=self.kept, row_table=self.row_table,
+                         accept_out=self.accept, stream=stream)
+        return self.tokens, self.logp
+
+    def _setting(self, name, value, off, dtype):
+        if torch.is_tensor(value):
+            return value
+        if value == off:
+            return None
+        at = (name, value)
+        if at not in self._settings:              # a program has a few: filled once, read by every step
+            self._settings[at] = torch.full((self.batch,), value, dtype=dtype, device=self.device)
+            torch.cuda.synchronize(self.device)   # ... on whatever stream
+        return self._settings[at]
+
+    def top_logprobs(self, logits, n: int, temperature: float = 1.0, stream=None):
+        """The ``n`` most likely tokens in the rows' present states: ``(ids, logp)`` ``[B][n]``."""
+        with torch.cuda.stream(stream or torch.cuda.current_stream(self.device)):      # (their memory, too)
+            ids = torch.empty((self.batch, n), dtype=torch.int32, device=self.device)
+            logp = torch.empty((self.batch, n), dtype=torch.float32, device=self.device)
+        cstr.cstr_top_logprobs(self.tables, logits, self.states, ids, logp, temperature=temperature,
+                               row_table=self.row_table, stream=stream)
+        return ids, logp
 
     def status(self, stream=None):
         """(rows with an out-of-range state, active rows without any allowed token) since last call."""

@@ -1,6 +1,7 @@
-"""Training on constrained answers: the policy loss as a differentiable torch function.
+"""Training on constrained answers: the policy loss and the divergence from a teacher's records as
+differentiable torch functions.
 
-The loss is over the constrained distribution (disallowed logits are -infinity, as
+The losses are over the constrained distribution (disallowed logits are -infinity, as
 in Algorithm 2's loop body), because that is the distribution the answers were sampled from.
 """
 
@@ -24,7 +25,7 @@ class _Once(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, _):
-        raise RuntimeError("constrained_policy_loss is differentiable once only")
+        raise RuntimeError("the constrained losses are differentiable once only")
 
 
 class _PolicyLoss(torch.autograd.Function):
@@ -77,3 +78,51 @@ def constrained_policy_loss(logits, actions, old_logp, advantages, tables=None, 
                 options=dict(row_table=row_table, clip_low=clip_low, clip_high=clip_high,
                              kl_coef=kl_coef, temperature=temperature))
     return _PolicyLoss.apply(logits, actions, old_logp, advantages, ref_logp, weight, args)
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, logp, weight, args):
+        loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+        cstr.cstr_distill_loss(args["tables"], logits, args["states"], ids, logp, loss, weight=weight, **args["options"])
+        # the backward pass takes the loss again, from copies of what the library may write in place meanwhile
+        if ctx.needs_input_grad[0]:
+            rows = (args["states"], ids, logp, weight, args["options"]["row_table"])
+            ctx.save_for_backward(logits, *(None if t is None else t.clone() for t in rows))
+            ctx.builds = _builds(args["tables"])
+        ctx.args = args
+        return loss
+
+    @staticmethod
+    def backward(ctx, grad_loss):
+        if not ctx.needs_input_grad[0]:
+            return (None,) * 5
+        if _builds(ctx.args["tables"]) != ctx.builds:
+            raise RuntimeError("a table of this loss was built again before its backward pass")
+        logits, states, ids, logp, weight, row_table = ctx.saved_tensors
+        grad = grad_loss.float()
+        grad = grad.contiguous() if weight is None else grad * weight.flatten()[:grad.shape[0]]
+        dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=logits.device)
+        cstr.cstr_distill_loss(ctx.args["tables"], logits, states, ids, logp, torch.empty_like(grad), weight=grad,
+                               dlogits=dlogits, **dict(ctx.args["options"], row_table=row_table))
+        if torch.is_grad_enabled():
+            dlogits = _Once.apply(dlogits, logits, grad_loss)
+        return dlogits, None, None, None, None
+
+
+def constrained_distill_loss(logits, teacher_ids, teacher_logp, tables=None, states=None, weight=None,
+                             tail: int = cstr.CSTR_TAIL_RENORM, temperature: float = 1.0, row_table=None):
+    """Loss ``[N]`` of ``cstr_distill_loss``, differentiable in ``logits`` (float32 or bfloat16 ``[N][V]``).
+    ``teacher_ids`` / ``teacher_logp`` ``[N][k]``: a teacher's records (``top_logprobs``)."""
+    tables = [tables] if isinstance(tables, cstr.Table) else list(tables or [])
+    args = dict(tables=tables, states=states, options=dict(row_table=row_table, tail=tail, temperature=temperature))
+    return _DistillLoss.apply(logits, teacher_ids, teacher_logp, weight, args)
+
+
+def top_logprobs(logits, n: int, tables=None, states=None, temperature: float = 1.0, row_table=None):
+    """``(ids, logp)`` ``[N][n]`` of ``cstr_top_logprobs``: a teacher's records of the rows' constrained
+    distributions (not differentiable)."""
+    ids = torch.empty((logits.shape[0], n), dtype=torch.int32, device=logits.device)
+    logp = torch.empty((logits.shape[0], n), dtype=torch.float32, device=logits.device)
+    cstr.cstr_top_logprobs(tables, logits, states, ids, logp, temperature=temperature, row_table=row_table)
+    return ids, logp

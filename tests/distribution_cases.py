@@ -126,3 +126,62 @@ def check_top(x, n, allowed=None, temperature=1.0, lse=True, tables=None, states
         assert np.array_equal(top[~fine], want[2][~fine])
         assert (np.abs(top[fine] - want[2][fine]) <= 2.0 ** -24 * (2.1 * math.log2(V + 1) + 36.0 + np.abs(want[2][fine]))).all()
     return want
+
+
+def check_distill(x, ids, teacher, tail, allowed=None, weight=None, tables=None, states=None, row_table=None,
+                  gradient=True, in_place=False, shift=0, stream=None, temperature=1.0):
+    """``x``: device logits (any row stride); ``ids`` / ``teacher``: host arrays.  ``shift``: elements by which
+    the gradient's rows begin later in their 16 bytes than the logits'."""
+    N, V = x.shape
+    allowed = np.ones((N, V), bool) if allowed is None else allowed
+    host = f8(x)
+    loss = torch.full((N,), math.nan, device=DEV)
+    d, space = None, None
+    if gradient:
+        space = torch.full((max(N, 1) * x.stride(0) + 8,), 77.0, dtype=x.dtype, device=DEV)
+        d = x if in_place else space.as_strided((N, V), x.stride(), (x.storage_offset() + shift) % 8)
+    args = [dev(ids, np.int32), dev(teacher, np.float32), dev(weight, np.float32), dev(states, np.int32), dev(row_table, np.int32)]
+    torch.cuda.synchronize()
+    cstr.cstr_distill_loss(tables, x, args[3], args[0], args[1], loss, weight=args[2], dlogits=d, tail=tail,
+                           temperature=temperature, row_table=args[4], stream=stream)
+    torch.cuda.synchronize()
+    given = np.asarray(teacher, np.float32).astype(np.float64)
+    w = None if weight is None else np.asarray(weight, np.float32).astype(np.float64)
+    tau = float(np.float32(temperature))
+    want = ref.distill(host, allowed, ids, given, tail, w, tau)
+    # log q: arguments rounded three times (their mean is at most log2 V), 2^-22 of an exponential, up to 128
+    # additions of a thread and 13 joins with two exponentials each; a lumped tail has two such sums
+    with np.errstate(over="ignore", invalid="ignore", divide="ignore"):
+        e_log = 2.0 ** -24 * (2.1 * math.log2(V + 1) + 128 + 13 * 12)
+        lw = np.ones(N) if w is None else np.abs(w)
+        t = np.where((ids >= 0) & (ids < V), np.exp(given), 0.0)
+        size = lw if tail == ref.RENORM else lw * (t.sum(1) + (1.0 if tail == ref.LUMP else 0.0))
+        fine = np.isfinite(want[0])
+        got = f8(loss)
+        assert np.array_equal(np.isfinite(got), fine), (got, want[0])
+        assert (np.abs(got - want[0])[fine] <= (3 * size * e_log + 2.0 ** -24 * np.abs(want[0]) + 1e-37)[fine]).all()
+        if gradient:
+            got = f8(d)
+            fine = np.isfinite(want[1])
+            assert np.array_equal(np.isfinite(got), fine)
+            z = np.where(allowed, host / tau, -np.inf)
+            q = np.exp(z - np.nanmax(z, 1, keepdims=True, initial=-1e300))
+            q = np.nan_to_num(q / q.sum(1, keepdims=True))
+            listed = np.zeros((N, V + 1))
+            for i in range(N):
+                np.add.at(listed[i], np.where((ids[i] >= 0) & (ids[i] < V), ids[i], V), t[i] if tail != ref.RENORM else 1.0)
+            listed = np.minimum(listed[:, :V], np.maximum(size / np.maximum(lw, 1e-300), 1.0)[:, None])
+            others = np.where(listed > 0, 0.0, q)
+            others = others / np.maximum(others.sum(1, keepdims=True), 1e-300) if tail == ref.LUMP else 0.0 * q
+            mine = size[:, None] * (q + others) + lw[:, None] * listed
+            far = 2.0 ** -24 * 2.1 * np.maximum(0.0, -np.log2(np.maximum(np.maximum(q, others), 1e-300)))
+            unit = {F32: 2.0 ** -24, BF: 2.0 ** -8}[x.dtype]
+            tol = unit * np.abs(want[1]) + mine * (3 * e_log + far) / tau + 1e-37
+            err = (np.abs(got - want[1]) - tol)[fine]
+            assert (err <= 0).all(), "gradient off by %g" % err.max()
+            assert (got[~allowed & fine] == 0).all()
+            if not in_place:
+                outside = torch.ones_like(space, dtype=torch.bool)
+                outside.as_strided((N, V), x.stride(), d.storage_offset()).fill_(False)
+                assert (space[outside] == 77.0).all()
+    return want

@@ -57,3 +57,19 @@ def test_binding_refuses_before_the_library(monkeypatch):
                  lambda: cstr.cstr_top_logprobs(None, x, None, torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, 2))):
         with pytest.raises(ValueError, match="CUDA tensor"):
             call()
+
+
+def test_distill_arguments(lib):
+    def loss(n_tables=0, states=None, logits=P, dtype=0, ld=8, v=8, temperature=1.0, ids=P, logp=P, k=4, tail=0, out=P, d=None,
+             rows=2):
+        return lib.cstr_distill_loss(None, n_tables, None, states, logits, dtype, ld, v, temperature, ids, logp, k, tail,
+                                     None, out, d, rows, None)
+    assert loss(n_tables=-1) == -2 and loss(rows=-1) == -2 and loss(v=0) == -2 and loss(v=8388609, ld=8388609) == -2
+    assert loss(dtype=2) == -5 and loss(ld=7) == -6 and loss(k=0) == -2 and loss(k=1025) == -2
+    assert loss(tail=-1) == -2 and loss(tail=3) == -2
+    for t in (0.0, -1.0, float("nan"), float("inf"), 1e-39):
+        assert loss(temperature=t) == -2, t
+    assert loss(logits=None) == -1 and loss(ids=None) == -1 and loss(logp=None) == -1 and loss(out=None) == -1
+    assert loss(n_tables=1) == -1 and loss(n_tables=1, states=P) == -1
+    assert loss(logits=ctypes.c_void_p(P.value + 2)) == -6 and loss(d=ctypes.c_void_p(P.value + 1), dtype=1) == -6
+    assert loss(rows=0, logits=None) == 0

@@ -43,3 +43,27 @@ def test_top_agrees_with_a_sorted_softmax():
     assert np.allclose(lse, np.log(p.sum(1))) and (np.diff(logp, axis=1) <= 0).all()
     for i in range(5):
         assert list(ids[i]).index(3) + 1 == list(ids[i]).index(7)
+
+
+@pytest.mark.parametrize("tail", [ref.DROP, ref.RENORM, ref.LUMP])
+def test_divergence_agrees_with_its_differences_and_is_zero_for_the_teacher(tail):
+    rng = np.random.default_rng(tail)
+    x = rng.standard_normal((4, 20)) * 2
+    ok = rng.random((4, 20)) < 0.8
+    ok[:, :3] = True
+    ids, logp, _ = ref.top(x + 0.3 * rng.standard_normal(x.shape), ok, 5)
+    ids[1, 3] = ids[1, 0]
+    ids[2, 4] = -1
+    loss, grad = ref.distill(x, ok, ids, logp, tail, temperature=0.8)
+    h = 1e-6
+    for v in range(20):
+        step = np.zeros_like(x)
+        step[:, v] = h
+        up, down = (ref.distill(x + s * step, ok, ids, logp, tail, temperature=0.8)[0] for s in (1, -1))
+        assert np.allclose((up - down) / (2 * h), grad[:, v], atol=1e-8)
+    ids, logp, _ = ref.top(x, ok, 5, 0.8)
+    same = ref.distill(x, ok, ids, logp, tail, temperature=0.8)
+    if tail == ref.LUMP:
+        assert np.abs(same[0]).max() < 1e-14 and np.abs(same[1]).max() < 1e-14
+    if tail == ref.DROP:
+        assert np.abs(same[0]).max() < 1e-14
