@@ -30,7 +30,8 @@ typedef unsigned long long u64;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr int kU = 4;                     // vectors of a lane in flight; a chunk is 32 * kU vectors
-constexpr int kBins = 2048;               // digits of a selection round; entries of the list
+constexpr int kBins = 2048;               // digits of a selection round, distances from the maximum
+constexpr int kList = 2048;               // entries of the list
 constexpr int kNone = 0x7fffffff;
 
 struct SampleParams {
@@ -143,8 +144,8 @@ template <bool BF16> struct Row {
     double c;                             // log2(e) / temperature
     float m;
     double unit;                          // 2^s
-    u64 *bins, *chunk_mass;
-    float *chunk_max;
+    u64 *list, *bins, *chunk_mass;
+    float *chunk_max, *lane_max;          // per chunk; per chunk and lane
     Word *word;                           // two, in turn
     u64 *scratch;                         // kWarps + 4
     int phase;
@@ -156,6 +157,17 @@ template <bool BF16> struct Row {
             cluster.sync();
         else
             __syncthreads();
+    }
+    // The end of a row that the first CTA finishes alone: it stays until nobody reads its memory any more.
+    // (The others' has been read: there is a barrier behind the last exchange.)
+    __device__ __forceinline__ void leave()
+    {
+        __syncthreads();
+        if (size > 1) {
+            asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+            if (part == 0)
+                asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        }
     }
     // Every CTA's word, one per lane; thread 0's `w` is this CTA's.
     __device__ __forceinline__ Word exchange(const Word &w)
@@ -367,6 +379,89 @@ template <bool BF16> struct Row {
         }
         return true;
     }
+    // Distance from the maximum as one of kBins numbers, ascending: 32 to an octave from 2^-30 on.
+    __device__ __forceinline__ int bin_of(float x) const
+    {
+        if (x == m)
+            return 0;
+        const int b = (int)(__float_as_uint(m - x) >> 18) - (((127 - 30) << 5) - 1);
+        return min(max(b, 1), kBins - 1);
+    }
+    // The lowest bin up to which f, summed over the lanes' maxima of the whole row, reaches `target`; the
+    // last bin where the row does not.  Every lane's maximum is a logit of its own, so that so much lies
+    // in the bins up to that one at least.
+    template <class F> __device__ __forceinline__ int reach(F f, u64 target, bool &reached)
+    {
+        unsigned *hist = reinterpret_cast<unsigned *>(bins);
+        for (int i = tid; i < kBins; i += kThreads)
+            hist[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < (c1 - c0) * 32; i += kThreads) {
+            const float x = lane_max[i];
+            const unsigned w = x > -CUDART_INF_F ? f(x) : 0u;
+            if (w)
+                atomicAdd(hist + bin_of(x), w);
+        }
+        barrier();
+        u64 w[8] = {}, s = 0;
+        for (int r = 0; r < size; ++r) {
+            const uint4 *h = reinterpret_cast<const uint4 *>(cluster.map_shared_rank(hist, r)) + tid * 2;
+            const uint4 a = h[0], b = h[1];
+            w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w;
+            w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            s += w[i];
+        const u64 upto = inclusive_scan(s, lane);
+        if (lane == 31)
+            scratch[warp] = upto;
+        if (tid == 0)
+            scratch[kWarps] = ~0ull;
+        __syncthreads();
+        u64 at = upto - s;
+        for (int i = 0; i < warp; ++i)
+            at += scratch[i];
+        if (at < target && at + s >= target) {
+            int i = 0;
+            while (i < 7 && at + w[i] < target)
+                at += w[i++];
+            scratch[kWarps] = tid * 8 + i;
+        }
+        __syncthreads();
+        const u64 b = scratch[kWarps];
+        reached = b != ~0ull;
+        return reached ? (int)b : kBins - 1;
+    }
+    // Logits of the row in bins up to `last`, as (order, token), into the list of the cluster's first CTA;
+    // returns how many there are (more than kList: the list is not whole).
+    __device__ __forceinline__ int gather(int last, int *count)
+    {
+        u64 *to = cluster.map_shared_rank(list, 0);
+        int *n = cluster.map_shared_rank(count, 0);
+        bool full = false;
+        for (int i = tid; i < (c1 - c0) * 32; i += kThreads) {
+            if (full || !(lane_max[i] > -CUDART_INF_F) || bin_of(lane_max[i]) > last)
+                continue;
+            const int v0 = (c0 + (i >> 5)) * kU * 32 + (i & 31);
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const uint4 raw = view.masked(v0 + u * 32);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = View::value(raw, e);
+                    if (!full && x > -CUDART_INF_F && bin_of(x) <= last) {
+                        const int at = atomicAdd(n, 1);
+                        full = at >= kList;
+                        if (!full)
+                            to[at] = ((u64)order_of(x) << 32) | (unsigned)(view.token(v0 + u * 32) + e);
+                    }
+                }
+            }
+        }
+        barrier();
+        return *n;
+    }
     // The largest of the CTAs' (warp 0's) tokens, for all
     __device__ __forceinline__ int everybody(int tok)
     {
@@ -375,9 +470,14 @@ template <bool BF16> struct Row {
     }
 };
 
-// Bitonic sort of n (a power of two) numbers in shared memory.
-__device__ __forceinline__ void sort_list(u64 *list, int n)
+// Bitonic sort of `found` numbers in shared memory (room for the next power of two).
+__device__ __forceinline__ void sort_list(u64 *list, int found)
 {
+    int n = 1;
+    while (n < found)
+        n <<= 1;
+    for (int i = found + threadIdx.x; i < n; i += kThreads)
+        list[i] = ~0ull;
     for (int k = 2; k <= n; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
             __syncthreads();
@@ -393,16 +493,103 @@ __device__ __forceinline__ void sort_list(u64 *list, int n)
     __syncthreads();
 }
 
+// The token of a row whose `found` candidates are in the list of this CTA: the tokens below `low` and
+// beyond top_k leave, then top_p of `whole` (0: of what is left) is kept.  done(token, logit, kept mass) by one thread.
+template <bool BF16, class F>
+__device__ __forceinline__ void from_list(Row<BF16> &r, int found, int top_k, float low, float top_p, u64 whole, float u, int *count,
+                                          F done)
+{
+    const int tid = r.tid, lane = r.lane, warp = r.warp;
+    sort_list(r.list, found);
+    if (tid == 0)
+        *count = 0;
+    __syncthreads();
+    // the cuts by rank and by logit keep a prefix
+    int n = 0;
+    for (int i = tid; i < found; i += kThreads)
+        n += logit_of((unsigned)(r.list[i] >> 32)) >= low;
+    n = __reduce_add_sync(kFull, n);
+    if (lane == 0 && n)
+        atomicAdd(count, n);
+    __syncthreads();
+    n = min(*count, top_k > 0 ? min(top_k, found) : found);
+    // running sums of the weights, kThreads of them at a time, into bins
+    u64 base = 0;
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+        const int i = i0 + tid;
+        const u64 w = i < n ? r.weight(logit_of((unsigned)(r.list[i] >> 32))) : 0;
+        const u64 upto = inclusive_scan(w, lane);
+        __syncthreads();
+        if (lane == 31)
+            r.scratch[warp] = upto;
+        __syncthreads();
+        u64 below = base;
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) {
+            below += j < warp ? r.scratch[j] : 0;
+            base += r.scratch[j];
+        }
+        if (i < n)
+            r.bins[i] = below + upto;
+    }
+    __syncthreads();
+    if (top_p < 1.f) {                                   // the first whose running sum reaches the target ends the prefix
+        const u64 target = part_of(whole ? whole : r.bins[n - 1], top_p, true);
+        int lo = 0, hi = n - 1;                          // (every thread looks for itself)
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (r.bins[mid] >= target)
+                hi = mid;
+            else
+                lo = mid + 1;
+        }
+        n = lo + 1;
+    }
+    const u64 kept = r.bins[n - 1], t = part_of(kept, u, false);
+    // by id: bit by bit, is the sum over the ids below the next half above t?
+    auto weight_at = [&](int i) { return r.bins[i] - (i ? r.bins[i - 1] : 0); };
+    unsigned id = 0;
+    u64 below = 0;
+    if (n <= 32) {
+        if (warp == 0) {
+            const u64 w = lane < n ? weight_at(lane) : 0;
+            const unsigned mine = lane < n ? (unsigned)r.list[lane] : ~0u;
+            u64 upto = 0;
+            for (int j = 0; j < n; ++j) {
+                const u64 o = __shfl_sync(kFull, w, j);
+                upto += __shfl_sync(kFull, mine, j) <= mine ? o : 0;
+            }
+            id = __reduce_min_sync(kFull, lane < n && upto > t ? mine : ~0u);
+            if (lane < n && mine == id)
+                done((int)id, logit_of((unsigned)(r.list[lane] >> 32)), kept);
+        }
+        __syncthreads();
+        return;
+    }
+    for (int bit = 22; bit >= 0; --bit) {
+        u64 s = 0;
+        for (int i = tid; i < n; i += kThreads)
+            s += ((unsigned)r.list[i] >> bit) == id << 1 ? weight_at(i) : 0;
+        s = r.block_sum(s);
+        const bool upper = below + s <= t;
+        below += upper ? s : 0;
+        id = id << 1 | (upper ? 1u : 0u);
+    }
+    for (int i = tid; i < n; i += kThreads)
+        if ((unsigned)r.list[i] == id)
+            done((int)id, logit_of((unsigned)(r.list[i] >> 32)), kept);
+}
+
 template <bool BF16, bool TOP>
 __global__ void __launch_bounds__(kThreads, 4)
 sample_kernel(const __grid_constant__ SampleParams p)
 {
     using View = RowView<BF16>;
     constexpr int N = View::N;
-    extern __shared__ u64 s_dynamic[];                   // bins, then masses and maxima of the chunks
+    extern __shared__ u64 s_dynamic[];                   // list, bins, then masses and maxima of the chunks
     __shared__ Word s_word[2];
     __shared__ u64 s_scratch[kWarps + 4];
-    __shared__ int s_count;
+    __shared__ int s_count, s_left;
     cstr_wait_for_earlier_kernels();
     cstr_let_next_kernel_start();
     cg::cluster_group cluster = cg::this_cluster();
@@ -467,9 +654,11 @@ sample_kernel(const __grid_constant__ SampleParams p)
     r.c1 = min(r.c0 + per, chunks);
     r.c = c;
     r.unit = __hiloint2double((1023 + p.scale_bits) << 20, 0);
-    r.bins = s_dynamic;
-    r.chunk_mass = s_dynamic + kBins;
+    r.list = s_dynamic;
+    r.bins = s_dynamic + kList;
+    r.chunk_mass = r.bins + kBins;
     r.chunk_max = reinterpret_cast<float *>(r.chunk_mass + p.per);
+    r.lane_max = r.chunk_max + p.per;
     r.word = s_word;
     r.scratch = s_scratch;
     r.phase = 0;
@@ -478,6 +667,8 @@ sample_kernel(const __grid_constant__ SampleParams p)
 
     // One pass over memory: maximum of every chunk, sum of its weights relative to it (bits of a double).
     const bool plain = !TOP && !cold && top_k <= 0 && top_p >= 1.f && min_p <= 0.f;
+    // top_p of the whole distribution: its sum decides, too
+    const bool exact_sum = plain || (!TOP && !cold && top_k <= 0 && top_p < 1.f && min_p <= 0.f);
     const float c32 = (float)c;
     for (int ch = r.c0 + warp; ch < r.c1; ch += kWarps) {
         uint4 raw[kU];
@@ -490,9 +681,10 @@ sample_kernel(const __grid_constant__ SampleParams p)
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 top = fmaxf(top, View::value(raw[i], e));
+        r.lane_max[(ch - r.c0) * 32 + lane] = top;
         top = warp_max(top);
         double sum = 0.0;
-        if (top == CUDART_INF_F || (plain && top > -CUDART_INF_F)) {
+        if (top == CUDART_INF_F || (exact_sum && top > -CUDART_INF_F)) {
 #pragma unroll
             for (int i = 0; i < kU; ++i)
 #pragma unroll
@@ -550,37 +742,42 @@ sample_kernel(const __grid_constant__ SampleParams p)
         if (m == -CUDART_INF_F)
             r.barrier();                                  // (the words have been read)
         else {
-            Cut cut = {-CUDART_INF_F, kNone};
-            r.select([](float, int) { return (u64)1; }, (u64)p.n, cut);
-            // every CTA's kept tokens into the list of the first one
-            u64 *list = cluster.map_shared_rank(r.bins, 0);
-            int *count = cluster.map_shared_rank(&s_count, 0);
-            r.each([&](float x, int tok) {
-                if (cut.keeps(x, tok)) {
-                    const int at = atomicAdd(count, 1);
-                    if (at < kBins)
-                        list[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
-                }
-            });
-            r.barrier();
-            found = min(s_count, p.n);
+            bool reached;
+            found = r.gather(r.reach([](float) { return 1u; }, (u64)p.n, reached), &s_count);
+            if (found > kList) {                          // many equal logits, or more tokens than half the lanes
+                Cut cut = {-CUDART_INF_F, kNone};
+                r.select([](float, int) { return (u64)1; }, (u64)p.n, cut);
+                if (tid == 0)
+                    s_count = 0;
+                r.barrier();
+                // every CTA's kept tokens into the list of the first one
+                u64 *list = cluster.map_shared_rank(r.list, 0);
+                int *count = cluster.map_shared_rank(&s_count, 0);
+                r.each([&](float x, int tok) {
+                    if (cut.keeps(x, tok)) {
+                        const int at = atomicAdd(count, 1);
+                        if (at < kList)
+                            list[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
+                    }
+                });
+                r.barrier();
+                found = s_count;
+            }
         }
-        if (part != 0)
+        if (part != 0) {
+            r.leave();
             return;
-        int power = 1;
-        while (power < found)
-            power <<= 1;
-        for (int i = found + tid; i < power; i += kThreads)
-            r.bins[i] = ~0ull;
-        sort_list(r.bins, power);
+        }
+        sort_list(r.list, found);
         const double log_total = log(total);
         for (int i = tid; i < p.n; i += kThreads) {
-            const u64 e = i < found ? r.bins[i] : 0;
+            const u64 e = i < found ? r.list[i] : 0;
             const float x = logit_of((unsigned)(e >> 32));
             const double z = x == m ? 0.0 : ((double)x - (double)m) * c * 0.6931471805599453;
             p.ids[(long long)row * p.n + i] = i < found ? (int)(unsigned)e : -1;
             p.logp[(long long)row * p.n + i] = i < found ? (float)(z - log_total) : -CUDART_INF_F;
         }
+        r.leave();
         return;
     }
 
@@ -632,10 +829,36 @@ sample_kernel(const __grid_constant__ SampleParams p)
         __syncthreads();
         mass = r.share_masses();
     } else {
-        if (min_p > 0.f) {
-            const float x = m == CUDART_INF_F ? m : fminf(m, __double2float_ru((double)m + log((double)min_p) * (1.4426950408889634 / c)));
-            tighten({x, kNone});
+        const float low = min_p <= 0.f ? -CUDART_INF_F : m == CUDART_INF_F ? m : fminf(m, __double2float_ru((double)m + log((double)min_p) * (1.4426950408889634 / c)));
+        // A list of the tokens that can be kept, where few can
+        bool reached = min_p > 0.f;
+        int last = min_p > 0.f ? r.bin_of(low) : kBins - 1;
+        if (top_k > 0 && top_k <= kList) {
+            bool some;
+            const int b = r.reach([](float) { return 1u; }, (u64)top_k, some);
+            last = min(last, b);
+            reached = true;
+        } else if (top_k <= 0 && min_p <= 0.f) {
+            // the lanes' maxima hold top_p of the whole sum (each counted somewhat too low)
+            const float most = 0x1p+31f / (float)(p.per * 32);
+            last = r.reach([&](float x) { return (unsigned)(x == m ? most : exp2_fast((x - m) * c32) * 0.9999847f * most); },
+                           (u64)((double)top_p * total * (double)most) + 2, reached);
         }
+        int found = kList + 1;
+        if (reached)
+            found = r.gather(last, &s_count);
+        if (found <= kList) {
+            if (part == 0)
+                from_list(r, found, top_k, low, top_p, exact_sum ? (u64)__double2ll_rn(total * r.unit) : 0, u, &s_left,
+                          [&](int tok, float x, u64 kept) {
+                              const double z = x == m ? 0.0 : ((double)x - (double)m) * c * 0.6931471805599453;
+                              finish(tok, (float)(z - log(total)), (float)((double)kept / r.unit / total));
+                          });
+            r.leave();
+            return;
+        }
+        if (min_p > 0.f)
+            tighten({low, kNone});
         if (top_k > 0) {
             Cut k;
             if (r.select([](float, int) { return (u64)1; }, (u64)top_k, k))
@@ -706,7 +929,7 @@ int run(const char *name, const cstr_table_t *const *tables, int32_t n_tables, c
     p.scale_bits = 62;
     while ((1LL << (62 - p.scale_bits)) < vocab_size)
         --p.scale_bits;
-    const int smem = (kBins + p.per) * 8 + p.per * 4;
+    const int smem = (kList + kBins + p.per) * 8 + p.per * 33 * 4;
     void (*kernel)(SampleParams) = bf16 ? sample_kernel<true, TOP> : sample_kernel<false, TOP>;
     if (size > 8)
         CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));

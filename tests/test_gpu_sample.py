@@ -232,3 +232,22 @@ def test_refusals_on_a_device():
         cstr.cstr_top_logprobs(None, x, None, torch.zeros(N, 1025, dtype=torch.int32, device=DEV), torch.zeros(N, 1025, device=DEV))
     assert e.value.code == -2
     cstr.cstr_sample(None, x[:0], None, i[:0], f[:0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_lists_that_overflow_or_hold_everything(dtype):
+    # candidates around the 2,048 that a list holds, by every way that leads there
+    N, V = 6, 9001
+    rng = np.random.default_rng(12)
+    x = logits(12, N, V, dtype, sigma=0.3, peaks=2)
+    u = rng.random(N).astype(np.float32)
+    x[0] = x[0].round()                                      # few values, thousands of each
+    check_sample(x, u, top_k=np.array([2047, 2048, 2049, 2048, 1500, 4096], np.int32))
+    check_sample(x, u, top_k=np.array([50, 600, 700, 8999, 9000, 9001], np.int32), top_p=np.full(N, 0.7, np.float32))
+    check_sample(x, u, min_p=np.array([1e-3, 1e-2, 0.5, 0.02, 1e-5, 1e-30], np.float32), top_k=np.full(N, 1200, np.int32))
+    check_sample(x, u, top_p=np.array([0.1, 0.2, 0.25, 0.3, 0.5, 0.05], np.float32))
+    check_top(x, 1024)
+    x[1, ::2] = 40.0                                         # 4,501 equal ones at the top
+    check_top(x, 1024)
+    check_sample(x, u, top_k=np.full(N, 100, np.int32))
+    check_sample(x, u, top_p=np.full(N, 0.01, np.float32))
