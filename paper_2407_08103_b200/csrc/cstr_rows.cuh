@@ -158,14 +158,12 @@ template <bool BF16> struct RowView {
     }
 };
 
-// 2^t for t <= 0 to 1.2e-12: t = n + f, the polynomial of degree 8 that meets 2^f at the nine
-// Chebyshev points of [-1/2, 1/2] (1.1e-12 at most, exact at 0), the exponent by integer addition.
-__device__ __forceinline__ double exp2_64(double t)
+// 2^(d c) for d c in [-1020, 0] to 1.2e-12: d c = n + f, the polynomial of degree 8 that meets 2^f at the
+// nine Chebyshev points of [-1/2, 1/2] (1.1e-12 at most, exact at 0), the exponent by integer addition.
+__device__ __forceinline__ double exp2_of_product(double d, double c)
 {
-    if (!(t > -1000.0))
-        return 0.0;
     const double shift = 6755399441055744.0;                 // 1.5 * 2^52: adding it rounds to a whole number
-    const double r = t + shift, f = t - (r - shift);
+    const double r = fma(d, c, shift), f = fma(d, c, shift - r);
     double p = 1.3255224887502117e-06;
     p = fma(p, f, 1.531007940254368e-05);
     p = fma(p, f, 0.0001540345585240991);
@@ -176,6 +174,11 @@ __device__ __forceinline__ double exp2_64(double t)
     p = fma(p, f, 0.6931471805459335);
     p = fma(p, f, 1.0);
     return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
+}
+// ... for any d c <= 0
+__device__ __forceinline__ double exp2_64(double d, double c)
+{
+    return d * c > -1000.0 ? exp2_of_product(d, c) : 0.0;
 }
 
 __device__ __forceinline__ float exp2_fast(float x)

@@ -29,7 +29,8 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
-constexpr int kU = 4;                     // vectors of a lane in flight; a chunk is 32 * kU vectors
+constexpr int kU = 4;                     // vectors of a lane in flight: a block is 32 * kU vectors
+constexpr int kMaxChunks = 128;           // chunks of a CTA, each of some blocks
 constexpr int kBins = 2048;               // digits of a selection round, distances from the maximum
 constexpr int kList = 2048;               // entries of the list
 constexpr int kNone = 0x7fffffff;
@@ -39,7 +40,7 @@ struct SampleParams {
     const void *logits;
     long long ld;
     int V, rows;
-    int per;                              // chunks of a CTA, at most
+    int per, blocks;                      // chunks of a CTA, at most; blocks of a chunk
     int scale_bits;                       // s
     u64 *oob;
     // sampling
@@ -140,7 +141,7 @@ template <bool BF16> struct Row {
     cg::cluster_group cluster;
     View view;
     int size, part, tid, lane, warp;
-    int c0, c1;                           // this CTA's chunks
+    int c0, c1, blocks;                   // this CTA's chunks, blocks of a chunk
     double c;                             // log2(e) / temperature
     float m;
     double unit;                          // 2^s
@@ -198,20 +199,44 @@ template <bool BF16> struct Row {
     }
     __device__ __forceinline__ u64 weight(float x) const
     {
-        const double w = x == m ? 1.0 : exp2_64(((double)x - (double)m) * c);
+        const double w = x == m ? 1.0 : exp2_64((double)x - (double)m, c);
         return (u64)__double2ll_rn(w * unit);
     }
-    // f(logit, token) for every allowed logit above -infinity of this CTA's chunks
-    template <class F> __device__ __forceinline__ void each(F f)
+    // Vectors first + 32 u + lane, disallowed logits as -infinity
+    __device__ __forceinline__ void load(int first, uint4 (&raw)[kU]) const
     {
-        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
-            uint4 raw[kU];
+        const int tok = view.token(first);
+        if (tok >= 0 && tok + 32 * kU * N <= view.V) {
+            const uint4 *at = reinterpret_cast<const uint4 *>(view.row - view.head * View::ESZ) + first + lane;
 #pragma unroll
             for (int u = 0; u < kU; ++u)
-                raw[u] = view.masked((ch * kU + u) * 32 + lane);
+                raw[u] = at[u * 32];
+            if (view.mrow && view.head == 0) {           // 32 vectors take N words of the mask
+                const uint32_t *w = view.mrow + (tok >> 5) + (lane * N >> 5);
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+                    raw[u] = View::mask(raw[u], __ldg(w + u * N) >> (lane * N & 31));
+            } else if (view.mrow) {
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+                    raw[u] = View::mask(raw[u], view.bits(first + u * 32 + lane));
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                raw[u] = view.masked(first + u * 32 + lane);
+        }
+    }
+    // f(logit, token) for every allowed logit above -infinity of chunk ch
+    template <class F> __device__ __forceinline__ void each_of(int ch, F f)
+    {
+#pragma unroll 1
+        for (int b = ch * blocks; b < (ch + 1) * blocks; ++b) {
+            uint4 raw[kU];
+            load(b * 32 * kU, raw);
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
-                const int tok = view.token((ch * kU + u) * 32 + lane);
+                const int tok = view.token(b * 32 * kU + u * 32 + lane);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float x = View::value(raw[u], e);
@@ -220,6 +245,85 @@ template <bool BF16> struct Row {
                 }
             }
         }
+    }
+    // ... of this CTA's chunks
+    template <class F> __device__ __forceinline__ void each(F f)
+    {
+        for (int ch = c0 + warp; ch < c1; ch += kWarps)
+            each_of(ch, f);
+    }
+    // Maximum of every lane's logits in a chunk, maximum of the chunk and its sum of 2^(c (x - maximum)) as the
+    // bits of a double: taken in 32 bits, or in 64.
+    enum { kMaximum, kSum32, kSum64 };
+    template <int WHAT> __device__ __forceinline__ void first_pass()
+    {
+        const float c32 = (float)c, reach = (float)(1000.0 / c);
+        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
+            float top = -CUDART_INF_F, s32 = 0.f;
+            double s64 = 0.0;
+#pragma unroll 1
+            for (int b = ch * blocks; b < (ch + 1) * blocks; ++b) {
+                uint4 raw[kU];
+                load(b * 32 * kU, raw);
+                float t = -CUDART_INF_F;
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        t = fmaxf(t, View::value(raw[u], e));
+                if (WHAT == kMaximum)
+                    top = fmaxf(top, t);
+                if (WHAT == kSum32) {
+                    if (t > top) {
+                        s32 *= exp2_fast((top - t) * c32);
+                        top = t;
+                    }
+                    const float ref = top == -CUDART_INF_F ? 0.f : top;
+#pragma unroll
+                    for (int u = 0; u < kU; ++u)
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            s32 += exp2_fast((View::value(raw[u], e) - ref) * c32);
+                }
+                if (WHAT == kSum64) {
+                    if (t > top) {
+                        s64 *= top == -CUDART_INF_F ? 0.0 : exp2_64((double)top - (double)t, c);
+                        top = t;
+                    }
+                    // logits far below add 2^-1000 - where floats are fine enough to say so
+                    const float least = top - reach;
+                    if (!(reach < 1e37f && fabsf(top) < reach * 1e6f)) {
+                        for (int u = 0; u < kU * N && top > -CUDART_INF_F; ++u) {
+                            const float x = View::value(raw[u / N], u % N);
+                            s64 += x == top ? 1.0 : exp2_64((double)x - (double)top, c);
+                        }
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < kU; ++u)
+#pragma unroll
+                            for (int e = 0; e < N; ++e)
+                                s64 += exp2_of_product((double)fmaxf(View::value(raw[u], e), least) - (double)top, c);
+                    }
+                }
+            }
+            lane_max[(ch - c0) * 32 + lane] = top;
+            const float most = warp_max(top);
+            double sum = 0.0;
+            if (WHAT == kSum32)
+                sum = s32 * exp2_fast(top == most ? 0.f : (top - most) * c32);
+            if (WHAT == kSum64 && top > -CUDART_INF_F)
+                sum = s64 * exp2_64((double)top - (double)most, c);
+            if (most == CUDART_INF_F) {                  // infinite logits share the sum
+                sum = 0.0;
+                each_of(ch, [&](float x, int) { sum += x == CUDART_INF_F ? 1.0 : 0.0; });
+            }
+            sum = warp_sum(sum);
+            if (lane == 0) {
+                chunk_max[ch - c0] = most;
+                chunk_mass[ch - c0] = (u64)__double_as_longlong(sum);
+            }
+        }
+        __syncthreads();
     }
     // This CTA's and the row's sums of the chunks' masses; returns the row's.
     __device__ __forceinline__ u64 share_masses()
@@ -237,17 +341,7 @@ template <bool BF16> struct Row {
     {
         for (int ch = c0 + warp; ch < c1; ch += kWarps) {
             u64 s = 0;
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int v = (ch * kU + u) * 32 + lane;
-                const uint4 raw = view.masked(v);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float x = View::value(raw, e);
-                    if (x > -CUDART_INF_F)
-                        s += f(x, view.token(v) + e);
-                }
-            }
+            each_of(ch, [&](float x, int tok) { s += f(x, tok); });
             s = warp_sum(s);
             if (lane == 0)
                 chunk_mass[ch - c0] = s;
@@ -278,8 +372,7 @@ template <bool BF16> struct Row {
                 break;
         }
         int last = -1;                                   // last token with any weight
-        for (int u = 0; u < kU; ++u) {
-            const int v = (ch * kU + u) * 32 + lane;
+        for (int v = ch * blocks * kU * 32 + lane; v < (ch + 1) * blocks * kU * 32; v += 32) {
             const uint4 raw = view.masked(v);
             u64 s = 0;
 #pragma unroll
@@ -311,91 +404,132 @@ template <bool BF16> struct Row {
             last = max(last, __shfl_xor_sync(kFull, last, off));
         return last;
     }
-    // The shortest prefix of the row's order whose sum of f reaches `target` (>= 1); false: the whole row
-    // does not.  Equal logits have equal f.
-    template <class F> __device__ __forceinline__ bool select(F f, u64 target, Cut &cut)
+    // Distance from the maximum as one of kBins numbers, ascending: 32 to an octave from 2^-30 on.
+    static constexpr int kFirstBin = ((127 - 30) << 5) - 1;
+    __device__ __forceinline__ int bin_of(float x) const
     {
-        unsigned prefix = 0;
-        u64 sum = 0, at = 0;                             // mass before the digit, mass of the digit
-        const int shifts[4] = {32, 21, 10, 0};
-#pragma unroll 1
-        for (int round = 0; round < 3; ++round) {
-            const int shift = shifts[round + 1], above = shifts[round];
-            const unsigned digits = 1u << (above - shift);
-            for (int i = tid; i < kBins; i += kThreads)
-                bins[i] = 0;
-            __syncthreads();
-            each([&](float x, int tok) {
-                const unsigned o = order_of(x);
-                if (round == 0 || (o >> above) == prefix)
-                    atomicAdd(bins + ((o >> shift) & (digits - 1)), f(x, tok));
-            });
-            barrier();
-            u64 w[kBins / kThreads], s = 0;
+        if (x == m)
+            return 0;
+        const int b = (int)(__float_as_uint(m - x) >> 18) - kFirstBin;
+        return min(max(b, 1), kBins - 1);
+    }
+    // The first bin at which the cluster's sum over `bins` reaches target - sum: adds to sum what lies
+    // before it, `at` is its own; -1: none does.  All CTAs' bins have been read when it returns.
+    __device__ __forceinline__ int merge_bins(u64 target, u64 &sum, u64 &at)
+    {
+        barrier();
+        u64 w[kBins / kThreads], s = 0;
 #pragma unroll
-            for (int i = 0; i < kBins / kThreads; ++i) {
-                w[i] = 0;
-                for (int r = 0; r < size; ++r)
-                    w[i] += *cluster.map_shared_rank(bins + tid * (kBins / kThreads) + i, r);
-                s += w[i];
+        for (int i = 0; i < kBins / kThreads; ++i)
+            w[i] = 0;
+        for (int r = 0; r < size; ++r) {
+            const ulonglong2 *h = reinterpret_cast<const ulonglong2 *>(cluster.map_shared_rank(bins, r)) + tid * (kBins / kThreads / 2);
+#pragma unroll
+            for (int i = 0; i < kBins / kThreads / 2; ++i) {
+                const ulonglong2 o = h[i];
+                w[2 * i] += o.x;
+                w[2 * i + 1] += o.y;
             }
-            const u64 upto = inclusive_scan(s, lane);
-            __syncthreads();
-            if (lane == 31)
-                scratch[warp] = upto;
-            if (tid == 0)
-                scratch[kWarps] = ~0ull;
-            __syncthreads();
-            u64 base = sum;
-            for (int i = 0; i < warp; ++i)
-                base += scratch[i];
-            if (base + upto >= target && base + upto - s < target) {
-                u64 b = base + upto - s;
-                int i = 0;
-                while (i < kBins / kThreads - 1 && b + w[i] < target)
-                    b += w[i++];
-                scratch[kWarps] = tid * (kBins / kThreads) + i;
-                scratch[kWarps + 1] = b;
-                scratch[kWarps + 2] = w[i];
-            }
-            __syncthreads();
-            const u64 digit = scratch[kWarps];
+        }
+#pragma unroll
+        for (int i = 0; i < kBins / kThreads; ++i)
+            s += w[i];
+        const u64 upto = inclusive_scan(s, lane);
+        if (lane == 31)
+            scratch[warp] = upto;
+        if (tid == 0)
+            scratch[kWarps] = ~0ull;
+        __syncthreads();
+        u64 base = sum + upto - s;
+        for (int i = 0; i < warp; ++i)
+            base += scratch[i];
+        if (base + s >= target && base < target) {
+            int i = 0;
+            u64 mine = 0;
+#pragma unroll
+            for (int j = 0; j < kBins / kThreads; ++j)
+                if (i == j) {
+                    mine = w[j];
+                    if (j < kBins / kThreads - 1 && base + w[j] < target) {
+                        base += w[j];
+                        ++i;
+                    }
+                }
+            scratch[kWarps] = tid * (kBins / kThreads) + i;
+            scratch[kWarps + 1] = base;
+            scratch[kWarps + 2] = mine;
+        }
+        __syncthreads();
+        const u64 found = scratch[kWarps];
+        if (found != ~0ull) {
             sum = scratch[kWarps + 1];
             at = scratch[kWarps + 2];
-            barrier();                                   // the bins have been read
-            if (digit == ~0ull)
-                return false;
-            prefix = (prefix << (above - shift)) | (unsigned)digit;
         }
-        cut.x = logit_of(prefix);
+        barrier();
+        return found == ~0ull ? -1 : (int)found;
+    }
+    template <class F> __device__ __forceinline__ void fill_bins(F f)      // f(logit, token, bin): weight, 0: none
+    {
+        for (int i = tid; i < kBins; i += kThreads)
+            bins[i] = 0;
+        __syncthreads();
+        each([&](float x, int tok) {
+            int bin;
+            const u64 w = f(x, tok, bin);
+            if (w)
+                atomicAdd(bins + bin, w);
+        });
+    }
+    // The shortest prefix of the row's order whose sum of f reaches `target` (>= 1); false: the whole row
+    // does not.  Equal logits have equal f.  First by distance from the maximum, which spreads the logits over
+    // the bins, then by 11 digits of the ordered bits at a time among those of one bin.
+    template <class F> __device__ __forceinline__ bool select(F f, u64 target, Cut &cut)
+    {
+        u64 sum = 0, at = 0;
+        fill_bins([&](float x, int tok, int &bin) {
+            bin = bin_of(x);
+            return f(x, tok);
+        });
+        const int b = merge_bins(target, sum, at);
+        if (b < 0)
+            return false;
+        // the bin's logits lie within m - [d0, d1], widened by the difference's rounding
+        const float d0 = b <= 1 ? 0.f : __uint_as_float((unsigned)(b + kFirstBin) << 18) * (1.f - 0x1p-22f);
+        const float d1 = b == 0 ? 0.f : b == kBins - 1 ? CUDART_INF_F : __uint_as_float((unsigned)(b + 1 + kFirstBin) << 18) * (1.f + 0x1p-22f);
+        unsigned lo = b == 0 ? order_of(m) : max(order_of(m), order_of(m - d0) - 2);
+        const unsigned hi = b == 0 ? lo : m == CUDART_INF_F ? order_of(-CUDART_INF_F) : min(order_of(m - d1) + 2, order_of(-CUDART_INF_F));
+        int bits = hi > lo ? 32 - __clz((int)(hi - lo)) : 0;
+#pragma unroll 1
+        while (bits > 0) {
+            const int shift = max(bits - 11, 0);
+            fill_bins([&](float x, int tok, int &bin) {
+                const unsigned o = order_of(x) - lo;
+                bin = (int)(o >> shift);
+                return o >> bits == 0 && bin_of(x) == b ? f(x, tok) : (u64)0;
+            });
+            const int digit = merge_bins(target, sum, at);
+            if (digit < 0)
+                return false;                            // (cannot be: the bin reached it)
+            lo += (unsigned)digit << shift;
+            bits = shift;
+        }
+        cut.x = logit_of(lo);
         cut.last = kNone;
         const u64 one = f(cut.x, 0), r = (target - sum + one - 1) / one;      // equal logits that are kept
         if (r * one < at) {
             const float x = cut.x;
             auto tie = [x](float v, int) { return (u64)(v == x); };
             mass_pass(tie);
-            const int tok = find(tie, r - 1);
-            cut.last = everybody(tok);
+            cut.last = everybody(find(tie, r - 1));
         }
         return true;
-    }
-    // Distance from the maximum as one of kBins numbers, ascending: 32 to an octave from 2^-30 on.
-    __device__ __forceinline__ int bin_of(float x) const
-    {
-        if (x == m)
-            return 0;
-        const int b = (int)(__float_as_uint(m - x) >> 18) - (((127 - 30) << 5) - 1);
-        return min(max(b, 1), kBins - 1);
     }
     // The lowest bin up to which f, summed over the lanes' maxima of the whole row, reaches `target`; the
     // last bin where the row does not.  Every lane's maximum is a logit of its own, so that so much lies
     // in the bins up to that one at least.
     template <class F> __device__ __forceinline__ int reach(F f, u64 target, bool &reached)
     {
-        unsigned *hist = reinterpret_cast<unsigned *>(bins);
-        for (int i = tid; i < kBins; i += kThreads)
-            hist[i] = 0;
-        __syncthreads();
+        unsigned *hist = reinterpret_cast<unsigned *>(bins);     // zero since the kernel began
         for (int i = tid; i < (c1 - c0) * 32; i += kThreads) {
             const float x = lane_max[i];
             const unsigned w = x > -CUDART_INF_F ? f(x) : 0u;
@@ -443,9 +577,8 @@ template <bool BF16> struct Row {
         for (int i = tid; i < (c1 - c0) * 32; i += kThreads) {
             if (full || !(lane_max[i] > -CUDART_INF_F) || bin_of(lane_max[i]) > last)
                 continue;
-            const int v0 = (c0 + (i >> 5)) * kU * 32 + (i & 31);
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
+            const int v0 = (c0 + (i >> 5)) * blocks * kU * 32 + (i & 31);
+            for (int u = 0; u < blocks * kU; ++u) {
                 const uint4 raw = view.masked(v0 + u * 32);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
@@ -649,7 +782,8 @@ sample_kernel(const __grid_constant__ SampleParams p)
     }
 
     Row<BF16> r = {cluster, View(p.logits, (long long)row * p.ld, p.V, mrow), size, part, tid, lane, warp};
-    const int chunks = (r.view.vectors() + 32 * kU - 1) / (32 * kU), per = (chunks + size - 1) / size;
+    r.blocks = p.blocks;
+    const int chunks = (r.view.vectors() + 32 * kU * p.blocks - 1) / (32 * kU * p.blocks), per = (chunks + size - 1) / size;
     r.c0 = min(part * per, chunks);
     r.c1 = min(r.c0 + per, chunks);
     r.c = c;
@@ -665,53 +799,22 @@ sample_kernel(const __grid_constant__ SampleParams p)
     if (tid == 0)
         s_count = 0;
 
-    // One pass over memory: maximum of every chunk, sum of its weights relative to it (bits of a double).
+    for (int i = tid; i < kBins / 2; i += kThreads)
+        r.bins[i] = 0;
+    // One pass over memory.  Where the whole sum decides about the token it is taken in 64 bits.
     const bool plain = !TOP && !cold && top_k <= 0 && top_p >= 1.f && min_p <= 0.f;
-    // top_p of the whole distribution: its sum decides, too
     const bool exact_sum = plain || (!TOP && !cold && top_k <= 0 && top_p < 1.f && min_p <= 0.f);
     const float c32 = (float)c;
-    for (int ch = r.c0 + warp; ch < r.c1; ch += kWarps) {
-        uint4 raw[kU];
-#pragma unroll
-        for (int i = 0; i < kU; ++i)
-            raw[i] = r.view.masked((ch * kU + i) * 32 + lane);
-        float top = -CUDART_INF_F;
-#pragma unroll
-        for (int i = 0; i < kU; ++i)
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                top = fmaxf(top, View::value(raw[i], e));
-        r.lane_max[(ch - r.c0) * 32 + lane] = top;
-        top = warp_max(top);
-        double sum = 0.0;
-        if (top == CUDART_INF_F || (exact_sum && top > -CUDART_INF_F)) {
-#pragma unroll
-            for (int i = 0; i < kU; ++i)
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float x = View::value(raw[i], e);
-                    sum += x == top ? 1.0 : exp2_64(((double)x - (double)top) * c);
-                }
-        } else if (top > -CUDART_INF_F) {
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < kU; ++i)
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    s += exp2_fast((View::value(raw[i], e) - top) * c32);
-            sum = s;
-        }
-        sum = warp_sum(sum);
-        if (lane == 0) {
-            r.chunk_max[ch - r.c0] = top;
-            r.chunk_mass[ch - r.c0] = (u64)__double_as_longlong(sum);
-        }
-    }
-    __syncthreads();
+    if (!TOP && cold)
+        r.template first_pass<Row<BF16>::kMaximum>();
+    else if (!TOP && exact_sum)
+        r.template first_pass<Row<BF16>::kSum64>();
+    else
+        r.template first_pass<Row<BF16>::kSum32>();
     auto chunk_sum = [&](int i, float ref) {              // relative to ref
         const float top = r.chunk_max[i];
         const double s = __longlong_as_double((long long)r.chunk_mass[i]);
-        return top == ref ? s : s * exp2_64(((double)top - (double)ref) * c);
+        return top == ref ? s : s * exp2_64((double)top - (double)ref, c);
     };
     float m = -CUDART_INF_F;
     for (int i = tid; i < r.c1 - r.c0; i += kThreads)
@@ -732,7 +835,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     r.m = m;
     double total = 0.0;                                   // of the row, relative to m
     if (lane < size && all.sum > 0.0)
-        total = all.m == m ? all.sum : all.sum * exp2_64(((double)all.m - (double)m) * c);
+        total = all.m == m ? all.sum : all.sum * exp2_64((double)all.m - (double)m, c);
     total = warp_sum(total);
 
     if (TOP) {
@@ -786,7 +889,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     if (m == -CUDART_INF_F) {
         // nothing above -infinity: the first allowed token that is not NaN, if there is one
         int first = kNone;
-        for (int i = r.c0 * kU * 32 * N - r.view.head + tid; i < min(p.V, r.c1 * kU * 32 * N - r.view.head); i += kThreads)
+        for (int i = r.c0 * p.blocks * kU * 32 * N - r.view.head + tid; i < min(p.V, r.c1 * p.blocks * kU * 32 * N - r.view.head); i += kThreads)
             if (i >= 0 && i < first && r.view.allowed(i) && r.view.one(i) == -CUDART_INF_F)
                 first = i;
         first = __reduce_min_sync(kFull, first);
@@ -847,6 +950,8 @@ sample_kernel(const __grid_constant__ SampleParams p)
         int found = kList + 1;
         if (reached)
             found = r.gather(last, &s_count);
+        else
+            r.barrier();                                  // (every CTA's bins have been read)
         if (found <= kList) {
             if (part == 0)
                 from_list(r, found, top_k, low, top_p, exact_sum ? (u64)__double2ll_rn(total * r.unit) : 0, u, &s_left,
@@ -864,7 +969,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
             if (r.select([](float, int) { return (u64)1; }, (u64)top_k, k))
                 tighten(k);
         }
-        mass = r.mass_pass(kept_weight);
+        mass = exact_sum ? (u64)__double2ll_rn(total * r.unit) : r.mass_pass(kept_weight);
         if (top_p < 1.f) {
             Cut k;
             if (r.select([&](float x, int) { return r.weight(x); }, part_of(mass, top_p, true), k))
@@ -886,11 +991,11 @@ sample_kernel(const __grid_constant__ SampleParams p)
 
 namespace {
 
-// CTAs of a row: 64 chunks each, smaller shares, down to 8, while there are fewer CTAs than two per SM
-int cluster_size(int rows, int chunks, int sms)
+// CTAs of a row, of so many blocks: two CTAs per SM, shares of at least 8 blocks
+int cluster_size(int rows, int blocks, int sms)
 {
     int size = 1;
-    while (size < kMaxCluster && (chunks > 64 * size || (rows * (long long)size <= sms && chunks >= 16 * size)))
+    while (size < kMaxCluster && rows * (long long)size < 2 * sms && blocks >= 16 * size)
         size *= 2;
     return size;
 }
@@ -921,10 +1026,12 @@ int run(const char *name, const cstr_table_t *const *tables, int32_t n_tables, c
     p.oob = CSTR_OOB_RECORD();
     const bool bf16 = dtype == CSTR_BF16;
     const int n = bf16 ? 8 : 4;
-    const int chunks = (vocab_size + n - 1 + 32 * kU * n - 1) / (32 * kU * n);       // (a row may begin inside a vector)
-    const int size = cluster_size(rows, chunks, sms);
+    const int blocks = (vocab_size + n - 1 + 32 * kU * n - 1) / (32 * kU * n);       // (a row may begin inside a vector)
+    const int size = cluster_size(rows, blocks, sms);
     if ((long long)rows * size > 0x7fffffffLL)
         return cstr_fail(CSTR_ERR_SHAPE, "%s: rows x vocabulary too large for one launch", name);
+    p.blocks = (blocks + kMaxChunks * size - 1) / (kMaxChunks * size);
+    const int chunks = (blocks + p.blocks - 1) / p.blocks;
     p.per = (chunks + size - 1) / size;
     p.scale_bits = 62;
     while ((1LL << (62 - p.scale_bits)) < vocab_size)

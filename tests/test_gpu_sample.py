@@ -251,3 +251,22 @@ def test_lists_that_overflow_or_hold_everything(dtype):
     check_top(x, 1024)
     check_sample(x, u, top_k=np.full(N, 100, np.int32))
     check_sample(x, u, top_p=np.full(N, 0.01, np.float32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("level,spread", [(-3e38, 0.0), (1e12, 1e6), (-1e12, 1e6), (1e38, 1e37), (1e-30, 1e-31), (5e10, 1.0)])
+def test_logits_of_any_size(dtype, level, spread):
+    # a common offset that floats resolve coarsely, masks of -infinity beside the lowest values, any temperature
+    N, V = 12, 3000
+    rng = np.random.default_rng(13)
+    x = (level + spread * torch.from_numpy(rng.standard_normal((N, V)))).to(dtype).to(DEV)
+    x[:, ::5] = -math.inf
+    x[1, 1:] = -math.inf
+    x[2, 7] = torch.finfo(dtype).min
+    temperature = np.array([1.0, 1.0, 1e6, 1e12, 1e37, 3e38, 1e30, 0.5, 1e-30, 2e5, 7.0, 1e33], np.float32)
+    u = rng.random(N).astype(np.float32)
+    check_sample(x, u, temperature=temperature)
+    check_sample(x, u, temperature=temperature, top_p=np.full(N, 0.6, np.float32))
+    check_sample(x, u, temperature=temperature, top_k=np.full(N, 60, np.int32), min_p=np.full(N, 0.3, np.float32))
+    check_top(x, 30)
+    check_top(x, 30, temperature=1e20)
