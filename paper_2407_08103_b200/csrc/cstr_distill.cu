@@ -107,12 +107,6 @@ template <bool BF16> __device__ __forceinline__ void store_one(char *row, int to
         ((float *)row)[tok] = x;
 }
 
-template <bool BF16> __device__ __forceinline__ float raw_value(uint4 u, int e)
-{
-    const unsigned w[4] = {u.x, u.y, u.z, u.w};
-    return BF16 ? __uint_as_float(e & 1 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16) : __uint_as_float(w[e % 4]);
-}
-
 template <bool BF16> __device__ __forceinline__ uint4 narrow(const float *d)
 {
     unsigned w[4];
@@ -255,7 +249,7 @@ distill_kernel(const __grid_constant__ DistillParams p)
         float x[N], top = -CUDART_INF_F;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            x[e] = raw_value<BF16>(raw, e);
+            x[e] = View::plain(raw, e);
             top = fmaxf(top, x[e]);
         }
         if (top > rest.m) {
@@ -356,7 +350,7 @@ distill_kernel(const __grid_constant__ DistillParams p)
         float d[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float x = raw_value<BF16>(raw, e);
+            const float x = View::plain(raw, e);
             d[e] = x == -CUDART_INF_F ? 0.f : f_rest * exp2_fast((x - low) * p.c);
         }
         put(v, d);

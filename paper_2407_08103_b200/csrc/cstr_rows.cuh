@@ -149,13 +149,13 @@ template <bool BF16> struct RowView {
     {
         return inside(v) ? mask(reinterpret_cast<const uint4 *>(row - head * ESZ)[v], bits(v)) : edge(v);
     }
-    // Logit e of a raw vector; NaN reads as -infinity.
-    static __device__ __forceinline__ float value(uint4 u, int e)
+    // Logit e of a raw vector; by value() NaN reads as -infinity.
+    static __device__ __forceinline__ float plain(uint4 u, int e)
     {
         const unsigned w[4] = {u.x, u.y, u.z, u.w};
-        const float f = BF16 ? __uint_as_float(e & 1 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16) : __uint_as_float(w[e % 4]);
-        return fmaxf(f, -CUDART_INF_F);
+        return BF16 ? __uint_as_float(e & 1 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16) : __uint_as_float(w[e % 4]);
     }
+    static __device__ __forceinline__ float value(uint4 u, int e) { return fmaxf(plain(u, e), -CUDART_INF_F); }
 };
 
 // 2^(d c) for d c in [-1020, 0] to 1.2e-12: d c = n + f, the polynomial of degree 8 that meets 2^f at the

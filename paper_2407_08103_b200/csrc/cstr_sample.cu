@@ -31,8 +31,8 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr int kU = 4;                     // vectors of a lane in flight: a block is 32 * kU vectors
 constexpr int kMaxChunks = 128;           // chunks of a CTA, each of some blocks
-constexpr int kBins = 2048;               // digits of a selection round, distances from the maximum
-constexpr int kList = 2048;               // entries of the list
+constexpr int kDigit = 9, kBins = 1 << kDigit;   // digits of a selection round, distances from the maximum
+constexpr int kList = 2048;               // entries of the list, and of the work space behind it
 constexpr int kNone = 0x7fffffff;
 
 struct SampleParams {
@@ -86,6 +86,24 @@ __device__ __forceinline__ u64 part_of(u64 a, float f, bool up)
         rest = lo << (64 - shift);
     }
     return whole + (up && rest ? 1 : 0);
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// s += 2^(c (x - ref)) for two logits, two to an instruction but for the exponential itself
+__device__ __forceinline__ void add_exponentials(float2 &s, float x, float y, float ref, float c)
+{
+    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %2};\nadd.rn.f32x2 a, a, b;\n"
+        "mov.b64 b, {%3, %3};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}\n"
+        : "+f"(x), "+f"(y) : "f"(-ref), "f"(c));
+    x = exp2_fast(x);
+    y = exp2_fast(y);
+    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}\n"
+        : "+f"(s.x), "+f"(s.y) : "f"(x), "f"(y));
 }
 
 __device__ __forceinline__ u64 inclusive_scan(u64 v, int lane)
@@ -145,8 +163,9 @@ template <bool BF16> struct Row {
     double c;                             // log2(e) / temperature
     float m;
     double unit;                          // 2^s
-    u64 *list, *bins, *chunk_mass;
+    u64 *list, *bins, *chunk_mass;        // (bins: the work space)
     float *chunk_max, *lane_max;          // per chunk; per chunk and lane
+    unsigned *mask_words;                 // of the first pass, as its ring in list and bins
     Word *word;                           // two, in turn
     u64 *scratch;                         // kWarps + 4
     int phase;
@@ -252,78 +271,157 @@ template <bool BF16> struct Row {
         for (int ch = c0 + warp; ch < c1; ch += kWarps)
             each_of(ch, f);
     }
+    // Each warp copies its blocks into a ring of its own, two ahead of the one in use; a lane reads back what
+    // it copied, but for the words of the mask.  Blocks at the row's ends are read when they are used.
+    static constexpr int kStage = kU * 32 * 16, kMaskWords = 32 * kU * N / 32 + 1;
+    __device__ __forceinline__ bool whole(int first) const
+    {
+        return view.token(first) >= 0 && view.token(first) + 32 * kU * N <= view.V;
+    }
+    __device__ __forceinline__ void fetch(int first, int stage) const
+    {
+        if (whole(first)) {
+            const char *from = view.row - view.head * View::ESZ + ((long long)first + lane) * 16;
+            const unsigned to = (unsigned)__cvta_generic_to_shared(reinterpret_cast<char *>(list) + (warp * 2 + stage) * kStage + lane * 16);
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + u * 512), "l"(from + u * 512) : "memory");
+            if (view.mrow) {
+                const int w0 = view.token(first) >> 5, last = (view.V - 1) >> 5;
+                const unsigned to_w = (unsigned)__cvta_generic_to_shared(mask_words + (warp * 2 + stage) * (kMaskWords + 3));
+                for (int i = lane; i < kMaskWords; i += 32)
+                    if (w0 + i <= last)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to_w + i * 4), "l"(view.mrow + w0 + i) : "memory");
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ void take(int first, int stage, uint4 (&raw)[kU]) const
+    {
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        if (whole(first)) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(list) + (warp * 2 + stage) * kStage) + lane;
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                raw[u] = from[u * 32];
+            if (view.mrow) {
+                const int at = (view.token(first) & 31) + lane * N;
+                const unsigned *w = mask_words + (warp * 2 + stage) * (kMaskWords + 3) + (at >> 5);
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+                    raw[u] = View::mask(raw[u], view.head == 0 ? w[u * N] >> (at & 31) : __funnelshift_r(w[u * N], w[u * N + 1], at & 31));
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                raw[u] = view.masked(first + u * 32 + lane);
+        }
+        __syncwarp();
+    }
     // Maximum of every lane's logits in a chunk, maximum of the chunk and its sum of 2^(c (x - maximum)) as the
     // bits of a double: taken in 32 bits, or in 64.
     enum { kMaximum, kSum32, kSum64 };
     template <int WHAT> __device__ __forceinline__ void first_pass()
     {
         const float c32 = (float)c, reach = (float)(1000.0 / c);
-        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
-            float top = -CUDART_INF_F, s32 = 0.f;
-            double s64 = 0.0;
-#pragma unroll 1
-            for (int b = ch * blocks; b < (ch + 1) * blocks; ++b) {
-                uint4 raw[kU];
-                load(b * 32 * kU, raw);
-                float t = -CUDART_INF_F;
+        float top = -CUDART_INF_F;
+        float2 s32 = {0.f, 0.f};
+        double s64 = 0.0;
+        auto use = [&](const uint4 (&raw)[kU]) {
+            float t = -CUDART_INF_F;
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+#pragma unroll
+                for (int e = 0; e < N; e += 2)
+                    t = max3(t, View::plain(raw[u], e), View::plain(raw[u], e + 1));
+            if (WHAT == kMaximum)
+                top = fmaxf(top, t);
+            if (WHAT == kSum32) {
+                if (t > top) {
+                    const float f = exp2_fast((top - t) * c32);
+                    s32.x *= f;
+                    s32.y *= f;
+                    top = t;
+                }
+                const float ref = top == -CUDART_INF_F ? 0.f : top;
 #pragma unroll
                 for (int u = 0; u < kU; ++u)
 #pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        t = fmaxf(t, View::value(raw[u], e));
-                if (WHAT == kMaximum)
-                    top = fmaxf(top, t);
-                if (WHAT == kSum32) {
-                    if (t > top) {
-                        s32 *= exp2_fast((top - t) * c32);
-                        top = t;
+                    for (int e = 0; e < N; e += 2)
+                        add_exponentials(s32, View::plain(raw[u], e), View::plain(raw[u], e + 1), ref, c32);
+            }
+            if (WHAT == kSum64) {
+                if (t > top) {
+                    s64 *= top == -CUDART_INF_F ? 0.0 : exp2_64((double)top - (double)t, c);
+                    top = t;
+                }
+                // logits far below (and NaN) add 2^-1000 - where floats are fine enough to say so
+                const float least = top - reach;
+                if (!(reach < 1e37f && fabsf(top) < reach * 1e6f)) {
+                    for (int u = 0; u < kU * N && top > -CUDART_INF_F; ++u) {
+                        const float x = View::value(raw[u / N], u % N);
+                        s64 += x == top ? 1.0 : exp2_64((double)x - (double)top, c);
                     }
-                    const float ref = top == -CUDART_INF_F ? 0.f : top;
+                } else {
 #pragma unroll
                     for (int u = 0; u < kU; ++u)
 #pragma unroll
                         for (int e = 0; e < N; ++e)
-                            s32 += exp2_fast((View::value(raw[u], e) - ref) * c32);
-                }
-                if (WHAT == kSum64) {
-                    if (t > top) {
-                        s64 *= top == -CUDART_INF_F ? 0.0 : exp2_64((double)top - (double)t, c);
-                        top = t;
-                    }
-                    // logits far below add 2^-1000 - where floats are fine enough to say so
-                    const float least = top - reach;
-                    if (!(reach < 1e37f && fabsf(top) < reach * 1e6f)) {
-                        for (int u = 0; u < kU * N && top > -CUDART_INF_F; ++u) {
-                            const float x = View::value(raw[u / N], u % N);
-                            s64 += x == top ? 1.0 : exp2_64((double)x - (double)top, c);
-                        }
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < kU; ++u)
-#pragma unroll
-                            for (int e = 0; e < N; ++e)
-                                s64 += exp2_of_product((double)fmaxf(View::value(raw[u], e), least) - (double)top, c);
-                    }
+                            s64 += exp2_of_product((double)fmaxf(View::plain(raw[u], e), least) - (double)top, c);
                 }
             }
+        };
+        auto close = [&](int ch) {
             lane_max[(ch - c0) * 32 + lane] = top;
             const float most = warp_max(top);
             double sum = 0.0;
             if (WHAT == kSum32)
-                sum = s32 * exp2_fast(top == most ? 0.f : (top - most) * c32);
+                sum = (s32.x + s32.y) * exp2_fast(top == most ? 0.f : (top - most) * c32);
             if (WHAT == kSum64 && top > -CUDART_INF_F)
                 sum = s64 * exp2_64((double)top - (double)most, c);
-            if (most == CUDART_INF_F) {                  // infinite logits share the sum
+            if (most == CUDART_INF_F || __any_sync(kFull, sum != sum)) {
+                // NaN adds nothing, infinite logits share the sum
                 sum = 0.0;
-                each_of(ch, [&](float x, int) { sum += x == CUDART_INF_F ? 1.0 : 0.0; });
+                each_of(ch, [&](float x, int) { sum += x == most ? 1.0 : exp2_64((double)x - (double)most, c); });
             }
             sum = warp_sum(sum);
             if (lane == 0) {
                 chunk_max[ch - c0] = most;
                 chunk_mass[ch - c0] = (u64)__double_as_longlong(sum);
             }
+            top = -CUDART_INF_F;
+            s32 = {0.f, 0.f};
+            s64 = 0.0;
+        };
+        int ch = c0 + warp, i = 0;                       // the block to use: the i-th of chunk ch
+        int ch2 = ch, i2 = 0;                            // the block to fetch
+        auto next = [&](int stage) {
+            if (ch2 < c1)
+                fetch((ch2 * blocks + i2) * 32 * kU, stage);
+            else
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++i2 == blocks) {
+                i2 = 0;
+                ch2 += kWarps;
+            }
+        };
+        next(0);
+        next(1);
+#pragma unroll 1
+        for (int stage = 0; ch < c1; stage ^= 1) {
+            uint4 raw[kU];
+            take((ch * blocks + i) * 32 * kU, stage, raw);
+            next(stage);
+            use(raw);
+            if (++i == blocks) {
+                close(ch);
+                i = 0;
+                ch += kWarps;
+            }
         }
-        __syncthreads();
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                                 // (the bins lie where other warps' rings were)
     }
     // This CTA's and the row's sums of the chunks' masses; returns the row's.
     __device__ __forceinline__ u64 share_masses()
@@ -404,8 +502,8 @@ template <bool BF16> struct Row {
             last = max(last, __shfl_xor_sync(kFull, last, off));
         return last;
     }
-    // Distance from the maximum as one of kBins numbers, ascending: 32 to an octave from 2^-30 on.
-    static constexpr int kFirstBin = ((127 - 30) << 5) - 1;
+    // Distance from the maximum as one of kBins numbers, ascending: 32 to an octave from 2^-6 on.
+    static constexpr int kFirstBin = ((127 - 6) << 5) - 1;
     __device__ __forceinline__ int bin_of(float x) const
     {
         if (x == m)
@@ -413,56 +511,43 @@ template <bool BF16> struct Row {
         const int b = (int)(__float_as_uint(m - x) >> 18) - kFirstBin;
         return min(max(b, 1), kBins - 1);
     }
-    // The first bin at which the cluster's sum over `bins` reaches target - sum: adds to sum what lies
-    // before it, `at` is its own; -1: none does.  All CTAs' bins have been read when it returns.
-    __device__ __forceinline__ int merge_bins(u64 target, u64 &sum, u64 &at)
+    // Of two bins a thread: the first at which their running sum reaches target, what lies before it and its own
+    // go to scratch[kWarps ..] (all ones: none does).
+    __device__ __forceinline__ void cross(const u64 (&w)[2], u64 target)
     {
-        barrier();
-        u64 w[kBins / kThreads], s = 0;
-#pragma unroll
-        for (int i = 0; i < kBins / kThreads; ++i)
-            w[i] = 0;
-        for (int r = 0; r < size; ++r) {
-            const ulonglong2 *h = reinterpret_cast<const ulonglong2 *>(cluster.map_shared_rank(bins, r)) + tid * (kBins / kThreads / 2);
-#pragma unroll
-            for (int i = 0; i < kBins / kThreads / 2; ++i) {
-                const ulonglong2 o = h[i];
-                w[2 * i] += o.x;
-                w[2 * i + 1] += o.y;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kBins / kThreads; ++i)
-            s += w[i];
-        const u64 upto = inclusive_scan(s, lane);
+        const u64 s = w[0] + w[1], upto = inclusive_scan(s, lane);
         if (lane == 31)
             scratch[warp] = upto;
         if (tid == 0)
             scratch[kWarps] = ~0ull;
         __syncthreads();
-        u64 base = sum + upto - s;
-        for (int i = 0; i < warp; ++i)
-            base += scratch[i];
-        if (base + s >= target && base < target) {
-            int i = 0;
-            u64 mine = 0;
+        u64 base = upto - s;
 #pragma unroll
-            for (int j = 0; j < kBins / kThreads; ++j)
-                if (i == j) {
-                    mine = w[j];
-                    if (j < kBins / kThreads - 1 && base + w[j] < target) {
-                        base += w[j];
-                        ++i;
-                    }
-                }
-            scratch[kWarps] = tid * (kBins / kThreads) + i;
-            scratch[kWarps + 1] = base;
-            scratch[kWarps + 2] = mine;
+        for (int i = 0; i < kWarps - 1; ++i)
+            base += i < warp ? scratch[i] : 0;
+        if (base < target && base + s >= target) {
+            const int second = base + w[0] < target;
+            scratch[kWarps] = tid * 2 + second;
+            scratch[kWarps + 1] = base + (second ? w[0] : 0);
+            scratch[kWarps + 2] = second ? w[1] : w[0];
         }
         __syncthreads();
+    }
+    // The first bin at which the cluster's sum over `bins` reaches target - sum: adds to sum what lies
+    // before it, `at` is its own; -1: none does.  All CTAs' bins have been read when it returns.
+    __device__ __forceinline__ int merge_bins(u64 target, u64 &sum, u64 &at)
+    {
+        barrier();
+        u64 w[2] = {0, 0};                               // two bins a thread
+        for (int r = 0; r < size; ++r) {
+            const ulonglong2 o = reinterpret_cast<const ulonglong2 *>(cluster.map_shared_rank(bins, r))[tid];
+            w[0] += o.x;
+            w[1] += o.y;
+        }
+        cross(w, target - sum);
         const u64 found = scratch[kWarps];
         if (found != ~0ull) {
-            sum = scratch[kWarps + 1];
+            sum += scratch[kWarps + 1];
             at = scratch[kWarps + 2];
         }
         barrier();
@@ -482,7 +567,7 @@ template <bool BF16> struct Row {
     }
     // The shortest prefix of the row's order whose sum of f reaches `target` (>= 1); false: the whole row
     // does not.  Equal logits have equal f.  First by distance from the maximum, which spreads the logits over
-    // the bins, then by 11 digits of the ordered bits at a time among those of one bin.
+    // the bins, then by kDigit digits of the ordered bits at a time among those of one bin.
     template <class F> __device__ __forceinline__ bool select(F f, u64 target, Cut &cut)
     {
         u64 sum = 0, at = 0;
@@ -501,7 +586,7 @@ template <bool BF16> struct Row {
         int bits = hi > lo ? 32 - __clz((int)(hi - lo)) : 0;
 #pragma unroll 1
         while (bits > 0) {
-            const int shift = max(bits - 11, 0);
+            const int shift = max(bits - kDigit, 0);
             fill_bins([&](float x, int tok, int &bin) {
                 const unsigned o = order_of(x) - lo;
                 bin = (int)(o >> shift);
@@ -537,58 +622,44 @@ template <bool BF16> struct Row {
                 atomicAdd(hist + bin_of(x), w);
         }
         barrier();
-        u64 w[8] = {}, s = 0;
+        u64 w[2] = {0, 0};
         for (int r = 0; r < size; ++r) {
-            const uint4 *h = reinterpret_cast<const uint4 *>(cluster.map_shared_rank(hist, r)) + tid * 2;
-            const uint4 a = h[0], b = h[1];
-            w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w;
-            w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
+            const uint2 o = reinterpret_cast<const uint2 *>(cluster.map_shared_rank(hist, r))[tid];
+            w[0] += o.x;
+            w[1] += o.y;
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            s += w[i];
-        const u64 upto = inclusive_scan(s, lane);
-        if (lane == 31)
-            scratch[warp] = upto;
-        if (tid == 0)
-            scratch[kWarps] = ~0ull;
-        __syncthreads();
-        u64 at = upto - s;
-        for (int i = 0; i < warp; ++i)
-            at += scratch[i];
-        if (at < target && at + s >= target) {
-            int i = 0;
-            while (i < 7 && at + w[i] < target)
-                at += w[i++];
-            scratch[kWarps] = tid * 8 + i;
-        }
-        __syncthreads();
+        cross(w, target);
         const u64 b = scratch[kWarps];
         reached = b != ~0ull;
         return reached ? (int)b : kBins - 1;
     }
     // Logits of the row in bins up to `last`, as (order, token), into the list of the cluster's first CTA;
     // returns how many there are (more than kList: the list is not whole).
-    __device__ __forceinline__ int gather(int last, int *count)
+    __device__ __forceinline__ int gather(int last, int *count, int *hits)
     {
+        // the lanes to look at, then all threads share their vectors
+        unsigned short *lanes = reinterpret_cast<unsigned short *>(bins + kList / 2);
+        for (int i = tid; i < (c1 - c0) * 32; i += kThreads)
+            if (lane_max[i] > -CUDART_INF_F && bin_of(lane_max[i]) <= last)
+                lanes[atomicAdd(hits, 1)] = (unsigned short)i;
+        __syncthreads();
         u64 *to = cluster.map_shared_rank(list, 0);
         int *n = cluster.map_shared_rank(count, 0);
         bool full = false;
-        for (int i = tid; i < (c1 - c0) * 32; i += kThreads) {
-            if (full || !(lane_max[i] > -CUDART_INF_F) || bin_of(lane_max[i]) > last)
-                continue;
-            const int v0 = (c0 + (i >> 5)) * blocks * kU * 32 + (i & 31);
-            for (int u = 0; u < blocks * kU; ++u) {
-                const uint4 raw = view.masked(v0 + u * 32);
+        const int each = blocks * kU, units = *hits * each;
+#pragma unroll 2
+        for (int q = tid; q < units; q += kThreads) {
+            const int h = q / each, i = lanes[h];
+            const int v = ((c0 + (i >> 5)) * each + (q - h * each)) * 32 + (i & 31);
+            const uint4 raw = view.masked(v);
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float x = View::value(raw, e);
-                    if (!full && x > -CUDART_INF_F && bin_of(x) <= last) {
-                        const int at = atomicAdd(n, 1);
-                        full = at >= kList;
-                        if (!full)
-                            to[at] = ((u64)order_of(x) << 32) | (unsigned)(view.token(v0 + u * 32) + e);
-                    }
+            for (int e = 0; e < N; ++e) {
+                const float x = View::value(raw, e);
+                if (!full && x > -CUDART_INF_F && bin_of(x) <= last) {
+                    const int at = atomicAdd(n, 1);
+                    full = at >= kList;
+                    if (!full)
+                        to[at] = ((u64)order_of(x) << 32) | (unsigned)(view.token(v) + e);
                 }
             }
         }
@@ -633,6 +704,45 @@ __device__ __forceinline__ void from_list(Row<BF16> &r, int found, int top_k, fl
                                           F done)
 {
     const int tid = r.tid, lane = r.lane, warp = r.warp;
+    if (found <= kThreads) {
+        // An entry a thread, compared with all others: its rank, what lies before it, then - of those that are
+        // kept - what its id and lower ones hold.
+        const bool in = tid < found;
+        const u64 key = in ? r.list[tid] : ~0ull;
+        const float x = logit_of((unsigned)(key >> 32));
+        u64 w = in ? r.weight(x) : 0;
+        if (in)
+            r.bins[tid] = w;
+        __syncthreads();
+        int rank = 0;
+        u64 before = 0;
+        if (warp * 32 < found)
+            for (int j = 0; j < found; ++j) {
+                const bool first = r.list[j] < key;
+                rank += first;
+                before += first ? r.bins[j] : 0;
+            }
+        // (the first token is kept in any case: min_p is at most 1, top_k at least 2, the target above 0)
+        bool keep = in && x >= low && (top_k <= 0 || rank < top_k);
+        if (top_p < 1.f) {
+            const u64 target = part_of(whole ? whole : r.block_sum(keep ? w : 0), top_p, true);
+            keep = keep && before < target;
+        }
+        w = keep ? w : 0;
+        const u64 kept = r.block_sum(w), t = part_of(kept, u, false);
+        __syncthreads();
+        if (in)
+            r.bins[tid] = w;
+        __syncthreads();
+        const unsigned id = (unsigned)key;
+        u64 upto = 0;
+        if (warp * 32 < found)
+            for (int j = 0; j < found; ++j)
+                upto += (unsigned)r.list[j] <= id ? r.bins[j] : 0;
+        if (keep && upto > t && upto - w <= t)
+            done((int)id, x, kept);
+        return;
+    }
     sort_list(r.list, found);
     if (tid == 0)
         *count = 0;
@@ -683,22 +793,6 @@ __device__ __forceinline__ void from_list(Row<BF16> &r, int found, int top_k, fl
     auto weight_at = [&](int i) { return r.bins[i] - (i ? r.bins[i - 1] : 0); };
     unsigned id = 0;
     u64 below = 0;
-    if (n <= 32) {
-        if (warp == 0) {
-            const u64 w = lane < n ? weight_at(lane) : 0;
-            const unsigned mine = lane < n ? (unsigned)r.list[lane] : ~0u;
-            u64 upto = 0;
-            for (int j = 0; j < n; ++j) {
-                const u64 o = __shfl_sync(kFull, w, j);
-                upto += __shfl_sync(kFull, mine, j) <= mine ? o : 0;
-            }
-            id = __reduce_min_sync(kFull, lane < n && upto > t ? mine : ~0u);
-            if (lane < n && mine == id)
-                done((int)id, logit_of((unsigned)(r.list[lane] >> 32)), kept);
-        }
-        __syncthreads();
-        return;
-    }
     for (int bit = 22; bit >= 0; --bit) {
         u64 s = 0;
         for (int i = tid; i < n; i += kThreads)
@@ -719,10 +813,14 @@ sample_kernel(const __grid_constant__ SampleParams p)
 {
     using View = RowView<BF16>;
     constexpr int N = View::N;
-    extern __shared__ u64 s_dynamic[];                   // list, bins, then masses and maxima of the chunks
+    extern __shared__ __align__(16) u64 s_dynamic[];      // list, bins, then masses and maxima of the chunks
     __shared__ Word s_word[2];
     __shared__ u64 s_scratch[kWarps + 4];
-    __shared__ int s_count, s_left;
+    __shared__ float s_max[kWarps];
+    __shared__ unsigned s_mask[kWarps * 2 * (Row<BF16>::kMaskWords + 3)];
+    __shared__ int s_count, s_left, s_hits;
+    static_assert(kBins == 2 * kThreads && kBins * 8 <= kList * 4 && kMaxChunks * 32 * 2 <= kList * 4, "bins and lanes share the work space");
+    static_assert(kWarps * 2 * Row<BF16>::kStage <= 2 * kList * 8, "the ring lies in list and work space");
     cstr_wait_for_earlier_kernels();
     cstr_let_next_kernel_start();
     cg::cluster_group cluster = cg::this_cluster();
@@ -790,17 +888,16 @@ sample_kernel(const __grid_constant__ SampleParams p)
     r.unit = __hiloint2double((1023 + p.scale_bits) << 20, 0);
     r.list = s_dynamic;
     r.bins = s_dynamic + kList;
-    r.chunk_mass = r.bins + kBins;
+    r.chunk_mass = r.bins + kList;
     r.chunk_max = reinterpret_cast<float *>(r.chunk_mass + p.per);
     r.lane_max = r.chunk_max + p.per;
+    r.mask_words = s_mask;
     r.word = s_word;
     r.scratch = s_scratch;
     r.phase = 0;
     if (tid == 0)
-        s_count = 0;
+        s_count = s_hits = 0;
 
-    for (int i = tid; i < kBins / 2; i += kThreads)
-        r.bins[i] = 0;
     // One pass over memory.  Where the whole sum decides about the token it is taken in 64 bits.
     const bool plain = !TOP && !cold && top_k <= 0 && top_p >= 1.f && min_p <= 0.f;
     const bool exact_sum = plain || (!TOP && !cold && top_k <= 0 && top_p < 1.f && min_p <= 0.f);
@@ -811,24 +908,37 @@ sample_kernel(const __grid_constant__ SampleParams p)
         r.template first_pass<Row<BF16>::kSum64>();
     else
         r.template first_pass<Row<BF16>::kSum32>();
+    reinterpret_cast<uint2 *>(r.bins)[tid] = make_uint2(0u, 0u);        // counts of 32 bits
     auto chunk_sum = [&](int i, float ref) {              // relative to ref
         const float top = r.chunk_max[i];
         const double s = __longlong_as_double((long long)r.chunk_mass[i]);
         return top == ref ? s : s * exp2_64((double)top - (double)ref, c);
     };
+    // every warp its own chunks, then all of the CTA's
     float m = -CUDART_INF_F;
-    for (int i = tid; i < r.c1 - r.c0; i += kThreads)
+    for (int i = warp + lane * kWarps; i < r.c1 - r.c0; i += 32 * kWarps)
         m = fmaxf(m, r.chunk_max[i]);
     m = warp_max(m);
-    if (lane == 0)
-        reinterpret_cast<float *>(s_scratch)[warp] = m;
-    __syncthreads();
-    m = warp_max(lane < kWarps ? reinterpret_cast<float *>(s_scratch)[lane] : -CUDART_INF_F);
     double sum = 0.0;
     if (m > -CUDART_INF_F)
-        for (int i = tid; i < r.c1 - r.c0; i += kThreads)
+        for (int i = warp + lane * kWarps; i < r.c1 - r.c0; i += 32 * kWarps)
             sum += chunk_sum(i, m);
-    sum = r.block_sum(sum);
+    sum = warp_sum(sum);
+    if (lane == 0) {
+        s_scratch[warp] = (u64)__double_as_longlong(sum);
+        s_max[warp] = m;
+    }
+    __syncthreads();
+    m = s_max[0];
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i)
+        m = fmaxf(m, s_max[i]);
+    sum = 0.0;
+    if (lane < kWarps && m > -CUDART_INF_F) {
+        const double s = __longlong_as_double((long long)s_scratch[lane]);
+        sum = s_max[lane] == m ? s : s * exp2_64((double)s_max[lane] - (double)m, c);
+    }
+    sum = warp_sum(sum);
     const Word all = r.exchange({sum, 0, m, 0});
     const float own_max = m;
     m = warp_max(lane < size ? all.m : -CUDART_INF_F);
@@ -846,7 +956,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
             r.barrier();                                  // (the words have been read)
         else {
             bool reached;
-            found = r.gather(r.reach([](float) { return 1u; }, (u64)p.n, reached), &s_count);
+            found = r.gather(r.reach([](float) { return 1u; }, (u64)p.n, reached), &s_count, &s_hits);
             if (found > kList) {                          // many equal logits, or more tokens than half the lanes
                 Cut cut = {-CUDART_INF_F, kNone};
                 r.select([](float, int) { return (u64)1; }, (u64)p.n, cut);
@@ -871,10 +981,22 @@ sample_kernel(const __grid_constant__ SampleParams p)
             r.leave();
             return;
         }
-        sort_list(r.list, found);
         const double log_total = log(total);
+        const u64 *sorted = r.list;
+        if (found <= kThreads) {                          // each to its rank
+            const u64 key = tid < found ? r.list[tid] : ~0ull;
+            int rank = 0;
+            if (warp * 32 < found)
+                for (int j = 0; j < found; ++j)
+                    rank += r.list[j] < key;
+            if (tid < found)
+                r.bins[rank] = key;
+            sorted = r.bins;
+            __syncthreads();
+        } else
+            sort_list(r.list, found);
         for (int i = tid; i < p.n; i += kThreads) {
-            const u64 e = i < found ? r.list[i] : 0;
+            const u64 e = i < found ? sorted[i] : 0;
             const float x = logit_of((unsigned)(e >> 32));
             const double z = x == m ? 0.0 : ((double)x - (double)m) * c * 0.6931471805599453;
             p.ids[(long long)row * p.n + i] = i < found ? (int)(unsigned)e : -1;
@@ -949,7 +1071,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
         }
         int found = kList + 1;
         if (reached)
-            found = r.gather(last, &s_count);
+            found = r.gather(last, &s_count, &s_hits);
         else
             r.barrier();                                  // (every CTA's bins have been read)
         if (found <= kList) {
@@ -1036,7 +1158,7 @@ int run(const char *name, const cstr_table_t *const *tables, int32_t n_tables, c
     p.scale_bits = 62;
     while ((1LL << (62 - p.scale_bits)) < vocab_size)
         --p.scale_bits;
-    const int smem = (kList + kBins + p.per) * 8 + p.per * 33 * 4;
+    const int smem = (2 * kList + p.per) * 8 + p.per * 33 * 4;
     void (*kernel)(SampleParams) = bf16 ? sample_kernel<true, TOP> : sample_kernel<false, TOP>;
     if (size > 8)
         CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
