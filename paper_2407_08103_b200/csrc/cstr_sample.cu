@@ -153,13 +153,36 @@ struct Cut {
     __device__ __forceinline__ bool tighter_than(const Cut &o) const { return x > o.x || (x == o.x && last < o.last); }
 };
 
+// Bitonic sort of `found` numbers in shared memory (room for the next power of two).
+__device__ __forceinline__ void sort_list(u64 *list, int found)
+{
+    int n = 1;
+    while (n < found)
+        n <<= 1;
+    for (int i = found + threadIdx.x; i < n; i += kThreads)
+        list[i] = ~0ull;
+    for (int k = 2; k <= n; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+                const int a = 2 * i - (i & (j - 1)), b = a + j;
+                const u64 x = list[a], y = list[b];
+                if ((x > y) == ((a & k) == 0)) {
+                    list[a] = y;
+                    list[b] = x;
+                }
+            }
+        }
+    __syncthreads();
+}
+
 template <bool BF16> struct Row {
     using View = RowView<BF16>;
     static constexpr int N = View::N;
     cg::cluster_group cluster;
     View view;
     int size, part, tid, lane, warp;
-    int c0, c1, blocks;                   // this CTA's chunks, blocks of a chunk
+    int c0, c1, blocks, per;              // this CTA's chunks, blocks of a chunk, chunks of every CTA
     double c;                             // log2(e) / temperature
     float m;
     double unit;                          // 2^s
@@ -533,71 +556,66 @@ template <bool BF16> struct Row {
         }
         __syncthreads();
     }
-    // The first bin at which the cluster's sum over `bins` reaches target - sum: adds to sum what lies
-    // before it, `at` is its own; -1: none does.  All CTAs' bins have been read when it returns.
-    __device__ __forceinline__ int merge_bins(u64 target, u64 &sum, u64 &at)
+    // The cluster's sums of two bins a thread (counted in T), after a barrier; the bins may be changed behind another.
+    template <class T> __device__ __forceinline__ void merge_bins(u64 (&w)[2])
     {
         barrier();
-        u64 w[2] = {0, 0};                               // two bins a thread
+        w[0] = w[1] = 0;
         for (int r = 0; r < size; ++r) {
-            const ulonglong2 o = reinterpret_cast<const ulonglong2 *>(cluster.map_shared_rank(bins, r))[tid];
-            w[0] += o.x;
-            w[1] += o.y;
+            const T *o = cluster.map_shared_rank(reinterpret_cast<T *>(bins), r) + tid * 2;
+            w[0] += o[0];
+            w[1] += o[1];
         }
-        cross(w, target - sum);
-        const u64 found = scratch[kWarps];
-        if (found != ~0ull) {
-            sum += scratch[kWarps + 1];
-            at = scratch[kWarps + 2];
-        }
-        barrier();
-        return found == ~0ull ? -1 : (int)found;
     }
-    template <class F> __device__ __forceinline__ void fill_bins(F f)      // f(logit, token, bin): weight, 0: none
+    template <class T, class F> __device__ __forceinline__ void fill_bins(F f)     // f(logit, token, bin): weight, 0: none
     {
-        for (int i = tid; i < kBins; i += kThreads)
-            bins[i] = 0;
+        T *to = reinterpret_cast<T *>(bins);
+        to[tid * 2] = to[tid * 2 + 1] = 0;
         __syncthreads();
         each([&](float x, int tok) {
             int bin;
-            const u64 w = f(x, tok, bin);
+            const T w = f(x, tok, bin);
             if (w)
-                atomicAdd(bins + bin, w);
+                atomicAdd(to + bin, w);
         });
     }
-    // The shortest prefix of the row's order whose sum of f reaches `target` (>= 1); false: the whole row
-    // does not.  Equal logits have equal f.  First by distance from the maximum, which spreads the logits over
-    // the bins, then by kDigit digits of the ordered bits at a time among those of one bin.
-    template <class F> __device__ __forceinline__ bool select(F f, u64 target, Cut &cut)
+    // The ordered bits that the logits of bins b1 .. b2 can have: lo + [0, 2^bits).  They lie within m - [d0, d1],
+    // widened by the difference's rounding.
+    __device__ __forceinline__ void range_of(int b1, int b2, unsigned &lo, int &bits) const
     {
-        u64 sum = 0, at = 0;
-        fill_bins([&](float x, int tok, int &bin) {
-            bin = bin_of(x);
-            return f(x, tok);
-        });
-        const int b = merge_bins(target, sum, at);
-        if (b < 0)
-            return false;
-        // the bin's logits lie within m - [d0, d1], widened by the difference's rounding
-        const float d0 = b <= 1 ? 0.f : __uint_as_float((unsigned)(b + kFirstBin) << 18) * (1.f - 0x1p-22f);
-        const float d1 = b == 0 ? 0.f : b == kBins - 1 ? CUDART_INF_F : __uint_as_float((unsigned)(b + 1 + kFirstBin) << 18) * (1.f + 0x1p-22f);
-        unsigned lo = b == 0 ? order_of(m) : max(order_of(m), order_of(m - d0) - 2);
-        const unsigned hi = b == 0 ? lo : m == CUDART_INF_F ? order_of(-CUDART_INF_F) : min(order_of(m - d1) + 2, order_of(-CUDART_INF_F));
-        int bits = hi > lo ? 32 - __clz((int)(hi - lo)) : 0;
-#pragma unroll 1
-        while (bits > 0) {
+        const float d0 = b1 <= 1 ? 0.f : __uint_as_float((unsigned)(b1 + kFirstBin) << 18) * (1.f - 0x1p-22f);
+        const float d1 = b2 == kBins - 1 ? CUDART_INF_F : __uint_as_float((unsigned)(b2 + 1 + kFirstBin) << 18) * (1.f + 0x1p-22f);
+        const unsigned least = order_of(-CUDART_INF_F);
+        lo = b1 == 0 ? order_of(m) : max(order_of(m), order_of(m - d0) - 2);
+        const unsigned hi = b2 == 0 ? lo : m == CUDART_INF_F ? least : min(order_of(m - d1) + 2, least);
+        bits = hi > lo ? 32 - __clz((int)(hi - lo)) : 0;
+    }
+    // The shortest prefix of the row's order whose sum of f, together with `sum` for the logits before them,
+    // reaches target, among the logits `in` with ordered bits lo + [0, 2^bits): by kDigit digits at a time.
+    // false: they do not.  Equal logits have equal f.
+    template <class T, class F, class P>
+    __device__ __forceinline__ bool digits(F f, P in, u64 target, u64 sum, unsigned lo, int bits, Cut &cut)
+    {
+        u64 at = 0;
+        do {
             const int shift = max(bits - kDigit, 0);
-            fill_bins([&](float x, int tok, int &bin) {
+            fill_bins<T>([&](float x, int tok, int &bin) {
                 const unsigned o = order_of(x) - lo;
                 bin = (int)(o >> shift);
-                return o >> bits == 0 && bin_of(x) == b ? f(x, tok) : (u64)0;
+                return (u64)o >> bits == 0 && in(x) ? f(x, tok) : (T)0;
             });
-            const int digit = merge_bins(target, sum, at);
-            if (digit < 0)
-                return false;                            // (cannot be: the bin reached it)
+            u64 w[2];
+            merge_bins<T>(w);
+            cross(w, target - sum);
+            const u64 digit = scratch[kWarps];
+            sum += digit == ~0ull ? 0 : scratch[kWarps + 1];
+            at = scratch[kWarps + 2];
+            barrier();
+            if (digit == ~0ull)
+                return false;
             lo += (unsigned)digit << shift;
             bits = shift;
-        }
+        } while (bits > 0);
         cut.x = logit_of(lo);
         cut.last = kNone;
         const u64 one = f(cut.x, 0), r = (target - sum + one - 1) / one;      // equal logits that are kept
@@ -608,6 +626,177 @@ template <bool BF16> struct Row {
             cut.last = everybody(find(tie, r - 1));
         }
         return true;
+    }
+    // ... of the whole row: first by distance from the maximum, which spreads the logits over the bins.
+    template <class T, class F> __device__ __forceinline__ bool select(F f, u64 target, Cut &cut)
+    {
+        fill_bins<T>([&](float x, int tok, int &bin) {
+            bin = bin_of(x);
+            return f(x, tok);
+        });
+        u64 w[2];
+        merge_bins<T>(w);
+        cross(w, target);
+        const u64 b = scratch[kWarps], sum = scratch[kWarps + 1];
+        barrier();
+        if (b == ~0ull)
+            return false;
+        unsigned lo;
+        int bits;
+        range_of((int)b, (int)b, lo, bits);
+        return digits<T>(f, [&](float x) { return bin_of(x) == (int)b; }, target, sum, lo, bits, cut);
+    }
+    // Ordered bits [o1, o2] within which the sum of the weights reaches target, by weights in 32 bits as whole
+    // numbers of 2^-31 of their sum `total`.  These are off by half a number each and by 2^-18 of all (arguments of
+    // exponentials): what is that near to the target is within.  Nothing relies on it.
+    __device__ __forceinline__ void narrow(double total, u64 target, unsigned &o1, unsigned &o2)
+    {
+        const float c32 = (float)c, k = (float)(0x1p+31 / total);
+        const u64 want = (u64)((double)target / unit / total * 0x1p+31), slack = 65536 + view.V / 2;
+        const u64 from = want > slack ? want - slack : 1, to = want + slack;
+        auto about = [&](float x) { return __float2uint_rn((x == m ? 1.f : exp2_fast((x - m) * c32)) * k); };
+        o1 = 1;
+        o2 = 0;
+        u64 w[2];
+        fill_bins<unsigned>([&](float x, int, int &bin) {
+            bin = bin_of(x);
+            return about(x);
+        });
+        merge_bins<unsigned>(w);
+        cross(w, from);
+        const u64 b1 = scratch[kWarps], sum = scratch[kWarps + 1];
+        __syncthreads();
+        cross(w, to);
+        const int b2 = (int)min(scratch[kWarps], (u64)kBins - 1);
+        barrier();
+        if (b1 == ~0ull)
+            return;
+        unsigned lo;
+        int bits;
+        range_of((int)b1, b2, lo, bits);
+        const int shift = max(bits - kDigit, 0);
+        fill_bins<unsigned>([&](float x, int, int &bin) {
+            const unsigned o = order_of(x) - lo;
+            const int b = bin_of(x);
+            bin = (int)(o >> shift);
+            return (u64)o >> bits == 0 && b >= (int)b1 && b <= b2 ? about(x) : 0u;
+        });
+        merge_bins<unsigned>(w);
+        cross(w, from - sum);
+        const u64 d1 = scratch[kWarps];
+        __syncthreads();
+        cross(w, to - sum);
+        const u64 d2 = min(scratch[kWarps], (u64)kBins - 1);
+        barrier();
+        if (d1 == ~0ull)
+            return;
+        o1 = lo + (unsigned)(d1 << shift);
+        o2 = (unsigned)min((u64)lo + ((d2 + 1) << shift) - 1, (u64)0xffffffffu);
+    }
+    // The chunks' masses of the logits above ordered bits o1 - their sum is returned -, those within [o1, o2] into
+    // the list of the cluster's first CTA, `found` of them.  (count is 0, and the barrier behind that has been passed.)
+    __device__ __forceinline__ u64 split(unsigned o1, unsigned o2, int *count, int &found)
+    {
+        u64 *to = cluster.map_shared_rank(list, 0);
+        int *n = cluster.map_shared_rank(count, 0);
+        bool full = false;
+        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
+            u64 s = 0;
+            each_of(ch, [&](float x, int tok) {
+                const unsigned o = order_of(x);
+                if (o < o1)
+                    s += weight(x);
+                else if (o <= o2 && !full) {
+                    const int at = atomicAdd(n, 1);
+                    full = at >= kList;
+                    if (!full)
+                        to[at] = ((u64)o << 32) | (unsigned)tok;
+                }
+            });
+            s = warp_sum(s);
+            if (lane == 0)
+                chunk_mass[ch - c0] = s;
+        }
+        __syncthreads();
+        const u64 above = share_masses();
+        found = *n;
+        return above;
+    }
+    // Running sums of the weights of the list's first n entries, kThreads of them at a time, into the work space.
+    __device__ __forceinline__ void running_sums(int n)
+    {
+        u64 base = 0;
+        for (int i0 = 0; i0 < n; i0 += kThreads) {
+            const int i = i0 + tid;
+            const u64 w = i < n ? weight(logit_of((unsigned)(list[i] >> 32))) : 0;
+            const u64 upto = inclusive_scan(w, lane);
+            __syncthreads();
+            if (lane == 31)
+                scratch[warp] = upto;
+            __syncthreads();
+            u64 below = base;
+#pragma unroll
+            for (int j = 0; j < kWarps; ++j) {
+                below += j < warp ? scratch[j] : 0;
+                base += scratch[j];
+            }
+            if (i < n)
+                bins[i] = below + upto;
+        }
+        __syncthreads();
+    }
+    // Entries up to the first whose running sum reaches target (all n where none does).
+    __device__ __forceinline__ int reached_by(u64 target, int n) const
+    {
+        int lo = 0, hi = n - 1;                          // (every thread looks for itself)
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (bins[mid] >= target)
+                hi = mid;
+            else
+                lo = mid + 1;
+        }
+        return lo + 1;
+    }
+    // The cut at which the row's mass reaches target, and what it keeps; afterwards the chunks' masses are those of
+    // the kept tokens.  Most of the row is counted as a whole, the logits around the border one by one.
+    __device__ __forceinline__ u64 cut_mass(double total, u64 target, int *count, Cut &cut)
+    {
+        unsigned o1, o2;
+        narrow(total, target, o1, o2);
+        if (tid == 0)
+            *count = 0;
+        barrier();
+        int found;
+        const u64 above = split(o1, o2, count, found);
+        Word w = {0.0, 0, 0.f, 0};
+        if (found <= kList && part == 0 && found > 0 && above < target) {
+            sort_list(list, found);
+            running_sums(found);
+            if (above + bins[found - 1] >= target) {
+                const int n = reached_by(target - above, found);
+                w = {0.0, above + bins[n - 1], logit_of((unsigned)(list[n - 1] >> 32)), (int)(unsigned)list[n - 1]};
+                for (int i = tid; i < n; i += kThreads) {
+                    const int ch = ((int)(unsigned)list[i] + view.head) / N / (32 * kU) / blocks, owner = ch / per;
+                    atomicAdd(cluster.map_shared_rank(chunk_mass + ch - owner * per, owner), bins[i] - (i ? bins[i - 1] : 0));
+                }
+            }
+        }
+        w = exchange(w);                                 // (the first CTA's)
+        const u64 kept = __shfl_sync(kFull, w.mass, 0);
+        cut.x = __shfl_sync(kFull, w.m, 0);
+        cut.last = __shfl_sync(kFull, w.token, 0);
+        if (kept) {
+            share_masses();
+            return kept;
+        }
+        // many equal logits at the border (or, never seen, a border outside)
+        auto f = [&](float x, int) { return weight(x); };
+        const int bits = o2 > o1 ? 32 - __clz((int)(o2 - o1)) : 0;
+        if (!(found > kList && above < target && digits<u64>(f, [&](float x) { return order_of(x) <= o2; }, target, above, o1, bits, cut)) &&
+            !select<u64>(f, target, cut))
+            cut = {-CUDART_INF_F, kNone};
+        return mass_pass([&](float x, int tok) { return cut.keeps(x, tok) ? weight(x) : (u64)0; });
     }
     // The lowest bin up to which f, summed over the lanes' maxima of the whole row, reaches `target`; the
     // last bin where the row does not.  Every lane's maximum is a logit of its own, so that so much lies
@@ -674,29 +863,6 @@ template <bool BF16> struct Row {
     }
 };
 
-// Bitonic sort of `found` numbers in shared memory (room for the next power of two).
-__device__ __forceinline__ void sort_list(u64 *list, int found)
-{
-    int n = 1;
-    while (n < found)
-        n <<= 1;
-    for (int i = found + threadIdx.x; i < n; i += kThreads)
-        list[i] = ~0ull;
-    for (int k = 2; k <= n; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
-                const int a = 2 * i - (i & (j - 1)), b = a + j;
-                const u64 x = list[a], y = list[b];
-                if ((x > y) == ((a & k) == 0)) {
-                    list[a] = y;
-                    list[b] = x;
-                }
-            }
-        }
-    __syncthreads();
-}
-
 // The token of a row whose `found` candidates are in the list of this CTA: the tokens below `low` and
 // beyond top_k leave, then top_p of `whole` (0: of what is left) is kept.  done(token, logit, kept mass) by one thread.
 template <bool BF16, class F>
@@ -756,38 +922,9 @@ __device__ __forceinline__ void from_list(Row<BF16> &r, int found, int top_k, fl
         atomicAdd(count, n);
     __syncthreads();
     n = min(*count, top_k > 0 ? min(top_k, found) : found);
-    // running sums of the weights, kThreads of them at a time, into bins
-    u64 base = 0;
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
-        const int i = i0 + tid;
-        const u64 w = i < n ? r.weight(logit_of((unsigned)(r.list[i] >> 32))) : 0;
-        const u64 upto = inclusive_scan(w, lane);
-        __syncthreads();
-        if (lane == 31)
-            r.scratch[warp] = upto;
-        __syncthreads();
-        u64 below = base;
-#pragma unroll
-        for (int j = 0; j < kWarps; ++j) {
-            below += j < warp ? r.scratch[j] : 0;
-            base += r.scratch[j];
-        }
-        if (i < n)
-            r.bins[i] = below + upto;
-    }
-    __syncthreads();
-    if (top_p < 1.f) {                                   // the first whose running sum reaches the target ends the prefix
-        const u64 target = part_of(whole ? whole : r.bins[n - 1], top_p, true);
-        int lo = 0, hi = n - 1;                          // (every thread looks for itself)
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (r.bins[mid] >= target)
-                hi = mid;
-            else
-                lo = mid + 1;
-        }
-        n = lo + 1;
-    }
+    r.running_sums(n);
+    if (top_p < 1.f)                                     // the first whose running sum reaches the target ends the prefix
+        n = r.reached_by(part_of(whole ? whole : r.bins[n - 1], top_p, true), n);
     const u64 kept = r.bins[n - 1], t = part_of(kept, u, false);
     // by id: bit by bit, is the sum over the ids below the next half above t?
     auto weight_at = [&](int i) { return r.bins[i] - (i ? r.bins[i - 1] : 0); };
@@ -882,6 +1019,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     Row<BF16> r = {cluster, View(p.logits, (long long)row * p.ld, p.V, mrow), size, part, tid, lane, warp};
     r.blocks = p.blocks;
     const int chunks = (r.view.vectors() + 32 * kU * p.blocks - 1) / (32 * kU * p.blocks), per = (chunks + size - 1) / size;
+    r.per = per;
     r.c0 = min(part * per, chunks);
     r.c1 = min(r.c0 + per, chunks);
     r.c = c;
@@ -959,7 +1097,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
             found = r.gather(r.reach([](float) { return 1u; }, (u64)p.n, reached), &s_count, &s_hits);
             if (found > kList) {                          // many equal logits, or more tokens than half the lanes
                 Cut cut = {-CUDART_INF_F, kNone};
-                r.select([](float, int) { return (u64)1; }, (u64)p.n, cut);
+                r.template select<unsigned>([](float, int) { return 1u; }, (u64)p.n, cut);
                 if (tid == 0)
                     s_count = 0;
                 r.barrier();
@@ -1088,16 +1226,13 @@ sample_kernel(const __grid_constant__ SampleParams p)
             tighten({low, kNone});
         if (top_k > 0) {
             Cut k;
-            if (r.select([](float, int) { return (u64)1; }, (u64)top_k, k))
+            if (r.template select<unsigned>([](float, int) { return 1u; }, (u64)top_k, k))
                 tighten(k);
         }
+        // (top_p's border lies within what the other cuts keep, or at its end)
         mass = exact_sum ? (u64)__double2ll_rn(total * r.unit) : r.mass_pass(kept_weight);
-        if (top_p < 1.f) {
-            Cut k;
-            if (r.select([&](float x, int) { return r.weight(x); }, part_of(mass, top_p, true), k))
-                tighten(k);
-            mass = r.mass_pass(kept_weight);
-        }
+        if (top_p < 1.f)
+            mass = r.cut_mass(total, part_of(mass, top_p, true), &s_count, cut);
     }
     token = r.find(kept_weight, part_of(mass, u, false));
     if (warp == 0 && lane == 0 && token >= 0) {

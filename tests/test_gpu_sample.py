@@ -270,3 +270,21 @@ def test_logits_of_any_size(dtype, level, spread):
     check_sample(x, u, temperature=temperature, top_k=np.full(N, 60, np.int32), min_p=np.full(N, 0.3, np.float32))
     check_top(x, 30)
     check_top(x, 30, temperature=1e20)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("step", [0.0, 0.02, 0.5, 3.0])
+def test_wide_nuclei_with_many_equal_logits(dtype, step):
+    # borders of top_p among thousands of tokens, alone or equal in thousands; odd row length, masked tokens
+    N, V = 5, 70001
+    rng = np.random.default_rng(14)
+    x = logits(14, N, V, F32, sigma=1.0, peaks=3)
+    x = (x if step == 0.0 else (x / step).round() * step).to(dtype)
+    x[:, 5::11] = -math.inf
+    x[0, 9::7] = math.nan
+    u = rng.random(N).astype(np.float32)
+    check_sample(x, u, top_p=np.array([0.99, 0.9, 0.5, 0.7, 0.999999], np.float32))
+    check_sample(x, u, top_p=np.array([0.99, 0.9, 0.5, 0.7, 0.8], np.float32), top_k=np.array([5000, 20000, 60000, 3000, 2049], np.int32),
+                 temperature=np.array([1.0, 0.5, 2.0, 30.0, 0.9], np.float32))
+    check_sample(x, u, top_p=np.full(N, 0.97, np.float32), min_p=np.array([1e-4, 1e-6, 1e-3, 3e-3, 0.0], np.float32),
+                 temperature=np.array([1.0, 2.0, 1.5, 1.0, 50.0], np.float32))
