@@ -158,27 +158,30 @@ template <bool BF16> struct RowView {
     static __device__ __forceinline__ float value(uint4 u, int e) { return fmaxf(plain(u, e), -CUDART_INF_F); }
 };
 
-// 2^(d c) for d c in [-1020, 0] to 1.2e-12: d c = n + f, the polynomial of degree 8 that meets 2^f at the
-// nine Chebyshev points of [-1/2, 1/2] (1.1e-12 at most, exact at 0), the exponent by integer addition.
-__device__ __forceinline__ double exp2_of_product(double d, double c)
+// 2^(d c16 / 16) for d c16 / 16 in [-1020, 0] to 2.6e-12 as a product of the two numbers that it returns:
+// d c16 = 16 n + j + g, the polynomial of degree 4 that meets 2^(g / 16) at the five Chebyshev points of
+// [-1/2, 1/2] (2.5e-12 at most, exact at 0), and table[j] = 2^(j / 16) with n added to its exponent.  The table's
+// 16 numbers fill the 32 banks of shared memory once: lanes never conflict.
+__device__ __forceinline__ double2 exp2_factors(double d, double c16, const double *table)
 {
     const double shift = 6755399441055744.0;                 // 1.5 * 2^52: adding it rounds to a whole number
-    const double r = fma(d, c, shift), f = fma(d, c, shift - r);
-    double p = 1.3255224887502117e-06;
-    p = fma(p, f, 1.531007940254368e-05);
-    p = fma(p, f, 0.0001540345585240991);
-    p = fma(p, f, 0.0013333450567999414);
-    p = fma(p, f, 0.009618129159402628);
-    p = fma(p, f, 0.05550410941205934);
-    p = fma(p, f, 0.2402265069581299);
-    p = fma(p, f, 0.6931471805459335);
-    p = fma(p, f, 1.0);
-    return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
+    const double r = fma(d, c16, shift), g = fma(d, c16, shift - r);
+    double p = 1.467638723829912e-07;
+    p = fma(p, g, 1.3551205154934813e-05);
+    p = fma(p, g, 0.0009383847926296651);
+    p = fma(p, g, 0.043321698760160544);
+    p = fma(p, g, 1.0);
+    const int i = __double2loint(r);
+    const double t = table[i & 15];
+    return make_double2(p, __hiloint2double(__double2hiint(t) + ((i >> 4) << 20), __double2loint(t)));
 }
-// ... for any d c <= 0
-__device__ __forceinline__ double exp2_64(double d, double c)
+// 2^(d c16 / 16) for any d c16 <= 0
+__device__ __forceinline__ double exp2_64(double d, double c16, const double *table)
 {
-    return d * c > -1000.0 ? exp2_of_product(d, c) : 0.0;
+    if (!(d * c16 > -16000.0))
+        return 0.0;
+    const double2 f = exp2_factors(d, c16, table);
+    return f.x * f.y;
 }
 
 __device__ __forceinline__ float exp2_fast(float x)

@@ -13,6 +13,7 @@
 // follows reads the row from the L2 cache: the pair (x, i) by counts or masses of three digits of the logit's
 // ordered bits, the token by sums of chunks of 128 vectors.
 #include <cooperative_groups.h>
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -183,7 +184,8 @@ template <bool BF16> struct Row {
     View view;
     int size, part, tid, lane, warp;
     int c0, c1, blocks, per;              // this CTA's chunks, blocks of a chunk, chunks of every CTA
-    double c;                             // log2(e) / temperature
+    double c, c16;                        // log2(e) / temperature, 16 times that
+    const double *table;                  // 2^(j / 16)
     float m;
     double unit;                          // 2^s
     u64 *list, *bins, *chunk_mass;        // (bins: the work space)
@@ -239,98 +241,46 @@ template <bool BF16> struct Row {
             r += s[i];
         return r;
     }
+    __device__ __forceinline__ double power(double d) const { return exp2_64(d, c16, table); }
     __device__ __forceinline__ u64 weight(float x) const
     {
-        const double w = x == m ? 1.0 : exp2_64((double)x - (double)m, c);
+        const double w = x == m ? 1.0 : power((double)x - (double)m);
         return (u64)__double2ll_rn(w * unit);
     }
-    // Vectors first + 32 u + lane, disallowed logits as -infinity
-    __device__ __forceinline__ void load(int first, uint4 (&raw)[kU]) const
-    {
-        const int tok = view.token(first);
-        if (tok >= 0 && tok + 32 * kU * N <= view.V) {
-            const uint4 *at = reinterpret_cast<const uint4 *>(view.row - view.head * View::ESZ) + first + lane;
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-                raw[u] = at[u * 32];
-            if (view.mrow && view.head == 0) {           // 32 vectors take N words of the mask
-                const uint32_t *w = view.mrow + (tok >> 5) + (lane * N >> 5);
-#pragma unroll
-                for (int u = 0; u < kU; ++u)
-                    raw[u] = View::mask(raw[u], __ldg(w + u * N) >> (lane * N & 31));
-            } else if (view.mrow) {
-#pragma unroll
-                for (int u = 0; u < kU; ++u)
-                    raw[u] = View::mask(raw[u], view.bits(first + u * 32 + lane));
-            }
-        } else {
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-                raw[u] = view.masked(first + u * 32 + lane);
-        }
-    }
-    // f(logit, token) for every allowed logit above -infinity of chunk ch
-    template <class F> __device__ __forceinline__ void each_of(int ch, F f)
-    {
-#pragma unroll 1
-        for (int b = ch * blocks; b < (ch + 1) * blocks; ++b) {
-            uint4 raw[kU];
-            load(b * 32 * kU, raw);
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int tok = view.token(b * 32 * kU + u * 32 + lane);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float x = View::value(raw[u], e);
-                    if (x > -CUDART_INF_F)
-                        f(x, tok + e);
-                }
-            }
-        }
-    }
-    // ... of this CTA's chunks
-    template <class F> __device__ __forceinline__ void each(F f)
-    {
-        for (int ch = c0 + warp; ch < c1; ch += kWarps)
-            each_of(ch, f);
-    }
-    // Each warp copies its blocks into a ring of its own, two ahead of the one in use; a lane reads back what
+    // Each warp copies its blocks into a ring of its own, STAGES ahead of the one in use; a lane reads back what
     // it copied, but for the words of the mask.  Blocks at the row's ends are read when they are used.
     static constexpr int kStage = kU * 32 * 16, kMaskWords = 32 * kU * N / 32 + 1;
     __device__ __forceinline__ bool whole(int first) const
     {
         return view.token(first) >= 0 && view.token(first) + 32 * kU * N <= view.V;
     }
-    __device__ __forceinline__ void fetch(int first, int stage) const
+    __device__ __forceinline__ void fetch(int first, char *stage, unsigned *words) const
     {
         if (whole(first)) {
             const char *from = view.row - view.head * View::ESZ + ((long long)first + lane) * 16;
-            const unsigned to = (unsigned)__cvta_generic_to_shared(reinterpret_cast<char *>(list) + (warp * 2 + stage) * kStage + lane * 16);
+            const unsigned to = (unsigned)__cvta_generic_to_shared(stage + lane * 16);
 #pragma unroll
             for (int u = 0; u < kU; ++u)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + u * 512), "l"(from + u * 512) : "memory");
             if (view.mrow) {
                 const int w0 = view.token(first) >> 5, last = (view.V - 1) >> 5;
-                const unsigned to_w = (unsigned)__cvta_generic_to_shared(mask_words + (warp * 2 + stage) * (kMaskWords + 3));
+                const unsigned to_w = (unsigned)__cvta_generic_to_shared(words);
                 for (int i = lane; i < kMaskWords; i += 32)
                     if (w0 + i <= last)
                         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to_w + i * 4), "l"(view.mrow + w0 + i) : "memory");
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __device__ __forceinline__ void take(int first, int stage, uint4 (&raw)[kU]) const
+    __device__ __forceinline__ void take(int first, const char *stage, const unsigned *words, uint4 (&raw)[kU]) const
     {
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
-        __syncwarp();
         if (whole(first)) {
-            const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(list) + (warp * 2 + stage) * kStage) + lane;
+            const uint4 *from = reinterpret_cast<const uint4 *>(stage) + lane;
 #pragma unroll
             for (int u = 0; u < kU; ++u)
                 raw[u] = from[u * 32];
             if (view.mrow) {
                 const int at = (view.token(first) & 31) + lane * N;
-                const unsigned *w = mask_words + (warp * 2 + stage) * (kMaskWords + 3) + (at >> 5);
+                const unsigned *w = words + (at >> 5);
 #pragma unroll
                 for (int u = 0; u < kU; ++u)
                     raw[u] = View::mask(raw[u], view.head == 0 ? w[u * N] >> (at & 31) : __funnelshift_r(w[u * N], w[u * N + 1], at & 31));
@@ -340,7 +290,61 @@ template <bool BF16> struct Row {
             for (int u = 0; u < kU; ++u)
                 raw[u] = view.masked(first + u * 32 + lane);
         }
-        __syncwarp();
+    }
+    // use(raw, first vector) for every block of this warp's chunks, close(chunk) behind each chunk.  `ring`: STAGES
+    // blocks for each warp; whoever used that memory before has passed a barrier.
+    template <int STAGES, class U, class C> __device__ __forceinline__ void stream(void *ring, U use, C close)
+    {
+        char *stage = reinterpret_cast<char *>(ring) + warp * STAGES * kStage;
+        unsigned *words = mask_words + warp * 2 * (kMaskWords + 3);
+        int ch = c0 + warp, i = 0;                       // the block to use: the i-th of chunk ch
+        int ch2 = ch, i2 = 0;                            // the block to fetch
+        auto next = [&](int s) {
+            if (ch2 < c1)
+                fetch((ch2 * blocks + i2) * 32 * kU, stage + s * kStage, words + s * (kMaskWords + 3));
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++i2 == blocks) {
+                i2 = 0;
+                ch2 += kWarps;
+            }
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
+            next(s);
+#pragma unroll 1
+        for (int s = 0; ch < c1; s = STAGES == 2 ? s ^ 1 : 0) {
+            const int first = (ch * blocks + i) * 32 * kU;
+            uint4 raw[kU];
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+            __syncwarp();
+            take(first, stage + s * kStage, words + s * (kMaskWords + 3), raw);
+            __syncwarp();
+            next(s);
+            use(raw, first);
+            if (++i == blocks) {
+                close(ch);
+                i = 0;
+                ch += kWarps;
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+    }
+    // f(logit, token) for every allowed logit above -infinity of this CTA's chunks, close(chunk) behind each
+    template <class F, class C> __device__ __forceinline__ void each(void *ring, F f, C close)
+    {
+        stream<1>(ring, [&](const uint4 (&raw)[kU], int first) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int tok = view.token(first + u * 32 + lane);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = View::plain(raw[u], e);
+                    if (x > -CUDART_INF_F)               // (and no NaN)
+                        f(x, tok + e);
+                }
+            }
+        }, close);
     }
     // Maximum of every lane's logits in a chunk, maximum of the chunk and its sum of 2^(c (x - maximum)) as the
     // bits of a double: taken in 32 bits, or in 64.
@@ -348,10 +352,11 @@ template <bool BF16> struct Row {
     template <int WHAT> __device__ __forceinline__ void first_pass()
     {
         const float c32 = (float)c, reach = (float)(1000.0 / c);
+        const double k16 = c16;
         float top = -CUDART_INF_F;
         float2 s32 = {0.f, 0.f};
         double s64 = 0.0;
-        auto use = [&](const uint4 (&raw)[kU]) {
+        auto use = [&](const uint4 (&raw)[kU], int) {
             float t = -CUDART_INF_F;
 #pragma unroll
             for (int u = 0; u < kU; ++u)
@@ -376,7 +381,7 @@ template <bool BF16> struct Row {
             }
             if (WHAT == kSum64) {
                 if (t > top) {
-                    s64 *= top == -CUDART_INF_F ? 0.0 : exp2_64((double)top - (double)t, c);
+                    s64 *= top == -CUDART_INF_F ? 0.0 : power((double)top - (double)t);
                     top = t;
                 }
                 // logits far below (and NaN) add 2^-1000 - where floats are fine enough to say so
@@ -384,14 +389,17 @@ template <bool BF16> struct Row {
                 if (!(reach < 1e37f && fabsf(top) < reach * 1e6f)) {
                     for (int u = 0; u < kU * N && top > -CUDART_INF_F; ++u) {
                         const float x = View::value(raw[u / N], u % N);
-                        s64 += x == top ? 1.0 : exp2_64((double)x - (double)top, c);
+                        s64 += x == top ? 1.0 : power((double)x - (double)top);
                     }
                 } else {
 #pragma unroll
                     for (int u = 0; u < kU; ++u)
 #pragma unroll
                         for (int e = 0; e < N; ++e)
-                            s64 += exp2_of_product((double)fmaxf(View::plain(raw[u], e), least) - (double)top, c);
+                            {
+                                const double2 f = exp2_factors((double)fmaxf(View::plain(raw[u], e), least) - (double)top, k16, table);
+                                s64 = fma(f.x, f.y, s64);
+                            }
                 }
             }
         };
@@ -402,11 +410,17 @@ template <bool BF16> struct Row {
             if (WHAT == kSum32)
                 sum = (s32.x + s32.y) * exp2_fast(top == most ? 0.f : (top - most) * c32);
             if (WHAT == kSum64 && top > -CUDART_INF_F)
-                sum = s64 * exp2_64((double)top - (double)most, c);
+                sum = s64 * power((double)top - (double)most);
             if (most == CUDART_INF_F || __any_sync(kFull, sum != sum)) {
                 // NaN adds nothing, infinite logits share the sum
                 sum = 0.0;
-                each_of(ch, [&](float x, int) { sum += x == most ? 1.0 : exp2_64((double)x - (double)most, c); });
+                for (int v = ch * blocks * kU * 32 + lane; v < (ch + 1) * blocks * kU * 32; v += 32) {
+                    const uint4 raw = view.masked(v);
+                    for (int e = 0; e < N; ++e) {
+                        const float x = View::value(raw, e);
+                        sum += x == most ? 1.0 : x == -CUDART_INF_F ? 0.0 : power((double)x - (double)most);
+                    }
+                }
             }
             sum = warp_sum(sum);
             if (lane == 0) {
@@ -417,34 +431,7 @@ template <bool BF16> struct Row {
             s32 = {0.f, 0.f};
             s64 = 0.0;
         };
-        int ch = c0 + warp, i = 0;                       // the block to use: the i-th of chunk ch
-        int ch2 = ch, i2 = 0;                            // the block to fetch
-        auto next = [&](int stage) {
-            if (ch2 < c1)
-                fetch((ch2 * blocks + i2) * 32 * kU, stage);
-            else
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            if (++i2 == blocks) {
-                i2 = 0;
-                ch2 += kWarps;
-            }
-        };
-        next(0);
-        next(1);
-#pragma unroll 1
-        for (int stage = 0; ch < c1; stage ^= 1) {
-            uint4 raw[kU];
-            take((ch * blocks + i) * 32 * kU, stage, raw);
-            next(stage);
-            use(raw);
-            if (++i == blocks) {
-                close(ch);
-                i = 0;
-                ch += kWarps;
-            }
-        }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncthreads();                                 // (the bins lie where other warps' rings were)
+        stream<2>(list, use, close);
     }
     // This CTA's and the row's sums of the chunks' masses; returns the row's.
     __device__ __forceinline__ u64 share_masses()
@@ -460,14 +447,13 @@ template <bool BF16> struct Row {
     // Sums of f(logit, token) by chunk; returns the row's.
     template <class F> __device__ __forceinline__ u64 mass_pass(F f)
     {
-        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
-            u64 s = 0;
-            each_of(ch, [&](float x, int tok) { s += f(x, tok); });
+        u64 s = 0;
+        each(list, [&](float x, int tok) { s += f(x, tok); }, [&](int ch) {
             s = warp_sum(s);
             if (lane == 0)
                 chunk_mass[ch - c0] = s;
-        }
-        __syncthreads();
+            s = 0;
+        });
         return share_masses();
     }
     // After a mass pass over f: the first token by id whose running sum exceeds t, in warp 0 of the CTA
@@ -572,12 +558,12 @@ template <bool BF16> struct Row {
         T *to = reinterpret_cast<T *>(bins);
         to[tid * 2] = to[tid * 2 + 1] = 0;
         __syncthreads();
-        each([&](float x, int tok) {
+        each(list, [&](float x, int tok) {
             int bin;
             const T w = f(x, tok, bin);
             if (w)
                 atomicAdd(to + bin, w);
-        });
+        }, [](int) {});
     }
     // The ordered bits that the logits of bins b1 .. b2 can have: lo + [0, 2^bits).  They lie within m - [d0, d1],
     // widened by the difference's rounding.
@@ -590,6 +576,11 @@ template <bool BF16> struct Row {
         const unsigned hi = b2 == 0 ? lo : m == CUDART_INF_F ? least : min(order_of(m - d1) + 2, least);
         bits = hi > lo ? 32 - __clz((int)(hi - lo)) : 0;
     }
+    // The least finite logit with ordered bits lo + [0, 2^bits)
+    static __device__ __forceinline__ float lowest(unsigned lo, int bits)
+    {
+        return logit_of((unsigned)min((u64)lo + ((u64)1 << bits) - 1, (u64)order_of(-FLT_MAX)));
+    }
     // The shortest prefix of the row's order whose sum of f, together with `sum` for the logits before them,
     // reaches target, among the logits `in` with ordered bits lo + [0, 2^bits): by kDigit digits at a time.
     // false: they do not.  Equal logits have equal f.
@@ -599,10 +590,12 @@ template <bool BF16> struct Row {
         u64 at = 0;
         do {
             const int shift = max(bits - kDigit, 0);
+            const float high = logit_of(lo), low = lowest(lo, bits);
             fill_bins<T>([&](float x, int tok, int &bin) {
-                const unsigned o = order_of(x) - lo;
-                bin = (int)(o >> shift);
-                return (u64)o >> bits == 0 && in(x) ? f(x, tok) : (T)0;
+                if (x > high || x < low || !in(x))
+                    return (T)0;
+                bin = (int)((order_of(x) - lo) >> shift);
+                return f(x, tok);
             });
             u64 w[2];
             merge_bins<T>(w);
@@ -675,11 +668,13 @@ template <bool BF16> struct Row {
         int bits;
         range_of((int)b1, b2, lo, bits);
         const int shift = max(bits - kDigit, 0);
+        const float high = logit_of(lo), low = lowest(lo, bits);
         fill_bins<unsigned>([&](float x, int, int &bin) {
-            const unsigned o = order_of(x) - lo;
+            if (x > high || x < low)
+                return 0u;
             const int b = bin_of(x);
-            bin = (int)(o >> shift);
-            return (u64)o >> bits == 0 && b >= (int)b1 && b <= b2 ? about(x) : 0u;
+            bin = (int)((order_of(x) - lo) >> shift);
+            return b >= (int)b1 && b <= b2 ? about(x) : 0u;
         });
         merge_bins<unsigned>(w);
         cross(w, from - sum);
@@ -700,24 +695,23 @@ template <bool BF16> struct Row {
         u64 *to = cluster.map_shared_rank(list, 0);
         int *n = cluster.map_shared_rank(count, 0);
         bool full = false;
-        for (int ch = c0 + warp; ch < c1; ch += kWarps) {
-            u64 s = 0;
-            each_of(ch, [&](float x, int tok) {
-                const unsigned o = order_of(x);
-                if (o < o1)
-                    s += weight(x);
-                else if (o <= o2 && !full) {
-                    const int at = atomicAdd(n, 1);
-                    full = at >= kList;
-                    if (!full)
-                        to[at] = ((u64)o << 32) | (unsigned)tok;
-                }
-            });
+        const float high = logit_of(o1), low = logit_of(min(o2, order_of(-FLT_MAX)));
+        double s = 0.0;
+        each(bins, [&](float x, int tok) {
+            if (x > high)
+                s += x == m ? 1.0 : power((double)x - (double)m);
+            else if (x >= low && !full) {
+                const int at = atomicAdd(n, 1);
+                full = at >= kList;
+                if (!full)
+                    to[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
+            }
+        }, [&](int ch) {
             s = warp_sum(s);
             if (lane == 0)
-                chunk_mass[ch - c0] = s;
-        }
-        __syncthreads();
+                chunk_mass[ch - c0] = (u64)__double2ll_rn(s * unit);
+            s = 0.0;
+        });
         const u64 above = share_masses();
         found = *n;
         return above;
@@ -793,7 +787,8 @@ template <bool BF16> struct Row {
         // many equal logits at the border (or, never seen, a border outside)
         auto f = [&](float x, int) { return weight(x); };
         const int bits = o2 > o1 ? 32 - __clz((int)(o2 - o1)) : 0;
-        if (!(found > kList && above < target && digits<u64>(f, [&](float x) { return order_of(x) <= o2; }, target, above, o1, bits, cut)) &&
+        const float low = logit_of(min(o2, order_of(-FLT_MAX)));
+        if (!(found > kList && above < target && digits<u64>(f, [&](float x) { return x >= low; }, target, above, o1, bits, cut)) &&
             !select<u64>(f, target, cut))
             cut = {-CUDART_INF_F, kNone};
         return mass_pass([&](float x, int tok) { return cut.keeps(x, tok) ? weight(x) : (u64)0; });
@@ -954,6 +949,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     __shared__ Word s_word[2];
     __shared__ u64 s_scratch[kWarps + 4];
     __shared__ float s_max[kWarps];
+    __shared__ double s_table[16];
     __shared__ unsigned s_mask[kWarps * 2 * (Row<BF16>::kMaskWords + 3)];
     __shared__ int s_count, s_left, s_hits;
     static_assert(kBins == 2 * kThreads && kBins * 8 <= kList * 4 && kMaxChunks * 32 * 2 <= kList * 4, "bins and lanes share the work space");
@@ -1023,6 +1019,8 @@ sample_kernel(const __grid_constant__ SampleParams p)
     r.c0 = min(part * per, chunks);
     r.c1 = min(r.c0 + per, chunks);
     r.c = c;
+    r.c16 = 16.0 * c;
+    r.table = s_table;
     r.unit = __hiloint2double((1023 + p.scale_bits) << 20, 0);
     r.list = s_dynamic;
     r.bins = s_dynamic + kList;
@@ -1035,6 +1033,9 @@ sample_kernel(const __grid_constant__ SampleParams p)
     r.phase = 0;
     if (tid == 0)
         s_count = s_hits = 0;
+    if (tid < 16)
+        s_table[tid] = exp2((double)tid / 16.0);
+    __syncthreads();
 
     // One pass over memory.  Where the whole sum decides about the token it is taken in 64 bits.
     const bool plain = !TOP && !cold && top_k <= 0 && top_p >= 1.f && min_p <= 0.f;
@@ -1050,7 +1051,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     auto chunk_sum = [&](int i, float ref) {              // relative to ref
         const float top = r.chunk_max[i];
         const double s = __longlong_as_double((long long)r.chunk_mass[i]);
-        return top == ref ? s : s * exp2_64((double)top - (double)ref, c);
+        return top == ref ? s : s * r.power((double)top - (double)ref);
     };
     // every warp its own chunks, then all of the CTA's
     float m = -CUDART_INF_F;
@@ -1074,7 +1075,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     sum = 0.0;
     if (lane < kWarps && m > -CUDART_INF_F) {
         const double s = __longlong_as_double((long long)s_scratch[lane]);
-        sum = s_max[lane] == m ? s : s * exp2_64((double)s_max[lane] - (double)m, c);
+        sum = s_max[lane] == m ? s : s * r.power((double)s_max[lane] - (double)m);
     }
     sum = warp_sum(sum);
     const Word all = r.exchange({sum, 0, m, 0});
@@ -1083,7 +1084,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     r.m = m;
     double total = 0.0;                                   // of the row, relative to m
     if (lane < size && all.sum > 0.0)
-        total = all.m == m ? all.sum : all.sum * exp2_64((double)all.m - (double)m, c);
+        total = all.m == m ? all.sum : all.sum * r.power((double)all.m - (double)m);
     total = warp_sum(total);
 
     if (TOP) {
@@ -1104,13 +1105,13 @@ sample_kernel(const __grid_constant__ SampleParams p)
                 // every CTA's kept tokens into the list of the first one
                 u64 *list = cluster.map_shared_rank(r.list, 0);
                 int *count = cluster.map_shared_rank(&s_count, 0);
-                r.each([&](float x, int tok) {
+                r.each(r.bins, [&](float x, int tok) {
                     if (cut.keeps(x, tok)) {
                         const int at = atomicAdd(count, 1);
                         if (at < kList)
                             list[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
                     }
-                });
+                }, [](int) {});
                 r.barrier();
                 found = s_count;
             }
@@ -1248,11 +1249,13 @@ sample_kernel(const __grid_constant__ SampleParams p)
 
 namespace {
 
-// CTAs of a row, of so many blocks: two CTAs per SM, shares of at least 8 blocks
-int cluster_size(int rows, int blocks, int sms)
+// CTAs of a row of so many blocks, `uneven`: some rows may take several more passes than others.
+int cluster_size(int rows, int blocks, int sms, bool uneven)
 {
     int size = 1;
-    while (size < kMaxCluster && rows * (long long)size < 2 * sms && blocks >= 16 * size)
+    while (size < 8 && rows * (long long)size < (uneven ? 8 : 3) * sms && blocks >= 16 * size)
+        size *= 2;
+    while (size < kMaxCluster && rows * (long long)kMaxCluster <= sms && blocks >= 16 * size)
         size *= 2;
     return size;
 }
@@ -1284,7 +1287,7 @@ int run(const char *name, const cstr_table_t *const *tables, int32_t n_tables, c
     const bool bf16 = dtype == CSTR_BF16;
     const int n = bf16 ? 8 : 4;
     const int blocks = (vocab_size + n - 1 + 32 * kU * n - 1) / (32 * kU * n);       // (a row may begin inside a vector)
-    const int size = cluster_size(rows, blocks, sms);
+    const int size = cluster_size(rows, blocks, sms, p.top_p && !p.top_k && !p.min_p);
     if ((long long)rows * size > 0x7fffffffLL)
         return cstr_fail(CSTR_ERR_SHAPE, "%s: rows x vocabulary too large for one launch", name);
     p.blocks = (blocks + kMaxChunks * size - 1) / (kMaxChunks * size);
