@@ -28,6 +28,7 @@ using namespace cstr_rows;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
+constexpr int kCtas = 8;                 // of an SM
 
 struct DistillParams {
     Tables t;
@@ -119,19 +120,34 @@ template <bool BF16> __device__ __forceinline__ uint4 narrow(const float *d)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// WIDE: rows of both buffers begin at the same place of their 16 bytes (or there is no gradient)
-template <bool BF16, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 6)
+// x = 2^(c (x - ref)), two logits per instruction but for the exponential itself
+template <int CNT> __device__ __forceinline__ void exponentials(float (&x)[CNT], float ref, float c)
+{
+#pragma unroll
+    for (int i = 0; i < CNT; i += 2) {
+        asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %2};\nadd.rn.f32x2 a, a, b;\n"
+            "mov.b64 b, {%3, %3};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}\n"
+            : "+f"(x[i]), "+f"(x[i + 1]) : "f"(-ref), "f"(c));
+        x[i] = exp2_fast(x[i]);
+        x[i + 1] = exp2_fast(x[i + 1]);
+    }
+}
+
+// WIDE: rows of both buffers begin at the same place of their 16 bytes (or there is no gradient).
+// kUnroll: vectors of a thread in flight.
+template <bool BF16, bool WIDE, int kUnroll>
+__global__ void __launch_bounds__(kThreads, kCtas)
 distill_kernel(const __grid_constant__ DistillParams p)
 {
     using View = RowView<BF16>;
     constexpr int N = View::N;
     extern __shared__ unsigned s_dynamic[];              // bitmap, then ids, weights and logits of the record
-    __shared__ Share s_warp[kWarps], s_share;
+    __shared__ Share s_warp[kWarps], s_share, s_sums;    // the warps', the CTA's, the row's
+    __shared__ MaxSum s_all;
     __shared__ float s_top[2][kWarps];                   // largest teacher value, largest logit of the record's part
     __shared__ float s_result[5];                        // factors of e in the rest, in the record, of t; maxima
     __shared__ float s_ref;
-    __shared__ int s_twice;
+    __shared__ int s_twice, s_count[kWarps];
     unsigned *bitmap = s_dynamic;
     int *s_id = reinterpret_cast<int *>(bitmap + p.words);
     float *s_t = reinterpret_cast<float *>(s_id + p.k), *s_x = s_t + p.k;
@@ -149,63 +165,138 @@ distill_kernel(const __grid_constant__ DistillParams p)
     char *d_row = (char *)p.dlogits + (long long)row * p.ld * View::ESZ;
     const int vectors = view.vectors(), per = (vectors + size - 1) / size;
     const int v0 = min(part * per, vectors), v1 = min(v0 + per, vectors);
-    const int lo = max(view.token(v0), 0), hi = min(view.token(v1), p.V);        // this CTA's tokens
-    auto put = [&](int v, const float *d) {
-        if (WIDE && view.inside(v))
-            __stcs(reinterpret_cast<uint4 *>(d_row - view.head * View::ESZ) + v, narrow<BF16>(d));
-        else
-            for (int e = 0; e < N; ++e)
-                if (view.token(v) + e >= 0 && view.token(v) + e < p.V)
-                    store_one<BF16>(d_row, view.token(v) + e, d[e]);
+    // the share's vectors that are inside the row; the row's first and last one may be not
+    const int i0 = v0 + (v0 == 0 && view.head > 0 ? 1 : 0), i1 = v1 - (v1 == vectors && i0 < v1 && !view.inside(vectors - 1) ? 1 : 0);
+    const int edge = tid == 0 && v0 < i0 ? v0 : tid == 32 && i1 < v1 ? i1 : -1;      // ... by one thread each
+    const uint4 *x_vec = reinterpret_cast<const uint4 *>(view.row - view.head * View::ESZ);
+    uint4 *d_vec = reinterpret_cast<uint4 *>(d_row - view.head * View::ESZ);
+    auto put_one = [&](int v, const float (&d)[N]) {
+        for (int e = 0; e < N; ++e)
+            if (view.token(v) + e >= 0 && view.token(v) + e < p.V)
+                store_one<BF16>(d_row, view.token(v) + e, d[e]);
     };
-    auto nothing = [&]() {
-        const float zero[N] = {};
-        if (p.dlogits)
-            for (int v = v0 + tid; v < v1; v += kThreads)
-                put(v, zero);
-        if (part == 0 && tid == 0)
-            p.loss[row] = 0.f;
+    auto put = [&](int v, const float (&d)[N]) {
+        if (WIDE)
+            __stcs(d_vec + v, narrow<BF16>(d));
+        else
+            put_one(v, d);
     };
     if (!active || w == 0.f) {
-        nothing();
+        const float zero[N] = {};
+        if (p.dlogits) {
+            for (int v = i0 + tid; v < i1; v += kThreads)
+                put(v, zero);
+            if (edge >= 0)
+                put_one(edge, zero);
+        }
+        if (part == 0 && tid == 0)
+            p.loss[row] = 0.f;
         return;
     }
 
-    // the record's tokens of this share
+    // the record's tokens of this share, in the record's order
+    const int lo = max(view.token(v0), 0), hi = min(view.token(v1), p.V), base = view.token(v0);
     const int32_t *ids = p.ids + (long long)row * p.k;
     const float *teacher = p.teacher + (long long)row * p.k;
     for (int i = tid; i < (int)p.words; i += kThreads)
         bitmap[i] = 0;
     if (tid == 0)
         s_twice = 0;
-    __syncthreads();
-    const bool renorm = p.tail == CSTR_TAIL_RENORM;
-    Record rec = {0.0, 0.0, 0.0, 0.0, -CUDART_INF_F, -CUDART_INF_F, 0.f};
-    for (int i = tid; i < p.k; i += kThreads) {
-        const int id = ids[i];
-        const float g = teacher[i];
-        s_id[i] = -1;
-        if (id < lo || id >= hi || g == -CUDART_INF_F)
-            continue;
-        const float x = view.allowed(id) ? view.one(id) : -CUDART_INF_F;
-        const int bit = id - view.token(v0);
-        const unsigned old = atomicOr(bitmap + (bit >> 5), 1u << (bit & 31));
-        if ((old >> (bit & 31)) & 1u)
-            s_twice = 1;
-        s_id[i] = id;
-        s_x[i] = x;
-        s_t[i] = g;
-        if (p.tail == CSTR_TAIL_LUMP)
-            rec.given += exp((double)g);
-        if (x != -CUDART_INF_F) {
-            rec.ref = fmaxf(rec.ref, g);
-            rec.x = fmaxf(rec.x, x);
-        }
-    }
+    int mine = 0;                                        // entries of this share
+    for (int i0 = 0; i0 < p.k; i0 += kThreads) {
+        const int i = i0 + tid, id = i < p.k ? ids[i] : -1;
+        const float g = i < p.k ? teacher[i] : 0.f;
+        const bool in = id >= lo && id < hi && g != -CUDART_INF_F;
+        const unsigned who = __ballot_sync(kFull, in);
+        if (lane == 0)
+            s_count[warp] = __popc(who);
+        __syncthreads();
+        int at = mine + __popc(who & ((1u << lane) - 1));
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        rec.ref = fmaxf(rec.ref, __shfl_xor_sync(kFull, rec.ref, off));
-        rec.x = fmaxf(rec.x, __shfl_xor_sync(kFull, rec.x, off));
+        for (int j = 0; j < kWarps; ++j) {
+            at += j < warp ? s_count[j] : 0;
+            mine += s_count[j];
+        }
+        if (in) {
+            s_id[at] = id;
+            s_t[at] = g;
+            const unsigned bit = 1u << ((id - base) & 31);
+            if (atomicOr(bitmap + ((id - base) >> 5), bit) & bit)
+                s_twice = 1;
+        }
+        __syncthreads();
+    }
+    // the first entry's logit comes while the others are read
+    const int id_0 = tid < mine ? s_id[tid] : -1;
+    const float x_0 = id_0 >= 0 && view.allowed(id_0) ? view.one(id_0) : -CUDART_INF_F;
+
+    // All tokens; with a lumped tail those outside the record.
+    const bool lump = p.tail == CSTR_TAIL_LUMP, renorm = p.tail == CSTR_TAIL_RENORM;
+    auto others = [&](int v) {
+        const int bit = (v - v0) * N;
+        return lump ? ~(bitmap[bit >> 5] >> (bit & 31)) : kFull;
+    };
+    MaxSum rest = {-CUDART_INF_F, 0.f};
+    auto add = [&](uint4 raw) {
+        float x[N], top = -CUDART_INF_F;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            x[e] = View::plain(raw, e);
+#pragma unroll
+        for (int e = 0; e < N; e += 2)
+            top = max3(top, x[e], x[e + 1]);
+        if (top > rest.m) {
+            rest.s *= exp2_fast((rest.m - top) * p.c);
+            rest.m = top;
+        }
+        exponentials(x, rest.m == -CUDART_INF_F ? 0.f : rest.m, p.c);
+        float s[2] = {rest.s, 0.f};
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            s[e & 1] += x[e];
+        rest.s = s[0] + s[1];
+    };
+#pragma unroll 1
+    for (int v = i0 + tid; v < i1; v += kUnroll * kThreads) {
+        uint4 raw[kUnroll];
+        unsigned bits[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            bits[u] = 0u;
+            raw[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (v + u * kThreads < i1) {
+                raw[u] = x_vec[v + u * kThreads];
+                bits[u] = view.bits(v + u * kThreads) & others(v + u * kThreads);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            add(View::mask(raw[u], bits[u]));
+    }
+    if (edge >= 0)
+        add(View::mask(view.edge(edge), others(edge)));
+
+    // the record's part: largest teacher value and logit, then the sums relative to them (by the warps that
+    // have entries)
+    const bool any = warp * 32 < mine;
+    Record rec = {0.0, 0.0, 0.0, 0.0, -CUDART_INF_F, -CUDART_INF_F, 0.f};
+    if (any) {
+        for (int i = tid; i < mine; i += kThreads) {
+            const int id = s_id[i];
+            const float x = i == tid ? x_0 : view.allowed(id) ? view.one(id) : -CUDART_INF_F, g = s_t[i];
+            s_x[i] = x;
+            if (lump)
+                rec.given += exp((double)g);
+            if (x != -CUDART_INF_F) {
+                rec.ref = fmaxf(rec.ref, g);
+                rec.x = fmaxf(rec.x, x);
+            }
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            rec.ref = fmaxf(rec.ref, __shfl_xor_sync(kFull, rec.ref, off));
+            rec.x = fmaxf(rec.x, __shfl_xor_sync(kFull, rec.x, off));
+        }
     }
     if (lane == 0) {
         s_top[0][warp] = rec.ref;
@@ -227,149 +318,189 @@ distill_kernel(const __grid_constant__ DistillParams p)
                     return false;
         return true;
     };
-    for (int i = tid; i < p.k; i += kThreads) {
-        if (s_id[i] < 0 || s_x[i] == -CUDART_INF_F)
-            continue;
-        const double log_t = (double)s_t[i] - (double)rec.ref, t = exp(log_t);
-        rec.t += t;
-        rec.t_log += t == 0.0 ? 0.0 : t * log_t;
-        rec.t_x += t * ((double)s_x[i] - (double)rec.x);
-        if (first(i))
-            rec.e += exp2_fast((s_x[i] - rec.x) * p.c);
-    }
-
-    // the others
-    auto bits_of = [&](int v) {
-        const int bit = (v - v0) * N;
-        return ~(bitmap[bit >> 5] >> (bit & 31));
-    };
-    MaxSum rest = {-CUDART_INF_F, 0.f};
-    for (int v = v0 + tid; v < v1; v += kThreads) {
-        const uint4 raw = View::mask(view.masked(v), bits_of(v));
-        float x[N], top = -CUDART_INF_F;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            x[e] = View::plain(raw, e);
-            top = fmaxf(top, x[e]);
+    if (any) {
+        for (int i = tid; i < mine; i += kThreads) {
+            if (s_x[i] == -CUDART_INF_F)
+                continue;
+            const double log_t = (double)s_t[i] - (double)rec.ref, t = exp(log_t);
+            rec.t += t;
+            rec.t_log += t == 0.0 ? 0.0 : t * log_t;
+            rec.t_x += t * ((double)s_x[i] - (double)rec.x);
+            if (lump && first(i))
+                rec.e += exp2_fast((s_x[i] - rec.x) * p.c);
         }
-        if (top > rest.m) {
-            rest.s *= exp2_fast((rest.m - top) * p.c);
-            rest.m = top;
-        }
-        const float ref = rest.m == -CUDART_INF_F ? 0.f : rest.m;
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            rest.s += exp2_fast((x[e] - ref) * p.c);
+        for (int off = 16; off > 0; off >>= 1) {
+            rec.t += __shfl_xor_sync(kFull, rec.t, off);
+            rec.t_log += __shfl_xor_sync(kFull, rec.t_log, off);
+            rec.t_x += __shfl_xor_sync(kFull, rec.t_x, off);
+            rec.given += __shfl_xor_sync(kFull, rec.given, off);
+            rec.e += __shfl_xor_sync(kFull, rec.e, off);
+        }
     }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
+    for (int off = 16; off > 0; off >>= 1)
         rest = join(rest, from_lane(rest, off), p.c);
-        rec.t += __shfl_xor_sync(kFull, rec.t, off);
-        rec.t_log += __shfl_xor_sync(kFull, rec.t_log, off);
-        rec.t_x += __shfl_xor_sync(kFull, rec.t_x, off);
-        rec.given += __shfl_xor_sync(kFull, rec.given, off);
-        rec.e += __shfl_xor_sync(kFull, rec.e, off);
-    }
     if (lane == 0)
         s_warp[warp] = {rest, rec};
     __syncthreads();
-    if (tid == 0) {
-        Share s = s_warp[0];
-        for (int i = 1; i < kWarps; ++i) {
-            const Share &o = s_warp[i];                  // (all with the same references)
-            s.rest = join(s.rest, o.rest, p.c);
-            s.record.t += o.record.t;
-            s.record.t_log += o.record.t_log;
-            s.record.t_x += o.record.t_x;
-            s.record.given += o.record.given;
-            s.record.e += o.record.e;
+    if (warp == 0) {
+        // (all with the same references)
+        Share s = s_warp[lane & (kWarps - 1)];
+#pragma unroll
+        for (int off = kWarps / 2; off > 0; off >>= 1)
+            s.rest = join(s.rest, from_lane(s.rest, off), p.c);
+        for (int i = 1; i * 32 < mine && i < kWarps; ++i) {
+            s.record.t += lane == 0 ? s_warp[i].record.t : 0.0;
+            s.record.t_log += lane == 0 ? s_warp[i].record.t_log : 0.0;
+            s.record.t_x += lane == 0 ? s_warp[i].record.t_x : 0.0;
+            s.record.given += lane == 0 ? s_warp[i].record.given : 0.0;
+            s.record.e += lane == 0 ? s_warp[i].record.e : 0.f;
         }
-        s_share = s;
+        if (lane == 0)
+            s_share = s;
+        __syncwarp();
     }
     if (size > 1)
         cluster.sync();
-    else
-        __syncthreads();
+    auto teachers_rest = [](const Share &s) {
+        const double left = 1.0 - s.record.given;
+        return left < 0.0 ? 0.0 : left;
+    };
     if (warp == 0) {
         Share s = {{-CUDART_INF_F, 0.f}, {0.0, 0.0, 0.0, 0.0, -CUDART_INF_F, -CUDART_INF_F, 0.f}};
         if (lane < size)
             s = *cluster.map_shared_rank(&s_share, lane);
-#pragma unroll
-        for (int off = 8; off > 0; off >>= 1) {
+        for (int off = size / 2; off > 0; off >>= 1) {
             s.rest = join(s.rest, from_lane(s.rest, off), p.c);
             s.record = join(s.record, from_lane(s.record, off), p.c);
         }
         if (lane == 0) {
-            Record r = s.record;
-            const MaxSum all = join(s.rest, {r.x, r.e}, p.c);
-            if (r.ref == CUDART_INF_F)
-                r.t = CUDART_NAN;                // a record with infinite logits is none
-            float loss = 0.f, f_rest = 0.f, f_listed = 0.f, f_t = 0.f;
+            const MaxSum all = lump ? join(s.rest, {s.record.x, s.record.e}, p.c) : s.rest;
+            if (s.record.ref == CUDART_INF_F)
+                s.record.t = CUDART_NAN;         // a record with infinite logits is none
+            s_sums = s;
+            s_all = all;
+            float f_rest = 0.f, f_listed = 0.f, f_t = 0.f;
             if (all.m != -CUDART_INF_F || all.s != 0.f) {
-                const double inv = p.inv_temp, total = all.s;
-                // log S relative to the record's largest logit
-                const double log_all = log(total) + (r.x == all.m ? 0.0 : ((double)all.m - (double)r.x) * inv);
-                // the rest's tokens are counted from their own maximum: they may lie far below the record's
-                const double down = s.rest.m == all.m ? 0.0 : ((double)s.rest.m - (double)all.m) * inv;
-                double value = r.t == 0.0 ? 0.0 : r.t_log - r.t_x * inv + r.t * log_all, sum = r.t, left = 0.0;
-                if (renorm) {
-                    value = r.t != 0.0 ? value / r.t - log(r.t) : 0.0;
-                    sum = r.t != 0.0 ? r.t / r.t : 0.0;
+                const float t = (float)s.record.t, wt = (float)((double)w * p.inv_temp);
+                float sum = renorm ? (t != 0.f ? t / t : 0.f) : t;
+                if (lump && s.rest.s != 0.f) {
+                    // the rest's tokens are counted from their own maximum: they may lie far below the record's
+                    const float left = (float)teachers_rest(s);
+                    sum += left;
+                    f_rest = wt * (sum * exp2_fast((s.rest.m - all.m) * p.c) / all.s - left / s.rest.s);
                 }
-                if (p.tail == CSTR_TAIL_LUMP && s.rest.s != 0.f) {
-                    left = 1.0 - r.given;
-                    left = left < 0.0 ? 0.0 : left;
-                    if (left != 0.0)
-                        value += left * (log(left) - (log((double)s.rest.s / total) + down));
-                }
-                const double wt = (double)w * inv;
-                loss = (float)((double)w * value);
-                f_listed = (float)(wt * (sum + left) / total);
-                f_rest = s.rest.s != 0.f ? (float)(wt * ((sum + left) * exp(down) / total - left / (double)s.rest.s)) : 0.f;
-                f_t = (float)(renorm ? (r.t != 0.0 ? wt / r.t : 0.0) : wt);
+                f_listed = wt * sum / all.s;
+                if (!lump)
+                    f_rest = f_listed;
+                f_t = renorm ? (t != 0.f ? wt / t : 0.f) : wt;
             }
-            if (part == 0)
-                p.loss[row] = loss;
             s_result[0] = f_rest;
             s_result[1] = f_listed;
             s_result[2] = f_t;
             s_result[3] = all.m;
             s_result[4] = s.rest.m;
-            s_ref = r.ref;
+            s_ref = s.record.ref;
         }
     }
-    if (size > 1)
-        cluster.sync();                          // the shares have been read
-    else
-        __syncthreads();
-    if (!p.dlogits)
+    if (size > 1) {                              // the shares have been read; the end waits for that
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    }
+    // The row's loss, by one thread: behind the gradient, which does not wait for it.
+    auto write_loss = [&]() {
+        const Share sums = s_sums;
+        const MaxSum all = s_all;
+        const Record &r = sums.record;
+        float loss = 0.f;
+        if (all.m != -CUDART_INF_F || all.s != 0.f) {
+            // log S relative to the record's largest logit
+            const double inv = p.inv_temp, total = all.s;
+            const double log_all = log(total) + (r.x == all.m ? 0.0 : ((double)all.m - (double)r.x) * inv);
+            double value = r.t == 0.0 ? 0.0 : r.t_log - r.t_x * inv + r.t * log_all;
+            if (renorm)
+                value = r.t != 0.0 ? value / r.t - log(r.t) : 0.0;
+            const double left = lump && sums.rest.s != 0.f ? teachers_rest(sums) : 0.0;
+            if (left != 0.0)
+                value += left * (log(left / ((double)sums.rest.s / total)) - (sums.rest.m == all.m ? 0.0 : ((double)sums.rest.m - (double)all.m) * inv));
+            loss = (float)((double)w * value);
+        }
+        p.loss[row] = loss;
+    };
+    if (!p.dlogits) {
+        if (part == 0 && tid == 0)
+            write_loss();
+        if (size > 1)
+            asm volatile("barrier.cluster.wait;" ::: "memory");
         return;
-    const float f_rest = s_result[0], f_listed = s_result[1], f_t = s_result[2], ref = s_result[3], low = s_result[4];
-    for (int v = v0 + tid; v < v1; v += kThreads) {
-        const uint4 raw = View::mask(view.masked(v), bits_of(v));
-        float d[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float x = View::plain(raw, e);
-            d[e] = x == -CUDART_INF_F ? 0.f : f_rest * exp2_fast((x - low) * p.c);
-        }
-        put(v, d);
     }
-    __syncthreads();                             // behind the zeros in their places
-    const double t_ref = s_ref;                          // 0 unless the record is renormalised
-    for (int i = tid; i < p.k; i += kThreads) {
-        if (s_id[i] < 0 || !first(i))
+    __syncthreads();
+    const float f_rest = s_result[0], low = s_result[4];
+    // A token that is left out is -infinity here: its exponential and with it its gradient are 0 - unless the
+    // factor or the maximum is not finite.
+    const bool plain = fabsf(f_rest) < CUDART_INF_F && fabsf(low) < CUDART_INF_F;
+    auto slope = [&](uint4 raw, float (&d)[N]) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            d[e] = View::plain(raw, e);
+        if (plain) {
+            exponentials(d, low, p.c);
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                d[e] *= f_rest;
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                d[e] = d[e] == -CUDART_INF_F ? 0.f : f_rest * exp2_fast((d[e] - low) * p.c);
+        }
+    };
+#pragma unroll 1
+    for (int v = i0 + tid; v < i1; v += kUnroll * kThreads) {
+        uint4 raw[kUnroll];
+        unsigned bits[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            bits[u] = 0u;
+            raw[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (v + u * kThreads < i1) {
+                raw[u] = __ldcs(x_vec + v + u * kThreads);
+                bits[u] = view.bits(v + u * kThreads) & others(v + u * kThreads);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            float d[N];
+            slope(View::mask(raw[u], bits[u]), d);
+            if (v + u * kThreads < i1)
+                put(v + u * kThreads, d);
+        }
+    }
+    if (edge >= 0) {
+        float d[N];
+        slope(View::mask(view.edge(edge), others(edge)), d);
+        put_one(edge, d);
+    }
+    __syncthreads();                             // the record's tokens behind what has been written in their places
+    const float f_listed = s_result[1], f_t = s_result[2], ref = s_result[3];
+    const double t_ref = s_ref;                  // 0 unless the record is renormalised
+    for (int i = tid; i < mine; i += kThreads) {
+        if (!first(i))
             continue;
         float d = 0.f;
         if (s_x[i] != -CUDART_INF_F) {
             double t = 0.0;
-            for (int j = i; j < (twice ? p.k : i + 1); ++j)
+            for (int j = i; j < (twice ? mine : i + 1); ++j)
                 if (s_id[j] == s_id[i])
                     t += exp((double)s_t[j] - t_ref);
             d = f_listed * exp2_fast((s_x[i] - ref) * p.c) - (float)(t * (double)f_t);
         }
         store_one<BF16>(d_row, s_id[i], d);
     }
+    if (part == 0 && tid == kThreads - 1)
+        write_loss();
+    if (size > 1)
+        asm volatile("barrier.cluster.wait;" ::: "memory");
 }
 
 int launch(void (*kernel)(DistillParams), const DistillParams &p, int size, int smem, cudaStream_t stream)
@@ -438,10 +569,13 @@ extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_ta
         if (device >= 0 && device < 64)
             known[device].store(sms, std::memory_order_relaxed);
     }
-    const long long share = bf16 ? 32768 : 16384;
+    // With a gradient shares of at most 64 KB, so that what the resident CTAs have read is still in the L2 cache
+    // when they write; without, as many CTAs as the SMs hold.  Smaller shares, down to 4,096 tokens, while there
+    // are fewer CTAs than that.
+    const long long share = dlogits ? (bf16 ? 32768 : 16384) : 0x7fffffffLL;
     int size = 1;
     while (size < kMaxCluster && (vocab_size > share * size ||
-                                  (rows * (long long)size <= sms && vocab_size >= 4096LL * size)))
+                                  (rows * (long long)size < kCtas * sms && vocab_size >= 8192LL * size)))
         size *= 2;
     if ((long long)rows * size > 0x7fffffffLL)
         return cstr_fail(CSTR_ERR_SHAPE, "cstr_distill_loss: rows x vocabulary too large for one launch");
@@ -450,7 +584,12 @@ extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_ta
     p.words = (unsigned)((per * (long long)n + 31) / 32);
     const int smem = (int)p.words * 4 + k * 12;
     const bool together = !dlogits || (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15u) == 0;
-    void (*kernel)(DistillParams) = bf16 ? (together ? distill_kernel<true, true> : distill_kernel<true, false>)
-                                         : (together ? distill_kernel<false, true> : distill_kernel<false, false>);
+    void (*kernel)(DistillParams);
+    if (!together)
+        kernel = bf16 ? distill_kernel<true, false, 1> : distill_kernel<false, false, 1>;
+    else if (dlogits)
+        kernel = bf16 ? distill_kernel<true, true, 1> : distill_kernel<false, true, 1>;
+    else
+        kernel = bf16 ? distill_kernel<true, true, 2> : distill_kernel<false, true, 2>;
     return launch(kernel, p, size, smem, (cudaStream_t)cuda_stream);
 }

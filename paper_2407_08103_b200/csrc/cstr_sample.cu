@@ -89,12 +89,6 @@ __device__ __forceinline__ u64 part_of(u64 a, float f, bool up)
     return whole + (up && rest ? 1 : 0);
 }
 
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
 // s += 2^(c (x - ref)) for two logits, two to an instruction but for the exponential itself
 __device__ __forceinline__ void add_exponentials(float2 &s, float x, float y, float ref, float c)
 {
