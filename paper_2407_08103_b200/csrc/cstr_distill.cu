@@ -569,13 +569,11 @@ extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_ta
         if (device >= 0 && device < 64)
             known[device].store(sms, std::memory_order_relaxed);
     }
-    // With a gradient shares of at most 64 KB, so that what the resident CTAs have read is still in the L2 cache
-    // when they write; without, as many CTAs as the SMs hold.  Smaller shares, down to 4,096 tokens, while there
-    // are fewer CTAs than that.
-    const long long share = dlogits ? (bf16 ? 32768 : 16384) : 0x7fffffffLL;
+    // As many CTAs as the SMs hold, three quarters of that with a gradient, while shares have 4,096 tokens or more.
+    // (512 x 256,000 fp32 with gradient: 273 us with two CTAs a row, 290 with 16, whose shares would still be in the
+    // L2 cache when the gradient is written, 420 with one; without one 126 us with four, 156 with two.)
     int size = 1;
-    while (size < kMaxCluster && (vocab_size > share * size ||
-                                  (rows * (long long)size < kCtas * sms && vocab_size >= 8192LL * size)))
+    while (size < kMaxCluster && rows * (long long)size < (dlogits ? 6 : 8) * sms && vocab_size >= 8192LL * size)
         size *= 2;
     if ((long long)rows * size > 0x7fffffffLL)
         return cstr_fail(CSTR_ERR_SHAPE, "cstr_distill_loss: rows x vocabulary too large for one launch");
