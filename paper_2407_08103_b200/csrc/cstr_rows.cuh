@@ -76,10 +76,11 @@ __device__ __forceinline__ bool row_state(const Tables &a, int row, int &table, 
     return true;
 }
 
-// State after an allowed token (next holds codes of internal ids; its sink means "no edge").
-__device__ __forceinline__ int next_state(const TableDesc &t, int state, int token)
+// State after an allowed token from internal state `inner` (next holds codes of internal ids; its sink means
+// "no edge").
+__device__ __forceinline__ int next_state(const TableDesc &t, int inner, int token)
 {
-    const long long at = (long long)token * t.lds + (t.rank ? t.rank[state] : state);
+    const long long at = (long long)token * t.lds + inner;
     int q = t.wide ? ((const int32_t *)t.next)[at] : (int)((const uint16_t *)t.next)[at];
     q = CSTR_UNPERM(q >> t.code_shift);
     return q == t.n_states ? CSTR_DEAD : t.unrank ? t.unrank[q] : q;

@@ -537,19 +537,19 @@ template <bool BF16> struct Row {
         __syncthreads();
     }
     // The cluster's sums of two bins a thread (counted in T), after a barrier; the bins may be changed behind another.
-    template <class T> __device__ __forceinline__ void merge_bins(u64 (&w)[2])
+    template <class T> __device__ __forceinline__ void merge_bins(u64 (&w)[2], int set = 0)
     {
         barrier();
         w[0] = w[1] = 0;
         for (int r = 0; r < size; ++r) {
-            const T *o = cluster.map_shared_rank(reinterpret_cast<T *>(bins), r) + tid * 2;
+            const T *o = cluster.map_shared_rank(reinterpret_cast<T *>(bins), r) + set * kBins + tid * 2;
             w[0] += o[0];
             w[1] += o[1];
         }
     }
-    template <class T, class F> __device__ __forceinline__ void fill_bins(F f)     // f(logit, token, bin): weight, 0: none
+    template <class T, class F> __device__ __forceinline__ void fill_bins(F f, int set = 0)     // f(logit, token, bin): weight, 0: none
     {
-        T *to = reinterpret_cast<T *>(bins);
+        T *to = reinterpret_cast<T *>(bins) + set * kBins;
         to[tid * 2] = to[tid * 2 + 1] = 0;
         __syncthreads();
         each(list, [&](float x, int tok) {
@@ -634,7 +634,7 @@ template <bool BF16> struct Row {
         return digits<T>(f, [&](float x) { return bin_of(x) == (int)b; }, target, sum, lo, bits, cut);
     }
     // Ordered bits [o1, o2] within which the sum of the weights reaches target, by weights in 32 bits as whole
-    // numbers of 2^-31 of their sum `total`.  These are off by half a number each and by 2^-18 of all (arguments of
+    // numbers of 2^-31 of their sum `total` (two sets of bins, to be changed behind a barrier).  These are off by half a number each and by 2^-18 of all (arguments of
     // exponentials): what is that near to the target is within.  Nothing relies on it.
     __device__ __forceinline__ void narrow(double total, u64 target, unsigned &o1, unsigned &o2)
     {
@@ -655,7 +655,6 @@ template <bool BF16> struct Row {
         __syncthreads();
         cross(w, to);
         const int b2 = (int)min(scratch[kWarps], (u64)kBins - 1);
-        barrier();
         if (b1 == ~0ull)
             return;
         unsigned lo;
@@ -669,14 +668,13 @@ template <bool BF16> struct Row {
             const int b = bin_of(x);
             bin = (int)((order_of(x) - lo) >> shift);
             return b >= (int)b1 && b <= b2 ? about(x) : 0u;
-        });
-        merge_bins<unsigned>(w);
+        }, 1);
+        merge_bins<unsigned>(w, 1);
         cross(w, from - sum);
         const u64 d1 = scratch[kWarps];
         __syncthreads();
         cross(w, to - sum);
         const u64 d2 = min(scratch[kWarps], (u64)kBins - 1);
-        barrier();
         if (d1 == ~0ull)
             return;
         o1 = lo + (unsigned)(d1 << shift);
@@ -690,15 +688,30 @@ template <bool BF16> struct Row {
         int *n = cluster.map_shared_rank(count, 0);
         bool full = false;
         const float high = logit_of(o1), low = logit_of(min(o2, order_of(-FLT_MAX)));
+        // (what is not above adds 2^-1000, where floats are fine enough to say so)
+        const float reach = (float)(1000.0 / c), least = m - reach;
+        const bool fine = reach < 1e37f && fabsf(m) < reach * 1e6f;
         double s = 0.0;
-        each(bins, [&](float x, int tok) {
-            if (x > high)
-                s += x == m ? 1.0 : power((double)x - (double)m);
-            else if (x >= low && !full) {
-                const int at = atomicAdd(n, 1);
-                full = at >= kList;
-                if (!full)
-                    to[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
+        stream<1>(bins, [&](const uint4 (&raw)[kU], int first) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int tok = view.token(first + u * 32 + lane);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = View::plain(raw[u], e);
+                    const double d = (double)(x > high ? x : least) - (double)m;
+                    if (fine) {
+                        const double2 f = exp2_factors(d, c16, table);
+                        s = fma(f.x, f.y, s);
+                    } else if (x > high)
+                        s += x == m ? 1.0 : power(d);
+                    if (x <= high && x >= low && !full) {
+                        const int at = atomicAdd(n, 1);
+                        full = at >= kList;
+                        if (!full)
+                            to[at] = ((u64)order_of(x) << 32) | (unsigned)(tok + e);
+                    }
+                }
             }
         }, [&](int ch) {
             s = warp_sum(s);
@@ -860,41 +873,53 @@ __device__ __forceinline__ void from_list(Row<BF16> &r, int found, int top_k, fl
 {
     const int tid = r.tid, lane = r.lane, warp = r.warp;
     if (found <= kThreads) {
-        // An entry a thread, compared with all others: its rank, what lies before it, then - of those that are
-        // kept - what its id and lower ones hold.
-        const bool in = tid < found;
-        const u64 key = in ? r.list[tid] : ~0ull;
+        // Each entry is compared with all others by as many threads as there are for it: its rank, what lies
+        // before it, then - of those that are kept - what its id and lower ones hold.
+        int share = 1;
+        while (share < 8 && found * share * 2 <= kThreads)
+            share *= 2;
+        const int at = tid / share, sub = tid & (share - 1);
+        const bool in = at < found;
+        const u64 key = in ? r.list[at] : ~0ull;
         const float x = logit_of((unsigned)(key >> 32));
         u64 w = in ? r.weight(x) : 0;
-        if (in)
-            r.bins[tid] = w;
+        if (in && sub == 0)
+            r.bins[at] = w;
         __syncthreads();
         int rank = 0;
         u64 before = 0;
-        if (warp * 32 < found)
-            for (int j = 0; j < found; ++j) {
+        if (warp * 32 < found * share) {
+            for (int j = sub; j < found; j += share) {
                 const bool first = r.list[j] < key;
                 rank += first;
                 before += first ? r.bins[j] : 0;
             }
+            for (int off = 1; off < share; off *= 2) {
+                rank += __shfl_xor_sync(kFull, rank, off);
+                before += __shfl_xor_sync(kFull, before, off);
+            }
+        }
         // (the first token is kept in any case: min_p is at most 1, top_k at least 2, the target above 0)
         bool keep = in && x >= low && (top_k <= 0 || rank < top_k);
         if (top_p < 1.f) {
-            const u64 target = part_of(whole ? whole : r.block_sum(keep ? w : 0), top_p, true);
+            const u64 target = part_of(whole ? whole : r.block_sum(keep && sub == 0 ? w : 0), top_p, true);
             keep = keep && before < target;
         }
         w = keep ? w : 0;
-        const u64 kept = r.block_sum(w), t = part_of(kept, u, false);
+        const u64 kept = r.block_sum(sub == 0 ? w : 0), t = part_of(kept, u, false);
         __syncthreads();
-        if (in)
-            r.bins[tid] = w;
+        if (in && sub == 0)
+            r.bins[at] = w;
         __syncthreads();
         const unsigned id = (unsigned)key;
         u64 upto = 0;
-        if (warp * 32 < found)
-            for (int j = 0; j < found; ++j)
+        if (warp * 32 < found * share) {
+            for (int j = sub; j < found; j += share)
                 upto += (unsigned)r.list[j] <= id ? r.bins[j] : 0;
-        if (keep && upto > t && upto - w <= t)
+            for (int off = 1; off < share; off *= 2)
+                upto += __shfl_xor_sync(kFull, upto, off);
+        }
+        if (keep && sub == 0 && upto > t && upto - w <= t)
             done((int)id, x, kept);
         return;
     }
@@ -976,11 +1001,13 @@ sample_kernel(const __grid_constant__ SampleParams p)
             active = false;
         u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
     }
+    // (the state's number in the table, before it is needed)
+    const int inner = !TOP && p.t.n > 0 && active && p.t.tab[table].rank ? p.t.tab[table].rank[state] : state;
     // token and state of a row, by one thread
     auto finish = [&](int token, float logp, float kept) {
         int next = CSTR_DEAD;
         if (token >= 0 && p.t.n > 0)
-            next = next_state(p.t.tab[table], state, token);
+            next = next_state(p.t.tab[table], inner, token);
         p.tokens[row] = token;
         if (p.states_out)
             p.states_out[row] = next;

@@ -46,6 +46,9 @@ EXPORTS = [
 # entry points of the checking build only (include/cstr_debug.h)
 DEBUG_EXPORTS = ["cstr_debug_bounds_status", "cstr_test_set_group_hash_bits", "cstr_test_set_wait_limit"]
 
+_F32 = _I32 = _U8 = None      # torch's types, from the first call that takes whole rows on
+_LOGIT_CODES = {}
+
 _lib = None
 _libs = {}            # path -> loaded library
 _active_path = None   # None: the release library at LIB_PATH
@@ -851,29 +854,49 @@ def cstr_policy_loss(tables, logits, states, actions, old_logp, advantages, loss
         _check(rc)
 
 
+def _load_types():
+    global _F32, _I32, _U8
+    import torch
+    _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+    _LOGIT_CODES.update({torch.float32: CSTR_F32, torch.bfloat16: CSTR_BF16})
+
+
 def _logit_rows(tables, logits, states):
     """Checks of the operators over whole rows -> (C array of tables or None, their number, address,
-    dtype code, ld, rows, vocabulary, device)."""
-    import torch
-    if isinstance(tables, Table):
-        tables = [tables]
-    tables = tables or []
-    if logits.dtype == torch.float32:
-        dtype = CSTR_F32
-    elif logits.dtype == torch.bfloat16:
-        dtype = CSTR_BF16
-    else:
+    dtype code, ld, shape, strides, device)."""
+    if _F32 is None:
+        _load_types()
+    if tables.__class__ is Table:
+        tables = (tables,)
+    code = _LOGIT_CODES.get(logits.dtype)
+    if code is None:
         raise TypeError("logits must be float32 or bfloat16")
-    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    shape, strides = logits.shape, logits.stride()
+    if len(shape) != 2 or (shape[1] > 1 and strides[1] != 1):
         raise ValueError("logits must be [N][V] with unit inner stride")
     if not logits.is_cuda:
         raise ValueError("logits must be a CUDA tensor")
     if bool(tables) != (states is not None):
         raise ValueError("states go with tables")
-    n, vocab = logits.shape
-    ld = logits.stride(0) if n > 1 else max(vocab, logits.stride(0))
-    arr = (ctypes.c_void_p * len(tables))(*[t.ptr.value for t in tables]) if tables else None
-    return arr, len(tables), logits.data_ptr(), dtype, ld, n, vocab, logits.device
+    ld = strides[0] if shape[0] > 1 else max(shape[1], strides[0])
+    arr, count = None, 0
+    if tables:
+        count = len(tables)
+        arr = (ctypes.c_void_p * count)(*[t.ptr.value for t in tables])
+    return arr, count, logits.data_ptr(), code, ld, shape, strides, logits.device
+
+
+def _records_arg(name, t, shape, device, dtype):
+    """Checked ``[N][n]`` array -> address."""
+    if t is None or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s on %s" % (name, dtype, list(shape), device))
+    return t.data_ptr()
+
+
+def _records_shape(name, t, n):
+    if t is None or t.dim() != 2 or t.shape[0] != n:
+        raise ValueError("%s must have two dimensions, [%d][n]" % (name, n))
+    return t.shape
 
 
 def cstr_sample(tables, logits, states, tokens_out, uniform, temperature=None, top_k=None, top_p=None,
@@ -885,25 +908,22 @@ def cstr_sample(tables, logits, states, tokens_out, uniform, temperature=None, t
     ``states_out`` int32 ``[N]``, ``accept_out`` uint8 ``[N]``; all but ``uniform`` and ``tokens_out`` may be
     None.  Without ``states_out`` the rows advance in place.  ``tables`` None or empty (with ``states``
     None): unconstrained."""
-    import torch
-    arr, count, address, dtype, ld, n, vocab, device = _logit_rows(tables, logits, states)
-    for name, t in (("uniform", uniform), ("tokens_out", tokens_out)):
-        if t is None:
-            raise ValueError("%s is required" % name)
+    arr, count, address, dtype, ld, (n, vocab), _, device = _logit_rows(tables, logits, states)
+    if uniform is None or tokens_out is None:
+        raise ValueError("uniform and tokens_out are required")
     if states is None and states_out is not None:
         raise ValueError("states_out goes with states")
-    f32, i32 = torch.float32, torch.int32
 
     def rows(name, t, dt):
-        return _rows_arg(name, t, n, device, dt)
-    before = rows("states", states, i32)
+        return None if t is None else _rows_arg(name, t, n, device, dt)
+    before = rows("states", states, _I32)
     rc = lib().cstr_sample(
-        arr, count, rows("row_table", row_table, i32), before,
-        before if states_out is None else rows("states_out", states_out, i32), address, dtype, ld, vocab,
-        rows("uniform", uniform, f32), rows("temperature", temperature, f32), rows("top_k", top_k, i32),
-        rows("top_p", top_p, f32), rows("min_p", min_p, f32), rows("tokens_out", tokens_out, i32),
-        rows("logp_out", logp_out, f32), rows("kept_out", kept_out, f32),
-        rows("accept_out", accept_out, torch.uint8), n, _raw_stream(stream, device))
+        arr, count, rows("row_table", row_table, _I32), before,
+        before if states_out is None else rows("states_out", states_out, _I32), address, dtype, ld, vocab,
+        rows("uniform", uniform, _F32), rows("temperature", temperature, _F32), rows("top_k", top_k, _I32),
+        rows("top_p", top_p, _F32), rows("min_p", min_p, _F32), rows("tokens_out", tokens_out, _I32),
+        rows("logp_out", logp_out, _F32), rows("kept_out", kept_out, _F32),
+        rows("accept_out", accept_out, _U8), n, _raw_stream(stream, device))
     if rc:
         _check(rc)
 
@@ -913,17 +933,13 @@ def cstr_top_logprobs(tables, logits, states, ids_out, logp_out, temperature: fl
     """The most likely tokens of every row's constrained distribution.  CUDA tensors: ``ids_out`` int32 and
     ``logp_out`` float32 ``[N][n]`` contiguous (``n`` up to ``CSTR_MAX_TOP``), ``lse_out`` float32 ``[N]`` or
     None; the others as in ``cstr_sample``."""
-    import torch
-    arr, count, address, dtype, ld, n, vocab, device = _logit_rows(tables, logits, states)
-    for name, t, dt in (("ids_out", ids_out, torch.int32), ("logp_out", logp_out, torch.float32)):
-        if t is None or t.dtype != dt or t.dim() != 2 or t.shape[0] != n or t.shape != ids_out.shape \
-                or not t.is_contiguous() or t.device != device:
-            raise ValueError("%s must be a contiguous %s tensor [N][n] on %s" % (name, dt, device))
+    arr, count, address, dtype, ld, (n, vocab), _, device = _logit_rows(tables, logits, states)
+    shape = _records_shape("ids_out", ids_out, n)
     rc = lib().cstr_top_logprobs(
-        arr, count, _rows_arg("row_table", row_table, n, device, torch.int32),
-        _rows_arg("states", states, n, device, torch.int32), address, dtype, ld, vocab, temperature,
-        ids_out.shape[1], ids_out.data_ptr(), logp_out.data_ptr(),
-        _rows_arg("lse_out", lse_out, n, device, torch.float32), n, _raw_stream(stream, device))
+        arr, count, _rows_arg("row_table", row_table, n, device, _I32),
+        _rows_arg("states", states, n, device, _I32), address, dtype, ld, vocab, temperature, shape[1],
+        _records_arg("ids_out", ids_out, shape, device, _I32), _records_arg("logp_out", logp_out, shape, device, _F32),
+        _rows_arg("lse_out", lse_out, n, device, _F32), n, _raw_stream(stream, device))
     if rc:
         _check(rc)
 
@@ -936,27 +952,24 @@ def cstr_distill_loss(tables, logits, states, teacher_ids, teacher_logp, loss_ou
     ``states`` / ``row_table`` int32 ``[N]``, ``loss_out`` / ``weight`` float32 ``[N]``.  ``tail``: one of
     ``CSTR_TAIL_DROP``, ``CSTR_TAIL_RENORM``, ``CSTR_TAIL_LUMP``.  ``tables`` None or empty (with ``states``
     None): unconstrained."""
-    import torch
-    arr, count, address, dtype, ld, n, vocab, device = _logit_rows(tables, logits, states)
+    arr, count, address, dtype, ld, (n, vocab), strides, device = _logit_rows(tables, logits, states)
     dp = None
     if dlogits is not None:
         if dlogits.dtype != logits.dtype:
             raise TypeError("dlogits must have the dtype of logits")
-        if dlogits.shape != logits.shape or dlogits.stride() != logits.stride() or dlogits.device != device:
+        if dlogits.stride() != strides or dlogits.shape != logits.shape or dlogits.device != device:
             raise ValueError("dlogits must have the layout of logits")
         dp = dlogits.data_ptr()
-    for name, t, dt in (("teacher_ids", teacher_ids, torch.int32), ("teacher_logp", teacher_logp, torch.float32)):
-        if t is None or t.dtype != dt or t.dim() != 2 or t.shape[0] != n or t.shape != teacher_ids.shape \
-                or not t.is_contiguous() or t.device != device:
-            raise ValueError("%s must be a contiguous %s tensor [N][k] on %s" % (name, dt, device))
     if loss_out is None:
         raise ValueError("loss_out is required")
+    shape = _records_shape("teacher_ids", teacher_ids, n)
     rc = lib().cstr_distill_loss(
-        arr, count, _rows_arg("row_table", row_table, n, device, torch.int32),
-        _rows_arg("states", states, n, device, torch.int32), address, dtype, ld, vocab, temperature,
-        teacher_ids.data_ptr(), teacher_logp.data_ptr(), teacher_ids.shape[1], tail,
-        _rows_arg("weight", weight, n, device, torch.float32),
-        _rows_arg("loss_out", loss_out, n, device, torch.float32), dp, n, _raw_stream(stream, device))
+        arr, count, _rows_arg("row_table", row_table, n, device, _I32),
+        _rows_arg("states", states, n, device, _I32), address, dtype, ld, vocab, temperature,
+        _records_arg("teacher_ids", teacher_ids, shape, device, _I32),
+        _records_arg("teacher_logp", teacher_logp, shape, device, _F32), shape[1], tail,
+        _rows_arg("weight", weight, n, device, _F32), _rows_arg("loss_out", loss_out, n, device, _F32), dp, n,
+        _raw_stream(stream, device))
     if rc:
         _check(rc)
 
