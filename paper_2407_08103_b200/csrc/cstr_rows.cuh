@@ -129,19 +129,24 @@ template <bool BF16> struct RowView {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    __device__ __forceinline__ uint4 edge(int v) const       // a vector that is partly (or not) inside
+    // A vector that is partly (or not) inside.  (A loop: it is rare, and its code is in many places.)
+    __device__ __forceinline__ uint4 edge(int v) const
     {
-        unsigned w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            w[i] = BF16 ? 0xff80ff80u : 0xff800000u;
-#pragma unroll
-            for (int h = 0; h < N / 4; ++h) {
-                const int tok = token(v) + i * (N / 4) + h;
-                if (tok >= 0 && tok < V && allowed(tok)) {
-                    const unsigned f = __float_as_uint(one(tok));
-                    w[i] = BF16 ? __byte_perm(w[i], f >> 16, h ? 0x5410 : 0x3254) : f;
-                }
+        unsigned w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+        for (int e = N - 1; e >= 0; --e) {               // into the highest place, moved down by those before it
+            const int tok = token(v) + e;
+            const unsigned f = __float_as_uint(tok >= 0 && tok < V && allowed(tok) ? one(tok) : -CUDART_INF_F);
+            if (BF16) {
+                w[3] = w[3] << 16 | w[2] >> 16;
+                w[2] = w[2] << 16 | w[1] >> 16;
+                w[1] = w[1] << 16 | w[0] >> 16;
+                w[0] = w[0] << 16 | f >> 16;
+            } else {
+                w[3] = w[2];
+                w[2] = w[1];
+                w[1] = w[0];
+                w[0] = f;
             }
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
@@ -155,6 +160,12 @@ template <bool BF16> struct RowView {
     {
         const unsigned w[4] = {u.x, u.y, u.z, u.w};
         return BF16 ? __uint_as_float(e & 1 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16) : __uint_as_float(w[e % 4]);
+    }
+    static __device__ __forceinline__ float at(uint4 u, int e)       // ... e known only when it runs
+    {
+        const int i = BF16 ? e >> 1 : e;
+        const unsigned w = i & 2 ? (i & 1 ? u.w : u.z) : (i & 1 ? u.y : u.x);
+        return __uint_as_float(!BF16 ? w : e & 1 ? w & 0xffff0000u : w << 16);
     }
     static __device__ __forceinline__ float value(uint4 u, int e) { return fmaxf(plain(u, e), -CUDART_INF_F); }
 };

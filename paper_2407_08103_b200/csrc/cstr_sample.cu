@@ -324,19 +324,29 @@ template <bool BF16> struct Row {
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncthreads();
     }
-    // f(logit, token) for every allowed logit above -infinity of this CTA's chunks, close(chunk) behind each
+    // f(raw vector, token of its first logit) for every vector of this CTA's chunks, close(chunk) behind each chunk.
+    // One vector's code, run kU times: a pass that a row takes once costs what its code takes to come.
+    template <class F, class C> __device__ __forceinline__ void each_vector(void *ring, F f, C close)
+    {
+        stream<1>(ring, [&](uint4 (&raw)[kU], int first) {
+#pragma unroll 1
+            for (int u = 0; u < kU; ++u) {
+                f(raw[0], view.token(first + u * 32 + lane));
+#pragma unroll
+                for (int i = 1; i < kU; ++i)
+                    raw[i - 1] = raw[i];
+            }
+        }, close);
+    }
+    // f(logit, token) for every allowed logit above -infinity
     template <class F, class C> __device__ __forceinline__ void each(void *ring, F f, C close)
     {
-        stream<1>(ring, [&](const uint4 (&raw)[kU], int first) {
+        each_vector(ring, [&](const uint4 &raw, int tok) {
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int tok = view.token(first + u * 32 + lane);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float x = View::plain(raw[u], e);
-                    if (x > -CUDART_INF_F)               // (and no NaN)
-                        f(x, tok + e);
-                }
+            for (int e = 0; e < N; ++e) {
+                const float x = View::plain(raw, e);
+                if (x > -CUDART_INF_F)                   // (and no NaN)
+                    f(x, tok + e);
             }
         }, close);
     }
@@ -350,7 +360,7 @@ template <bool BF16> struct Row {
         float top = -CUDART_INF_F;
         float2 s32 = {0.f, 0.f};
         double s64 = 0.0;
-        auto use = [&](const uint4 (&raw)[kU], int) {
+        auto use = [&](uint4 (&raw)[kU], int) {
             float t = -CUDART_INF_F;
 #pragma unroll
             for (int u = 0; u < kU; ++u)
@@ -684,34 +694,28 @@ template <bool BF16> struct Row {
     // the list of the cluster's first CTA, `found` of them.  (count is 0, and the barrier behind that has been passed.)
     __device__ __forceinline__ u64 split(unsigned o1, unsigned o2, int *count, int &found)
     {
-        u64 *to = cluster.map_shared_rank(list, 0);
-        int *n = cluster.map_shared_rank(count, 0);
         bool full = false;
         const float high = logit_of(o1), low = logit_of(min(o2, order_of(-FLT_MAX)));
         // (what is not above adds 2^-1000, where floats are fine enough to say so)
         const float reach = (float)(1000.0 / c), least = m - reach;
         const bool fine = reach < 1e37f && fabsf(m) < reach * 1e6f;
         double s = 0.0;
-        stream<1>(bins, [&](const uint4 (&raw)[kU], int first) {
+        each_vector(bins, [&](const uint4 &raw, int tok) {
+            unsigned near = 0;                           // logits around the border
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int tok = view.token(first + u * 32 + lane);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float x = View::plain(raw[u], e);
-                    const double d = (double)(x > high ? x : least) - (double)m;
-                    if (fine) {
-                        const double2 f = exp2_factors(d, c16, table);
-                        s = fma(f.x, f.y, s);
-                    } else if (x > high)
-                        s += x == m ? 1.0 : power(d);
-                    if (x <= high && x >= low && !full) {
-                        const int at = atomicAdd(n, 1);
-                        full = at >= kList;
-                        if (!full)
-                            to[at] = ((u64)order_of(x) << 32) | (unsigned)(tok + e);
-                    }
-                }
+            for (int e = 0; e < N; ++e) {
+                const float x = View::plain(raw, e);
+                const double d = (double)(x > high ? x : least) - (double)m;
+                if (fine) {
+                    const double2 f = exp2_factors(d, c16, table);
+                    s = fma(f.x, f.y, s);
+                } else if (x > high)
+                    s += x == m ? 1.0 : power(d);
+                near |= x <= high && x >= low ? 1u << e : 0u;
+            }
+            for (; near; near &= near - 1) {
+                const int e = __ffs((int)near) - 1;
+                collect(View::at(raw, e), tok + e, count, full);
             }
         }, [&](int ch) {
             s = warp_sum(s);
@@ -719,9 +723,8 @@ template <bool BF16> struct Row {
                 chunk_mass[ch - c0] = (u64)__double2ll_rn(s * unit);
             s = 0.0;
         });
-        const u64 above = share_masses();
-        found = *n;
-        return above;
+        found = collected(count);
+        return share_masses();
     }
     // Running sums of the weights of the list's first n entries, kThreads of them at a time, into the work space.
     __device__ __forceinline__ void running_sums(int n)
@@ -824,8 +827,35 @@ template <bool BF16> struct Row {
         reached = b != ~0ull;
         return reached ? (int)b : kBins - 1;
     }
-    // Logits of the row in bins up to `last`, as (order, token), into the list of the cluster's first CTA;
-    // returns how many there are (more than kList: the list is not whole).
+    // Entries of the row's list, the first CTA's: each CTA collects its own, whose number is in count[0], and the
+    // others' go there in one piece.  (A remote counter answers in a microsecond.)
+    __device__ __forceinline__ void collect(float x, int tok, int *count, bool &full)
+    {
+        const int at = full ? kList : atomicAdd(count, 1);
+        full = at >= kList;
+        if (!full)
+            list[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
+    }
+    // Returns how many there are (more than kList: the list is not whole); the counters are behind a barrier.
+    __device__ __forceinline__ int collected(int *count)
+    {
+        __syncthreads();
+        int *all = cluster.map_shared_rank(count, 0);
+        if (part != 0 && *count > 0) {
+            const int n = min(*count, kList);
+            if (tid == 0)
+                scratch[0] = (u64)atomicAdd(all, *count);
+            __syncthreads();
+            const long long at = (long long)scratch[0];
+            u64 *to = cluster.map_shared_rank(list, 0);
+            for (int i = tid; i < n; i += kThreads)
+                if (at + i < kList)
+                    to[at + i] = list[i];
+        }
+        barrier();
+        return *all;
+    }
+    // Logits of the row in bins up to `last`, as (order, token), into the list; returns how many there are.
     __device__ __forceinline__ int gather(int last, int *count, int *hits)
     {
         // the lanes to look at, then all threads share their vectors
@@ -834,8 +864,6 @@ template <bool BF16> struct Row {
             if (lane_max[i] > -CUDART_INF_F && bin_of(lane_max[i]) <= last)
                 lanes[atomicAdd(hits, 1)] = (unsigned short)i;
         __syncthreads();
-        u64 *to = cluster.map_shared_rank(list, 0);
-        int *n = cluster.map_shared_rank(count, 0);
         bool full = false;
         const int each = blocks * kU, units = *hits * each;
 #pragma unroll 2
@@ -843,19 +871,18 @@ template <bool BF16> struct Row {
             const int h = q / each, i = lanes[h];
             const int v = ((c0 + (i >> 5)) * each + (q - h * each)) * 32 + (i & 31);
             const uint4 raw = view.masked(v);
+            unsigned near = 0;
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float x = View::value(raw, e);
-                if (!full && x > -CUDART_INF_F && bin_of(x) <= last) {
-                    const int at = atomicAdd(n, 1);
-                    full = at >= kList;
-                    if (!full)
-                        to[at] = ((u64)order_of(x) << 32) | (unsigned)(view.token(v) + e);
-                }
+                near |= x > -CUDART_INF_F && bin_of(x) <= last ? 1u << e : 0u;
+            }
+            for (; near; near &= near - 1) {
+                const int e = __ffs((int)near) - 1;
+                collect(View::at(raw, e), view.token(v) + e, count, full);
             }
         }
-        barrier();
-        return *n;
+        return collected(count);
     }
     // The largest of the CTAs' (warp 0's) tokens, for all
     __device__ __forceinline__ int everybody(int tok)
@@ -1123,18 +1150,12 @@ sample_kernel(const __grid_constant__ SampleParams p)
                 if (tid == 0)
                     s_count = 0;
                 r.barrier();
-                // every CTA's kept tokens into the list of the first one
-                u64 *list = cluster.map_shared_rank(r.list, 0);
-                int *count = cluster.map_shared_rank(&s_count, 0);
+                bool full = false;
                 r.each(r.bins, [&](float x, int tok) {
-                    if (cut.keeps(x, tok)) {
-                        const int at = atomicAdd(count, 1);
-                        if (at < kList)
-                            list[at] = ((u64)order_of(x) << 32) | (unsigned)tok;
-                    }
+                    if (cut.keeps(x, tok))
+                        r.collect(x, tok, &s_count, full);
                 }, [](int) {});
-                r.barrier();
-                found = s_count;
+                found = r.collected(&s_count);
             }
         }
         if (part != 0) {
@@ -1270,11 +1291,16 @@ sample_kernel(const __grid_constant__ SampleParams p)
 
 namespace {
 
-// CTAs of a row of so many blocks, `uneven`: some rows may take several more passes than others.
+// CTAs of a row of so many blocks, `uneven`: some rows may take several more passes than others.  Three CTAs an SM,
+// in shares of at least 8 blocks, up to four where shares are of 128 (512 x 256,000, the 256 most likely: 144 us
+// with two CTAs a row, 169 with one, 160 with four; 128 x 128,256 bf16 from the whole distribution: 43 us with
+// four, 54 with eight); eight with uneven rows (300 x 128,256 with top_p alone: 207 us with four, 470 with one).
+// Sixteen only where all rows run at once (4 x 256,000 18.6 us, with eight 21.9).
 int cluster_size(int rows, int blocks, int sms, bool uneven)
 {
     int size = 1;
-    while (size < 8 && rows * (long long)size < (uneven ? 8 : 3) * sms && blocks >= 16 * size)
+    while (size < 8 && ((rows * (long long)size < (uneven ? 8 : 3) * sms && blocks >= 16 * size) ||
+                        (rows * (long long)size < 4 * sms && blocks >= 256 * size)))
         size *= 2;
     while (size < kMaxCluster && rows * (long long)kMaxCluster <= sms && blocks >= 16 * size)
         size *= 2;
