@@ -9,9 +9,13 @@
 // The sums over the record are taken in 64 bits (a divergence is a small difference of them), those over the
 // vocabulary in 32.
 //
-// Bound: logits read once, gradient written once; the second pass finds the row in the L2 cache, as in the
-// policy loss: a cluster of up to 16 CTAs shares a row.  A bitmap in shared memory marks the record's tokens of
-// a CTA's share; their gradients are written behind the others'.
+// Bound: logits read once, gradient written once.  A cluster of CTAs shares a row, sized so that there are about as
+// many CTAs as the SMs hold (eight of 32 registers each: 2,048 x 32,000 bf16 80 us, 3.3 TB/s, with six 89 us): the
+// phases of a row - its record, one pass, the join, the gradient - take as long as their latencies, and other rows
+// fill them.  512 x 256,000 fp32 with gradient 270 us, 3.9 TB/s of what has to move (5.8 TB/s of what does: the
+// gradient's pass finds half the row in the L2 cache), its loss alone 126 us.  A bitmap in shared memory marks the
+// record's tokens of a CTA's share; their gradients are written behind the others'.  Measured and dropped: the
+// record left to one warp (512 x 256,000 311 us against 290 then), the row brought to the L2 cache ahead (288).
 #include <cooperative_groups.h>
 #include <math.h>
 #include <string.h>
@@ -42,6 +46,7 @@ struct DistillParams {
     const float *teacher, *weight;
     float *loss;
     unsigned words;                  // of a CTA's bitmap
+    unsigned long long *oob;
 };
 
 struct MaxSum {
@@ -203,8 +208,8 @@ distill_kernel(const __grid_constant__ DistillParams p)
     if (tid == 0)
         s_twice = 0;
     int mine = 0;                                        // entries of this share
-    for (int i0 = 0; i0 < p.k; i0 += kThreads) {
-        const int i = i0 + tid, id = i < p.k ? ids[i] : -1;
+    for (int k0 = 0; k0 < p.k; k0 += kThreads) {
+        const int i = k0 + tid, id = i < p.k ? ids[i] : -1;
         const float g = i < p.k ? teacher[i] : 0.f;
         const bool in = id >= lo && id < hi && g != -CUDART_INF_F;
         const unsigned who = __ballot_sync(kFull, in);
@@ -221,7 +226,7 @@ distill_kernel(const __grid_constant__ DistillParams p)
             s_id[at] = id;
             s_t[at] = g;
             const unsigned bit = 1u << ((id - base) & 31);
-            if (atomicOr(bitmap + ((id - base) >> 5), bit) & bit)
+            if (CSTR_INB(p.oob, (id - base) >> 5, p.words, CSTR_SITE_DISTILL) && (atomicOr(bitmap + ((id - base) >> 5), bit) & bit))
                 s_twice = 1;
         }
         __syncthreads();
@@ -485,7 +490,7 @@ distill_kernel(const __grid_constant__ DistillParams p)
     const float f_listed = s_result[1], f_t = s_result[2], ref = s_result[3];
     const double t_ref = s_ref;                  // 0 unless the record is renormalised
     for (int i = tid; i < mine; i += kThreads) {
-        if (!first(i))
+        if (!first(i) || !CSTR_INB(p.oob, s_id[i], p.V, CSTR_SITE_DISTILL))
             continue;
         float d = 0.f;
         if (s_x[i] != -CUDART_INF_F) {
@@ -562,6 +567,7 @@ extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_ta
     p.teacher = teacher_logp;
     p.weight = weight;
     p.loss = loss_out;
+    p.oob = CSTR_OOB_RECORD();
     static std::atomic<int> known[64];
     int sms = device >= 0 && device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
     if (sms == 0) {

@@ -48,6 +48,8 @@ int cstr_check_device(int handle_device, const char *what);
 #define CSTR_SITE_PDA 15            // push-down kernels
 #define CSTR_SITE_CACHE 16          // key / value cache: insertion, attention weights
 #define CSTR_SITE_LOSS 17           // policy loss
+#define CSTR_SITE_SAMPLE 18         // sampling
+#define CSTR_SITE_DISTILL 19        // distillation: the record's tokens
 #ifdef CSTR_BOUNDS_CHECK
 // Device address of the current device's record (allocated on first use), or null.
 unsigned long long *cstr_oob_record();

@@ -9,9 +9,16 @@
 // decide are taken in 64 bits and added as whole numbers of 2^-s (s = 62 - log2 V), whose sums are exact
 // whatever their order - atomics included - so a row's token does not depend on the launch.
 //
-// A cluster of up to 16 CTAs shares a row.  The row's maximum and sum come from one pass over memory; what
-// follows reads the row from the L2 cache: the pair (x, i) by counts or masses of three digits of the logit's
-// ordered bits, the token by sums of chunks of 128 vectors.
+// A cluster of up to 16 CTAs shares a row.  One pass over memory (the bound: 512 x 256,000 fp32 84 of 118 us, 5.2 of
+// 6.55 TB/s in it) leaves the maximum of every lane's logits, and maxima and sums of chunks.  The k-th largest of the
+// lanes' maxima is a lower bound of the k-th largest logit, and the mass that they hold one of the row's: so a
+// histogram of them tells which few lanes hold every token that can be kept, and only those are looked at again.
+// The candidates meet in a list of the first CTA, where they are compared with each other.  Where too many tokens
+// can be kept (a nucleus of thousands, many equal logits) the row is read again from the L2 cache: two histograms
+// by weights in 32 bits bring the border down to some hundred tokens, one pass counts what lies above them and puts
+// them into the list (300 x 128,256 with top_p 0.95, a quarter of the rows that wide, 207 us; by three exact
+// histograms with 64-bit counters 998 us).  Without any cut the weights of all tokens are needed in 64 bits in the
+// first pass; that is bound by the double precision pipe (512 x 256,000 150 us of it).
 #include <cooperative_groups.h>
 #include <float.h>
 #include <math.h>
@@ -184,9 +191,10 @@ template <bool BF16> struct Row {
     double unit;                          // 2^s
     u64 *list, *bins, *chunk_mass;        // (bins: the work space)
     float *chunk_max, *lane_max;          // per chunk; per chunk and lane
-    unsigned *mask_words;                 // of the first pass, as its ring in list and bins
+    unsigned *mask_words;                 // of the blocks under way
     Word *word;                           // two, in turn
     u64 *scratch;                         // kWarps + 4
+    u64 *oob;                             // checking build: bounds record
     int phase;
     u64 before, mine;                     // mass of the lower parts, of this one (after a mass pass)
 
@@ -399,11 +407,10 @@ template <bool BF16> struct Row {
 #pragma unroll
                     for (int u = 0; u < kU; ++u)
 #pragma unroll
-                        for (int e = 0; e < N; ++e)
-                            {
-                                const double2 f = exp2_factors((double)fmaxf(View::plain(raw[u], e), least) - (double)top, k16, table);
-                                s64 = fma(f.x, f.y, s64);
-                            }
+                        for (int e = 0; e < N; ++e) {
+                            const double2 f = exp2_factors((double)fmaxf(View::plain(raw[u], e), least) - (double)top, k16, table);
+                            s64 = fma(f.x, f.y, s64);
+                        }
                 }
             }
         };
@@ -482,7 +489,8 @@ template <bool BF16> struct Row {
             if (ch + 32 >= c1)
                 break;
         }
-        int last = -1;                                   // last token with any weight
+        int last = -1, first = kNone;                    // last token with any weight, first with the largest logit
+        float top = -CUDART_INF_F;
         for (int v = ch * blocks * kU * 32 + lane; v < (ch + 1) * blocks * kU * 32; v += 32) {
             const uint4 raw = view.masked(v);
             u64 s = 0;
@@ -492,6 +500,10 @@ template <bool BF16> struct Row {
                 const u64 w = x > -CUDART_INF_F ? f(x, view.token(v) + e) : 0;
                 s += w;
                 last = w ? view.token(v) + e : last;
+                if (x > top) {
+                    top = x;
+                    first = view.token(v) + e;
+                }
             }
             const u64 upto = base + inclusive_scan(s, lane);
             const unsigned over = __ballot_sync(kFull, upto > t);
@@ -509,11 +521,12 @@ template <bool BF16> struct Row {
             }
             base = __shfl_sync(kFull, upto, 31);
         }
-        // the chunk's mass and its tokens' differ by rounding (masses taken from the first pass)
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1)
-            last = max(last, __shfl_xor_sync(kFull, last, off));
-        return last;
+        // The chunk's mass and its tokens' differ by rounding where the former is a sum of unrounded weights: the last
+        // token, or where all weights round to nothing the chunk's first in the row's order, which is kept if any is.
+        last = __reduce_max_sync(kFull, last);
+        const float most = warp_max(top);
+        first = __reduce_min_sync(kFull, top == most ? first : kNone);
+        return last >= 0 ? last : first;
     }
     // Distance from the maximum as one of kBins numbers, ascending: 32 to an octave from 2^-6 on.
     static constexpr int kFirstBin = ((127 - 6) << 5) - 1;
@@ -782,7 +795,8 @@ template <bool BF16> struct Row {
                 w = {0.0, above + bins[n - 1], logit_of((unsigned)(list[n - 1] >> 32)), (int)(unsigned)list[n - 1]};
                 for (int i = tid; i < n; i += kThreads) {
                     const int ch = ((int)(unsigned)list[i] + view.head) / N / (32 * kU) / blocks, owner = ch / per;
-                    atomicAdd(cluster.map_shared_rank(chunk_mass + ch - owner * per, owner), bins[i] - (i ? bins[i - 1] : 0));
+                    if (CSTR_INB(oob, owner, size, CSTR_SITE_SAMPLE))
+                        atomicAdd(cluster.map_shared_rank(chunk_mass + ch - owner * per, owner), bins[i] - (i ? bins[i - 1] : 0));
                 }
             }
         }
@@ -1033,7 +1047,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     // token and state of a row, by one thread
     auto finish = [&](int token, float logp, float kept) {
         int next = CSTR_DEAD;
-        if (token >= 0 && p.t.n > 0)
+        if (token >= 0 && p.t.n > 0 && CSTR_INB(p.oob, token, p.V, CSTR_SITE_SAMPLE))
             next = next_state(p.t.tab[table], inner, token);
         p.tokens[row] = token;
         if (p.states_out)
@@ -1078,6 +1092,7 @@ sample_kernel(const __grid_constant__ SampleParams p)
     r.mask_words = s_mask;
     r.word = s_word;
     r.scratch = s_scratch;
+    r.oob = p.oob;
     r.phase = 0;
     if (tid == 0)
         s_count = s_hits = 0;
