@@ -76,8 +76,15 @@ class ConstrainedDecoder:
             return value
         if value == off:
             return None
+        if value != value:
+            raise ValueError("%s is not a number" % name)
         at = (name, value)
         if at not in self._settings:              # a program has a few: filled once, read by every step
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("%s = %r: take one step with it before the capture" % (name, value))
+            if len(self._settings) >= 64:         # (an annealed setting: the steps under way still read the old ones)
+                torch.cuda.synchronize(self.device)
+                self._settings.clear()
             self._settings[at] = torch.full((self.batch,), value, dtype=dtype, device=self.device)
             torch.cuda.synchronize(self.device)   # ... on whatever stream
         return self._settings[at]
