@@ -13,7 +13,9 @@
  *      with -infinity, select a token, advance the state - for a whole batch;
  *   3. what a batch of constrained rows needs of the model around that step:
  *      attention over a prompt that all rows share and each row's own cache, the
- *      cache's upkeep, and the policy loss over the constrained distribution.
+ *      cache's upkeep, and the policy loss over the constrained distribution;
+ *   4. whole constrained distributions: drawing from them under temperature, top-k,
+ *      top-p and min-p, their most likely tokens, and learning from such records.
  *
  * Conventions
  *   - Every function returns 0 (CSTR_OK) or a negative CSTR_ERR_* code and
@@ -651,9 +653,10 @@ int cstr_cache_status(cstr_cache_t *cache, void *cuda_stream, int64_t *gave_up);
  *   token  = the first kept token by id for which the sum of p over the kept tokens up to it exceeds
  *            uniform * the sum of p over all kept tokens
  *   state  = next[state][token]
- * The weights that decide are taken and added in 64 bits.  temperature 0: the first token of the order
- * (as cstr_step without noise), logp 0, kept 1.  Infinite logits share the probability equally.  Where A is
- * empty, an allowed -infinity still beats none: the lowest such id, logp -infinity, kept 0.
+ * The weights that decide are taken and added in 64 bits, logp and kept may come from sums in 32.
+ * temperature 0: the first token of the order (as cstr_step without noise), logp 0, kept 1.  Infinite logits
+ * share the probability equally.  Where A is empty, an allowed -infinity still beats none: the lowest such id,
+ * logp -infinity, kept 0.
  *   tables, n_tables, row_table   as in cstr_step; n_tables 0 .. CSTR_MAX_TABLES
  *   states_in, states_out  DEVICE int32 [rows], may be the same array; NULL when n_tables is 0
  *   logits      DEVICE [rows][ld] of dtype CSTR_F32 or CSTR_BF16, on whole elements;  ld >= vocab_size

@@ -20,8 +20,6 @@
 #include <math.h>
 #include <string.h>
 
-#include <atomic>
-
 #include "cstr_rows.cuh"
 
 namespace cg = cooperative_groups;
@@ -508,15 +506,6 @@ distill_kernel(const __grid_constant__ DistillParams p)
         asm volatile("barrier.cluster.wait;" ::: "memory");
 }
 
-int launch(void (*kernel)(DistillParams), const DistillParams &p, int size, int smem, cudaStream_t stream)
-{
-    if (size > 8)
-        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    if (smem > 40 * 1024)
-        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    return cstr_launch(kernel, (long long)p.rows * size, kThreads, size, smem, stream, p);
-}
-
 }  // namespace
 
 extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
@@ -568,18 +557,16 @@ extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_ta
     p.weight = weight;
     p.loss = loss_out;
     p.oob = CSTR_OOB_RECORD();
-    static std::atomic<int> known[64];
-    int sms = device >= 0 && device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
-    if (sms == 0) {
-        CSTR_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-        if (device >= 0 && device < 64)
-            known[device].store(sms, std::memory_order_relaxed);
-    }
+    int sms = 0;
+    if (const int rc = cstr_rows::sm_count(device, sms))
+        return rc;
     // As many CTAs as the SMs hold, three quarters of that with a gradient, while shares have 4,096 tokens or more.
     // (512 x 256,000 fp32 with gradient: 273 us with two CTAs a row, 290 with 16, whose shares would still be in the
     // L2 cache when the gradient is written, 420 with one; without one 126 us with four, 156 with two.)
+    // Bitmaps of at most 32 KB (with 16 CTAs 64 KB).
     int size = 1;
-    while (size < kMaxCluster && rows * (long long)size < (dlogits ? 6 : 8) * sms && vocab_size >= 8192LL * size)
+    while (size < kMaxCluster && (vocab_size > 262144LL * size ||
+                                  (rows * (long long)size < (dlogits ? 6 : 8) * sms && vocab_size >= 8192LL * size)))
         size *= 2;
     if ((long long)rows * size > 0x7fffffffLL)
         return cstr_fail(CSTR_ERR_SHAPE, "cstr_distill_loss: rows x vocabulary too large for one launch");
@@ -589,11 +576,15 @@ extern "C" int cstr_distill_loss(const cstr_table_t *const *tables, int32_t n_ta
     const int smem = (int)p.words * 4 + k * 12;
     const bool together = !dlogits || (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15u) == 0;
     void (*kernel)(DistillParams);
+    const int kind = (!together ? 0 : dlogits ? 2 : 4) + bf16;
     if (!together)
         kernel = bf16 ? distill_kernel<true, false, 1> : distill_kernel<false, false, 1>;
     else if (dlogits)
         kernel = bf16 ? distill_kernel<true, true, 1> : distill_kernel<false, true, 1>;
     else
         kernel = bf16 ? distill_kernel<true, true, 2> : distill_kernel<false, true, 2>;
-    return launch(kernel, p, size, smem, (cudaStream_t)cuda_stream);
+    static cstr_rows::LaunchLimits<6> limits;
+    if (const int rc = limits.set(kernel, kind, device, kMaxCluster, (CSTR_MAX_ROW / kMaxCluster / 32 + 2) * 4 + CSTR_MAX_TOP * 12))
+        return rc;
+    return cstr_launch(kernel, (long long)rows * size, kThreads, size, smem, (cudaStream_t)cuda_stream, p);
 }

@@ -5,6 +5,8 @@
 
 #include <math_constants.h>
 
+#include <atomic>
+
 #include "cstr_internal.cuh"
 
 namespace cstr_rows {
@@ -57,6 +59,37 @@ inline int take_tables(const char *name, const cstr_table_t *const *tables, int3
         d.wide = t->wide;
         d.code_shift = t->code_shift;
     }
+    return CSTR_OK;
+}
+
+// Limits of a kernel that its launches may need, set once per device, always to the same values: calls from several
+// threads may not undo each other's.
+template <int kKinds> struct LaunchLimits {
+    std::atomic<bool> done[64][kKinds];
+    template <class K> int set(K kernel, int kind, int device, int cluster, int smem)
+    {
+        if (device >= 0 && device < 64 && done[device][kind].load(std::memory_order_acquire))
+            return CSTR_OK;
+        if (cluster > 8)
+            CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        if (smem > 48 * 1024)
+            CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        if (device >= 0 && device < 64)
+            done[device][kind].store(true, std::memory_order_release);
+        return CSTR_OK;
+    }
+};
+
+// SMs of a device, asked for once.
+inline int sm_count(int device, int &sms)
+{
+    static std::atomic<int> known[64];
+    sms = device >= 0 && device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+    if (sms > 0)
+        return CSTR_OK;
+    CSTR_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    if (device >= 0 && device < 64)
+        known[device].store(sms, std::memory_order_relaxed);
     return CSTR_OK;
 }
 

@@ -24,8 +24,6 @@
 #include <math.h>
 #include <string.h>
 
-#include <atomic>
-
 #include "cstr_rows.cuh"
 
 namespace cg = cooperative_groups;
@@ -1334,13 +1332,9 @@ int run(const char *name, const cstr_table_t *const *tables, int32_t n_tables, c
     CSTR_CUDA_TRY(cudaGetDevice(&device));
     if (const int rc = cstr_rows::take_tables(name, tables, n_tables, row_table, states, vocab_size, device, p.t))
         return rc;
-    static std::atomic<int> known[64];
-    int sms = device >= 0 && device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
-    if (sms == 0) {
-        CSTR_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-        if (device >= 0 && device < 64)
-            known[device].store(sms, std::memory_order_relaxed);
-    }
+    int sms = 0;
+    if (const int rc = cstr_rows::sm_count(device, sms))
+        return rc;
     p.logits = logits;
     p.ld = ld;
     p.V = vocab_size;
@@ -1358,13 +1352,12 @@ int run(const char *name, const cstr_table_t *const *tables, int32_t n_tables, c
     p.scale_bits = 62;
     while ((1LL << (62 - p.scale_bits)) < vocab_size)
         --p.scale_bits;
-    const int smem = (2 * kList + p.per) * 8 + p.per * 33 * 4;
+    auto bytes = [](int chunks) { return (2 * kList + chunks) * 8 + chunks * 33 * 4; };
     void (*kernel)(SampleParams) = bf16 ? sample_kernel<true, TOP> : sample_kernel<false, TOP>;
-    if (size > 8)
-        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    if (smem > 48 * 1024)
-        CSTR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    return cstr_launch(kernel, (long long)rows * size, kThreads, size, smem, stream, p);
+    static cstr_rows::LaunchLimits<2> limits;
+    if (const int rc = limits.set(kernel, bf16, device, kMaxCluster, bytes(kMaxChunks)))
+        return rc;
+    return cstr_launch(kernel, (long long)rows * size, kThreads, size, bytes(p.per), stream, p);
 }
 
 int check_rows(const char *name, int32_t n_tables, int32_t dtype, int64_t ld, int32_t vocab_size, int32_t rows)

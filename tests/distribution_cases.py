@@ -150,9 +150,9 @@ def check_distill(x, ids, teacher, tail, allowed=None, weight=None, tables=None,
     tau = float(np.float32(temperature))
     want = ref.distill(host, allowed, ids, given, tail, w, tau)
     # log q: arguments rounded three times (their mean is at most log2 V), 2^-22 of an exponential, up to 128
-    # additions of a thread and 13 joins with two exponentials each; a lumped tail has two such sums
+    # additions of a thread (more where 16 CTAs of 256 have more than that in each of two sums) and 13 joins with two exponentials each; a lumped tail has two such sums
     with np.errstate(over="ignore", invalid="ignore", divide="ignore"):
-        e_log = 2.0 ** -24 * (2.1 * math.log2(V + 1) + 128 + 13 * 12)
+        e_log = 2.0 ** -24 * (2.1 * math.log2(V + 1) + max(128, V / 8192) + 13 * 12)
         lw = np.ones(N) if w is None else np.abs(w)
         t = np.where((ids >= 0) & (ids < V), np.exp(given), 0.0)
         size = lw if tail == ref.RENORM else lw * (t.sum(1) + (1.0 if tail == ref.LUMP else 0.0))

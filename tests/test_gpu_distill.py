@@ -241,3 +241,19 @@ def test_refusals_on_a_device():
             cstr.cstr_distill_loss(None, x, None, i, f, out, **kw)
         assert e.value.code == -2
     cstr.cstr_distill_loss(None, x[:0], None, i[:0], f[:0], out[:0])
+
+
+def test_longest_rows():
+    # bitmaps of many words; more rows than CTAs of one row each could keep such bitmaps for
+    rng = np.random.default_rng(16)
+    x = logits(16, 1, 2000003, BF, offset=1)
+    ids = np.stack([rng.choice(2000003, 700, replace=False)]).astype(np.int32)
+    logp = np.log(rng.dirichlet(np.ones(701), 1)[:, :700]).astype(np.float32)
+    check_distill(x, ids, logp, cstr.CSTR_TAIL_LUMP)
+    N, V = 900, 600011
+    x = torch.zeros(N, V, dtype=BF, device=DEV)
+    loss = torch.empty(N, device=DEV)
+    i = torch.randint(0, V, (N, 1), dtype=torch.int32, device=DEV)
+    cstr.cstr_distill_loss(None, x, None, i, torch.zeros(N, 1, device=DEV), loss, tail=cstr.CSTR_TAIL_LUMP)
+    # log V, from sums of 600,011 ones in 32 bits: exact but for the joins (16 of them) and the logarithm's rounding
+    assert (loss - math.log(V)).abs().max() <= 2.0 ** -24 * (16 * 12 + 14)

@@ -288,3 +288,54 @@ def test_wide_nuclei_with_many_equal_logits(dtype, step):
                  temperature=np.array([1.0, 0.5, 2.0, 30.0, 0.9], np.float32))
     check_sample(x, u, top_p=np.full(N, 0.97, np.float32), min_p=np.array([1e-4, 1e-6, 1e-3, 3e-3, 0.0], np.float32),
                  temperature=np.array([1.0, 2.0, 1.5, 1.0, 50.0], np.float32))
+
+
+def test_longest_rows():
+    # shares of many blocks, counts and masses over millions of tokens; a row that begins inside a vector
+    rng = np.random.default_rng(15)
+    x = logits(15, 2, 2000003, BF, offset=3)
+    u = rng.random(2).astype(np.float32)
+    check_sample(x, u)
+    check_sample(x, u, top_p=np.array([0.4, 0.9], np.float32), top_k=np.array([0, 100], np.int32))
+    top = torch.empty(2, 40, dtype=torch.int32, device=DEV), torch.empty(2, 40, device=DEV)
+    cstr.cstr_top_logprobs(None, x, None, *top)
+    assert torch.equal(top[0][:, 0].long(), x.float().argmax(1))
+    longest = torch.zeros(1, 8388608, device=DEV)
+    longest[0, 8388607] = 3.0
+    for uniform, want in ((0.0, 0), (0.5, 4194313), (1.0, 8388607)):
+        token = torch.empty(1, dtype=torch.int32, device=DEV)
+        cstr.cstr_sample(None, longest, None, token, torch.tensor([uniform], device=DEV))
+        # half of V - 1 + e^3 lies 9.04 tokens behind the middle
+        assert token.item() == want
+
+
+def test_two_threads_call_at_once():
+    # rows of different lengths need different amounts of shared memory and clusters
+    import threading
+    cases = [(logits(i, 8, V, F32), torch.rand(8, device=DEV)) for i, V in enumerate((700, 300007, 40001, 128256))]
+    want = []
+    for x, u in cases:
+        out = torch.empty(8, dtype=torch.int32, device=DEV)
+        cstr.cstr_sample(None, x, None, out, u, top_p=torch.full((8,), 0.9, device=DEV))
+        want.append(out)
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(k):
+        stream = torch.cuda.Stream()
+        p = torch.full((8,), 0.9, device=DEV)
+        torch.cuda.synchronize()
+        for i in range(40):
+            x, u = cases[(i + k) % 4]
+            out = torch.empty(8, dtype=torch.int32, device=DEV)
+            stream.wait_stream(torch.cuda.current_stream())
+            cstr.cstr_sample(None, x, None, out, u, top_p=p, stream=stream)
+            stream.synchronize()
+            if not torch.equal(out, want[(i + k) % 4]):
+                bad.append((k, i))
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
