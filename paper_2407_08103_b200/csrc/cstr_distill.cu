@@ -15,7 +15,7 @@
 // fill them.  512 x 256,000 fp32 with gradient 270 us, 3.9 TB/s of what has to move (5.8 TB/s of what does: the
 // gradient's pass finds half the row in the L2 cache), its loss alone 126 us.  A bitmap in shared memory marks the
 // record's tokens of a CTA's share; their gradients are written behind the others'.  Measured and dropped: the
-// record left to one warp (512 x 256,000 311 us against 290 then), the row brought to the L2 cache ahead (288).
+// record left to one warp (512 x 256,000 311 us against 290 then), the row brought to the L2 cache ahead (288), the gradient's pass backwards (279 against 272).
 #include <cooperative_groups.h>
 #include <math.h>
 #include <string.h>
@@ -239,7 +239,10 @@ distill_kernel(const __grid_constant__ DistillParams p)
         const int bit = (v - v0) * N;
         return lump ? ~(bitmap[bit >> 5] >> (bit & 31)) : kFull;
     };
+    // A likely token's sum swallows the last bits of hundreds of unlikely ones, all to the same side: what was added
+    // too much is kept along (log q of 512 x 256,000: root mean square error 1.0e-6 without).
     MaxSum rest = {-CUDART_INF_F, 0.f};
+    float over = 0.f;
     auto add = [&](uint4 raw) {
         float x[N], top = -CUDART_INF_F;
 #pragma unroll
@@ -249,15 +252,19 @@ distill_kernel(const __grid_constant__ DistillParams p)
         for (int e = 0; e < N; e += 2)
             top = max3(top, x[e], x[e + 1]);
         if (top > rest.m) {
-            rest.s *= exp2_fast((rest.m - top) * p.c);
+            const float f = exp2_fast((rest.m - top) * p.c);
+            rest.s *= f;
+            over *= f;
             rest.m = top;
         }
         exponentials(x, rest.m == -CUDART_INF_F ? 0.f : rest.m, p.c);
-        float s[2] = {rest.s, 0.f};
+        float s[2] = {x[0], x[1]};
 #pragma unroll
-        for (int e = 0; e < N; ++e)
+        for (int e = 2; e < N; ++e)
             s[e & 1] += x[e];
-        rest.s = s[0] + s[1];
+        const float y = s[0] + s[1] - over, sum = rest.s + y;
+        over = sum - rest.s - y;
+        rest.s = sum;
     };
 #pragma unroll 1
     for (int v = i0 + tid; v < i1; v += kUnroll * kThreads) {
@@ -278,6 +285,7 @@ distill_kernel(const __grid_constant__ DistillParams p)
     }
     if (edge >= 0)
         add(View::mask(view.edge(edge), others(edge)));
+    rest.s -= over;
 
     // the record's part: largest teacher value and logit, then the sums relative to them (by the warps that
     // have entries)
