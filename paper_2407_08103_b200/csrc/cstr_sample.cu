@@ -9,7 +9,7 @@
 // decide are taken in 64 bits and added as whole numbers of 2^-s (s = 62 - log2 V), whose sums are exact
 // whatever their order - atomics included - so a row's token does not depend on the launch.
 //
-// A cluster of up to 16 CTAs shares a row.  One pass over memory (the bound: 512 x 256,000 fp32 84 of 118 us, 5.2 of
+// A cluster of up to 16 CTAs shares a row.  One pass over memory (the bound: 512 x 256,000 fp32 84 of 116 us, 6.2 of
 // 6.55 TB/s in it) leaves the maximum of every lane's logits, and maxima and sums of chunks.  The k-th largest of the
 // lanes' maxima is a lower bound of the k-th largest logit, and the mass that they hold one of the row's: so a
 // histogram of them tells which few lanes hold every token that can be kept, and only those are looked at again.
@@ -265,9 +265,10 @@ template <bool BF16> struct Row {
             if (view.mrow) {
                 const int w0 = view.token(first) >> 5, last = (view.V - 1) >> 5;
                 const unsigned to_w = (unsigned)__cvta_generic_to_shared(words);
-                for (int i = lane; i < kMaskWords; i += 32)
-                    if (w0 + i <= last)
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to_w + i * 4), "l"(view.mrow + w0 + i) : "memory");
+                if (lane < kMaskWords && w0 + lane <= last)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to_w + lane * 4), "l"(view.mrow + w0 + lane) : "memory");
+                if (kMaskWords > 32 && view.head != 0 && lane == 0 && w0 + 32 <= last)      // (bf16: the 33rd word)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to_w + 128), "l"(view.mrow + w0 + 32) : "memory");
             }
         }
     }
@@ -278,12 +279,17 @@ template <bool BF16> struct Row {
 #pragma unroll
             for (int u = 0; u < kU; ++u)
                 raw[u] = from[u * 32];
-            if (view.mrow) {
+            if (view.mrow && view.head == 0) {
+                const unsigned *w = words + (lane * N >> 5);
+#pragma unroll
+                for (int u = 0; u < kU; ++u)
+                    raw[u] = View::mask(raw[u], w[u * N] >> (lane * N & 31));
+            } else if (view.mrow) {
                 const int at = (view.token(first) & 31) + lane * N;
                 const unsigned *w = words + (at >> 5);
 #pragma unroll
                 for (int u = 0; u < kU; ++u)
-                    raw[u] = View::mask(raw[u], view.head == 0 ? w[u * N] >> (at & 31) : __funnelshift_r(w[u * N], w[u * N + 1], at & 31));
+                    raw[u] = View::mask(raw[u], __funnelshift_r(w[u * N], w[u * N + 1], at & 31));
             }
         } else {
 #pragma unroll
@@ -416,11 +422,17 @@ template <bool BF16> struct Row {
             lane_max[(ch - c0) * 32 + lane] = top;
             const float most = warp_max(top);
             double sum = 0.0;
-            if (WHAT == kSum32)
-                sum = (s32.x + s32.y) * exp2_fast(top == most ? 0.f : (top - most) * c32);
+            if (WHAT == kSum32) {
+                float s = (s32.x + s32.y) * exp2_fast(top == most ? 0.f : (top - most) * c32);
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1)
+                    s += __shfl_xor_sync(kFull, s, off);
+                sum = s;
+            }
             if (WHAT == kSum64 && top > -CUDART_INF_F)
                 sum = s64 * power((double)top - (double)most);
-            if (most == CUDART_INF_F || __any_sync(kFull, sum != sum)) {
+            const bool again = most == CUDART_INF_F || __any_sync(kFull, sum != sum);
+            if (again) {
                 // NaN adds nothing, infinite logits share the sum
                 sum = 0.0;
                 for (int v = ch * blocks * kU * 32 + lane; v < (ch + 1) * blocks * kU * 32; v += 32) {
@@ -431,7 +443,8 @@ template <bool BF16> struct Row {
                     }
                 }
             }
-            sum = warp_sum(sum);
+            if (WHAT == kSum64 || again)
+                sum = warp_sum(sum);
             if (lane == 0) {
                 chunk_max[ch - c0] = most;
                 chunk_mass[ch - c0] = (u64)__double_as_longlong(sum);
