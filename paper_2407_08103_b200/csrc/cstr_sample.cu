@@ -247,6 +247,11 @@ template <bool BF16> struct Row {
         const double w = x == m ? 1.0 : power((double)x - (double)m);
         return (u64)__double2ll_rn(w * unit);
     }
+    // Below which size of x the float x - reach may stand for a logit whose weight is 2^-1000, as an argument of
+    // exp2_factors: its rounding, half a unit in the last place of x and reach together, is 2^-24 (10^5 + 1) < 0.6 % of
+    // reach, so that the exponent stays above -1007 (10^6, with 6 %, would leave what a double's exponent holds); and
+    // x - reach is finite.
+    static __device__ __forceinline__ float clamp_limit(float reach) { return reach < 1e37f ? fminf(reach * 1e5f, 1e38f) : 0.f; }
     // Each warp copies its blocks into a ring of its own, STAGES ahead of the one in use; a lane reads back what
     // it copied, but for the words of the mask.  Blocks at the row's ends are read when they are used.
     static constexpr int kStage = kU * 32 * 16, kMaskWords = 32 * kU * N / 32 + 1;
@@ -367,7 +372,7 @@ template <bool BF16> struct Row {
     enum { kMaximum, kSum32, kSum64 };
     template <int WHAT> __device__ __forceinline__ void first_pass()
     {
-        const float c32 = (float)c, reach = (float)(1000.0 / c);
+        const float c32 = (float)c, reach = (float)(1000.0 / c), limit = clamp_limit(reach);
         const double k16 = c16;
         float top = -CUDART_INF_F;
         float2 s32 = {0.f, 0.f};
@@ -400,9 +405,9 @@ template <bool BF16> struct Row {
                     s64 *= top == -CUDART_INF_F ? 0.0 : power((double)top - (double)t);
                     top = t;
                 }
-                // logits far below (and NaN) add 2^-1000 - where floats are fine enough to say so
+                // logits far below (and NaN) add 2^-1000 or so - where floats are fine enough to say that
                 const float least = top - reach;
-                if (!(reach < 1e37f && fabsf(top) < reach * 1e6f)) {
+                if (!(fabsf(top) < limit)) {
                     for (int u = 0; u < kU * N && top > -CUDART_INF_F; ++u) {
                         const float x = View::value(raw[u / N], u % N);
                         s64 += x == top ? 1.0 : power((double)x - (double)top);
@@ -720,9 +725,9 @@ template <bool BF16> struct Row {
     {
         bool full = false;
         const float high = logit_of(o1), low = logit_of(min(o2, order_of(-FLT_MAX)));
-        // (what is not above adds 2^-1000, where floats are fine enough to say so)
+        // (what is not above adds 2^-1000 or so, where floats are fine enough to say that)
         const float reach = (float)(1000.0 / c), least = m - reach;
-        const bool fine = reach < 1e37f && fabsf(m) < reach * 1e6f;
+        const bool fine = fabsf(m) < clamp_limit(reach);
         double s = 0.0;
         each_vector(bins, [&](const uint4 &raw, int tok) {
             unsigned near = 0;                           // logits around the border
