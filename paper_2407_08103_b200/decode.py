@@ -13,6 +13,16 @@ import torch
 from . import cstr
 
 
+def _capturing(stream):
+    """Whether the current stream or the one that was passed is being captured."""
+    if torch.cuda.is_current_stream_capturing():
+        return True
+    if stream is None:
+        return False
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class ConstrainedDecoder:
     """``tables``: one built Table, or several for a mixed-constraint batch with
     ``row_table`` (int32 per row) choosing each row's table."""
@@ -32,7 +42,9 @@ class ConstrainedDecoder:
         self.accept = torch.empty(batch, dtype=torch.uint8, device=self.device)
         self.logp = torch.empty(batch, dtype=torch.float32, device=self.device)
         self.kept = torch.empty(batch, dtype=torch.float32, device=self.device)
-        self._settings = {}                       # per-row tensors of settings given as numbers
+        self._settings = {}                       # per-row tensors of settings given as numbers, and the streams that read them
+        self._captured = {}                       # ... those that captured steps read
+        self._fills = None                        # the stream that fills them
         self._start = self._start_states()
         self.reset()
 
@@ -61,17 +73,18 @@ class ConstrainedDecoder:
         """One decoding step that draws each row's token from one uniform number (float32 ``[B]``) under
         ``cstr_sample``'s cuts; returns ``(tokens, logp)`` (device tensors, reused by the next call), and
         ``self.kept`` holds the probability that the cuts left.  A setting is a number, or a tensor with one
-        entry per row."""
+        entry per row.  A number is held as a tensor of the decoder's: under capture it has to have been used
+        before, and the decoder keeps it from then on; a tensor is the caller's to keep."""
         cstr.cstr_sample(self.tables, logits, self.states, self.tokens, uniform,
-                         temperature=self._setting("temperature", temperature, 1.0, torch.float32),
-                         top_k=self._setting("top_k", top_k, 0, torch.int32),
-                         top_p=self._setting("top_p", top_p, 1.0, torch.float32),
-                         min_p=self._setting("min_p", min_p, 0.0, torch.float32),
+                         temperature=self._setting("temperature", temperature, 1.0, torch.float32, stream),
+                         top_k=self._setting("top_k", top_k, 0, torch.int32, stream),
+                         top_p=self._setting("top_p", top_p, 1.0, torch.float32, stream),
+                         min_p=self._setting("min_p", min_p, 0.0, torch.float32, stream),
                          logp_out=self.logp, kept_out=self.kept, row_table=self.row_table,
                          accept_out=self.accept, stream=stream)
         return self.tokens, self.logp
 
-    def _setting(self, name, value, off, dtype):
+    def _setting(self, name, value, off, dtype, stream):
         if torch.is_tensor(value):
             return value
         if value == off:
@@ -79,15 +92,25 @@ class ConstrainedDecoder:
         if value != value:
             raise ValueError("%s is not a number" % name)
         at = (name, value)
-        if at not in self._settings:              # a program has a few: filled once, read by every step
-            if torch.cuda.is_current_stream_capturing():
+        capturing = _capturing(stream)
+        if at not in self._settings and at not in self._captured:    # a program has a few: filled once, read by every step
+            if capturing:
                 raise RuntimeError("%s = %r: take one step with it before the capture" % (name, value))
-            if len(self._settings) >= 64:         # (an annealed setting: the steps under way still read the old ones)
-                torch.cuda.synchronize(self.device)
+            if len(self._settings) >= 64:         # (an annealed setting; what steps under way still read is theirs, see below)
                 self._settings.clear()
-            self._settings[at] = torch.full((self.batch,), value, dtype=dtype, device=self.device)
-            torch.cuda.synchronize(self.device)   # ... on whatever stream
-        return self._settings[at]
+            self._fills = self._fills or torch.cuda.Stream(self.device)
+            with torch.cuda.stream(self._fills):
+                self._settings[at] = (torch.full((self.batch,), value, dtype=dtype, device=self.device), set())
+            self._fills.synchronize()             # the filling alone: every stream and capture may read it from now on
+        row, streams = entry = self._captured.get(at) or self._settings[at]
+        if capturing:                             # replays read it as long as the graph lives: it is not dropped any more
+            self._captured[at] = entry
+            return row
+        raw = cstr._raw_stream(stream, row.device)
+        if raw not in streams:                    # its memory is not handed out again before that stream's steps are done
+            row.record_stream(stream or torch.cuda.current_stream(row.device))
+            streams.add(raw)
+        return row
 
     def top_logprobs(self, logits, n: int, temperature: float = 1.0, stream=None):
         """The ``n`` most likely tokens in the rows' present states: ``(ids, logp)`` ``[B][n]``."""
