@@ -113,7 +113,8 @@ class ConstrainedDecoder:
         return row
 
     def top_logprobs(self, logits, n: int, temperature: float = 1.0, stream=None):
-        """The ``n`` most likely tokens in the rows' present states: ``(ids, logp)`` ``[B][n]``."""
+        """The ``n`` most likely tokens in the rows' present states: ``(ids, logp)`` ``[B][n]``.  A record of what
+        ``sample`` (or ``step``) draws from these logits is taken before it: that call moves the states on."""
         with torch.cuda.stream(stream or torch.cuda.current_stream(self.device)):      # (their memory, too)
             ids = torch.empty((self.batch, n), dtype=torch.int32, device=self.device)
             logp = torch.empty((self.batch, n), dtype=torch.float32, device=self.device)
