@@ -112,10 +112,13 @@ class _DistillLoss(torch.autograd.Function):
 
 def constrained_distill_loss(logits, teacher_ids, teacher_logp, tables=None, states=None, weight=None,
                              tail: int = cstr.CSTR_TAIL_RENORM, temperature: float = 1.0, row_table=None):
-    """Loss ``[N]`` of ``cstr_distill_loss``, differentiable in ``logits`` (float32 or bfloat16 ``[N][V]``).
+    """Loss ``[N]`` of ``cstr_distill_loss``, differentiable in ``logits`` alone (float32 or bfloat16 ``[N][V]``):
+    ``teacher_logp`` and ``weight`` are taken as constants and get no gradient.
     ``teacher_ids`` / ``teacher_logp`` ``[N][k]``: a teacher's records (``top_logprobs``)."""
     tables = [tables] if isinstance(tables, cstr.Table) else list(tables or [])
     args = dict(tables=tables, states=states, options=dict(row_table=row_table, tail=tail, temperature=temperature))
+    # (a loss that depended on these alone would look differentiable and leave them without a gradient)
+    teacher_logp, weight = (t if t is None else t.detach() for t in (teacher_logp, weight))
     return _DistillLoss.apply(logits, teacher_ids, teacher_logp, weight, args)
 
 
