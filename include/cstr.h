@@ -25,7 +25,7 @@
  *     such arrays; the library owns what is behind its opaque handles and frees
  *     it in the matching cstr_free_*.  Handles are bound to the CUDA device
  *     that was current when they were created; that device must be current in
- *     later calls.
+ *     later calls, and DEVICE arrays have to lie on it.
  *   - cuda_stream is a cudaStream_t passed as void* (NULL = default stream).
  *   - S = DFA states, V = vocabulary size, W = ceil(V / 32) mask words.
  */

@@ -48,6 +48,7 @@ DEBUG_EXPORTS = ["cstr_debug_bounds_status", "cstr_test_set_group_hash_bits", "c
 
 _F32 = _I32 = _U8 = None      # torch's types, from the first call that takes whole rows on
 _LOGIT_CODES = {}
+_get_device = None            # torch's number of the current device
 
 _lib = None
 _libs = {}            # path -> loaded library
@@ -651,6 +652,15 @@ def _raw_stream(stream, device):
     return stream.cuda_stream
 
 
+def _check_current(device):
+    """Tensors of another device than the current one, on which the kernel would run: without tables no handle's
+    check shows that."""
+    if _get_device is None:
+        _load_types()
+    if device.index != _get_device():
+        raise ValueError("the tensors are on %s, device %d is current" % (device, _get_device()))
+
+
 def _rows_arg(name, t, batch, device, dtype):
     """Checked per-row vector -> address (None -> NULL)."""
     if t is None:
@@ -835,6 +845,7 @@ def cstr_policy_loss(tables, logits, states, actions, old_logp, advantages, loss
         dp = dlogits.data_ptr()
     if bool(tables) != (states is not None):
         raise ValueError("states go with tables")
+    _check_current(device)
     for name, t in (("actions", actions), ("old_logp", old_logp), ("advantages", advantages),
                     ("loss_out", loss_out), ("logp_out", logp_out)):
         if t is None:
@@ -855,8 +866,9 @@ def cstr_policy_loss(tables, logits, states, actions, old_logp, advantages, loss
 
 
 def _load_types():
-    global _F32, _I32, _U8
+    global _F32, _I32, _U8, _get_device
     import torch
+    _get_device = torch._C._cuda_getDevice
     _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
     _LOGIT_CODES.update({torch.float32: CSTR_F32, torch.bfloat16: CSTR_BF16})
 
@@ -878,6 +890,7 @@ def _logit_rows(tables, logits, states):
         raise ValueError("logits must be a CUDA tensor")
     if bool(tables) != (states is not None):
         raise ValueError("states go with tables")
+    _check_current(logits.device)
     ld = strides[0] if shape[0] > 1 else max(shape[1], strides[0])
     arr, count = None, 0
     if tables:
