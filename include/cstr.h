@@ -653,7 +653,9 @@ int cstr_cache_status(cstr_cache_t *cache, void *cuda_stream, int64_t *gave_up);
  *   token  = the first kept token by id for which the sum of p over the kept tokens up to it exceeds
  *            uniform * the sum of p over all kept tokens
  *   state  = next[state][token]
- * The weights that decide are taken and added in 64 bits, logp and kept may come from sums in 32.
+ * The weights that decide are taken in 64 bits, to 2.6e-12 of themselves, and added in 64; what lies nearer than that to
+ * a border between two tokens may go to either, and need not go the same way in a launch of other rows.  logp and kept
+ * may come from sums in 32 bits, where logits that are further apart than the largest float count as infinitely far.
  * temperature 0: the first token of the order (as cstr_step without noise), logp 0, kept 1.  Infinite logits
  * share the probability equally.  Where A is empty, an allowed -infinity still beats none: the lowest such id,
  * logp -infinity, kept 0.
@@ -686,8 +688,8 @@ int cstr_sample(const cstr_table_t *const *tables, int32_t n_tables, const int32
  *   logp_out    DEVICE float [rows][n]: their log p;  n 1 .. CSTR_MAX_TOP
  *   lse_out     DEVICE float [rows] or NULL: log sum over A of exp(logits / temperature)
  *   temperature finite, above 4.3e-39 (its reciprocal times log2(e) is a float)
- * Entries past the tokens of A hold id -1 and logp -infinity, and so does all of an inactive row (lse
- * -infinity).  Other arguments as in cstr_sample; states NULL exactly when n_tables is 0.
+ * The log probabilities come from sums in 32 bits.  Entries past the tokens of A hold id -1 and logp -infinity, and
+ * so does all of an inactive row (lse -infinity).  Other arguments as in cstr_sample; states NULL exactly when n_tables is 0.
  * Only enqueues one kernel on cuda_stream; no allocation, no host synchronisation.
  */
 int cstr_top_logprobs(const cstr_table_t *const *tables, int32_t n_tables, const int32_t *row_table,
@@ -750,7 +752,7 @@ int cstr_policy_loss(const cstr_table_t *const *tables, int32_t n_tables, const 
  *                     the tokens of A without an entry:  + w r (log r - log Q), nothing where r or Q is 0
  *   dlogits[v] = d loss / d logits[v]: 0 outside A
  * An id that is listed twice counts with both entries.  Sums over the record are taken in 64 bits, those over
- * the vocabulary in 32; dlogits is rounded once to its type.
+ * the vocabulary in 32, and so are the gradient's differences of probabilities; dlogits is rounded once to its type.
  *   teacher_ids   DEVICE int32 [rows][k];  teacher_logp  DEVICE float [rows][k];  k 1 .. CSTR_MAX_TOP
  *   weight        DEVICE float [rows] or NULL (1): w, e.g. 1 / tokens, 0 for padding
  *   loss_out      DEVICE float [rows]

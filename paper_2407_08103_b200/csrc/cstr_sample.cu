@@ -6,8 +6,11 @@
 // for one pair (x, i).  With weights w_v = 2^(c (x_v - m)), c = log2(e) / temperature, m the row's maximum, the
 // token is the first one by id whose running sum over the kept weights exceeds u times their sum.  Borders
 // between tokens lie 1 / V apart, so that sums in 32 bits would take a neighbour now and then: the weights that
-// decide are taken in 64 bits and added as whole numbers of 2^-s (s = 62 - log2 V), whose sums are exact
-// whatever their order - atomics included - so a row's token does not depend on the launch.
+// decide are taken in double precision, to 2.6e-12 of themselves, and weights of single tokens are added as whole
+// numbers of 2^-s (s = 62 - log2 V), whose sums are exact whatever their order, atomics included.  Chunks of a row
+// that count as a whole (without a cut, with top_p alone, above the border of a wide nucleus) are summed in double
+// precision and rounded to such a number once: where a chunk begins depends on the rows of the launch, and its last
+// units of 2^-s with it.
 //
 // A cluster of up to 16 CTAs shares a row.  One pass over memory (the bound: 512 x 256,000 fp32 84 of 116 us, 6.2 of
 // 6.55 TB/s in it) leaves the maximum of every lane's logits, and maxima and sums of chunks.  The k-th largest of the
@@ -16,8 +19,8 @@
 // The candidates meet in a list of the first CTA, where they are compared with each other.  Where too many tokens
 // can be kept (a nucleus of thousands, many equal logits) the row is read again from the L2 cache: two histograms
 // by weights in 32 bits bring the border down to some hundred tokens, one pass counts what lies above them and puts
-// them into the list (300 x 128,256 with top_p 0.95, a quarter of the rows that wide, 207 us; by three exact
-// histograms with 64-bit counters 998 us).  Without any cut the weights of all tokens are needed in 64 bits in the
+// them into the list (300 x 128,256 with top_p 0.95, a quarter of the rows that wide, 226 - 268 us by the rows' widths; by
+// three exact histograms with 64-bit counters 998 us).  Without any cut the weights of all tokens are needed in 64 bits in the
 // first pass; that is bound by the double precision pipe (512 x 256,000 150 us of it).
 #include <cooperative_groups.h>
 #include <float.h>
@@ -1322,10 +1325,12 @@ sample_kernel(const __grid_constant__ SampleParams p)
 
 namespace {
 
-// CTAs of a row of so many blocks, `uneven`: some rows may take several more passes than others.  Three CTAs an SM,
+// CTAs of a row of so many blocks, `uneven`: some rows may take several more passes than others - as far as the host
+// knows: it sees which settings are given, not what they hold, and where top_k or min_p is given they mostly leave
+// rows that can be listed.  (Given with nothing in it, such a setting costs the second of the figures below.)  Three CTAs an SM,
 // in shares of at least 8 blocks, up to four where shares are of 128 (512 x 256,000, the 256 most likely: 144 us
 // with two CTAs a row, 169 with one, 160 with four; 128 x 128,256 bf16 from the whole distribution: 43 us with
-// four, 54 with eight); eight with uneven rows (300 x 128,256 with top_p alone: 207 us with four, 470 with one).
+// four, 54 with eight); eight with uneven rows (300 x 128,256 with top_p 0.95: 235 - 268 us with four, 319 - 366 with two).
 // Sixteen only where all rows run at once (4 x 256,000 18.6 us, with eight 21.9).
 int cluster_size(int rows, int blocks, int sms, bool uneven)
 {
