@@ -91,6 +91,8 @@ class ConstrainedDecoder:
             return None
         if value != value:
             raise ValueError("%s is not a number" % name)
+        if dtype == torch.int32 and value % 1 != 0:
+            raise ValueError("%s = %r is not a whole number" % (name, value))
         at = (name, value)
         capturing = _capturing(stream)
         if at not in self._settings and at not in self._captured:    # a program has a few: filled once, read by every step
