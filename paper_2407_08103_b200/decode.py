@@ -75,44 +75,49 @@ class ConstrainedDecoder:
         ``self.kept`` holds the probability that the cuts left.  A setting is a number, or a tensor with one
         entry per row.  A number is held as a tensor of the decoder's: under capture it has to have been used
         before, and the decoder keeps it from then on; a tensor is the caller's to keep."""
+        reader = (_capturing(stream), cstr._raw_stream(stream, logits.device), stream)
         cstr.cstr_sample(self.tables, logits, self.states, self.tokens, uniform,
-                         temperature=self._setting("temperature", temperature, 1.0, torch.float32, stream),
-                         top_k=self._setting("top_k", top_k, 0, torch.int32, stream),
-                         top_p=self._setting("top_p", top_p, 1.0, torch.float32, stream),
-                         min_p=self._setting("min_p", min_p, 0.0, torch.float32, stream),
+                         temperature=self._setting("temperature", temperature, 1.0, torch.float32, reader),
+                         top_k=self._setting("top_k", top_k, 0, torch.int32, reader),
+                         top_p=self._setting("top_p", top_p, 1.0, torch.float32, reader),
+                         min_p=self._setting("min_p", min_p, 0.0, torch.float32, reader),
                          logp_out=self.logp, kept_out=self.kept, row_table=self.row_table,
                          accept_out=self.accept, stream=stream)
         return self.tokens, self.logp
 
-    def _setting(self, name, value, off, dtype, stream):
+    def _setting(self, name, value, off, dtype, reader):
+        """``reader``: whether a capture is under way, the stream's address, the stream (None: the current one)."""
         if torch.is_tensor(value):
             return value
         if value == off:
             return None
+        at, (capturing, raw, stream) = (name, value), reader
+        entry = self._settings.get(at) or self._captured.get(at)
+        if entry is None:                         # a program has a few: filled once, read by every step
+            entry = self._filled(name, value, dtype, capturing)
+        row, streams = entry
+        if capturing:                             # replays read it as long as the graph lives: it is not dropped any more
+            self._captured[at] = entry
+        elif raw not in streams:                  # its memory is not handed out again before that stream's steps are done
+            row.record_stream(stream or torch.cuda.current_stream(row.device))
+            streams.add(raw)
+        return row
+
+    def _filled(self, name, value, dtype, capturing):
         if value != value:
             raise ValueError("%s is not a number" % name)
         if dtype == torch.int32 and value % 1 != 0:
             raise ValueError("%s = %r is not a whole number" % (name, value))
-        at = (name, value)
-        capturing = _capturing(stream)
-        if at not in self._settings and at not in self._captured:    # a program has a few: filled once, read by every step
-            if capturing:
-                raise RuntimeError("%s = %r: take one step with it before the capture" % (name, value))
-            if len(self._settings) >= 64:         # (an annealed setting; what steps under way still read is theirs, see below)
-                self._settings.clear()
-            self._fills = self._fills or torch.cuda.Stream(self.device)
-            with torch.cuda.stream(self._fills):
-                self._settings[at] = (torch.full((self.batch,), value, dtype=dtype, device=self.device), set())
-            self._fills.synchronize()             # the filling alone: every stream and capture may read it from now on
-        row, streams = entry = self._captured.get(at) or self._settings[at]
-        if capturing:                             # replays read it as long as the graph lives: it is not dropped any more
-            self._captured[at] = entry
-            return row
-        raw = cstr._raw_stream(stream, row.device)
-        if raw not in streams:                    # its memory is not handed out again before that stream's steps are done
-            row.record_stream(stream or torch.cuda.current_stream(row.device))
-            streams.add(raw)
-        return row
+        if capturing:
+            raise RuntimeError("%s = %r: take one step with it before the capture" % (name, value))
+        if len(self._settings) >= 64:             # (an annealed setting; what steps under way still read is recorded)
+            self._settings.clear()
+        self._fills = self._fills or torch.cuda.Stream(self.device)
+        with torch.cuda.stream(self._fills):
+            entry = (torch.full((self.batch,), value, dtype=dtype, device=self.device), set())
+        self._fills.synchronize()                 # the filling alone: every stream and capture may read it from now on
+        self._settings[name, value] = entry
+        return entry
 
     def top_logprobs(self, logits, n: int, temperature: float = 1.0, stream=None):
         """The ``n`` most likely tokens in the rows' present states: ``(ids, logp)`` ``[B][n]``.  A record of what
